@@ -338,7 +338,7 @@ def _own(s):
         if not c["train"]:
             return [tp.gated_forward(s["x"], s["w_gu"], s["w_down"], c["act"])]
         y, saved = tp.gated_forward(s["x"], s["w_gu"], s["w_down"], c["act"], save=True)
-        return [y, *tp.gated_backward(s["dy"], s["x"], s["w_gu"], s["w_down"], saved, c["act"])]
+        return [y, *tp.gated_backward(s["dy"], s["x"], s["w_gu"], s["w_down"], saved)]
     if c["op"] == "norm":
         if c["out"] != "norm":
             q, scale, v = tp.rms_norm_q8(s["x"], s["w"], s["res"], eps=EPS)
