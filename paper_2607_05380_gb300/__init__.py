@@ -36,7 +36,11 @@ SYMBOLS = ["pack_create", "pack_destroy", "pack_set_stream", "pack_train_step", 
            "pack_online_members", "pack_online_ensemble", "pack_online_snapshot", "pack_online_predict",
            "pack_online_last_error", "pack_train_step_stacked", "pack_forward_backward_stacked", "pack_set_muon",
            "pack_debug_muon_dir", "pack_create_emb", "pack_get_emb", "pack_set_emb", "pack_member_emb",
-           "pack_debug_mask_arena", "pack_debug_philox", "pack_debug_gemm_timeout", "pack_debug_bias_path"]
+           "pack_debug_mask_arena", "pack_debug_philox", "pack_debug_gemm_timeout", "pack_debug_bias_path",
+           # include/tabpack_ops.h
+           "pack_ops_check", "pack_gated_bytes", "pack_gated_forward", "pack_gated_backward", "pack_rms_norm",
+           "pack_rms_norm_bytes", "pack_rms_norm_backward", "pack_product_q8_bytes", "pack_product_q8",
+           "pack_distill_bytes", "pack_distill"]
 
 
 class TabpackError(RuntimeError):
@@ -70,7 +74,7 @@ def load_library(path: str = LIB_PATH):
     if not os.path.exists(path):
         raise ImportError(f"libtabpack.so not built at {path}: run paper_2607_05380_gb300.build.build()")
     L = ctypes.CDLL(path)
-    P, i32, i64, u32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
+    P, i32, i64, u32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float
     st = ctypes.c_int
     sig = {
         "pack_create": (st, [ctypes.POINTER(Config), P, P, P, P, P, P, ctypes.POINTER(P)]),
@@ -121,6 +125,17 @@ def load_library(path: str = LIB_PATH):
         "pack_debug_philox": (st, [P, P, i32, P]),
         "pack_debug_gemm_timeout": (st, [P, ctypes.c_double, i32]),
         "pack_debug_bias_path": (st, [P, i32]),
+        "pack_ops_check": (st, [P]),
+        "pack_gated_bytes": (st, [i64, i32, i32, i32, i32, P, P, P]),
+        "pack_gated_forward": (st, [P, i64, P, P, i64, i32, i32, i32, i32, i32, P, P, P, i64, P]),
+        "pack_gated_backward": (st, [P, i64, P, i64, P, P, P, i64, i32, i32, i32, i32, P, P, P, P, i64, P]),
+        "pack_rms_norm": (st, [P, i64, P, i64, P, i64, i32, f32, i32, P, P, P, P, P]),
+        "pack_rms_norm_bytes": (st, [i64, i32, P]),
+        "pack_rms_norm_backward": (st, [P, i64, P, i64, P, P, i64, i64, i32, f32, i32, P, P, P, i64, P]),
+        "pack_product_q8_bytes": (st, [i64, i32, i32, i32, P]),
+        "pack_product_q8": (st, [P, i64, P, P, P, P, i64, i32, i32, i32, P, P, i64, P]),
+        "pack_distill_bytes": (st, [i64, i64, P]),
+        "pack_distill": (st, [P, i64, i64, i32, P, P, i32, P, f32, f32, i32, P, P, P, i64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -494,3 +509,7 @@ class OnlineEnsemble:
         _ocheck(load_library().pack_online_predict(self._h, _dptr(X, t.float32), X.shape[0], _dptr(out, t.float32)),
                 self._h)
         return out
+
+
+from .ops import (ACTIVATIONS, distill, gated_backward, gated_forward, ops_check, product_q8,  # noqa: E402,F401
+                  rms_norm, rms_norm_backward, rms_norm_q8)
