@@ -18,57 +18,75 @@ using namespace tp;
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int32_t kMaxD = 16384;
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;
 constexpr int kBwdBlocks = 2 * kSms;
+constexpr int threads(int warps_per_row) { return warps_per_row > 8 ? 32 * warps_per_row : 256; }
 
-__device__ __forceinline__ bool aligned16(const void* p, int64_t ld, int bytes) {
+inline bool aligned16(const void* p, int64_t ld, int bytes) {
   return ((uintptr_t)p & 15) == 0 && ((ld * bytes) & 15) == 0;
 }
 
-// Eight elements of a row from column c on (zeros past d).
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int c, int d, bool vec, float (&v)[8]) {
-  if (vec && c + 8 <= d) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4*>(p + c), b = *reinterpret_cast<const float4*>(p + c + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(p + c);
-      const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+// A lane's elements of a row: kV * 8 of them, as groups of kE = 8 at columns
+// (i * lanes + lane) * 8 where every address is a multiple of 16 bytes and d
+// of 8, else one by one.  A group is inside the row or past it (zeros): the
+// loads are predicated, not branched around, so that all are in flight at
+// once (8192 rows of 2048, bf16, forward: 90 us with a branch per group).
+template <typename T, int kW, int kV, int kE>
+struct Lane {
+  static constexpr int kGroups = kV * 8 / kE;
+  float v[kGroups][kE];
+  static __device__ __forceinline__ int col(int i, int wl) { return (i * 32 * kW + wl) * kE; }
+  __device__ __forceinline__ void load(const T* p, int wl, int d) {
+    if constexpr (kE == 8) {
+      uint4 u[kGroups][sizeof(T) / 2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __uint_as_float(u[e] << 16);
-        v[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
+      for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+          u[i][h] = col(i, wl) < d ? *(reinterpret_cast<const uint4*>(p + col(i, wl)) + h) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+          const uint32_t w[4] = {u[i][h].x, u[i][h].y, u[i][h].z, u[i][h].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) {
+              v[i][4 * h + e] = __uint_as_float(w[e]);
+            } else {
+              v[i][2 * e] = __uint_as_float(w[e] << 16);
+              v[i][2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+            }
+          }
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) v[i][0] = col(i, wl) < d ? Elem<T>::to_f(p[col(i, wl)]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int wl, int d) const {
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      if (col(i, wl) >= d) continue;
+      T* o = p + col(i, wl);
+      if constexpr (kE == 1) {
+        o[0] = Elem<T>::from_f(v[i][0]);
+      } else if constexpr (sizeof(T) == 4) {
+        reinterpret_cast<float4*>(o)[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        reinterpret_cast<float4*>(o)[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+      } else {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[i][2 * e], v[i][2 * e + 1]);
+          u[e] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        *reinterpret_cast<uint4*>(o) = make_uint4(u[0], u[1], u[2], u[3]);
       }
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < d ? Elem<T>::to_f(p[c + e]) : 0.f;
   }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int c, int d, bool vec, const float (&v)[8]) {
-  if (vec && c + 8 <= d) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4*>(p + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint32_t u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-        u[e] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      *reinterpret_cast<uint4*>(p + c) = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < d) p[c + e] = Elem<T>::from_f(v[e]);
-  }
-}
+};
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -89,47 +107,36 @@ struct FwdArgs {
   float eps;
 };
 
-// kW warps per row, kV groups of eight elements per lane.
-template <typename T, int kW, int kV>
-__global__ void __launch_bounds__(kThreads) k_rms_fwd(const FwdArgs<T> g) {
-  __shared__ float red[8];
-  __shared__ uint32_t redu[8];
+// kW warps per row, 8 kV elements per lane.
+template <typename T, int kW, int kV, int kE>
+__global__ void __launch_bounds__(threads(kW)) k_rms_fwd(const FwdArgs<T> g) {
+  using L = Lane<T, kW, kV, kE>;
+  __shared__ float red[16];
+  __shared__ uint32_t redu[16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW, d = g.d;
-  const int64_t row = (int64_t)blockIdx.x * (8 / kW) + grp;
+  const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW;
+  const int64_t row = (int64_t)blockIdx.x * (threads(kW) / 32 / kW) + grp;
   const bool live = row < g.rows;
-  const bool vx = aligned16(g.x, g.ldx, sizeof(T)), vr = aligned16(g.res, g.ldr, sizeof(T));
-  const bool vw = aligned16(g.w, 0, 4), vs = aligned16(g.sum, d, sizeof(T)), vy = aligned16(g.y, d, sizeof(T));
-  const bool vq = ((uintptr_t)g.q & 7) == 0 && (d & 7) == 0;
+  const int d = live ? g.d : 0;   // a row past the last one has no elements
   pdl_trigger();
   pdl_wait();
-  float v[kV][8];
-  float ss = 0.f;
-  if (live) {
+  L v, w;
+  v.load(g.x + row * g.ldx, wl, d);
+  if (g.res) {
+    w.load(g.res + row * g.ldr, wl, d);
 #pragma unroll
-    for (int i = 0; i < kV; ++i) {
-      const int c = (i * 32 * kW + wl) * 8;
-      load8(g.x + row * g.ldx, c, d, vx, v[i]);
-    }
-    if (g.res) {
+    for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        const int c = (i * 32 * kW + wl) * 8;
-        float r[8];
-        load8(g.res + row * g.ldr, c, d, vr, r);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] += r[e];
-      }
-    }
-    if (g.sum) {
-#pragma unroll
-      for (int i = 0; i < kV; ++i) store8(g.sum + row * d, (i * 32 * kW + wl) * 8, d, vs, v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kV; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss += v[i][e] * v[i][e];
+      for (int e = 0; e < kE; ++e) v.v[i][e] += w.v[i][e];
   }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < L::kGroups; ++i)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) ss += v.v[i][e] * v.v[i][e];
+  if (g.sum) v.store(g.sum + row * d, wl, d);
+  Lane<float, kW, kV, kE> wt;
+  wt.load(g.w, wl, d);
   ss = warp_sum(ss);
   if constexpr (kW > 1) {
     if (lane == 0) red[warp] = ss;
@@ -138,22 +145,17 @@ __global__ void __launch_bounds__(kThreads) k_rms_fwd(const FwdArgs<T> g) {
 #pragma unroll
     for (int k = 0; k < kW; ++k) ss += red[grp * kW + k];
   }
-  const float r = 1.f / sqrtf(ss / (float)d + g.eps);
+  const float r = 1.f / sqrtf(ss / (float)g.d + g.eps);
   uint32_t top = 0;   // the largest |n|, as bits: a NaN is above infinity
-  if (live) {
 #pragma unroll
-    for (int i = 0; i < kV; ++i) {
-      const int c = (i * 32 * kW + wl) * 8;
-      float w[8];
-      load8(g.w, c, d, vw, w);
+  for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[i][e] = v[i][e] * r * w[e];
-        if (c + e < d) top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
-      }
-      if (g.y) store8(g.y + row * d, c, d, vy, v[i]);
+    for (int e = 0; e < kE; ++e) {
+      v.v[i][e] = v.v[i][e] * r * wt.v[i][e];
+      // (past the row: 0, or NaN where r is infinite, which is kept out)
+      if (L::col(i, wl) < d) top = max(top, __float_as_uint(v.v[i][e]) & 0x7FFFFFFFu);
     }
-  }
+  if (g.y) v.store(g.y + row * d, wl, d);
   if (g.q == nullptr) return;
   top = warp_max(top);
   if constexpr (kW > 1) {
@@ -163,26 +165,23 @@ __global__ void __launch_bounds__(kThreads) k_rms_fwd(const FwdArgs<T> g) {
 #pragma unroll
     for (int k = 0; k < kW; ++k) top = max(top, redu[grp * kW + k]);
   }
-  if (!live) return;
   const bool finite = top < 0x7F800000u;
   const float scale = finite ? __uint_as_float(top) / 127.f : __uint_as_float(0x7FC00000u);
-  if (wl == 0) g.scale[row] = scale;
+  if (live && wl == 0) g.scale[row] = scale;
   const bool some = finite && scale > 0.f;
   int8_t* q = g.q + row * d;
 #pragma unroll
-  for (int i = 0; i < kV; ++i) {
-    const int c = (i * 32 * kW + wl) * 8;
-    uint32_t b[8];
+  for (int i = 0; i < L::kGroups; ++i) {
+    if (L::col(i, wl) >= d) continue;
+    uint32_t b[kE];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)   // the clamp: a scale that lost bits below the normal numbers
-      b[e] = some ? (uint32_t)(uint8_t)(int8_t)max(-127, min(127, __float2int_rn(v[i][e] / scale))) : 0u;
-    if (vq && c + 8 <= d)
-      *reinterpret_cast<uint2*>(q + c) = make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24,
-                                                    b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+    for (int e = 0; e < kE; ++e)   // the clamp: a scale that lost bits below the normal numbers
+      b[e] = some ? (uint32_t)(uint8_t)(int8_t)max(-127, min(127, __float2int_rn(v.v[i][e] / scale))) : 0u;
+    if constexpr (kE == 8)
+      *reinterpret_cast<uint2*>(q + L::col(i, wl)) = make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24,
+                                                                b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
     else
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < d) q[c + e] = (int8_t)b[e];
+      q[L::col(i, wl)] = (int8_t)b[0];
   }
 }
 
@@ -197,101 +196,79 @@ struct BwdArgs {
   float eps;
 };
 
-template <typename T, int kW, int kV>
-__global__ void __launch_bounds__(kThreads) k_rms_bwd(const BwdArgs<T> g) {
-  constexpr int kRows = 8 / kW;            // rows at a time
-  __shared__ float red[2][2][8];
-  __shared__ float join[kRows > 1 ? kRows * 32 * kW * kV * 8 : 1];
+template <typename T, int kW, int kV, int kE>
+__global__ void __launch_bounds__(threads(kW), kW > 8 ? 1 : 2) k_rms_bwd(const BwdArgs<T> g) {
+  using L = Lane<T, kW, kV, kE>;
+  constexpr int kRows = threads(kW) / 32 / kW;   // rows at a time
+  constexpr int kCols = 32 * kW * kV * 8;
+  __shared__ float red[2][2][16];
+  __shared__ float join[kRows > 1 ? kRows * kCols : 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW, d = g.d;
-  const bool vy = aligned16(g.dy, g.lddy, sizeof(T)), vs = aligned16(g.s, g.lds, sizeof(T));
-  const bool vd = aligned16(g.dsum, g.lddsum, sizeof(T)), vw = aligned16(g.w, 0, 4), vx = aligned16(g.dx, d, sizeof(T));
+  const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW;
   pdl_trigger();
   pdl_wait();
-  float acc[kV][8];
+  Lane<float, kW, kV, kE> w, acc;
+  w.load(g.w, wl, g.d);
 #pragma unroll
-  for (int i = 0; i < kV; ++i)
+  for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
+    for (int e = 0; e < kE; ++e) acc.v[i][e] = 0.f;
   int turn = 0;
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < g.rows; base += (int64_t)gridDim.x * kRows, turn ^= 1) {
     const int64_t row = base + grp;
-    const bool live = row < g.rows;
-    float s[kV][8], t[kV][8];
+    const int d = row < g.rows ? g.d : 0;   // a row past the last one has no elements
+    L s, t, o;
+    s.load(g.s + row * g.lds, wl, d);
+    t.load(g.dy + row * g.lddy, wl, d);
+    if (g.dsum) o.load(g.dsum + row * g.lddsum, wl, d);
     float ss = 0.f, ts = 0.f;
-    if (live) {
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        const int c = (i * 32 * kW + wl) * 8;
-        load8(g.s + row * g.lds, c, d, vs, s[i]);
-        load8(g.dy + row * g.lddy, c, d, vy, t[i]);
+    for (int i = 0; i < L::kGroups; ++i)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        ss += s.v[i][e] * s.v[i][e];
+        ts += t.v[i][e] * w.v[i][e] * s.v[i][e];
       }
-#pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        float w[8];
-        load8(g.w, (i * 32 * kW + wl) * 8, d, vw, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          ss += s[i][e] * s[i][e];
-          ts += t[i][e] * w[e] * s[i][e];
-        }
-      }
-    }
     ss = warp_sum(ss);
     ts = warp_sum(ts);
     if constexpr (kW > 1) {
-      // two sets of sums in turn: the next row's may be written while this row's are read
+      // two sets of sums in turn: the next rows' may be written while these are read
       if (lane == 0) red[turn][0][warp] = ss, red[turn][1][warp] = ts;
       __syncthreads();
       ss = ts = 0.f;
 #pragma unroll
       for (int k = 0; k < kW; ++k) ss += red[turn][0][grp * kW + k], ts += red[turn][1][grp * kW + k];
     }
-    if (live) {
-      const float r = 1.f / sqrtf(ss / (float)d + g.eps);
-      const float f = r * r * (ts / (float)d);
+    const float r = 1.f / sqrtf(ss / (float)g.d + g.eps);
+    const float f = r * r * (ts / (float)g.d);
+    if (d) {
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        const int c = (i * 32 * kW + wl) * 8;
-        float w[8], o[8];
-        load8(g.w, c, d, vw, w);
+      for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          o[e] = r * (t[i][e] * w[e] - s[i][e] * f);
-          acc[i][e] += t[i][e] * s[i][e] * r;
+        for (int e = 0; e < kE; ++e) {
+          acc.v[i][e] += t.v[i][e] * s.v[i][e] * r;
+          t.v[i][e] = r * (t.v[i][e] * w.v[i][e] - s.v[i][e] * f);
+          if (g.dsum) t.v[i][e] += o.v[i][e];
         }
-        if (g.dsum) {
-          load8(g.dsum + row * g.lddsum, c, d, vd, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += w[e];
-        }
-        store8(g.dx + row * d, c, d, vx, o);
-      }
     }
+    t.store(g.dx + row * d, wl, d);
   }
   if (g.part == nullptr) return;
-  float* part = g.part + (int64_t)blockIdx.x * d;
+  float* part = g.part + (int64_t)blockIdx.x * g.d;
   if constexpr (kRows > 1) {
-    constexpr int kCols = 32 * kW * kV * 8;
 #pragma unroll
-    for (int i = 0; i < kV; ++i)
+    for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) join[grp * kCols + (i * 32 * kW + wl) * 8 + e] = acc[i][e];
+      for (int e = 0; e < kE; ++e) join[grp * kCols + L::col(i, wl) + e] = acc.v[i][e];
     __syncthreads();
-    for (int c = threadIdx.x; c < d; c += kThreads) {
+    for (int c = threadIdx.x; c < g.d; c += threads(kW)) {
       float a = join[c];
 #pragma unroll
       for (int k = 1; k < kRows; ++k) a += join[k * kCols + c];
       part[c] = a;
     }
   } else {
-#pragma unroll
-    for (int i = 0; i < kV; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = (i * 32 * kW + wl) * 8 + e;
-        if (c < d) part[c] = acc[i][e];
-      }
+    acc.store(part, wl, g.d);
   }
 }
 
@@ -314,30 +291,42 @@ __global__ void __launch_bounds__(256) k_rms_dw(const float* part, int n, int d,
   }
 }
 
-// Warps per row and groups per lane for a row of d elements.
+// Warps per row and groups of eight per lane for a row of d elements.
+template <int kW, int kV>
+struct Width {
+  static constexpr int w = kW, v = kV;
+};
 template <typename F>
 void by_width(int d, F f) {
-  if (d <= 256) f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-  else if (d <= 512) f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-  else if (d <= 1024) f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-  else if (d <= 2048) f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
-  else if (d <= 4096) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-  else if (d <= 8192) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
-  else f(std::integral_constant<int, 8>(), std::integral_constant<int, 8>());
+  if (d <= 256) f(Width<1, 1>());
+  else if (d <= 512) f(Width<1, 2>());
+  else if (d <= 1024) f(Width<2, 2>());
+  else if (d <= 2048) f(Width<4, 2>());
+  else if (d <= 4096) f(Width<8, 2>());
+  else if (d <= 8192) f(Width<16, 2>());
+  else f(Width<16, 4>());
 }
-int rows_per_block(int d) { return d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }
+int rows_per_block(int d) { return d <= 512 ? 8 : d <= 1024 ? 4 : d <= 2048 ? 2 : 1; }
 int bwd_blocks(int64_t rows, int d) { return (int)std::min<int64_t>(ceil_div(rows, rows_per_block(d)), kBwdBlocks); }
 
 template <typename T>
 void forward(const FwdArgs<T>& a, cudaStream_t st) {
-  by_width(a.d, [&](auto w, auto v) {
-    launch_pdl(k_rms_fwd<T, w.value, v.value>, dim3((unsigned)ceil_div(a.rows, 8 / w.value)), dim3(kThreads), 0, st, a);
+  const bool vec = a.d % 8 == 0 && aligned16(a.x, a.ldx, sizeof(T)) && aligned16(a.res, a.ldr, sizeof(T)) &&
+                   aligned16(a.w, 0, 4) && aligned16(a.sum, 0, 4) && aligned16(a.y, 0, 4) && ((uintptr_t)a.q & 7) == 0;
+  by_width(a.d, [&](auto s) {
+    const dim3 grid((unsigned)ceil_div(a.rows, rows_per_block(a.d))), block(threads(s.w));
+    if (vec) launch_pdl(k_rms_fwd<T, s.w, s.v, 8>, grid, block, 0, st, a);
+    else launch_pdl(k_rms_fwd<T, s.w, s.v, 1>, grid, block, 0, st, a);
   });
 }
 template <typename T>
 void backward(const BwdArgs<T>& a, cudaStream_t st) {
-  by_width(a.d, [&](auto w, auto v) {
-    launch_pdl(k_rms_bwd<T, w.value, v.value>, dim3((unsigned)bwd_blocks(a.rows, a.d)), dim3(kThreads), 0, st, a);
+  const bool vec = a.d % 8 == 0 && aligned16(a.dy, a.lddy, sizeof(T)) && aligned16(a.s, a.lds, sizeof(T)) &&
+                   aligned16(a.dsum, a.lddsum, sizeof(T)) && aligned16(a.w, 0, 4) && aligned16(a.dx, 0, 4);
+  by_width(a.d, [&](auto s) {
+    const dim3 grid((unsigned)bwd_blocks(a.rows, a.d)), block(threads(s.w));
+    if (vec) launch_pdl(k_rms_bwd<T, s.w, s.v, 8>, grid, block, 0, st, a);
+    else launch_pdl(k_rms_bwd<T, s.w, s.v, 1>, grid, block, 0, st, a);
   });
 }
 
