@@ -527,6 +527,26 @@ def test_distill_masks(tp, dtype, n):
     assert not dz[z == -math.inf].any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [9, 40, 600, 2500])
+@pytest.mark.parametrize("low", [-1e4, -1e10, -3.3e38])
+def test_distill_finite_masks(tp, dtype, n, low):
+    """Classes ruled out by a large negative number instead of -inf, rows where
+    that is all there is, and rows far from zero."""
+    z, ids, top, labels = _distill_case(2, 12, n, 3, dtype, n)
+    z[:, 2] = low
+    z[:, 3, n // 2:] = low
+    z[:, 4, : n // 2] = -math.inf
+    z[:, 4, n // 2:] = low
+    z[:, 5] += 1024.0
+    z[:, 6] = (-low if low > -1e38 else 3e38)
+    ids[2:5] = n - 1
+    labels[2:5] = n - 1
+    ids[3] = labels[3] = 0
+    for tau in (1.0, 2.0, 3.0):
+        _check_distill(tp, z, ids, top, labels, tau, 0.6, (n, low))
+
+
 @pytest.mark.parametrize("n", [20, 3000])
 def test_distill_entries(tp, n):
     """Entries of the same class add up, ids out of range and logits of -inf
