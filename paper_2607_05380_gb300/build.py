@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libtabpack.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["tabpack.cu", "kernels.cu", "select.cu", "select_static.cu", "tc_gemm.cu", "head_tc.cu", "online.cu",
-           "prod.cu", "gated.cu", "norm.cu", "quant.cu", "distill.cu"]
+           "prod.cu", "rows.cu", "gated.cu", "norm.cu", "quant.cu", "distill.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

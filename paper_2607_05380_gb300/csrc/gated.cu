@@ -15,6 +15,7 @@
 // because the tensor cores take them so; every sum is fp32.  32-bit blocks
 // keep fp32 and multiply in three bf16 parts each (see prod.cu).
 #include "prod.cuh"
+#include "rows.cuh"
 
 using namespace tp;
 
@@ -145,7 +146,12 @@ void plan_backward(Plans& p, const Geo& g, const ProdOperand& dy, const ProdOper
   job(l, g.d_out, g.f, g.rows, 4, 5, true, true, 1, dwd, g.f);
 }
 
-tp_status run(Plans& p, Stager& st, void* partial, cudaStream_t stream, const char* who) {
+tp_status run(Plans& p, Stager& st, Carver& c, int64_t workspace_bytes, cudaStream_t stream, const char* who) {
+  const int64_t need = c.used + plan(p);
+  if (workspace_bytes < need) return ops_fail(TP_EINVAL, "%s: a workspace of %lld bytes is needed", who, (long long)need);
+  const tp_status s = ops_device();
+  if (s != TP_OK) return s;
+  void* partial = c.take(0);
   const char* what = "staging launch";
   cudaError_t e = stage_run(st.launch, stream);
   for (int k = 0; e == cudaSuccess && k < 2; ++k) e = prod_run(p.l[k], partial, stream, &what);
@@ -198,22 +204,29 @@ tp_status pack_gated_forward(const void* x, int64_t ldx, const void* w_gate_up, 
   if (rows == 0) return TP_OK;
   if (!x || !w_gate_up || !w_down || !y) return ops_fail(TP_EINVAL, "null argument");
   if ((uintptr_t)saved & 255) return ops_fail(TP_EINVAL, "saved must be 256-byte aligned");
-  int64_t need = 0;
-  pack_gated_bytes(rows, d, f, d_out, precision, nullptr, &need, nullptr);
-  if (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255))
-    return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
-  if ((s = ops_device()) != TP_OK) return s;
+  if (!workspace || ((uintptr_t)workspace & 255)) return ops_fail(TP_EINVAL, "the workspace must be 256-byte aligned");
   const Geo g(rows, d, f, d_out, precision);
   Carver c(workspace);
   void* own = c.take(Saved(g, nullptr).h_bytes);
   const Saved sv(g, saved ? saved : own);
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  // a few rows: the weights stream past them, twice, with nothing in between
+  if (!g.f32 && f % 8 == 0 && rows_fit(rows, x, ldx, w_gate_up, d, 2) && rows_fit(rows, sv.h, g.ldf, w_down, f, 2)) {
+    if (workspace_bytes < c.used) return ops_fail(TP_EINVAL, "a workspace of %lld bytes is needed", (long long)c.used);
+    if ((s = ops_device()) != TP_OK) return s;
+    cudaError_t e = rows_gated(x, ldx, w_gate_up, rows, d, f, act, sv.h, g.ldf, saved ? sv.a : nullptr,
+                               saved ? sv.p : nullptr, stream);
+    if (e == cudaSuccess) e = rows_plain(sv.h, g.ldf, w_down, rows, f, d_out, y, stream);
+    if (e == cudaSuccess) return TP_OK;
+    cudaGetLastError();   // reported here
+    return ops_fail(TP_ECUDA, "pack_gated_forward: %s", cudaGetErrorString(e));
+  }
   Stager st(g, c);
   const ProdOperand xo = st.operand(x, ldx, rows, d, 1), wgu = st.operand(w_gate_up, d, 2 * (int64_t)f, d, 2);
   const ProdOperand wd = st.operand(w_down, f, d_out, f, 1);
   Plans p;
   plan_forward(p, g, act, xo, wgu, wd, sv, saved != nullptr, y);
-  plan(p);
-  return run(p, st, c.take(0), (cudaStream_t)cuda_stream, "pack_gated_forward");
+  return run(p, st, c, workspace_bytes, stream, "pack_gated_forward");
 }
 
 tp_status pack_gated_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate_up,
@@ -237,11 +250,7 @@ tp_status pack_gated_backward(const void* dy, int64_t lddy, const void* x, int64
   }
   if (!dy || !x || !w_gate_up || !w_down || !saved || !dx) return ops_fail(TP_EINVAL, "null argument");
   if ((uintptr_t)saved & 255) return ops_fail(TP_EINVAL, "saved must be 256-byte aligned");
-  int64_t need = 0;
-  pack_gated_bytes(rows, d, f, d_out, precision, nullptr, nullptr, &need);
-  if (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255))
-    return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
-  if ((s = ops_device()) != TP_OK) return s;
+  if (!workspace || ((uintptr_t)workspace & 255)) return ops_fail(TP_EINVAL, "the workspace must be 256-byte aligned");
   const Geo g(rows, d, f, d_out, precision);
   const Saved sv(g, const_cast<void*>(saved));
   Carver c(workspace);
@@ -251,8 +260,7 @@ tp_status pack_gated_backward(const void* dy, int64_t lddy, const void* x, int64
   const ProdOperand wgu = st.operand(w_gate_up, d, 2 * (int64_t)f, d, 2), wd = st.operand(w_down, f, d_out, f, 1);
   Plans p;
   plan_backward(p, g, dyo, xo, wgu, wd, sv, dgu, dx, dw_gate_up, dw_down);
-  plan(p);
-  return run(p, st, c.take(0), stream, "pack_gated_backward");
+  return run(p, st, c, workspace_bytes, stream, "pack_gated_backward");
 }
 
 }  // extern "C"

@@ -27,12 +27,15 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <mutex>
+#include <type_traits>
 
 #include "kernels.cuh"
 #include "prod.cuh"
+#include "rows.cuh"
 #include "tc_ptx.cuh"
 
 namespace tp {
@@ -60,7 +63,7 @@ struct Tail {
 struct ProdArgs {
   CUtensorMap map[kProdMaps];
   ProdJob job[kProdJobs];
-  int32_t n_jobs, n_tiles, act, fp16, f32, n_tile, chains, stages;
+  int32_t n_jobs, n_tiles, fp16, n_tile, chains, stages;
 };
 static_assert(sizeof(ProdArgs) <= 4096, "kernel parameters");
 
@@ -178,23 +181,6 @@ __device__ __forceinline__ void emit_parts(uint8_t* buf, int lane, float (&v)[32
   }
 }
 
-// act(g) and act'(g); the exponential to 2 ulp where the results are rounded to bf16
-template <bool kF32>
-__device__ __forceinline__ float act_value(int act, float g, float& d) {
-  if (act == TP_ACT_RELU) {
-    d = g > 0.f ? 1.f : 0.f;
-    return g != g ? g : fmaxf(g, 0.f);
-  }
-  if (act == TP_ACT_SILU) {
-    const float s = 1.f / (1.f + (kF32 ? expf(-g) : __expf(-g)));
-    d = s * (1.f + g * (1.f - s));
-    return g * s;
-  }
-  const float p = 0.5f * erfcf(-0.70710678118654752f * g);
-  d = p + g * 0.39894228040143268f * (kF32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g));
-  return g * p;
-}
-
 // 32 values of a row (fp32 or bf16) from column c0 on, zeros past n_lim.
 template <bool kF32>
 __device__ __forceinline__ void load_row(const void* base, int64_t at, int c0, int n_lim, float (&v)[32]) {
@@ -223,7 +209,7 @@ __device__ __forceinline__ void load_row(const void* base, int64_t at, int c0, i
 
 // The epilogue of one 32 x 32 chunk; acc: its accumulator (kEpiGated: the
 // gate product), acc2: the up product.
-template <int kEpi, bool kF32>
+template <int kEpi, int kAct, bool kF32>
 __device__ __forceinline__ void epilogue(const ProdArgs& g, const ProdJob& j, uint8_t* buf, int lane, float (&acc)[32],
                                          float (&acc2)[32], int r0, int c0) {
   const int row = r0 + lane;
@@ -233,7 +219,7 @@ __device__ __forceinline__ void epilogue(const ProdArgs& g, const ProdJob& j, ui
 #pragma unroll
     for (int e = 0; e < 32; ++e) {
       float d;
-      const float a = act_value<kF32>(g.act, acc[e], d);
+      const float a = act_value<kAct, kF32>(acc[e], d);
       da[e] = acc2[e] * d;
       acc2[e] *= a;
       acc[e] = a;
@@ -274,7 +260,7 @@ __device__ __forceinline__ void epilogue(const ProdArgs& g, const ProdJob& j, ui
   }
 }
 
-template <int kCta, int kEpi, bool kF32>
+template <int kCta, int kEpi, int kAct, bool kF32>
 __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ ProdArgs g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -475,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
         if (j.splits > 1)
           emit_f32(buf, lane, a, j.partial + (int64_t)u.split * j.M * j.ldp, j.ldp, r0, j.M, c0, j.N, true);
         else
-          epilogue<kEpi, kF32>(g, j, buf, lane, a, a2, r0, c0);
+          epilogue<kEpi, kAct, kF32>(g, j, buf, lane, a, a2, r0, c0);
       }
       tc_fence_before();
       __syncwarp();
@@ -648,7 +634,7 @@ double kblock_ns(int cta, int n_tile) {
   return std::max(mma, (kABytes + n_tile / cta * 128.0) / 100.0);
 }
 
-template <int kCta, int kEpi, bool kF32>
+template <int kCta, int kEpi, int kAct, bool kF32>
 cudaError_t launch(const ProdArgs& a, int max_clusters, cudaStream_t st) {
   const int stage_bytes = kABytes + a.n_tile / kCta * 128;
   const int smem = a.stages * stage_bytes + kEpiWarps * kBufBytes + (int)sizeof(Tail) + 1024;
@@ -665,12 +651,32 @@ cudaError_t launch(const ProdArgs& a, int max_clusters, cudaStream_t st) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = kCta == 2 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_prod<kCta, kEpi, kF32>, a);
+  return cudaLaunchKernelEx(&cfg, k_prod<kCta, kEpi, kAct, kF32>, a);
 }
 
-template <int kCta, int kEpi, bool kF32>
-cudaError_t allow_smem() {
-  return cudaFuncSetAttribute(k_prod<kCta, kEpi, kF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+// The kernels that launches choose from: f(kernel's constants).
+template <typename F>
+cudaError_t with_kernel(int cta, int epi, int act, bool f32, F f) {
+  auto cta_of = [&](auto e, auto a, auto t) {
+    if (cta == 2) return f(std::integral_constant<int, 2>(), e, a, t);
+    return f(std::integral_constant<int, 1>(), e, a, t);
+  };
+  auto type_of = [&](auto e, auto a) {
+    // 32-bit operands take tiles of one CTA only (prod_plan)
+    if (f32) {
+      if constexpr (e.value != kEpiQuant) return f(std::integral_constant<int, 1>(), e, a, std::true_type());
+      else return cta_of(e, a, std::true_type());
+    }
+    return cta_of(e, a, std::false_type());
+  };
+  using None = std::integral_constant<int, -1>;
+  using Gated = std::integral_constant<int, kEpiGated>;
+  if (epi == kEpiPlain) return type_of(std::integral_constant<int, kEpiPlain>(), None());
+  if (epi == kEpiDgated) return type_of(std::integral_constant<int, kEpiDgated>(), None());
+  if (epi == kEpiQuant) return type_of(std::integral_constant<int, kEpiQuant>(), None());
+  if (act == TP_ACT_RELU) return type_of(Gated(), std::integral_constant<int, TP_ACT_RELU>());
+  if (act == TP_ACT_SILU) return type_of(Gated(), std::integral_constant<int, TP_ACT_SILU>());
+  return type_of(Gated(), std::integral_constant<int, TP_ACT_GELU>());
 }
 
 constexpr int kMaxDevices = 64;
@@ -691,14 +697,14 @@ cudaError_t device_state(DeviceState* out) {
   DeviceState& d = g_dev[dev];
   if (!d.ready) {
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    if ((e = allow_smem<1, kEpiPlain, false>()) != cudaSuccess || (e = allow_smem<2, kEpiPlain, false>()) != cudaSuccess ||
-        (e = allow_smem<1, kEpiPlain, true>()) != cudaSuccess || (e = allow_smem<1, kEpiGated, false>()) != cudaSuccess ||
-        (e = allow_smem<2, kEpiGated, false>()) != cudaSuccess || (e = allow_smem<1, kEpiGated, true>()) != cudaSuccess ||
-        (e = allow_smem<1, kEpiDgated, false>()) != cudaSuccess || (e = allow_smem<2, kEpiDgated, false>()) != cudaSuccess ||
-        (e = allow_smem<1, kEpiDgated, true>()) != cudaSuccess || (e = allow_smem<1, kEpiQuant, false>()) != cudaSuccess ||
-        (e = allow_smem<2, kEpiQuant, false>()) != cudaSuccess || (e = allow_smem<1, kEpiQuant, true>()) != cudaSuccess ||
-        (e = allow_smem<2, kEpiQuant, true>()) != cudaSuccess)
-      return e;
+    auto allow = [](auto c, auto k, auto a, auto t) {
+      return cudaFuncSetAttribute(k_prod<c.value, k.value, a.value, t.value>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  kSmemMax);
+    };
+    for (int v = 0; v < 4 * 3 * 4; ++v) {   // CTAs and type, activation, epilogue
+      const int epi = v & 3, act = (v >> 2) % 3, ct = (v >> 2) / 3;
+      if ((e = with_kernel(1 + (ct & 1), epi, act, ct >> 1, allow)) != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * d.sms);
     cfg.blockDim = dim3(kThreads);
@@ -709,7 +715,7 @@ cudaError_t device_state(DeviceState* out) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if ((e = cudaOccupancyMaxActiveClusters(&d.pairs, (void*)k_prod<2, kEpiGated, false>, &cfg)) != cudaSuccess) return e;
+    if ((e = cudaOccupancyMaxActiveClusters(&d.pairs, (void*)k_prod<2, kEpiPlain, -1, false>, &cfg)) != cudaSuccess) return e;
     d.ready = true;
   }
   *out = d;
@@ -729,9 +735,14 @@ tp_status ops_fail(tp_status s, const char* fmt, ...) {
 }
 
 tp_status ops_device() {
+  static std::atomic<bool> found{false};
+  if (found.load(std::memory_order_relaxed)) return TP_OK;
   int n = 0;
   const cudaError_t e = cudaGetDeviceCount(&n);
-  if (e == cudaSuccess && n > 0) return TP_OK;
+  if (e == cudaSuccess && n > 0) {
+    found.store(true, std::memory_order_relaxed);
+    return TP_OK;
+  }
   cudaGetLastError();
   return ops_fail(TP_ECUDA, "no CUDA device: %s", cudaGetErrorString(e));
 }
@@ -816,7 +827,7 @@ cudaError_t prod_run(ProdLaunch& l, void* partial, cudaStream_t st, const char**
   JoinArgs join;
   join.n_jobs = 0, join.epi = l.epi;
   Carver c(partial);
-  a.n_jobs = l.n_jobs, a.n_tiles = l.n_tiles, a.act = l.act, a.fp16 = l.fp16, a.f32 = l.f32, a.n_tile = l.n_tile;
+  a.n_jobs = l.n_jobs, a.n_tiles = l.n_tiles, a.fp16 = l.fp16, a.n_tile = l.n_tile;
   a.chains = l.chains, a.stages = stage_count(l.cta, l.n_tile);
   bool done[kProdMaps] = {};
   int64_t join_work = 0;
@@ -837,19 +848,9 @@ cudaError_t prod_run(ProdLaunch& l, void* partial, cudaStream_t st, const char**
   }
   *what = "product launch";
   const int clusters = l.cta == 2 ? dev.pairs : dev.sms;
-  if (l.epi == kEpiPlain)
-    e = l.f32 ? launch<1, kEpiPlain, true>(a, clusters, st)
-              : l.cta == 2 ? launch<2, kEpiPlain, false>(a, clusters, st) : launch<1, kEpiPlain, false>(a, clusters, st);
-  else if (l.epi == kEpiGated)
-    e = l.f32 ? launch<1, kEpiGated, true>(a, clusters, st)
-              : l.cta == 2 ? launch<2, kEpiGated, false>(a, clusters, st) : launch<1, kEpiGated, false>(a, clusters, st);
-  else if (l.epi == kEpiDgated)
-    e = l.f32 ? launch<1, kEpiDgated, true>(a, clusters, st)
-              : l.cta == 2 ? launch<2, kEpiDgated, false>(a, clusters, st) : launch<1, kEpiDgated, false>(a, clusters, st);
-  else if (l.cta == 2)
-    e = l.f32 ? launch<2, kEpiQuant, true>(a, clusters, st) : launch<2, kEpiQuant, false>(a, clusters, st);
-  else
-    e = l.f32 ? launch<1, kEpiQuant, true>(a, clusters, st) : launch<1, kEpiQuant, false>(a, clusters, st);
+  e = with_kernel(l.cta, l.epi, l.act, l.f32, [&](auto c, auto k, auto a_, auto t) {
+    return launch<c.value, k.value, a_.value, t.value>(a, clusters, st);
+  });
   if (e == cudaSuccess && join.n_jobs) {
     *what = "join launch";
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(join_work, 256), kSms * 8), join.n_jobs);

@@ -5,6 +5,7 @@
 // through them as fp16, in which every int8 and every product of two is
 // exact, with fp32 accumulators: sums are exact below 2^24.
 #include "prod.cuh"
+#include "rows.cuh"
 
 using namespace tp;
 
@@ -57,11 +58,18 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
   if (ldq < k) return ops_fail(TP_EINVAL, "ldq %lld is less than k %d", (long long)ldq, k);
   if (rows == 0) return TP_OK;
   if (!q || !scale || !w || !w_scale || !y) return ops_fail(TP_EINVAL, "null argument");
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (rows_fit(rows, q, ldq, w, k, 1)) {   // a few rows: the weights stream past them
+    if ((s = ops_device()) != TP_OK) return s;
+    const cudaError_t e = rows_quant(q, ldq, scale, w, w_scale, bias, rows, k, n, precision == TP_FP32, y, st);
+    if (e == cudaSuccess) return TP_OK;
+    cudaGetLastError();   // reported here
+    return ops_fail(TP_ECUDA, "pack_product_q8: %s", cudaGetErrorString(e));
+  }
   Work o(rows, k, n, precision);
   if (workspace_bytes < o.bytes || !workspace || ((uintptr_t)workspace & 255))
     return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)o.bytes);
   if ((s = ops_device()) != TP_OK) return s;
-  cudaStream_t st = (cudaStream_t)cuda_stream;
   char* x16 = (char*)workspace;
   char* w16 = x16 + o.qx;
   StageLaunch sl;

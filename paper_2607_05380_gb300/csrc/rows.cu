@@ -1,0 +1,239 @@
+// rows.cu -- the products of a few rows (a serving call): y[m, n] = sum_k
+// x[m, k] w[n, k] with one epilogue, for the gated block's two products (bf16)
+// and the 8-bit product (int8 as fp16, exact).
+//
+// Bound by the weights' bytes: each is read once, straight into the registers
+// of the warp that multiplies it, as the 16-row operand of mma.sync (the rows
+// of x are its 8 columns); tcgen05 would want the weights in shared memory
+// and 128 rows of x.  A CTA takes 16 output columns (the gated block: 16 pairs) and its
+// eight warps take K in turns of 64; their sums meet in shared memory and are
+// added in a fixed order.  The order of k inside a step is free as long as
+// both operands agree on it, so a lane's elements are 16 consecutive ones:
+// two 16-byte loads (one of int8), with no shuffles.
+//
+// The weights' first steps are asked for (into L2) before the previous kernel
+// of the stream has finished.
+#include "kernels.cuh"
+#include "rows.cuh"
+
+namespace tp {
+namespace {
+
+constexpr int kWarps = 8, kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
+
+enum Mode { kGated, kPlain, kQuant };
+
+struct RowArgs {
+  const void *x, *w;
+  int64_t ldx, up;        // up: elements from a gate row to its up row
+  int32_t rows, k, n;
+  void* out;              // [rows, ldo]
+  int64_t ldo;
+  __nv_bfloat16 *a, *p;   // kGated: act(g), u act'(g) (NULL: not wanted)
+  const float *sx, *sw, *bias;
+  int32_t act, f32;
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Four int8 as two pairs of fp16: 1024 + (v + 128) has v + 128 in its low bits.
+__device__ __forceinline__ void s8_to_f16(uint32_t v, uint32_t& lo, uint32_t& hi) {
+  v ^= 0x80808080u;
+  const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+  uint32_t a = __byte_perm(v, 0x64646464u, 0x4140), b = __byte_perm(v, 0x64646464u, 0x4342);
+  __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+  lo = *reinterpret_cast<uint32_t*>(&x);
+  hi = *reinterpret_cast<uint32_t*>(&y);
+}
+
+// A lane's 16 elements from element k on, as eight pairs; zeros past K.
+template <int kMode>
+__device__ __forceinline__ void load16(const void* row, int k, int K, bool ok, uint4 (&v)[2]) {
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  if constexpr (kMode == kQuant) {
+    v[0] = ok && k < K ? *reinterpret_cast<const uint4*>((const int8_t*)row + k) : zero;
+  } else {
+    const uint4* p = reinterpret_cast<const uint4*>((const __nv_bfloat16*)row + k);
+    v[0] = ok && k < K ? p[0] : zero;
+    v[1] = ok && k + 8 < K ? p[1] : zero;
+  }
+}
+template <int kMode>
+__device__ __forceinline__ void pairs(const uint4 (&v)[2], uint32_t (&r)[8]) {
+  if constexpr (kMode == kQuant) {
+    s8_to_f16(v[0].x, r[0], r[1]);
+    s8_to_f16(v[0].y, r[2], r[3]);
+    s8_to_f16(v[0].z, r[4], r[5]);
+    s8_to_f16(v[0].w, r[6], r[7]);
+  } else {
+    r[0] = v[0].x, r[1] = v[0].y, r[2] = v[0].z, r[3] = v[0].w;
+    r[4] = v[1].x, r[5] = v[1].y, r[6] = v[1].z, r[7] = v[1].w;
+  }
+}
+
+// kNT: groups of eight rows of x; kAct: of the gated block.
+template <int kMode, int kNT, int kAct>
+__global__ void __launch_bounds__(32 * kWarps) k_rows(const RowArgs g) {
+  constexpr int kR = kMode == kGated ? 2 : 1;           // 16-row tiles of the weights
+  constexpr int kTok = 8 * kNT, kBytes = kMode == kQuant ? 1 : 2;
+  __shared__ float red[kWarps][kR][kTok][kStride];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16;
+  pdl_trigger();
+  const char* w = (const char*)g.w;
+  int64_t at[kR][2];                                     // byte offsets of the lane's two rows of each tile
+  bool ok[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = n0 + gid + 8 * h;
+    ok[h] = r < g.n;
+#pragma unroll
+    for (int q = 0; q < kR; ++q) at[q][h] = ((int64_t)(ok[h] ? r : 0) * g.k + q * g.up) * kBytes;
+  }
+  const int blocks = (g.k + 63) >> 6;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int k = 64 * (warp + kWarps * s) + 16 * t;
+    if (k < g.k) {
+#pragma unroll
+      for (int q = 0; q < kR; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(w + at[q][h] + (int64_t)k * kBytes));
+    }
+  }
+  pdl_wait();
+  float acc[kR][kNT][4];
+#pragma unroll
+  for (int q = 0; q < kR; ++q)
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[q][j][e] = 0.f;
+
+  // two steps at a time where the registers allow it: their loads are in flight together
+  constexpr int kS = kNT <= 2 ? 2 : 1;
+  for (int b = warp; b < blocks; b += kS * kWarps) {
+    uint4 wv[kS][kR][2][2], xv[kS][kNT][2];
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      const int k = 64 * (b + kWarps * s) + 16 * t;
+#pragma unroll
+      for (int q = 0; q < kR; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load16<kMode>(w + at[q][h], k, g.k, ok[h], wv[s][q][h]);
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        const int m = 8 * j + gid;
+        load16<kMode>((const char*)g.x + (int64_t)min(m, g.rows - 1) * g.ldx * kBytes, k, g.k, m < g.rows, xv[s][j]);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      uint32_t r[kR][2][8];
+#pragma unroll
+      for (int q = 0; q < kR; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) pairs<kMode>(wv[s][q][h], r[q][h]);
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        uint32_t x[8];
+        pairs<kMode>(xv[s][j], x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int q = 0; q < kR; ++q) {
+            const uint32_t a[4] = {r[q][0][2 * i], r[q][1][2 * i], r[q][0][2 * i + 1], r[q][1][2 * i + 1]};
+            if constexpr (kMode == kQuant) mma_f16(acc[q][j], a, x[2 * i], x[2 * i + 1]);
+            else mma_bf16(acc[q][j], a, x[2 * i], x[2 * i + 1]);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < kR; ++q)
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+      red[warp][q][8 * j + 2 * t][gid] = acc[q][j][0];
+      red[warp][q][8 * j + 2 * t + 1][gid] = acc[q][j][1];
+      red[warp][q][8 * j + 2 * t][gid + 8] = acc[q][j][2];
+      red[warp][q][8 * j + 2 * t + 1][gid + 8] = acc[q][j][3];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * kTok; i += 32 * kWarps) {
+    const int m = i >> 4, c = i & 15, n = n0 + c;
+    if (m >= g.rows || n >= g.n) continue;
+    float s[kR];
+#pragma unroll
+    for (int q = 0; q < kR; ++q) {
+      s[q] = red[0][q][m][c];
+#pragma unroll
+      for (int v = 1; v < kWarps; ++v) s[q] += red[v][q][m][c];
+    }
+    const int64_t o = (int64_t)m * g.ldo + n;
+    if constexpr (kMode == kGated) {
+      float d;
+      const float a = act_value<kAct, false>(s[0], d);
+      ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(a * s[kR - 1]);
+      if (g.a) {
+        g.a[o] = __float2bfloat16_rn(a);
+        g.p[o] = __float2bfloat16_rn(s[kR - 1] * d);
+      }
+    } else {
+      float v = s[0];
+      if constexpr (kMode == kQuant) v = v * g.sx[m] * g.sw[n] + (g.bias ? g.bias[n] : 0.f);
+      if (g.f32) ((float*)g.out)[o] = v;
+      else ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(v);
+    }
+  }
+}
+
+template <int kMode, int kAct>
+cudaError_t start(const RowArgs& a, cudaStream_t st) {
+  const dim3 grid((unsigned)ceil_div(a.n, 16)), block(32 * kWarps);
+  if (a.rows <= 8) launch_pdl(k_rows<kMode, 1, kAct>, grid, block, 0, st, a);
+  else if (a.rows <= 16) launch_pdl(k_rows<kMode, 2, kAct>, grid, block, 0, st, a);
+  else launch_pdl(k_rows<kMode, 4, kAct>, grid, block, 0, st, a);
+  return cudaGetLastError();
+}
+
+bool fits(const void* p, int64_t bytes) { return ((uintptr_t)p & 15) == 0 && bytes % 16 == 0; }
+
+}  // namespace
+
+bool rows_fit(int64_t rows, const void* x, int64_t ldx, const void* w, int32_t k, int elem) {
+  return rows <= kFewRows && fits(x, ldx * elem) && fits(w, (int64_t)k * elem);
+}
+
+cudaError_t rows_gated(const void* x, int64_t ldx, const void* w_gu, int64_t rows, int32_t d, int32_t f, int act, void* h,
+                       int64_t ldh, void* a, void* p, cudaStream_t st) {
+  const RowArgs r{x, w_gu, ldx, (int64_t)f * d, (int32_t)rows, d, f, h, ldh, (__nv_bfloat16*)a, (__nv_bfloat16*)p,
+                  nullptr, nullptr, nullptr, act, 0};
+  if (act == TP_ACT_RELU) return start<kGated, TP_ACT_RELU>(r, st);
+  if (act == TP_ACT_SILU) return start<kGated, TP_ACT_SILU>(r, st);
+  return start<kGated, TP_ACT_GELU>(r, st);
+}
+
+cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, void* y, cudaStream_t st) {
+  return start<kPlain, -1>(RowArgs{x, w, ldx, 0, (int32_t)rows, k, n, y, n, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0}, st);
+}
+
+cudaError_t rows_quant(const int8_t* q, int64_t ldq, const float* sx, const int8_t* w, const float* sw, const float* bias,
+                       int64_t rows, int32_t k, int32_t n, bool f32, void* y, cudaStream_t st) {
+  return start<kQuant, -1>(RowArgs{q, w, ldq, 0, (int32_t)rows, k, n, y, n, nullptr, nullptr, sx, sw, bias, 0, f32}, st);
+}
+
+}  // namespace tp
