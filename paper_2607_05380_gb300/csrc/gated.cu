@@ -26,10 +26,9 @@ struct Geo {
   int32_t d, f, d_out;
   bool f32;
   int parts;                     // bf16 parts of an operand
-  int64_t ldd, ldf, ldo;         // pitches of staged matrices
+  int64_t ldf;                   // pitch of h, act(g), u act'(g) and their gradients: whole 32-byte sectors
   Geo(int64_t r, int32_t d_, int32_t f_, int32_t o, int32_t prec)
-      : rows(r), d(d_), f(f_), d_out(o), f32(prec == TP_FP32), parts(f32 ? 3 : 1), ldd(round_up(d_, 8)),
-        ldf(round_up(f_, 8)), ldo(round_up(o, 8)) {}
+      : rows(r), d(d_), f(f_), d_out(o), f32(prec == TP_FP32), parts(f32 ? 3 : 1), ldf(round_up(f_, 16)) {}
 };
 
 // What a forward pass keeps: h as bf16 parts, act(g) and u act'(g) in the
@@ -46,6 +45,10 @@ struct Saved {
     bytes = c.used;
   }
 };
+
+bool by_rows(const Geo& g) {
+  return !g.f32 && rows_take(g.rows, (int64_t)g.f * (2 * (int64_t)g.d + g.d_out), 2 * ((int64_t)g.d | g.f), false);
+}
 
 constexpr int32_t kMaxDim = 1 << 17;
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;
@@ -179,7 +182,7 @@ tp_status pack_gated_bytes(int64_t rows, int32_t d, int32_t f, int32_t d_out, in
     const ProdOperand wd = st.operand(nullptr, f, d_out, f, 1);
     Plans p;
     plan_forward(p, g, 0, x, wgu, wd, sv, false, nullptr);
-    *forward = rows ? c.used + plan(p) : 0;
+    *forward = rows == 0 ? 0 : by_rows(g) ? sv.h_bytes : c.used + plan(p);
   }
   if (backward) {
     Carver c(nullptr);
@@ -211,7 +214,7 @@ tp_status pack_gated_forward(const void* x, int64_t ldx, const void* w_gate_up, 
   const Saved sv(g, saved ? saved : own);
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   // a few rows: the weights stream past them, twice, with nothing in between
-  if (!g.f32 && f % 8 == 0 && rows_fit(rows, x, ldx, w_gate_up, d, 2) && rows_fit(rows, sv.h, g.ldf, w_down, f, 2)) {
+  if (by_rows(g)) {
     if (workspace_bytes < c.used) return ops_fail(TP_EINVAL, "a workspace of %lld bytes is needed", (long long)c.used);
     if ((s = ops_device()) != TP_OK) return s;
     cudaError_t e = rows_gated(x, ldx, w_gate_up, rows, d, f, act, sv.h, g.ldf, saved ? sv.a : nullptr,

@@ -82,6 +82,24 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
       : "memory");
 }
 
+// A warp's 32 lanes x 32 columns of TMEM; the values are there after tmem_wait
+// and may be used once tmem_got has tied them to it.
+__device__ __forceinline__ void tmem_ask32(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_got(uint32_t (&v)[32]) {
+#pragma unroll
+  for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(v[e]));
+}
+
 // A tile's place: job, output origin and K blocks.
 struct Tile {
   int job, m0, n0, kb0, kbn, split;
@@ -164,57 +182,91 @@ __device__ __forceinline__ void emit_f32(uint8_t* buf, int lane, const float (&v
     }
   }
 }
+// Eight words of a lane's own row: a whole 32-byte sector (address a multiple of 32).
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void load32(const void* p, uint32_t* w) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+// A lane's 32 columns of its row straight to memory, in whole sectors: `out`
+// is row r's column c0.  Columns from n on are written too where n is not a
+// multiple of a sector's elements: rows have room for whole sectors.
+__device__ __forceinline__ void put_bf16(const uint32_t (&pk)[16], __nv_bfloat16* out, bool live, int n) {
+  if (!live) return;
+  store32(out, pk);
+  if (n > 16) store32(out + 16, pk + 8);
+}
+__device__ __forceinline__ void put_f32(const float (&v)[32], float* out, bool live, int n) {
+  if (!live) return;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * s + e]);
+    if (n > 8 * s) store32(out + 8 * s, w);
+  }
+}
+__device__ __forceinline__ void pack32(const float (&v)[32], uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+}
 // fp32 values as one bf16 number each, or as three whose sum they are
-// (buffers `part` elements apart).
-__device__ __forceinline__ void emit_parts(uint8_t* buf, int lane, float (&v)[32], bool three, __nv_bfloat16* out,
-                                           int64_t part, int64_t ld, int r0, int m_lim, int c0, int n_lim, bool vec) {
+// (buffers `part` elements apart), into rows with room for whole sectors.
+template <bool kThree>
+__device__ __forceinline__ void put_parts(float (&v)[32], __nv_bfloat16* out, int64_t part, bool live, int n) {
   uint32_t pk[16];
 #pragma unroll 1
-  for (int q = 0; q < (three ? 3 : 1); ++q) {
+  for (int q = 0; q < (kThree ? 3 : 1); ++q) {
+    pack32(v, pk);
+    put_bf16(pk, out + q * part, live, n);
+    if constexpr (kThree) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      pk[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-      v[2 * e] -= __uint_as_float(pk[e] << 16);
-      v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
+      for (int e = 0; e < 16; ++e) {
+        v[2 * e] -= __uint_as_float(pk[e] << 16);
+        v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
+      }
     }
-    emit_bf16(buf, lane, pk, out + q * part, ld, r0, m_lim, c0, n_lim, vec);
   }
 }
 
-// 32 values of a row (fp32 or bf16) from column c0 on, zeros past n_lim.
-template <bool kF32>
-__device__ __forceinline__ void load_row(const void* base, int64_t at, int c0, int n_lim, float (&v)[32]) {
-  if constexpr (kF32) {
-    const float* p = (const float*)base + at + c0;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      // the pitch is a multiple of 8 elements: whole groups may be read
-      const float4 w = c0 + 4 * s < n_lim ? *reinterpret_cast<const float4*>(p + 4 * s) : make_float4(0.f, 0.f, 0.f, 0.f);
-      v[4 * s] = w.x, v[4 * s + 1] = w.y, v[4 * s + 2] = w.z, v[4 * s + 3] = w.w;
+// What the epilogue reads besides the accumulator: kEpiDgated of a bf16 block,
+// u act'(g) and act(g) of the lane's row, asked for one chunk ahead.
+struct Ahead {
+  uint32_t p[16], a[16];
+  __device__ __forceinline__ void load(const ProdJob& j, int row, int c0) {
+    const int64_t at = (int64_t)min(row, j.M - 1) * j.ldo + c0;
+    const __nv_bfloat16 *pp = (const __nv_bfloat16*)j.p + at, *pa = (const __nv_bfloat16*)j.a + at;
+    load32(pp, p);
+    load32(pa, a);
+    if (c0 + 16 < j.N) {   // (a row has room for whole sectors)
+      load32(pp + 16, p + 8);
+      load32(pa + 16, a + 8);
     }
-  } else {
-    const __nv_bfloat16* p = (const __nv_bfloat16*)base + at + c0;
+  }
+};
+__device__ __forceinline__ void times(float (&f)[32], const uint32_t (&w)[16], const float (&acc)[32]) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const uint4 w = c0 + 8 * s < n_lim ? *reinterpret_cast<const uint4*>(p + 8 * s) : make_uint4(0u, 0u, 0u, 0u);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[8 * s + 2 * e] = __uint_as_float(u[e] << 16);
-        v[8 * s + 2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
-      }
-    }
+  for (int e = 0; e < 16; ++e) {
+    f[2 * e] = __uint_as_float(w[e] << 16) * acc[2 * e];
+    f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * acc[2 * e + 1];
   }
 }
 
 // The epilogue of one 32 x 32 chunk; acc: its accumulator (kEpiGated: the
 // gate product), acc2: the up product.
 template <int kEpi, int kAct, bool kF32>
-__device__ __forceinline__ void epilogue(const ProdArgs& g, const ProdJob& j, uint8_t* buf, int lane, float (&acc)[32],
-                                         float (&acc2)[32], int r0, int c0) {
-  const int row = r0 + lane;
+__device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lane, float (&acc)[32], float (&acc2)[32],
+                                         const Ahead& ah, int r0, int c0) {
+  const int row = r0 + lane, n = j.N - c0;
+  const bool live = row < j.M;
+  const int64_t at = (int64_t)row * j.ldo + c0;
   if constexpr (kEpi == kEpiGated) {
-    const bool keep = j.a != nullptr;
     float da[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) {
@@ -224,39 +276,58 @@ __device__ __forceinline__ void epilogue(const ProdArgs& g, const ProdJob& j, ui
       acc2[e] *= a;
       acc[e] = a;
     }
-    if (keep) {
+    if (j.a != nullptr) {
       if constexpr (kF32) {
-        emit_f32(buf, lane, acc, (float*)j.a, j.ldo, r0, j.M, c0, j.N, true);
-        emit_f32(buf, lane, da, (float*)j.p, j.ldo, r0, j.M, c0, j.N, true);
+        put_f32(acc, (float*)j.a + at, live, n);
+        put_f32(da, (float*)j.p + at, live, n);
       } else {
-        emit_parts(buf, lane, acc, false, (__nv_bfloat16*)j.a, 0, j.ldo, r0, j.M, c0, j.N, true);
-        emit_parts(buf, lane, da, false, (__nv_bfloat16*)j.p, 0, j.ldo, r0, j.M, c0, j.N, true);
+        put_parts<false>(acc, (__nv_bfloat16*)j.a + at, 0, live, n);
+        put_parts<false>(da, (__nv_bfloat16*)j.p + at, 0, live, n);
       }
     }
-    emit_parts(buf, lane, acc2, kF32, (__nv_bfloat16*)j.out, j.part, j.ldo, r0, j.M, c0, j.N, true);
+    put_parts<kF32>(acc2, (__nv_bfloat16*)j.out + at, j.part, live, n);
   } else if constexpr (kEpi == kEpiDgated) {
     float f[32];
-    const int64_t at = (int64_t)min(row, j.M - 1) * j.ldo;
-    load_row<kF32>(j.p, at, c0, j.N, f);
+    __nv_bfloat16* out = (__nv_bfloat16*)j.out + at;
+    if constexpr (kF32) {
+      const int64_t from = (int64_t)min(row, j.M - 1) * j.ldo + c0;
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        const float* src = (const float*)(h ? j.a : j.p) + from;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) f[e] *= acc[e];
-    emit_parts(buf, lane, f, kF32, (__nv_bfloat16*)j.out, j.part, j.ldo, r0, j.M, c0, j.N, true);
-    load_row<kF32>(j.a, at, c0, j.N, f);
+        for (int s = 0; s < 4; ++s) {
+          uint32_t w[8] = {};
+          if (n > 8 * s) load32(src + 8 * s, w);
 #pragma unroll
-    for (int e = 0; e < 32; ++e) f[e] *= acc[e];
-    emit_parts(buf, lane, f, kF32, (__nv_bfloat16*)j.out + j.half, j.part, j.ldo, r0, j.M, c0, j.N, true);
+          for (int e = 0; e < 8; ++e) f[8 * s + e] = __uint_as_float(w[e]) * acc[8 * s + e];
+        }
+        put_parts<true>(f, out + h * j.half, j.part, live, n);
+      }
+    } else {
+      times(f, ah.p, acc);
+      put_parts<false>(f, out, 0, live, n);
+      times(f, ah.a, acc);
+      put_parts<false>(f, out + j.half, 0, live, n);
+    }
   } else {
     if constexpr (kEpi == kEpiQuant) {
-      const float sx = row < j.M ? j.sx[row] : 0.f;
+      const float sx = live ? j.sx[row] : 0.f;
       const int c = c0 + lane;
       const float sw = c < j.N ? j.sw[c] : 0.f, b = c < j.N && j.bias ? j.bias[c] : 0.f;
 #pragma unroll
       for (int e = 0; e < 32; ++e)
         acc[e] = acc[e] * sx * __shfl_sync(0xffffffffu, sw, e) + __shfl_sync(0xffffffffu, b, e);
     }
-    const bool vec = vec_ok(j.out, j.ldo, kF32 ? 4 : 2);
-    if constexpr (kF32) emit_f32(buf, lane, acc, (float*)j.out, j.ldo, r0, j.M, c0, j.N, vec);
-    else emit_parts(buf, lane, acc, false, (__nv_bfloat16*)j.out, 0, j.ldo, r0, j.M, c0, j.N, vec);
+    // whole sectors where the rows lie on them, else through the warp's buffer
+    if constexpr (kF32) {
+      if (n >= 32 && ((uintptr_t)j.out & 31) == 0 && (j.ldo & 7) == 0) put_f32(acc, (float*)j.out + at, live, n);
+      else emit_f32(buf, lane, acc, (float*)j.out, j.ldo, r0, j.M, c0, j.N, vec_ok(j.out, j.ldo, 4));
+    } else {
+      uint32_t pk[16];
+      pack32(acc, pk);
+      if (n >= 32 && ((uintptr_t)j.out & 31) == 0 && (j.ldo & 15) == 0) put_bf16(pk, (__nv_bfloat16*)j.out + at, live, n);
+      else emit_bf16(buf, lane, pk, (__nv_bfloat16*)j.out, j.ldo, r0, j.M, c0, j.N, vec_ok(j.out, j.ldo, 2));
+    }
   }
 }
 
@@ -429,39 +500,53 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     for (int t = clu; t < g.n_tiles; t += n_clu) {
       const Tile u = tile_at<kCta>(g, t);
       const ProdJob& j = g.job[u.job];
+      const int r0 = u.m0 + rank * 128 + 32 * q;
+      Ahead ahead;
+      constexpr bool kAhead = kEpi == kEpiDgated && !kF32;
+      if constexpr (kAhead)
+        if (r0 < j.M && u.n0 * cols + 32 * half < j.N) ahead.load(j, r0 + lane, u.n0 * cols + 32 * half);
       if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[acc], acc_phase, abort_flag, err, 2 * kWaitNs, 46))) break;
       tc_fence_after();
       const uint32_t ta = tmem + ((uint32_t)(32 * q) << 16) + acc * kAccCols;
-      const int r0 = u.m0 + rank * 128 + 32 * q;
       const bool second = g.chains == 2 && u.kbn > 1;
 #pragma unroll 1
       for (int c = 32 * half; c < cols; c += 64) {
-        uint32_t v[32];
+        const int c0 = u.n0 * cols + c;
+        if (r0 >= j.M || c0 >= j.N) break;   // warp-uniform
+        uint32_t v[32], v2[32];
         float a[32], a2[32];
-        tmem_ld32(ta + c, v);
+        tmem_ask32(ta + c, v);
+        if constexpr (kEpi == kEpiGated) tmem_ask32(ta + cols + c, v2);
+        tmem_wait();
+        tmem_got(v);
+        if constexpr (kEpi == kEpiGated) tmem_got(v2);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) a[e] = __uint_as_float(v[e]);
-        if (second) {
-          tmem_ld32(ta + kAccCols / 2 + c, v);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) a[e] += __uint_as_float(v[e]);
+        for (int e = 0; e < 32; ++e) {
+          a[e] = __uint_as_float(v[e]);
+          if constexpr (kEpi == kEpiGated) a2[e] = __uint_as_float(v2[e]);
         }
-        if constexpr (kEpi == kEpiGated) {
-          tmem_ld32(ta + cols + c, v);
+        if (second) {
+          tmem_ask32(ta + kAccCols / 2 + c, v);
+          if constexpr (kEpi == kEpiGated) tmem_ask32(ta + kAccCols / 2 + cols + c, v2);
+          tmem_wait();
+          tmem_got(v);
+          if constexpr (kEpi == kEpiGated) tmem_got(v2);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) a2[e] = __uint_as_float(v[e]);
-          if (second) {
-            tmem_ld32(ta + kAccCols / 2 + cols + c, v);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) a2[e] += __uint_as_float(v[e]);
+          for (int e = 0; e < 32; ++e) {
+            a[e] += __uint_as_float(v[e]);
+            if constexpr (kEpi == kEpiGated) a2[e] += __uint_as_float(v2[e]);
           }
         }
-        const int c0 = u.n0 * cols + c;
-        if (r0 >= j.M || c0 >= j.N) continue;   // warp-uniform
-        if (j.splits > 1)
+        if (j.splits > 1) {
           emit_f32(buf, lane, a, j.partial + (int64_t)u.split * j.M * j.ldp, j.ldp, r0, j.M, c0, j.N, true);
-        else
-          epilogue<kEpi, kAct, kF32>(g, j, buf, lane, a, a2, r0, c0);
+          continue;
+        }
+        Ahead now;
+        if constexpr (kAhead) {
+          now = ahead;
+          if (c + 64 < cols && c0 + 64 < j.N) ahead.load(j, r0 + lane, c0 + 64);
+        }
+        epilogue<kEpi, kAct, kF32>(j, buf, lane, a, a2, now, r0, c0);
       }
       tc_fence_before();
       __syncwarp();

@@ -46,7 +46,7 @@ tp_status pack_product_q8_bytes(int64_t rows, int32_t k, int32_t n, int32_t prec
   const tp_status s = check(rows, k, n, precision);
   if (s != TP_OK) return s;
   if (!workspace) return ops_fail(TP_EINVAL, "null argument");
-  *workspace = rows ? Work(rows, k, n, precision).bytes : 0;
+  *workspace = rows == 0 || rows_take(rows, (int64_t)k * n, k, true) ? 0 : Work(rows, k, n, precision).bytes;
   return TP_OK;
 }
 
@@ -59,7 +59,7 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
   if (rows == 0) return TP_OK;
   if (!q || !scale || !w || !w_scale || !y) return ops_fail(TP_EINVAL, "null argument");
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (rows_fit(rows, q, ldq, w, k, 1)) {   // a few rows: the weights stream past them
+  if (rows_take(rows, (int64_t)k * n, k, true)) {   // a few rows: the weights stream past them
     if ((s = ops_device()) != TP_OK) return s;
     const cudaError_t e = rows_quant(q, ldq, scale, w, w_scale, bias, rows, k, n, precision == TP_FP32, y, st);
     if (e == cudaSuccess) return TP_OK;

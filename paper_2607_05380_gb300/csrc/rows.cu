@@ -5,21 +5,23 @@
 // Bound by the weights' bytes: each is read once, straight into the registers
 // of the warp that multiplies it, as the 16-row operand of mma.sync (the rows
 // of x are its 8 columns); tcgen05 would want the weights in shared memory
-// and 128 rows of x.  A CTA takes 16 output columns (the gated block: 16 pairs) and its
-// eight warps take K in turns of 64; their sums meet in shared memory and are
-// added in a fixed order.  The order of k inside a step is free as long as
-// both operands agree on it, so a lane's elements are 16 consecutive ones:
-// two 16-byte loads (one of int8), with no shuffles.
+// and 128 rows of x.  A CTA takes 16 or 32 output columns (the gated block: 16
+// pairs) and up to 32 rows of x; its eight or sixteen warps take K in turns of
+// 64; their sums meet in shared memory and are added in a fixed order.  The
+// order of k inside a turn is free as long as both operands agree on it, so a
+// lane's 16 elements are those of two 16-byte loads (one of int8), which the
+// four lanes of a row make of whole sectors, with no shuffles.
 //
 // The weights' first steps are asked for (into L2) before the previous kernel
 // of the stream has finished.
 #include "kernels.cuh"
+#include "prod.cuh"
 #include "rows.cuh"
 
 namespace tp {
 namespace {
 
-constexpr int kWarps = 8, kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
+constexpr int kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
 
 enum Mode { kGated, kPlain, kQuant };
 
@@ -59,16 +61,41 @@ __device__ __forceinline__ void s8_to_f16(uint32_t v, uint32_t& lo, uint32_t& hi
   hi = *reinterpret_cast<uint32_t*>(&y);
 }
 
-// A lane's 16 elements from element k on, as eight pairs; zeros past K.
-template <int kMode>
-__device__ __forceinline__ void load16(const void* row, int k, int K, bool ok, uint4 (&v)[2]) {
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  if constexpr (kMode == kQuant) {
-    v[0] = ok && k < K ? *reinterpret_cast<const uint4*>((const int8_t*)row + k) : zero;
+// 16 bytes, `left` of which lie inside the row, by loads of kLd bytes that the
+// address is a multiple of; zeros past the row.
+template <int kLd>
+__device__ __forceinline__ uint4 bytes16(const char* p, int left) {
+  if constexpr (kLd == 16) {
+    return left > 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
   } else {
-    const uint4* p = reinterpret_cast<const uint4*>((const __nv_bfloat16*)row + k);
-    v[0] = ok && k < K ? p[0] : zero;
-    v[1] = ok && k + 8 < K ? p[1] : zero;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kLd == 4) {
+        w[i] = 4 * i < left ? *reinterpret_cast<const uint32_t*>(p + 4 * i) : 0u;
+      } else if constexpr (kLd == 2) {
+        const uint32_t lo = 4 * i < left ? *reinterpret_cast<const uint16_t*>(p + 4 * i) : 0u;
+        w[i] = lo | (4 * i + 2 < left ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + 4 * i + 2) << 16 : 0u);
+      } else {
+        w[i] = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[i] |= 4 * i + e < left ? (uint32_t)*reinterpret_cast<const uint8_t*>(p + 4 * i + e) << (8 * e) : 0u;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// Lane t's 16 elements of the 64 from element k on; zeros past K.
+template <int kMode, int kLd>
+__device__ __forceinline__ void load16(const char* row, int k, int t, int K, bool ok, uint4 (&v)[2]) {
+  if constexpr (kMode == kQuant) {
+    k += 16 * t;
+    v[0] = bytes16<kLd>(row + k, ok ? K - k : 0);
+  } else {
+    k += 8 * t;
+    v[0] = bytes16<kLd>(row + (int64_t)k * 2, ok ? 2 * (K - k) : 0);
+    v[1] = bytes16<kLd>(row + (int64_t)k * 2 + 64, ok ? 2 * (K - k - 32) : 0);
   }
 }
 template <int kMode>
@@ -84,29 +111,31 @@ __device__ __forceinline__ void pairs(const uint4 (&v)[2], uint32_t (&r)[8]) {
   }
 }
 
-// kNT: groups of eight rows of x; kAct: of the gated block.
-template <int kMode, int kNT, int kAct>
-__global__ void __launch_bounds__(32 * kWarps) k_rows(const RowArgs g) {
-  constexpr int kR = kMode == kGated ? 2 : 1;           // 16-row tiles of the weights
-  constexpr int kTok = 8 * kNT, kBytes = kMode == kQuant ? 1 : 2;
+// kR: 16-row tiles of the weights (kGated: gate and up); kNT: groups of eight
+// rows of x; kLd: bytes of a load; kAct: of the gated block.
+template <int kMode, int kR, int kNT, int kWarps, int kLd, int kAct>
+__global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) k_rows(const RowArgs g) {
+  constexpr int kBytes = kMode == kQuant ? 1 : 2, kCols = kMode == kGated ? 16 : 16 * kR;
+  constexpr int kTok = kWarps * kR * kNT > 64 ? 16 : 8 * kNT;   // rows whose sums are joined at a time
   __shared__ float red[kWarps][kR][kTok][kStride];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * kCols, m0 = blockIdx.y * 8 * kNT;
   pdl_trigger();
   const char* w = (const char*)g.w;
   int64_t at[kR][2];                                     // byte offsets of the lane's two rows of each tile
-  bool ok[2];
+  bool ok[kR][2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = n0 + gid + 8 * h;
-    ok[h] = r < g.n;
+  for (int q = 0; q < kR; ++q)
 #pragma unroll
-    for (int q = 0; q < kR; ++q) at[q][h] = ((int64_t)(ok[h] ? r : 0) * g.k + q * g.up) * kBytes;
-  }
+    for (int h = 0; h < 2; ++h) {
+      const int r = n0 + gid + 8 * h + (kMode == kGated ? 0 : 16 * q);
+      ok[q][h] = r < g.n;
+      at[q][h] = ((int64_t)(ok[q][h] ? r : 0) * g.k + (kMode == kGated ? q * g.up : 0)) * kBytes;
+    }
   const int blocks = (g.k + 63) >> 6;
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    const int k = 64 * (warp + kWarps * s) + 16 * t;
+    const int k = 64 * (warp + kWarps * s) + (kMode == kQuant ? 16 : 8) * t;
     if (k < g.k) {
 #pragma unroll
       for (int q = 0; q < kR; ++q)
@@ -130,15 +159,15 @@ __global__ void __launch_bounds__(32 * kWarps) k_rows(const RowArgs g) {
     uint4 wv[kS][kR][2][2], xv[kS][kNT][2];
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const int k = 64 * (b + kWarps * s) + 16 * t;
+      const int k = 64 * (b + kWarps * s);
 #pragma unroll
       for (int q = 0; q < kR; ++q)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) load16<kMode>(w + at[q][h], k, g.k, ok[h], wv[s][q][h]);
+        for (int h = 0; h < 2; ++h) load16<kMode, kLd>(w + at[q][h], k, t, g.k, ok[q][h], wv[s][q][h]);
 #pragma unroll
       for (int j = 0; j < kNT; ++j) {
-        const int m = 8 * j + gid;
-        load16<kMode>((const char*)g.x + (int64_t)min(m, g.rows - 1) * g.ldx * kBytes, k, g.k, m < g.rows, xv[s][j]);
+        const int m = m0 + 8 * j + gid;
+        load16<kMode, kLd>((const char*)g.x + (int64_t)min(m, g.rows - 1) * g.ldx * kBytes, k, t, g.k, m < g.rows, xv[s][j]);
       }
     }
 #pragma unroll
@@ -164,58 +193,88 @@ __global__ void __launch_bounds__(32 * kWarps) k_rows(const RowArgs g) {
     }
   }
 #pragma unroll
-  for (int q = 0; q < kR; ++q)
+  for (int j0 = 0; j0 < kNT; j0 += kTok / 8) {
+    if (j0) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kNT; ++j) {
-      red[warp][q][8 * j + 2 * t][gid] = acc[q][j][0];
-      red[warp][q][8 * j + 2 * t + 1][gid] = acc[q][j][1];
-      red[warp][q][8 * j + 2 * t][gid + 8] = acc[q][j][2];
-      red[warp][q][8 * j + 2 * t + 1][gid + 8] = acc[q][j][3];
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * kTok; i += 32 * kWarps) {
-    const int m = i >> 4, c = i & 15, n = n0 + c;
-    if (m >= g.rows || n >= g.n) continue;
-    float s[kR];
+    for (int q = 0; q < kR; ++q)
 #pragma unroll
-    for (int q = 0; q < kR; ++q) {
-      s[q] = red[0][q][m][c];
-#pragma unroll
-      for (int v = 1; v < kWarps; ++v) s[q] += red[v][q][m][c];
-    }
-    const int64_t o = (int64_t)m * g.ldo + n;
-    if constexpr (kMode == kGated) {
-      float d;
-      const float a = act_value<kAct, false>(s[0], d);
-      ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(a * s[kR - 1]);
-      if (g.a) {
-        g.a[o] = __float2bfloat16_rn(a);
-        g.p[o] = __float2bfloat16_rn(s[kR - 1] * d);
+      for (int j = 0; j < kTok / 8; ++j) {
+        const float(&v)[4] = acc[q][j0 + j];
+        red[warp][q][8 * j + 2 * t][gid] = v[0];
+        red[warp][q][8 * j + 2 * t + 1][gid] = v[1];
+        red[warp][q][8 * j + 2 * t][gid + 8] = v[2];
+        red[warp][q][8 * j + 2 * t + 1][gid + 8] = v[3];
       }
-    } else {
-      float v = s[0];
-      if constexpr (kMode == kQuant) v = v * g.sx[m] * g.sw[n] + (g.bias ? g.bias[n] : 0.f);
-      if (g.f32) ((float*)g.out)[o] = v;
-      else ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(v);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kCols * kTok; i += 32 * kWarps) {
+      const int ml = i / kCols, c = i % kCols, m = m0 + 8 * j0 + ml, n = n0 + c;
+      if (m >= g.rows || n >= g.n) continue;
+      auto sum = [&](int q) {
+        float s = red[0][q][ml][c & 15];
+#pragma unroll
+        for (int v = 1; v < kWarps; ++v) s += red[v][q][ml][c & 15];
+        return s;
+      };
+      const int64_t o = (int64_t)m * g.ldo + n;
+      if constexpr (kMode == kGated) {
+        float d;
+        const float a = act_value<kAct, false>(sum(0), d), u = sum(kR - 1);
+        ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(a * u);
+        if (g.a) {
+          g.a[o] = __float2bfloat16_rn(a);
+          g.p[o] = __float2bfloat16_rn(u * d);
+        }
+      } else {
+        float v = sum(c >> 4);
+        if constexpr (kMode == kQuant) v = v * g.sx[m] * g.sw[n] + (g.bias ? g.bias[n] : 0.f);
+        if (g.f32) ((float*)g.out)[o] = v;
+        else ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(v);
+      }
     }
   }
 }
 
+template <int kMode, int kR, int kWarps, int kLd, int kAct>
+void launch(const RowArgs& a, cudaStream_t st) {
+  const dim3 block(32 * kWarps), grid((unsigned)ceil_div(a.n, kMode == kGated ? 16 : 16 * kR), (unsigned)ceil_div(a.rows, 32));
+  if (a.rows <= 8) launch_pdl(k_rows<kMode, kR, 1, kWarps, kLd, kAct>, grid, block, 0, st, a);
+  else if (a.rows <= 16) launch_pdl(k_rows<kMode, kR, 2, kWarps, kLd, kAct>, grid, block, 0, st, a);
+  else launch_pdl(k_rows<kMode, kR, 4, kWarps, kLd, kAct>, grid, block, 0, st, a);
+}
 template <int kMode, int kAct>
 cudaError_t start(const RowArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)ceil_div(a.n, 16)), block(32 * kWarps);
-  if (a.rows <= 8) launch_pdl(k_rows<kMode, 1, kAct>, grid, block, 0, st, a);
-  else if (a.rows <= 16) launch_pdl(k_rows<kMode, 2, kAct>, grid, block, 0, st, a);
-  else launch_pdl(k_rows<kMode, 4, kAct>, grid, block, 0, st, a);
+  constexpr int kBytes = kMode == kQuant ? 1 : 2, kR = kMode == kGated ? 2 : 1;
+  const uintptr_t low = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)(a.ldx * kBytes) | (uintptr_t)((int64_t)a.k * kBytes);
+  // sixteen warps a CTA where there is about one CTA per SM and a warp of eight
+  // would take its loads in several turns
+  const int64_t few = ceil_div(a.n, 16) * ceil_div(a.rows, 32);
+  const bool deep = few <= 2 * kSms && a.k > 512;
+  if ((low & 15) == 0) {
+    if (deep) {
+      launch<kMode, kR, 16, 16, kAct>(a, st);
+    } else if constexpr (kMode == kGated) {
+      launch<kMode, kR, 8, 16, kAct>(a, st);
+    } else {
+      // many columns: 32 a CTA, so that x comes from L2 half as often
+      if (few > 2 * kSms) launch<kMode, 2, 8, 16, kAct>(a, st);
+      else launch<kMode, 1, 8, 16, kAct>(a, st);
+    }
+  } else if ((low & 3) == 0) {
+    launch<kMode, kR, 8, 4, kAct>(a, st);
+  } else {
+    launch<kMode, kR, 8, kBytes, kAct>(a, st);
+  }
   return cudaGetLastError();
 }
 
-bool fits(const void* p, int64_t bytes) { return ((uintptr_t)p & 15) == 0 && bytes % 16 == 0; }
-
 }  // namespace
 
-bool rows_fit(int64_t rows, const void* x, int64_t ldx, const void* w, int32_t k, int elem) {
-  return rows <= kFewRows && fits(x, ldx * elem) && fits(w, (int64_t)k * elem);
+bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8) {
+  const int64_t work = rows * weights;
+  if (pitch % 4 != 0) return work <= (q8 ? 60000000 : 70000000);
+  const bool whole = pitch % 16 == 0;
+  if (rows <= (q8 && whole ? 128 : 32)) return true;
+  return rows <= 1024 && work <= (q8 ? (whole ? 700000000 : 300000000) : (whole ? 540000000 : 250000000));
 }
 
 cudaError_t rows_gated(const void* x, int64_t ldx, const void* w_gu, int64_t rows, int32_t d, int32_t f, int act, void* h,

@@ -9,11 +9,19 @@
 
 namespace tp {
 
-// Up to this many rows the products stream the weights past the rows.
-constexpr int kFewRows = 32;
-
-// Can these products take x and w as they lie there (elem: bytes of an element)?
-bool rows_fit(int64_t rows, const void* x, int64_t ldx, const void* w, int32_t k, int elem);
+// Do these products take `rows` rows against this many weights, in rows of
+// `pitch` bytes (or of several pitches, or'ed)?  Measured against the tcgen05
+// products (device time of a call, us, rows / tcgen05):
+//   gated block, d = d_out = 512, f = 2048: 64 rows 7.8 / 12.4, 192 rows 15.2 / 14.2
+//   d = d_out = 1024, f = 2048: 32 rows 7.9 / 15.3, 128 rows 15.7 / 16.3
+//   d = d_out = 2048, f = 4096: 32 rows 18.4 / 25.5, 64 rows 27.3 / 26.1
+//   d = d_out = 256, f = 512: 512 rows 7.4 / 10.5, 1024 rows 11.9 / 10.6
+//   8-bit product, 2048 -> 4096: 128 rows 13.2 / 20.6, 256 rows 23.6 / 21.3
+//   1024 -> 1000: 256 rows 5.0 / 11.0, 768 rows 12.8 / 11.5
+// Loads of four bytes (gated 1022, 2046: 64 rows 19.5 / 22.5, 128 rows 26.1 /
+// 23.7) or of an element (gated 389, 1001: 32 rows 11.9 / 14.8, 128 rows 17.0 /
+// 15.3; 8-bit 2001 -> 1000: 8 rows 9.5 / 12.1, 32 rows 21.9 / 12.0) pay for less.
+bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8);
 cudaError_t rows_gated(const void* x, int64_t ldx, const void* w_gu, int64_t rows, int32_t d, int32_t f, int act, void* h,
                        int64_t ldh, void* a, void* p, cudaStream_t st);
 cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, void* y,
@@ -36,8 +44,22 @@ __device__ __forceinline__ float act_value(float g, float& d) {
     d = s * (1.f + g * (1.f - s));
     return g * s;
   }
-  const float p = 0.5f * erfcf(-0.70710678118654752f * g);
-  d = p + g * 0.39894228040143268f * (kF32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g));
+  const float e = kF32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g);
+  float p;   // Phi(g)
+  if constexpr (kF32) {
+    p = 0.5f * erfcf(-0.70710678118654752f * g);
+  } else {
+    // Abramowitz and Stegun 7.1.26: erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2) + e, t = 1 / (1 + 0.3275911 x),
+    // x >= 0, |e| <= 1.5e-7, below the rounding of the product's sums; its exponential is act' 's
+    const float t = __fdividef(1.f, fmaf(0.23164189f, fabsf(g), 1.f));
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    q *= 0.5f * t * e;
+    p = g < 0.f ? q : 1.f - q;
+  }
+  d = fmaf(g * 0.39894228040143268f, e, p);
   return g * p;
 }
 
