@@ -86,7 +86,6 @@ struct Stager {
 
 struct Plans {
   ProdLaunch l[2];
-  int64_t partial = 0;
 };
 
 void job(ProdLaunch& l, int64_t M, int64_t N, int64_t K, int ma, int mb, bool a_mn, bool b_mn, int halves, void* out,
@@ -105,12 +104,8 @@ void start(ProdLaunch& l, const Geo& g, int epi, int act) {
 }
 
 int64_t plan(Plans& p) {
-  for (ProdLaunch& l : p.l) {
-    int64_t b = 0;
-    prod_plan(l, &b);
-    if (b > p.partial) p.partial = b;
-  }
-  return p.partial;
+  for (ProdLaunch& l : p.l) prod_plan(l);
+  return prod_bytes(p.l, 2);
 }
 
 void plan_forward(Plans& p, const Geo& g, int act, const ProdOperand& x, const ProdOperand& wgu, const ProdOperand& wd,
@@ -154,10 +149,10 @@ tp_status run(Plans& p, Stager& st, Carver& c, int64_t workspace_bytes, cudaStre
   if (workspace_bytes < need) return ops_fail(TP_EINVAL, "%s: a workspace of %lld bytes is needed", who, (long long)need);
   const tp_status s = ops_device();
   if (s != TP_OK) return s;
-  void* partial = c.take(0);
+  void* products = c.take(0);
   const char* what = "staging launch";
   cudaError_t e = stage_run(st.launch, stream);
-  for (int k = 0; e == cudaSuccess && k < 2; ++k) e = prod_run(p.l[k], partial, stream, &what);
+  if (e == cudaSuccess) e = prod_run_all(p.l, 2, products, stream, &what);
   if (e == cudaSuccess) return TP_OK;
   cudaGetLastError();   // reported here
   return ops_fail(TP_ECUDA, "%s: %s: %s", who, what, cudaGetErrorString(e));

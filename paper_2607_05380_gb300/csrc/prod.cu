@@ -18,8 +18,13 @@
 // n 10^-8 of its value off, so a chain takes at most kChainKb K blocks; a
 // tile has two, and longer reductions are split.
 //
-// Reductions are split over CTAs where a launch has too few tiles; the parts'
-// sums are then added in a fixed order by k_prod_join.
+// Where the tiles do not come out even over the SMs, the K blocks of the last
+// one to two rounds' tiles are shared out evenly instead: a cluster's run of
+// them ends inside a tile, whose first part it takes before all else and whose
+// fp32 sums it leaves in the workspace, and begins inside another, whose last
+// part it takes at the end, adding the sums that the clusters before it have
+// left there long since, in order.  All clusters are resident (grid <= what
+// fits), and a cluster publishes before it waits.
 //
 // Every wait is bounded (2 s): a role that gives up sets the error word that
 // pack_ops_check reads and an abort flag; the others then stop, copies and
@@ -42,7 +47,8 @@ namespace tp {
 
 namespace {
 
-constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kEpiWarps = 8, kThreads = 96 + 32 * kEpiWarps;   // and a producer each for A and B, and the MMA issuer
+constexpr int kWarpB = 2 + kEpiWarps;
 constexpr int kABytes = 128 * 128;       // 128 rows of a K block
 constexpr int kBox = 64 * 128;           // a 64 x 64 MN-major box
 constexpr int kMaxStages = 8;
@@ -63,24 +69,91 @@ struct Tail {
 struct ProdArgs {
   CUtensorMap map[kProdMaps];
   ProdJob job[kProdJobs];
-  int32_t n_jobs, n_tiles, fp16, n_tile, chains, stages;
+  int32_t n_jobs, n_tiles, n_maps, fp16, n_tile, chains, stages;
+  int32_t whole, part_kb;   // part_kb: longest reduction between two additions in fp32
+  float* slots;             // [2][clusters][CTA][128 n_tile]: published sums; a cluster's own
+  int* flags;               // [clusters][CTA][epilogue warp]
+  int32_t cut[kSms + 1];
 };
 static_assert(sizeof(ProdArgs) <= 4096, "kernel parameters");
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+// The producer and the MMA issuer walk their loops as whole, converged warps
+// and leave the single thread to a predicate inside the instruction sequences
+// below: the loops' values then live in the uniform registers that TMA and
+// tcgen05.mma take their operands from.  (One lane in a branch of its own
+// moved every operand there anew: 290 ns a K block whatever the tile's width.)
+__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                         uint64_t budget_ns, int site) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait_slow(bar, parity, abort_flag, err, budget_ns, site));
+}
+__device__ __forceinline__ void expect_elect(uint32_t bar, uint32_t bytes) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          dst),
-      "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}\n" ::"r"(
+          bar),
+      "r"(bytes)
       : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
-      "%5}], [%2];" ::"r"(dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-      : "memory");
+// kCta 2: the copy completes on barrier `bar` of the pair's leader (a shared::cluster address)
+template <int kCta>
+__device__ __forceinline__ void tma_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  if constexpr (kCta == 2)
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e "
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, "
+        "%5}], [%2];\n}\n" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e "
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
+        "[%2];\n}\n" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
 }
+// One K block: four MMAs (K = 16 each), whose operands lie ka and kb (of 16
+// bytes) apart; the first one adds to the accumulator if `add`.  Then `bar`
+// (in every CTA of the tile) is told once they are over.
+#define TP_MMA4(GROUP, COMMIT)                                                                                        \
+  "{\n .reg .pred e, p, t;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n elect.sync _|e, 0xffffffff;\n"                        \
+  " setp.ne.b32 p, %4, 0;\n setp.eq.b32 t, 0, 0;\n"                                                                   \
+  " add.s64 a1, %1, %5;\n add.s64 a2, a1, %5;\n add.s64 a3, a2, %5;\n"                                                \
+  " add.s64 b1, %2, %6;\n add.s64 b2, b1, %6;\n add.s64 b3, b2, %6;\n"                                                \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], %1, %2, %3, p;\n"                                             \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a1, b1, %3, t;\n"                                             \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a2, b2, %3, t;\n"                                             \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a3, b3, %3, t;\n" COMMIT "}\n"
+#define TP_COMMIT1 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n"
+#define TP_COMMIT2 \
+  " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%7], %8;\n"
+template <int kCta>
+__device__ __forceinline__ void mma_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add, uint64_t ka,
+                                          uint64_t kb, uint32_t bar) {
+  if constexpr (kCta == 2)
+    asm volatile(TP_MMA4("2", TP_COMMIT2)::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add), "l"(ka), "l"(kb), "r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile(TP_MMA4("1", TP_COMMIT1)::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add), "l"(ka), "l"(kb), "r"(bar)
+                 : "memory");
+}
+template <int kCta>
+__device__ __forceinline__ void commit_elect(uint32_t bar) {
+  if constexpr (kCta == 2)
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e "
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}\n" ::"r"(
+            bar),
+        "h"((uint16_t)3)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e "
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // A warp's 32 lanes x 32 columns of TMEM; the values are there after tmem_wait
 // and may be used once tmem_got has tied them to it.
@@ -100,31 +173,114 @@ __device__ __forceinline__ void tmem_got(uint32_t (&v)[32]) {
   for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(v[e]));
 }
 
-// A tile's place: job, output origin and K blocks.
-struct Tile {
-  int job, m0, n0, kb0, kbn, split;
+// One accumulation: K blocks kb0 .. kb0 + kbn - 1 of a tile.
+struct Item {
+  int job, m0, n0, kb0, kbn;
+  bool carry_in, carry_out;   // the reduction continues one that this cluster left in its own slot / is continued
+  bool publish;               // leaves its sums for the cluster that finishes the tile
+  int add0;                   // finishes a tile: adds the sums of clusters add0 .. this one - 1
 };
-template <int kCta>
-__device__ __forceinline__ Tile tile_at(const ProdArgs& g, int t) {
-  Tile r;
-  r.job = 0;
-  for (int j = 1; j < g.n_jobs; ++j)
-    if (t >= g.job[j].tile0) r.job = j;
-  const ProdJob& b = g.job[r.job];
-  int local = t - b.tile0;
-  const int per = b.tm * b.tn;
-  r.split = local / per;
-  local -= r.split * per;
-  // eight row blocks at a time walk the columns, so that a wave's tiles share operands in L2
-  const int group = local / (8 * b.tn);
-  const int rows = min(8, b.tm - 8 * group);
-  local -= group * 8 * b.tn;
-  r.m0 = (8 * group + local % rows) * 128 * kCta;
-  r.n0 = local / rows;
-  r.kb0 = r.split * b.kb_split;
-  r.kbn = min(b.kb_split, b.kb - r.kb0);
-  return r;
+struct Place { int tile, kb; };
+
+// Where the K block numbered pos of the shared-out tiles lies.
+__host__ __device__ __forceinline__ Place place_of(const ProdArgs& g, int pos) {
+  for (int j = 0; j < g.n_jobs; ++j) {
+    const int first = max(g.job[j].tile0, g.whole), end = j + 1 < g.n_jobs ? g.job[j + 1].tile0 : g.n_tiles;
+    const int units = max(0, end - first) * g.job[j].kb;
+    if (pos < units) return Place{first + pos / g.job[j].kb, pos % g.job[j].kb};
+    pos -= units;
+  }
+  return Place{g.n_tiles, 0};
 }
+
+// A cluster's items in the order it takes them; every role walks them alike.
+template <int kCta>
+struct Walk {
+  const ProdArgs& g;
+  const int clu, n_clu;
+  Place from, to;
+  int phase = 0, next_tile = 0;
+  int tile = 0, kb = 0, kb_end = 0, kind = 0, add0 = 0;   // the run of K blocks that items are cut from
+  bool first = false;
+
+  __host__ __device__ __forceinline__ Walk(const ProdArgs& g_, int c, int n) : g(g_), clu(c), n_clu(n) {
+    from = to = Place{g.n_tiles, 0};
+    if (g.whole < g.n_tiles) from = place_of(g, g.cut[c]), to = place_of(g, g.cut[c + 1]);
+  }
+  __host__ __device__ __forceinline__ int job_of(int t) const {
+    int j = 0;
+    for (int k = 1; k < g.n_jobs; ++k)
+      if (t >= g.job[k].tile0) j = k;
+    return j;
+  }
+  // kind 0: a whole tile, 1: published, 2: finishes a tile that others began
+  __host__ __device__ __forceinline__ void run(int t, int a, int b, int k) { tile = t, kb = a, kb_end = b, kind = k, first = true; }
+  __host__ __device__ __forceinline__ bool next_run() {
+    while (phase < 4) {
+      if (phase == 0) {
+        phase = 1;
+        next_tile = clu;
+        if (from.tile == to.tile) {
+          if (from.kb < to.kb) {
+            run(to.tile, from.kb, to.kb, 1);
+            return true;
+          }
+        } else if (to.kb > 0) {
+          run(to.tile, 0, to.kb, 1);
+          return true;
+        }
+      } else if (phase == 1) {
+        if (next_tile < g.whole) {
+          run(next_tile, 0, g.job[job_of(next_tile)].kb, 0);
+          next_tile += n_clu;
+          return true;
+        }
+        phase = 2;
+        next_tile = from.kb ? from.tile + 1 : from.tile;
+      } else if (phase == 2) {
+        if (next_tile < to.tile) {
+          run(next_tile, 0, g.job[job_of(next_tile)].kb, 0);
+          ++next_tile;
+          return true;
+        }
+        phase = 3;
+      } else {
+        phase = 4;
+        if (from.tile < to.tile && from.kb > 0) {
+          run(from.tile, from.kb, g.job[job_of(from.tile)].kb, 2);
+          add0 = clu;   // back to the cluster that began the tile
+          while (add0 > 0) {
+            const Place p = place_of(g, g.cut[add0]);
+            if (p.tile != tile || p.kb == 0) break;
+            --add0;
+          }
+          return true;
+        }
+      }
+    }
+    return false;
+  }
+  __host__ __device__ __forceinline__ bool next(Item& it) {
+    if (kb >= kb_end && !next_run()) return false;
+    it.job = job_of(tile);
+    const ProdJob& b = g.job[it.job];
+    // eight row blocks at a time walk the columns, so that a round's tiles share operands in L2
+    int local = tile - b.tile0;
+    const int group = local / (8 * b.tn), rows = min(8, b.tm - 8 * group);
+    local -= group * 8 * b.tn;
+    it.m0 = (8 * group + local % rows) * 128 * kCta;
+    it.n0 = local / rows;
+    it.kb0 = kb;
+    it.kbn = min(kb_end - kb, g.part_kb);
+    it.carry_in = !first;
+    kb += it.kbn;
+    it.carry_out = kb < kb_end;
+    it.publish = kind == 1;
+    it.add0 = kind == 2 ? add0 : clu;
+    first = false;
+    return true;
+  }
+};
 
 __device__ __forceinline__ bool vec_ok(const void* p, int64_t ld, int bytes) {
   return ((uintptr_t)p & 15) == 0 && ((ld * bytes) & 15) == 0;
@@ -235,6 +391,20 @@ __device__ __forceinline__ void put_parts(float (&v)[32], __nv_bfloat16* out, in
   }
 }
 
+// A lane's 32 columns in a slot: groups of four, the lanes' side by side.
+__device__ __forceinline__ void put_slot(float* p, int lane, const float (&v)[32]) {
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    reinterpret_cast<float4*>(p)[32 * s + lane] = make_float4(v[4 * s], v[4 * s + 1], v[4 * s + 2], v[4 * s + 3]);
+}
+__device__ __forceinline__ void add_slot(const float* p, int lane, float (&v)[32]) {
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const float4 w = __ldcg(reinterpret_cast<const float4*>(p) + 32 * s + lane);
+    v[4 * s] += w.x, v[4 * s + 1] += w.y, v[4 * s + 2] += w.z, v[4 * s + 3] += w.w;
+  }
+}
+
 // What the epilogue reads besides the accumulator: kEpiDgated of a bf16 block,
 // u act'(g) and act(g) of the lane's row, asked for one chunk ahead.
 struct Ahead {
@@ -340,14 +510,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
   const int stages = g.stages;
   uint8_t* bufs = smem + stages * stage_bytes;
   Tail* tl = (Tail*)(bufs + kEpiWarps * kBufBytes);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = kCta == 2 ? (int)cluster_rank() : 0;
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int rank = kCta == 2 ? (int)uniform(cluster_rank()) : 0;
   const bool leader = rank == 0;
   const int clu = blockIdx.x / kCta, n_clu = gridDim.x / kCta;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
-      mbar_init(&tl->full[s], 1);
+      mbar_init(&tl->full[s], 2);   // one per producer
       mbar_init(&tl->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -375,60 +545,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
   __syncthreads();
   tc_fence_after();
   if (kCta == 2) cluster_sync();   // the peer's barriers exist before any copy or arrival targets them
+  if (warp == 0 && lane < kProdMaps && lane < g.n_maps)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&g.map[lane]) : "memory");
   pdl_wait();                      // the set-up above overlaps the previous kernel
-  const uint32_t tmem = tl->tmem_base;
+  const uint32_t tmem = uniform(tl->tmem_base);
   volatile int* abort_flag = &tl->abort;
   int* err = &g_prod_err;
 
-  if (warp == 0) {
-    // ------------------------------------------------------------ producer
-    uint32_t stage = 0, phase = 0, issued = 0, last_parity = 0;
+  if (warp == 0 || warp == kWarpB) {
+    // -------------------------------------------------- producers of A and B
+    const bool is_a = warp == 0;
+    uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
-    for (int t = clu; ok && t < g.n_tiles; t += n_clu) {
-      const Tile u = tile_at<kCta>(g, t);
+    const uint32_t s0 = smem_u32(smem), full0 = smem_u32(&tl->full[0]);
+    const uint32_t lead0 = kCta == 2 ? mapa(full0, 0) : full0;   // the barriers that copies complete on
+    Walk<kCta> walk(g, clu, n_clu);
+    Item u;
+    while (ok && walk.next(u)) {
       const ProdJob& j = g.job[u.job];
-      const int nbA = j.a_mn ? 2 : 1;
-      // B: K-major one box of nh rows (kEpiGated in one CTA: gate and up rows apart), MN-major boxes of 64
-      constexpr bool kTwoHalves = kEpi == kEpiGated && kCta == 1;
-      const int nbB = j.b_mn ? nh >> 6 : (kTwoHalves ? 2 : 1);
-      const int qb = lane - nbA;
-      const bool is_a = lane < nbA, mine = is_a || qb < nbB;
       const CUtensorMap* map = &g.map[is_a ? j.map_a : j.map_b];
-      const bool mn = is_a ? j.a_mn != 0 : j.b_mn != 0;
-      int xy, add_seg = 0;
-      uint32_t off;
-      if (is_a) {
-        xy = u.m0 + rank * 128 + 64 * lane;
-        off = (uint32_t)lane * kBox;
-      } else if (kEpi == kEpiGated) {
-        // the tile's columns: n_tile / 2 of the gate, then the same of the up half
-        xy = u.n0 * (g.n_tile / 2);
-        add_seg = (kCta == 2 ? rank : qb) * j.up;
-        off = kABytes + (kCta == 2 ? 0u : (uint32_t)qb * (g.n_tile / 2) * 128);
-      } else {
-        xy = u.n0 * g.n_tile + rank * nh + 64 * qb;
-        off = kABytes + (uint32_t)qb * kBox;
-      }
+      const bool mn = (is_a ? j.a_mn : j.b_mn) != 0;
+      // kEpiGated: n_tile / 2 columns of the gate, then the same of the up half (in a pair one each)
+      constexpr bool kHalves = kEpi == kEpiGated && kCta == 1;
+      const int half_n = g.n_tile / 2, rows = is_a ? 128 : nh;
+      const int x0 = is_a ? u.m0 + rank * 128 : kEpi == kEpiGated ? u.n0 * half_n : u.n0 * g.n_tile + rank * nh;
+      const uint32_t off = is_a ? 0 : kABytes;
       for (int q = 0; ok && q < j.n_pairs; ++q) {
-        const int seg = (is_a ? j.sa[q] : j.sb[q]) + add_seg;
+        const int z = is_a ? j.sa[q] : j.sb[q] + (kEpi == kEpiGated && kCta == 2 ? rank * j.up : 0);
         for (int kb = u.kb0; kb < u.kb0 + u.kbn; ++kb) {
-          bool got = true;
-          if (lane == 0) {
-            got = mbar_wait(&tl->empty[stage], phase ^ 1u, abort_flag, err, kWaitNs, 41);
-            if (got && leader) mbar_expect_tx(&tl->full[stage], kCta * stage_bytes);
-          }
-          if (!__shfl_sync(0xffffffffu, got, 0)) {
+          if (!wait_all(&tl->empty[stage], phase ^ 1u, abort_flag, err, kWaitNs, 41)) {
             ok = false;
             break;
           }
-          if (mine) {
-            const uint32_t dst = smem_u32(smem + stage * stage_bytes) + off;
-            const int x = mn ? xy : 64 * kb, y = mn ? 64 * kb : xy;
-            if constexpr (kCta == 2) tma_load_3d_pair(dst, map, mapa(smem_u32(&tl->full[stage]), 0), x, y, seg);
-            else tma_load_3d(dst, map, &tl->full[stage], x, y, seg);
+          const uint32_t dst = s0 + stage * stage_bytes + off, bar = lead0 + 8 * stage;
+          const int k = 64 * kb;
+          if (leader) expect_elect(full0 + 8 * stage, (uint32_t)(kCta * 128) * rows);
+          // K-major: one box of all rows (gate and up rows apart); MN-major: boxes of 64
+          if (mn) {
+            tma_elect<kCta>(dst, map, bar, x0, k, z);
+            if (rows > 64) tma_elect<kCta>(dst + kBox, map, bar, x0 + 64, k, z);
+            if (rows > 128) {
+              tma_elect<kCta>(dst + 2 * kBox, map, bar, x0 + 128, k, z);
+              tma_elect<kCta>(dst + 3 * kBox, map, bar, x0 + 192, k, z);
+            }
+          } else {
+            tma_elect<kCta>(dst, map, bar, k, x0, z);
+            if (kHalves && !is_a) tma_elect<kCta>(dst + half_n * 128, map, bar, k, x0, z + j.up);
           }
           issued |= 1u << stage;
-          last_parity = (last_parity & ~(1u << stage)) | (phase << stage);
           if (++stage == (uint32_t)stages) {
             stage = 0;
             phase ^= 1u;
@@ -436,46 +600,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
         }
       }
     }
-    if (lane == 0 && leader)   // every copy has landed before the CTA leaves
+    // every copy has landed before the CTA leaves: a stage's last one is of this
+    // turn of the ring below `stage`, of the one before from there on
+    if (leader && is_a)
       for (int s = 0; s < stages; ++s)
         if (issued & (1u << s)) {
           int dummy = 0;
-          mbar_wait(&tl->full[s], (last_parity >> s) & 1u, &dummy, err, kWaitNs, 42);
+          mbar_wait(&tl->full[s], s < (int)stage ? phase : phase ^ 1u, &dummy, err, kWaitNs, 42);
         }
   } else if (warp == 1) {
-    if (lane == 0 && leader) {
+    if (leader) {
       // --------------------------------------------------------------- MMA
-      const uint32_t s0 = smem_u32(smem);
+      const uint32_t s0 = smem_u32(smem), empty0 = smem_u32(&tl->empty[0]);
       const uint64_t dA_k = smem_desc(s0, 16, 1024), dA_mn = smem_desc(s0, kBox, 1024);
       const uint64_t dB_k = smem_desc(s0 + kABytes, 16, 1024), dB_mn = smem_desc(s0 + kABytes, kBox, 1024);
       const uint32_t step = stage_bytes >> 4;
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
       bool ok = true;
-      for (int t = clu; ok && t < g.n_tiles; t += n_clu) {
-        const Tile u = tile_at<kCta>(g, t);
+      Walk<kCta> walk(g, clu, n_clu);
+      Item u;
+      while (ok && walk.next(u)) {
         const ProdJob& j = g.job[u.job];
-        if (!mbar_wait(&tl->tempty[acc], acc_phase ^ 1u, abort_flag, err, 2 * kWaitNs, 43)) break;
+        if (!wait_all(&tl->tempty[acc], acc_phase ^ 1u, abort_flag, err, 2 * kWaitNs, 43)) break;
         tc_fence_after();
         const uint32_t d0 = tmem + acc * kAccCols;
         uint32_t idesc = instr_desc(128 * kCta, g.n_tile, j.a_mn, j.b_mn);
         if (g.fp16) idesc &= ~((1u << 7) | (1u << 10));
         const uint64_t ta = j.a_mn ? dA_mn : dA_k, tb = j.b_mn ? dB_mn : dB_k;
-        const uint32_t ka = j.a_mn ? 2048 >> 4 : 32 >> 4, kb_ = j.b_mn ? 2048 >> 4 : 32 >> 4;
+        const uint64_t ka = j.a_mn ? 2048 >> 4 : 32 >> 4, kb_ = j.b_mn ? 2048 >> 4 : 32 >> 4;
         const int split_at = g.chains == 2 ? (u.kbn + 1) >> 1 : u.kbn;   // first K block of the second chain
         for (int q = 0; ok && q < j.n_pairs; ++q) {
           for (int kb = 0; kb < u.kbn; ++kb) {
-            if (!mbar_wait(&tl->full[stage], phase, abort_flag, err, 2 * kWaitNs, 44)) {
+            if (!wait_all(&tl->full[stage], phase, abort_flag, err, 2 * kWaitNs, 44)) {
               ok = false;
               break;
             }
-            const uint64_t sa = ta + stage * step, sb = tb + stage * step;
             const uint32_t d = d0 + (kb >= split_at ? kAccCols / 2 : 0);
-            const uint32_t first = q > 0 || (kb != 0 && kb != split_at) ? 1u : 0u;
-            umma_bf16<kCta>(d, sa, sb, idesc, first);
-            umma_bf16<kCta>(d, sa + ka, sb + kb_, idesc, 1u);
-            umma_bf16<kCta>(d, sa + 2 * ka, sb + 2 * kb_, idesc, 1u);
-            umma_bf16<kCta>(d, sa + 3 * ka, sb + 3 * kb_, idesc, 1u);
-            umma_commit<kCta>(&tl->empty[stage]);
+            const uint32_t add = q > 0 || (kb != 0 && kb != split_at) ? 1u : 0u;
+            mma_elect<kCta>(d, ta + stage * step, tb + stage * step, idesc, add, ka, kb_, empty0 + 8 * stage);
             if (++stage == (uint32_t)stages) {
               stage = 0;
               phase ^= 1u;
@@ -483,11 +645,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
           }
         }
         if (!ok) break;
-        umma_commit<kCta>(&tl->tfull[acc]);
+        commit_elect<kCta>(smem_u32(&tl->tfull[acc]));
         acc ^= 1u;
         if (acc == 0) acc_phase ^= 1u;
       }
-      umma_commit<kCta>(&tl->done);   // all MMAs are over before TMEM is freed
+      commit_elect<kCta>(smem_u32(&tl->done));   // all MMAs are over before TMEM is freed
       int dummy = 0;
       mbar_wait(&tl->done, 0, &dummy, err, kWaitNs, 45);
     }
@@ -497,16 +659,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     uint8_t* buf = bufs + (warp - 2) * kBufBytes;
     uint32_t acc = 0, acc_phase = 0;
     const int cols = kEpi == kEpiGated ? g.n_tile / 2 : g.n_tile;
-    for (int t = clu; t < g.n_tiles; t += n_clu) {
-      const Tile u = tile_at<kCta>(g, t);
+    // this warp's 32 lanes x n_tile columns in the slots, a chunk of 32 columns after another
+    const int64_t slot = (int64_t)128 * g.n_tile, mine = (int64_t)(clu * kCta + rank) * slot + (int64_t)32 * q * g.n_tile;
+    float* own = g.slots + (int64_t)n_clu * kCta * slot + mine;
+    Walk<kCta> walk(g, clu, n_clu);
+    Item u;
+    while (walk.next(u)) {
       const ProdJob& j = g.job[u.job];
       const int r0 = u.m0 + rank * 128 + 32 * q;
       Ahead ahead;
       constexpr bool kAhead = kEpi == kEpiDgated && !kF32;
+      const bool finish = !u.publish && !u.carry_out;
       if constexpr (kAhead)
-        if (r0 < j.M && u.n0 * cols + 32 * half < j.N) ahead.load(j, r0 + lane, u.n0 * cols + 32 * half);
+        if (finish && r0 < j.M && u.n0 * cols + 32 * half < j.N) ahead.load(j, r0 + lane, u.n0 * cols + 32 * half);
       if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[acc], acc_phase, abort_flag, err, 2 * kWaitNs, 46))) break;
       tc_fence_after();
+      bool there = true;
+      if (finish)
+        for (int k = u.add0; k < clu; ++k)   // (a cluster without K blocks leaves nothing)
+          if (g.cut[k] < g.cut[k + 1])
+            there = there && dep_wait(g.flags + (k * kCta + rank) * kEpiWarps + warp - 2, 1, 1, abort_flag, err,
+                                      2 * kWaitNs, 47, lane);
+      if (!there) break;
       const uint32_t ta = tmem + ((uint32_t)(32 * q) << 16) + acc * kAccCols;
       const bool second = g.chains == 2 && u.kbn > 1;
 #pragma unroll 1
@@ -537,9 +711,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
             if constexpr (kEpi == kEpiGated) a2[e] += __uint_as_float(v2[e]);
           }
         }
-        if (j.splits > 1) {
-          emit_f32(buf, lane, a, j.partial + (int64_t)u.split * j.M * j.ldp, j.ldp, r0, j.M, c0, j.N, true);
+        // sums of the same reduction from before
+        if (u.carry_in) {
+          add_slot(own + 32 * c, lane, a);
+          if constexpr (kEpi == kEpiGated) add_slot(own + 32 * (cols + c), lane, a2);
+        }
+        if (!finish) {
+          float* to = u.carry_out ? own : g.slots + mine;
+          put_slot(to + 32 * c, lane, a);
+          if constexpr (kEpi == kEpiGated) put_slot(to + 32 * (cols + c), lane, a2);
           continue;
+        }
+        for (int k = u.add0; k < clu; ++k) {
+          if (g.cut[k] == g.cut[k + 1]) continue;
+          const float* of = g.slots + mine - (int64_t)(clu - k) * kCta * slot;
+          add_slot(of + 32 * c, lane, a);
+          if constexpr (kEpi == kEpiGated) add_slot(of + 32 * (cols + c), lane, a2);
         }
         Ahead now;
         if constexpr (kAhead) {
@@ -554,6 +741,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
         if constexpr (kCta == 2) mbar_arrive_cluster_relaxed(mapa(smem_u32(&tl->tempty[acc]), 0));
         else mbar_arrive_relaxed(&tl->tempty[acc]);
       }
+      if (u.publish && !u.carry_out && lane == 0)   // after the warp's stores (the barrier above)
+        red_release_add(g.flags + (clu * kCta + rank) * kEpiWarps + warp - 2, 1);
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
     }
@@ -569,52 +758,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
       asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     else
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
-  }
-}
-
-// ------------------------------------------------- joining split reductions
-struct JoinArgs {
-  ProdJob job[kProdJobs];
-  int32_t n_jobs, epi;
-};
-// out = the splits' sums added in order (kEpiQuant: scaled); four columns per thread.
-template <bool kF32>
-__global__ void __launch_bounds__(256) k_prod_join(const __grid_constant__ JoinArgs g) {
-  pdl_trigger();
-  pdl_wait();
-  const ProdJob& j = g.job[blockIdx.y];
-  const int groups = (j.N + 3) >> 2;
-  const int64_t total = (int64_t)j.M * groups, plane = (int64_t)j.M * j.ldp;
-  const bool vec = vec_ok(j.out, j.ldo, kF32 ? 4 : 2);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / groups;
-    const int c = (int)(i - r * groups) * 4;
-    const float* p = j.partial + r * j.ldp + c;
-    float4 s = *reinterpret_cast<const float4*>(p);
-#pragma unroll 4
-    for (int k = 1; k < j.splits; ++k) {
-      const float4 v = *reinterpret_cast<const float4*>(p + k * plane);
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    float e[4] = {s.x, s.y, s.z, s.w};
-    if (g.epi == kEpiQuant) {
-      const float sx = j.sx[r];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + k < j.N) e[k] = e[k] * sx * j.sw[c + k] + (j.bias ? j.bias[c + k] : 0.f);
-    }
-    if constexpr (kF32) {
-      float* o = (float*)j.out + r * j.ldo + c;
-      if (vec && c + 4 <= j.N) *reinterpret_cast<float4*>(o) = make_float4(e[0], e[1], e[2], e[3]);
-      else
-        for (int k = 0; k < 4 && c + k < j.N; ++k) o[k] = e[k];
-    } else {
-      __nv_bfloat16* o = (__nv_bfloat16*)j.out + r * j.ldo + c;
-      if (vec && c + 4 <= j.N)
-        *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]));
-      else
-        for (int k = 0; k < 4 && c + k < j.N; ++k) o[k] = __float2bfloat16_rn(e[k]);
-    }
   }
 }
 
@@ -712,19 +855,22 @@ int stage_count(int cta, int n_tile) {
   return std::min<int>(kMaxStages, (kSmemMax - 1024 - kEpiWarps * kBufBytes - (int)sizeof(Tail)) / bytes);
 }
 
-// Nanoseconds of one K block of a tile: the tensor cores' 6.28 (12.56) TFLOP/s
-// a CTA (pair), or the staged bytes at about 100 GB/s an SM.
-double kblock_ns(int cta, int n_tile) {
-  const double mma = 128.0 * cta * n_tile * 64 * 2 / (12560.0 * cta);
-  return std::max(mma, (kABytes + n_tile / cta * 128.0) / 100.0);
-}
+// A tile's shape and its times in ns, measured (bf16, operands in L2): a K
+// block, what a launch of one tile per cluster takes besides (the epilogue
+// among it), and the epilogue alone, which the next tile's K blocks hide.
+struct Shape {
+  int cta, n;
+  double kb, fixed, epi;
+};
+constexpr Shape kShapes[] = {{2, 256, 287, 7000, 2800}, {2, 128, 195, 5600, 1400}, {1, 256, 320, 5900, 2800},
+                             {1, 128, 213, 4400, 1400}, {1, 64, 180, 3900, 700}};
 
 template <int kCta, int kEpi, int kAct, bool kF32>
-cudaError_t launch(const ProdArgs& a, int max_clusters, cudaStream_t st) {
+cudaError_t launch(const ProdArgs& a, int clusters, cudaStream_t st) {
   const int stage_bytes = kABytes + a.n_tile / kCta * 128;
   const int smem = a.stages * stage_bytes + kEpiWarps * kBufBytes + (int)sizeof(Tail) + 1024;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kCta * std::min(a.n_tiles, max_clusters));
+  cfg.gridDim = dim3(kCta * clusters);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -843,105 +989,181 @@ void prod_pairs(ProdJob& j, bool f32, int halves) {
   j.n_pairs = n;
 }
 
-void prod_plan(ProdLaunch& l, int64_t* partial_bytes) {
-  struct Shape { int cta, n; };
-  // a CTA pair's tile, then narrower ones of one CTA: few rows or columns
-  static const Shape shapes[4] = {{2, 256}, {1, 256}, {1, 128}, {1, 64}};
-  const bool may_split = l.epi == kEpiPlain || l.epi == kEpiQuant;
-  const bool parts = l.f32 && !l.fp16;         // 32-bit operands: two chains in a 128-column tile
-  double best = 1e300;
-  ProdLaunch pick = l;
-  for (const Shape& s : shapes) {
-    if (parts && (s.cta != 1 || s.n > 128)) continue;
-    const int units = kSms / s.cta, chains = parts ? 2 : 1;
-    const int cols = l.epi == kEpiGated ? s.n / 2 : s.n;
-    for (int level = 0; level < (may_split ? 6 : 1); ++level) {
-      ProdLaunch p = l;
-      p.cta = s.cta, p.n_tile = s.n, p.chains = chains, p.n_tiles = 0;
-      double work = 0, longest = 0, join = 0;
-      bool any = false;
-      for (int k = 0; k < l.n_jobs; ++k) {
-        ProdJob& j = p.job[k];
-        j.kb = (int)ceil_div(j.K, 64);
-        j.tm = (int)ceil_div(j.M, 128 * s.cta);
-        j.tn = (int)ceil_div(j.N, cols);
-        int per = j.kb;
-        if (may_split) {
-          per = std::max(std::min(j.kb, 4), (int)ceil_div(j.kb, 1 << level));
-          if (parts) per = std::min(per, 2 * kChainKb);
-        }
-        j.splits = (int)ceil_div(j.kb, per);
-        j.kb_split = (int)ceil_div(j.kb, j.splits);
-        j.splits = (int)ceil_div(j.kb, j.kb_split);
-        j.tile0 = p.n_tiles;
-        const int64_t tiles = (int64_t)j.tm * j.tn * j.splits;
-        p.n_tiles += (int)tiles;
-        // a tile's K blocks, and what its epilogue keeps the next tile waiting
-        const double t = 300.0 + (double)j.n_pairs * j.kb_split * kblock_ns(s.cta, s.n);
-        work += t * tiles;
-        longest = std::max(longest, t);
-        if (j.splits > 1) {
-          any = true;
-          join += 2.0 * j.splits * j.M * j.N * 4 / 5000.0;
-        }
-      }
-      const double waves = (double)ceil_div(p.n_tiles, units) * work / p.n_tiles;
-      const double est = std::max(std::max(waves, longest), work / units) + join + (any ? 2500.0 : 0.0);
-      if (est < best * 0.98) {
-        best = est;
-        pick = p;
-      }
+namespace {
+
+// Shares out the tiles from p.whole on: runs of K blocks that end all clusters
+// at about the same time.  ns: time of a K block of a segment pair.
+void share_out(ProdLaunch& p, double ns) {
+  const int C = p.clusters;
+  double load[kSms] = {}, total = 0;
+  for (int k = 0; k < p.n_jobs; ++k) {
+    const ProdJob& j = p.job[k];
+    const int first = j.tile0, end = first + j.tm * j.tn;
+    const double t = j.n_pairs * j.kb * ns;
+    for (int c = 0; c < C; ++c) {   // whole tiles first .. min(end, whole) - 1 with number c modulo C
+      const int last = std::min(end, p.whole);
+      if (last > first) load[c] += t * ((last - 1 - c + C) / C - (first - 1 - c + C) / C);
     }
+    total += t * std::max(0, end - std::max(first, p.whole));
   }
-  l = pick;
-  int64_t bytes = 0;
-  for (int k = 0; k < l.n_jobs; ++k) {
-    ProdJob& j = l.job[k];
-    j.ldp = round_up(j.N, 4);
-    if (j.splits > 1) bytes += round_up((int64_t)j.splits * j.M * j.ldp * 4, 256);
+  // the level to which `total` fills up the clusters
+  double level = total;
+  for (int c = 0; c < C; ++c) level += load[c];
+  level /= C;
+  for (int round = 0; round < 3; ++round) {
+    double room = total;
+    int n = 0;
+    for (int c = 0; c < C; ++c)
+      if (load[c] < level) room += load[c], ++n;
+    level = room / n;
   }
-  *partial_bytes = bytes;
+  // cut the tiles' K blocks at the clusters' shares; a cut less than two K
+  // blocks from a tile's edge moves to the edge
+  int job = 0, tile = p.whole, pos = 0;
+  double want = 0, done = 0;   // time up to tile's first K block
+  auto step = [&] {
+    while (job + 1 < p.n_jobs && tile >= p.job[job + 1].tile0) ++job;
+  };
+  step();
+  p.cut[0] = 0;
+  for (int c = 0; c < C; ++c) {
+    want += std::max(0.0, level - load[c]);
+    while (tile < p.n_tiles) {
+      const ProdJob& j = p.job[job];
+      const double t = j.n_pairs * j.kb * ns;
+      if (c + 1 < C && done + t > want) break;
+      done += t;
+      pos += j.kb;
+      ++tile;
+      step();
+    }
+    int in = 0;
+    if (tile < p.n_tiles) {
+      const ProdJob& j = p.job[job];
+      in = (int)((want - done) / (j.n_pairs * ns));
+      if (in < 2) in = 0;
+      else if (j.kb - in < 2) in = j.kb;
+    }
+    p.cut[c + 1] = std::max(p.cut[c], pos + in);
+  }
 }
 
-cudaError_t prod_run(ProdLaunch& l, void* partial, cudaStream_t st, const char** what) {
+}  // namespace
+
+void prod_plan(ProdLaunch& l) {
+  // longest tiles first: dealt out round robin, the last round's short ones then go to the clusters with least
+  std::sort(l.job, l.job + l.n_jobs, [](const ProdJob& a, const ProdJob& b) {
+    return (int64_t)a.n_pairs * ceil_div(a.K, 64) > (int64_t)b.n_pairs * ceil_div(b.K, 64);
+  });
+  const bool parts = l.f32 && !l.fp16;         // 32-bit operands: two chains in a 128-column tile
+  double best = 1e300;
+  const Shape* pick = nullptr;
+  int pick_whole = 0, pick_clusters = 0;
+  auto lay = [&](ProdLaunch& p, const Shape& s) {
+    p.cta = s.cta, p.n_tile = s.n, p.chains = parts ? 2 : 1, p.n_tiles = 0;
+    for (int k = 0; k < p.n_jobs; ++k) {
+      ProdJob& j = p.job[k];
+      j.kb = (int)ceil_div(j.K, 64);
+      j.tm = (int)ceil_div(j.M, 128 * s.cta);
+      j.tn = (int)ceil_div(j.N, p.epi == kEpiGated ? s.n / 2 : s.n);
+      j.tile0 = p.n_tiles;
+      p.n_tiles += j.tm * j.tn;
+    }
+  };
+  for (const Shape& s : kShapes) {
+    if (parts && (s.cta != 1 || s.n > 128)) continue;
+    lay(l, s);
+    const int C = kSms / s.cta;
+    double work = 0, longest = 0, blocks = 0;
+    for (int k = 0; k < l.n_jobs; ++k) {
+      const ProdJob& j = l.job[k];
+      const double tiles = (double)j.tm * j.tn, t = std::max(j.n_pairs * j.kb * s.kb, s.epi) + 100.0;
+      work += t * tiles;
+      blocks += tiles * j.n_pairs * j.kb;
+      longest = std::max(longest, t);
+    }
+    // every tile whole
+    const double rounds = (double)ceil_div(l.n_tiles, C);
+    const double even = s.fixed + std::max(longest, rounds * work / l.n_tiles) + (l.n_jobs > 1 ? 0.5 * longest : 0.0);
+    if (even < best) best = even, pick = &s, pick_whole = l.n_tiles, pick_clusters = C;
+    // the last one to two rounds shared out, where there are few; runs of at least four K blocks, at most eight
+    // clusters a tile.  (Of many rounds the last ones' tiles, cut, no longer share operands in L2 with their
+    // neighbours: 16384 rows, 1024 -> 4096, backward, 631 us against 555 us whole.)
+    const int whole = std::max(0, l.n_tiles / C - 1) * C;
+    const int clusters = (int)std::min<double>(std::min<double>(C, std::max(1.0, blocks / 4)), 8.0 * l.n_tiles);
+    const double adds = std::max(1.0, (double)clusters / (l.n_tiles - whole));
+    const double shared = s.fixed + work / clusters + 6000.0 + (1.0 + adds) * s.epi;
+    if (clusters > 1 && l.n_tiles <= 3 * C && (clusters == C || whole == 0) && shared < 0.93 * best)
+      best = shared, pick = &s, pick_whole = whole, pick_clusters = clusters;
+  }
+  lay(l, *pick);
+  l.whole = pick_whole;
+  l.clusters = std::min(pick_clusters, l.whole == l.n_tiles ? l.n_tiles : pick_clusters);
+  const int64_t slot = (int64_t)l.clusters * l.cta * 128 * l.n_tile * 4;
+  l.slot_bytes = l.flag_bytes = 0;
+  if (l.whole < l.n_tiles) {
+    share_out(l, pick->kb);
+    l.slot_bytes = slot;
+    l.flag_bytes = (int64_t)l.clusters * l.cta * kEpiWarps * 4;
+  }
+  if (parts)
+    for (int k = 0; k < l.n_jobs; ++k)
+      if (l.job[k].kb > 2 * kChainKb) l.slot_bytes = 2 * slot;
+}
+
+cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, const char** what) {
   DeviceState dev;
   *what = "kernel attributes";
   cudaError_t e = device_state(&dev);
   if (e != cudaSuccess) return e;
+  const int fit = l.cta == 2 ? dev.pairs : dev.sms;
+  if (fit < l.clusters) {   // not a whole GB300: only whole tiles can be taken by fewer clusters
+    *what = "the product is planned for 152 SMs";
+    if (l.whole < l.n_tiles) return cudaErrorInvalidConfiguration;
+  }
+  const int clusters = std::min(fit, l.clusters);
   ProdArgs a;
-  JoinArgs join;
-  join.n_jobs = 0, join.epi = l.epi;
-  Carver c(partial);
-  a.n_jobs = l.n_jobs, a.n_tiles = l.n_tiles, a.fp16 = l.fp16, a.n_tile = l.n_tile;
+  a.n_jobs = l.n_jobs, a.n_tiles = l.n_tiles, a.n_maps = 0, a.fp16 = l.fp16, a.n_tile = l.n_tile;
   a.chains = l.chains, a.stages = stage_count(l.cta, l.n_tile);
+  a.whole = l.whole, a.part_kb = l.f32 && !l.fp16 ? 2 * kChainKb : 1 << 30;
+  a.slots = (float*)slots, a.flags = (int*)flags;
+  for (int c = 0; c <= kSms; ++c) a.cut[c] = c <= l.clusters && l.whole < l.n_tiles ? l.cut[c] : 0;
   bool done[kProdMaps] = {};
-  int64_t join_work = 0;
   *what = "cuTensorMapEncodeTiled";
   for (int k = 0; k < l.n_jobs; ++k) {
     ProdJob& j = l.job[k];
-    if (j.splits > 1) {
-      j.partial = (float*)c.take((int64_t)j.splits * j.M * j.ldp * 4);
-      join.job[join.n_jobs++] = j;
-      join_work = std::max<int64_t>(join_work, (int64_t)j.M * ceil_div(j.N, 4));
-    }
     a.job[k] = j;
     // an operand is read with the same boxes by every product of a launch
     const int nh = l.epi == kEpiGated ? l.n_tile / 2 : l.n_tile / l.cta;
     if (!done[j.map_a] && !encode(&a.map[j.map_a], l.op[j.map_a], l.fp16, j.a_mn ? 64 : 128)) return cudaErrorInvalidValue;
     if (!done[j.map_b] && !encode(&a.map[j.map_b], l.op[j.map_b], l.fp16, j.b_mn ? 64 : nh)) return cudaErrorInvalidValue;
     done[j.map_a] = done[j.map_b] = true;
+    a.n_maps = std::max(a.n_maps, std::max(j.map_a, j.map_b) + 1);
   }
   *what = "product launch";
-  const int clusters = l.cta == 2 ? dev.pairs : dev.sms;
-  e = with_kernel(l.cta, l.epi, l.act, l.f32, [&](auto c, auto k, auto a_, auto t) {
+  return with_kernel(l.cta, l.epi, l.act, l.f32, [&](auto c, auto k, auto a_, auto t) {
     return launch<c.value, k.value, a_.value, t.value>(a, clusters, st);
   });
-  if (e == cudaSuccess && join.n_jobs) {
-    *what = "join launch";
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(join_work, 256), kSms * 8), join.n_jobs);
-    if (l.f32) launch_pdl(k_prod_join<true>, grid, dim3(256), 0, st, join);
-    else launch_pdl(k_prod_join<false>, grid, dim3(256), 0, st, join);
-    e = cudaGetLastError();
+}
+
+int64_t prod_bytes(const ProdLaunch* l, int n) {
+  int64_t slots = 0, flags = 0;
+  for (int k = 0; k < n; ++k) slots = std::max(slots, round_up(l[k].slot_bytes, 256)), flags += l[k].flag_bytes;
+  return slots + round_up(flags, 256);
+}
+
+cudaError_t prod_run_all(ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what) {
+  int64_t slots = 0, flags = 0;
+  for (int k = 0; k < n; ++k) slots = std::max(slots, round_up(l[k].slot_bytes, 256)), flags += l[k].flag_bytes;
+  char* at = (char*)workspace + slots;
+  cudaError_t e = cudaSuccess;
+  if (flags) {
+    *what = "clearing flags";
+    e = cudaMemsetAsync(at, 0, flags, st);
+  }
+  for (int k = 0; e == cudaSuccess && k < n; ++k) {
+    e = prod_run(l[k], workspace, at, st, what);
+    at += l[k].flag_bytes;
   }
   return e;
 }

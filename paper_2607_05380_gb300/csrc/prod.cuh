@@ -52,10 +52,8 @@ struct ProdJob {
   int64_t half;                    // kEpiDgated: elements from dg to du
   void *a, *p;                     // kEpiGated / kEpiDgated: act(g), u act'(g) (NULL: not wanted)
   const float *sx, *sw, *bias;     // kEpiQuant
-  // the plan (set by prod_plan)
-  int32_t kb, tm, tn, splits, kb_split, tile0;
-  float* partial;                  // splits > 1: [splits][M][ldp] fp32
-  int64_t ldp;
+  // the plan (set by prod_plan): K blocks, tiles, the first one's number
+  int32_t kb, tm, tn, tile0;
 };
 
 struct ProdLaunch {
@@ -63,8 +61,13 @@ struct ProdLaunch {
   int32_t n_jobs, n_ops;
   ProdOperand op[kProdMaps];
   ProdJob job[kProdJobs];
-  // the plan
-  int32_t cta, n_tile, chains, n_tiles;
+  // the plan: CTAs per tile, its columns, accumulator chains, tiles; clusters
+  // (tile slots that run at once), and how the tiles are shared out: tiles
+  // below whole go round robin, one cluster each; the others' K blocks, one
+  // tile after another, are cut at cut[1], cut[2], ... into one run a cluster
+  int32_t cta, n_tile, chains, n_tiles, clusters, whole;
+  int32_t cut[kSms + 1];
+  int64_t slot_bytes, flag_bytes;  // workspace for cut tiles' sums and their flags
 };
 
 // 32-bit mode: the six products of two parts that are above 2^-24, smallest
@@ -72,10 +75,14 @@ struct ProdLaunch {
 // gated block (segment = half * 3 + part).
 void prod_pairs(ProdJob& j, bool f32, int halves);
 
-// Chooses tiles and splits; *partial_bytes: workspace for the splits' sums.
-void prod_plan(ProdLaunch& l, int64_t* partial_bytes);
-// Runs a planned launch; partial: at least *partial_bytes (256-byte aligned).
-cudaError_t prod_run(ProdLaunch& l, void* partial, cudaStream_t st, const char** what);
+// Chooses tiles and shares them out.
+void prod_plan(ProdLaunch& l);
+// Runs a planned launch; slots: at least slot_bytes, flags: flag_bytes of zeros
+// (256-byte aligned).
+cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, const char** what);
+// Runs n planned launches one after another in a workspace of prod_bytes.
+int64_t prod_bytes(const ProdLaunch* l, int n);
+cudaError_t prod_run_all(ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what);
 
 // Copies operands into a layout that TMA takes: rows of `cols` elements to
 // rows of pitch ldp (a multiple of 8), in segments of rows_seg rows; fp32

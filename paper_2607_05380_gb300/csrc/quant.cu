@@ -24,17 +24,17 @@ tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
 
 struct Work {
   ProdLaunch l;
-  int64_t ldk, qx, qw, partial, bytes;
+  int64_t ldk, qx, qw, bytes;
   Work(int64_t rows, int32_t k, int32_t n, int32_t precision) {
     l = ProdLaunch{};
     l.epi = kEpiQuant, l.fp16 = 1, l.f32 = precision == TP_FP32, l.n_jobs = 1;
     ProdJob& j = l.job[0];
     j.M = (int32_t)rows, j.N = n, j.K = k;
     j.map_a = 0, j.map_b = 1, j.n_pairs = 1;
-    prod_plan(l, &partial);
+    prod_plan(l);
     ldk = round_up(k, 8);
     qx = round_up(rows * ldk * 2, 256), qw = round_up(n * ldk * 2, 256);
-    bytes = qx + qw + partial;
+    bytes = qx + qw + prod_bytes(&l, 1);
   }
 };
 
@@ -82,7 +82,7 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
   j.out = y, j.ldo = n, j.sx = scale, j.sw = w_scale, j.bias = bias;
   const char* what = "staging launch";
   cudaError_t e = stage_run(sl, st);
-  if (e == cudaSuccess) e = prod_run(o.l, w16 + o.qw, st, &what);
+  if (e == cudaSuccess) e = prod_run_all(&o.l, 1, w16 + o.qw, st, &what);
   if (e == cudaSuccess) return TP_OK;
   cudaGetLastError();   // reported here
   return ops_fail(TP_ECUDA, "pack_product_q8: %s: %s", what, cudaGetErrorString(e));
