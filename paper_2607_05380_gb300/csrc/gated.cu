@@ -47,7 +47,8 @@ struct Saved {
 };
 
 bool by_rows(const Geo& g) {
-  return !g.f32 && rows_take(g.rows, (int64_t)g.f * (2 * (int64_t)g.d + g.d_out), 2 * ((int64_t)g.d | g.f), false);
+  const int64_t weights = (int64_t)g.f * (2 * (int64_t)g.d + g.d_out);
+  return g.f32 ? rows_take32(g.rows, weights) : rows_take(g.rows, weights, 2 * ((int64_t)g.d | g.f), false);
 }
 
 constexpr int32_t kMaxDim = 1 << 17;
@@ -150,9 +151,8 @@ tp_status run(Plans& p, Stager& st, Carver& c, int64_t workspace_bytes, cudaStre
   const tp_status s = ops_device();
   if (s != TP_OK) return s;
   void* products = c.take(0);
-  const char* what = "staging launch";
-  cudaError_t e = stage_run(st.launch, stream);
-  if (e == cudaSuccess) e = prod_run_all(p.l, 2, products, stream, &what);
+  const char* what = "";
+  const cudaError_t e = prod_run_all(st.launch, p.l, 2, products, stream, &what);
   if (e == cudaSuccess) return TP_OK;
   cudaGetLastError();   // reported here
   return ops_fail(TP_ECUDA, "%s: %s: %s", who, what, cudaGetErrorString(e));
@@ -212,9 +212,12 @@ tp_status pack_gated_forward(const void* x, int64_t ldx, const void* w_gate_up, 
   if (by_rows(g)) {
     if (workspace_bytes < c.used) return ops_fail(TP_EINVAL, "a workspace of %lld bytes is needed", (long long)c.used);
     if ((s = ops_device()) != TP_OK) return s;
-    cudaError_t e = rows_gated(x, ldx, w_gate_up, rows, d, f, act, sv.h, g.ldf, saved ? sv.a : nullptr,
-                               saved ? sv.p : nullptr, stream);
-    if (e == cudaSuccess) e = rows_plain(sv.h, g.ldf, w_down, rows, f, d_out, y, stream);
+    // h for the second product: a bf16 block's kept one, a 32-bit block's in fp32
+    const int64_t ldh = g.f32 ? f : g.ldf;
+    void* h = g.f32 ? own : sv.h;
+    cudaError_t e = rows_gated(RowsGated{x, w_gate_up, ldx, rows, d, f, act, g.f32, h, ldh, saved ? sv.a : nullptr,
+                                         saved ? sv.p : nullptr, sv.h, g.ldf, rows * g.ldf}, stream);
+    if (e == cudaSuccess) e = rows_plain(h, ldh, w_down, rows, f, d_out, g.f32, y, stream);
     if (e == cudaSuccess) return TP_OK;
     cudaGetLastError();   // reported here
     return ops_fail(TP_ECUDA, "pack_gated_forward: %s", cudaGetErrorString(e));

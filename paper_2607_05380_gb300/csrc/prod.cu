@@ -766,6 +766,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
 __global__ void __launch_bounds__(256) k_stage(const __grid_constant__ StageLaunch g) {
   pdl_trigger();
   pdl_wait();
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < g.n_zero; i += 256) g.zero[i] = 0;
   const StageJob& j = g.job[blockIdx.y];
   const int groups = (int)(j.ldp >> 3);
   const int64_t total = j.rows * groups;
@@ -893,11 +895,7 @@ cudaError_t with_kernel(int cta, int epi, int act, bool f32, F f) {
     return f(std::integral_constant<int, 1>(), e, a, t);
   };
   auto type_of = [&](auto e, auto a) {
-    // 32-bit operands take tiles of one CTA only (prod_plan)
-    if (f32) {
-      if constexpr (e.value != kEpiQuant) return f(std::integral_constant<int, 1>(), e, a, std::true_type());
-      else return cta_of(e, a, std::true_type());
-    }
+    if (f32) return cta_of(e, a, std::true_type());
     return cta_of(e, a, std::false_type());
   };
   using None = std::integral_constant<int, -1>;
@@ -1051,10 +1049,15 @@ void share_out(ProdLaunch& p, double ns) {
 }  // namespace
 
 void prod_plan(ProdLaunch& l) {
-  // longest tiles first: dealt out round robin, the last round's short ones then go to the clusters with least
-  std::sort(l.job, l.job + l.n_jobs, [](const ProdJob& a, const ProdJob& b) {
-    return (int64_t)a.n_pairs * ceil_div(a.K, 64) > (int64_t)b.n_pairs * ceil_div(b.K, 64);
-  });
+  // whole tiles: the longest first; dealt out round robin, the last round's short ones then go to the clusters
+  // with least.  Shared out: the longest last, among those that are cut.
+  auto order = [&](bool longest_first) {
+    std::stable_sort(l.job, l.job + l.n_jobs, [=](const ProdJob& a, const ProdJob& b) {
+      const int64_t x = (int64_t)a.n_pairs * ceil_div(a.K, 64), y = (int64_t)b.n_pairs * ceil_div(b.K, 64);
+      return longest_first ? x > y : x < y;
+    });
+  };
+  order(true);
   const bool parts = l.f32 && !l.fp16;         // 32-bit operands: two chains in a 128-column tile
   double best = 1e300;
   const Shape* pick = nullptr;
@@ -1071,7 +1074,7 @@ void prod_plan(ProdLaunch& l) {
     }
   };
   for (const Shape& s : kShapes) {
-    if (parts && (s.cta != 1 || s.n > 128)) continue;
+    if (parts && s.n > 128) continue;
     lay(l, s);
     const int C = kSms / s.cta;
     double work = 0, longest = 0, blocks = 0;
@@ -1086,17 +1089,21 @@ void prod_plan(ProdLaunch& l) {
     const double rounds = (double)ceil_div(l.n_tiles, C);
     const double even = s.fixed + std::max(longest, rounds * work / l.n_tiles) + (l.n_jobs > 1 ? 0.5 * longest : 0.0);
     if (even < best) best = even, pick = &s, pick_whole = l.n_tiles, pick_clusters = C;
-    // the last one to two rounds shared out, where there are few; runs of at least four K blocks, at most eight
-    // clusters a tile.  (Of many rounds the last ones' tiles, cut, no longer share operands in L2 with their
-    // neighbours: 16384 rows, 1024 -> 4096, backward, 631 us against 555 us whole.)
+    // the last one to two rounds shared out: runs of at least four K blocks, at most sixteen clusters a tile.
+    // (Of many rounds the last ones' tiles, cut, no longer share operands in L2 with their neighbours: 16384 rows,
+    // 1024 -> 4096, backward, 631 us against 555 us whole.)
     const int whole = std::max(0, l.n_tiles / C - 1) * C;
-    const int clusters = (int)std::min<double>(std::min<double>(C, std::max(1.0, blocks / 4)), 8.0 * l.n_tiles);
-    const double adds = std::max(1.0, (double)clusters / (l.n_tiles - whole));
-    const double shared = s.fixed + work / clusters + 6000.0 + (1.0 + adds) * s.epi;
-    if (clusters > 1 && l.n_tiles <= 3 * C && (clusters == C || whole == 0) && shared < 0.93 * best)
+    const int clusters = (int)std::min<double>(std::min<double>(C, std::max(1.0, blocks / 4)), 16.0 * work / longest);
+    const double share = work / clusters, adds = std::max(1.0, longest / share);
+    const double shared = s.fixed + share + 6000.0 + (1.0 + adds) * s.epi;
+    if (clusters > 1 && (clusters == C || whole == 0) && shared < (l.n_tiles <= 3 * C ? 0.93 : 0.8) * best)
       best = shared, pick = &s, pick_whole = whole, pick_clusters = clusters;
   }
   lay(l, *pick);
+  if (pick_whole < l.n_tiles) {
+    order(false);
+    lay(l, *pick);
+  }
   l.whole = pick_whole;
   l.clusters = std::min(pick_clusters, l.whole == l.n_tiles ? l.n_tiles : pick_clusters);
   const int64_t slot = (int64_t)l.clusters * l.cta * 128 * l.n_tile * 4;
@@ -1146,20 +1153,31 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, c
   });
 }
 
-int64_t prod_bytes(const ProdLaunch* l, int n) {
-  int64_t slots = 0, flags = 0;
+namespace {
+void sizes(const ProdLaunch* l, int n, int64_t& slots, int64_t& flags) {
+  slots = flags = 0;
   for (int k = 0; k < n; ++k) slots = std::max(slots, round_up(l[k].slot_bytes, 256)), flags += l[k].flag_bytes;
+}
+}  // namespace
+
+int64_t prod_bytes(const ProdLaunch* l, int n) {
+  int64_t slots, flags;
+  sizes(l, n, slots, flags);
   return slots + round_up(flags, 256);
 }
 
-cudaError_t prod_run_all(ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what) {
-  int64_t slots = 0, flags = 0;
-  for (int k = 0; k < n; ++k) slots = std::max(slots, round_up(l[k].slot_bytes, 256)), flags += l[k].flag_bytes;
+cudaError_t prod_run_all(StageLaunch& stage, ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what) {
+  int64_t slots, flags;
+  sizes(l, n, slots, flags);
   char* at = (char*)workspace + slots;
   cudaError_t e = cudaSuccess;
-  if (flags) {
+  stage.zero = (int*)at, stage.n_zero = (int)(flags / 4);   // the flags, by the staging launch if there is one
+  if (flags && stage.n == 0) {
     *what = "clearing flags";
     e = cudaMemsetAsync(at, 0, flags, st);
+  } else {
+    *what = "staging launch";
+    e = stage_run(stage, st);
   }
   for (int k = 0; e == cudaSuccess && k < n; ++k) {
     e = prod_run(l[k], workspace, at, st, what);

@@ -80,10 +80,6 @@ void prod_plan(ProdLaunch& l);
 // Runs a planned launch; slots: at least slot_bytes, flags: flag_bytes of zeros
 // (256-byte aligned).
 cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, const char** what);
-// Runs n planned launches one after another in a workspace of prod_bytes.
-int64_t prod_bytes(const ProdLaunch* l, int n);
-cudaError_t prod_run_all(ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what);
-
 // Copies operands into a layout that TMA takes: rows of `cols` elements to
 // rows of pitch ldp (a multiple of 8), in segments of rows_seg rows; fp32
 // elements become three bf16 parts (segments s * 3 .. s * 3 + 2 of segment s),
@@ -98,9 +94,15 @@ struct StageJob {
 constexpr int kStageJobs = 4;
 struct StageLaunch {
   StageJob job[kStageJobs];
-  int32_t n;
+  int32_t n, n_zero;
+  int* zero;                // n_zero words are set to 0 beside the copies
 };
 cudaError_t stage_run(const StageLaunch& s, cudaStream_t st);
+
+// Runs the staging copies (none: n = 0) and then n planned launches one after
+// another in a workspace of prod_bytes.
+int64_t prod_bytes(const ProdLaunch* l, int n);
+cudaError_t prod_run_all(StageLaunch& stage, ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what);
 
 // Is a 16-bit operand fit for TMA as it lies there?
 inline bool tma_ready(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }

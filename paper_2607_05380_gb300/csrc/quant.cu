@@ -80,9 +80,8 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
   o.l.op[1] = ProdOperand{w16, o.ldk, n, k, 0, 1};
   ProdJob& j = o.l.job[0];
   j.out = y, j.ldo = n, j.sx = scale, j.sw = w_scale, j.bias = bias;
-  const char* what = "staging launch";
-  cudaError_t e = stage_run(sl, st);
-  if (e == cudaSuccess) e = prod_run_all(&o.l, 1, w16 + o.qw, st, &what);
+  const char* what = "";
+  const cudaError_t e = prod_run_all(sl, &o.l, 1, w16 + o.qw, st, &what);
   if (e == cudaSuccess) return TP_OK;
   cudaGetLastError();   // reported here
   return ops_fail(TP_ECUDA, "pack_product_q8: %s: %s", what, cudaGetErrorString(e));

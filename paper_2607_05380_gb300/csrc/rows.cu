@@ -14,6 +14,8 @@
 //
 // The weights' first steps are asked for (into L2) before the previous kernel
 // of the stream has finished.
+#include <type_traits>
+
 #include "kernels.cuh"
 #include "prod.cuh"
 #include "rows.cuh"
@@ -31,9 +33,11 @@ struct RowArgs {
   int32_t rows, k, n;
   void* out;              // [rows, ldo]
   int64_t ldo;
-  __nv_bfloat16 *a, *p;   // kGated: act(g), u act'(g) (NULL: not wanted)
+  void *a, *p;            // kGated: act(g), u act'(g), pitch ld_keep (NULL: not wanted)
+  __nv_bfloat16* parts;   // 32-bit blocks that keep something: h as three bf16 parts, `part` elements apart
+  int64_t ld_keep, part;
   const float *sx, *sw, *bias;
-  int32_t act, f32;
+  int32_t f32;            // kQuant: 32-bit output
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -221,8 +225,9 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) k_rows(const RowArgs
         const float a = act_value<kAct, false>(sum(0), d), u = sum(kR - 1);
         ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(a * u);
         if (g.a) {
-          g.a[o] = __float2bfloat16_rn(a);
-          g.p[o] = __float2bfloat16_rn(u * d);
+          const int64_t at_keep = (int64_t)m * g.ld_keep + n;
+          ((__nv_bfloat16*)g.a)[at_keep] = __float2bfloat16_rn(a);
+          ((__nv_bfloat16*)g.p)[at_keep] = __float2bfloat16_rn(u * d);
         }
       } else {
         float v = sum(c >> 4);
@@ -232,6 +237,118 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) k_rows(const RowArgs
       }
     }
   }
+}
+
+// ------------------------------------------------------ 32-bit gated blocks
+// Few rows of fp32: multiply-adds, bound by the weights' bytes up to eight rows
+// a pass.  A warp takes kC weight rows (the gated block: kC / 2 pairs) and
+// kM rows of x; its lanes take K in groups of four, kC weight loads for kM
+// loads of x (which the block's warps share in L1).  kVec: whole groups
+// at multiples of 16 bytes; else element by element, in the same order.
+template <int kC, int kM, bool kGate, bool kVec, int kAct>
+__global__ void __launch_bounds__(256) k_rows32(const RowArgs g) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kN = kGate ? kC / 2 : kC;                 // output columns
+  const int n0 = (blockIdx.x * 8 + warp) * kN, m0 = blockIdx.y * kM;
+  pdl_trigger();
+  pdl_wait();
+  if (n0 >= g.n) return;
+  const float *x[kM], *w[kC];
+#pragma unroll
+  for (int m = 0; m < kM; ++m) x[m] = (const float*)g.x + (int64_t)min(m0 + m, g.rows - 1) * g.ldx;
+#pragma unroll
+  for (int c = 0; c < kC; ++c)
+    w[c] = (const float*)g.w + (int64_t)min(n0 + c % kN, g.n - 1) * g.k + (kGate && c >= kN ? g.up : 0);
+  float acc[kC * kM];
+#pragma unroll
+  for (int i = 0; i < kC * kM; ++i) acc[i] = 0.f;
+#pragma unroll 2
+  for (int k = 4 * lane; k < g.k; k += 128) {
+    auto four = [&](const float* p, float (&v)[4]) {
+      if constexpr (kVec) {
+        const float4 q = *reinterpret_cast<const float4*>(p + k);
+        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = k + e < g.k ? p[k + e] : 0.f;
+      }
+    };
+    float wv[kC][4], xv[kM][4];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) four(w[c], wv[c]);
+#pragma unroll
+    for (int m = 0; m < kM; ++m) four(x[m], xv[m]);
+#pragma unroll
+    for (int m = 0; m < kM; ++m)
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[kM * c + m] = fmaf(wv[c][e], xv[m][e], acc[kM * c + m]);
+  }
+  // the lanes' sums: halving exchanges until every lane holds one of the kC kM
+  // values, the lane's high bits its number, then the lanes of a value
+  constexpr int kVals = kC * kM, kRep = 32 / kVals;
+#pragma unroll
+  for (int h = kVals / 2; h >= 1; h >>= 1) {
+    const bool up = (lane & (h * kRep)) != 0;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float keep = up ? acc[h + i] : acc[i], send = up ? acc[i] : acc[h + i];
+      acc[i] = keep + __shfl_xor_sync(0xffffffffu, send, h * kRep);
+    }
+  }
+  float v = acc[0];
+#pragma unroll
+  for (int r = kRep / 2; r >= 1; r >>= 1) v += __shfl_xor_sync(0xffffffffu, v, r);
+  const int at = lane / kRep, c = at / kM, m = m0 + at % kM;
+  float u = 0.f;
+  if (kGate) u = __shfl_down_sync(0xffffffffu, v, 16);   // the pair's up column: half the values on
+  const int n = n0 + c;
+  if (c >= kN || m >= g.rows || n >= g.n || lane % kRep != 0) return;
+  const int64_t o = (int64_t)m * g.ldo + n;
+  if constexpr (kGate) {
+    float d;
+    const float a = act_value<kAct, true>(v, d);
+    float h = a * u;
+    ((float*)g.out)[o] = h;
+    if (g.a) {
+      const int64_t at_keep = (int64_t)m * g.ld_keep + n;
+      ((float*)g.a)[at_keep] = a;
+      ((float*)g.p)[at_keep] = u * d;
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const __nv_bfloat16 b = __float2bfloat16_rn(h);
+        g.parts[q * g.part + at_keep] = b;
+        h -= __bfloat162float(b);
+      }
+    }
+  } else {
+    ((float*)g.out)[o] = v;
+  }
+}
+
+template <bool kGate, int kAct>
+cudaError_t start32(const RowArgs& a, cudaStream_t st) {
+  const bool vec = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)(a.ldx * 4) | (uintptr_t)((int64_t)a.k * 4)) & 15) == 0;
+  const dim3 block(256);
+  // four weight rows a warp where that leaves a block for every SM
+  const bool four = ceil_div(a.n, kGate ? 16 : 32) >= kSms;
+  auto go = [&](auto c, auto m, auto v) {
+    const int cols = 8 * (kGate ? c.value / 2 : c.value);
+    launch_pdl(k_rows32<c.value, m.value, kGate, v.value, kAct>,
+               dim3((unsigned)ceil_div(a.n, cols), (unsigned)ceil_div(a.rows, m.value)), block, 0, st, a);
+  };
+  auto go_v = [&](auto c, auto m) {
+    if (vec) go(c, m, std::true_type());
+    else go(c, m, std::false_type());
+  };
+  auto go_m = [&](auto c) {
+    if (a.rows == 1) go_v(c, std::integral_constant<int, 1>());
+    else go_v(c, std::integral_constant<int, 8>());
+  };
+  if (four) go_m(std::integral_constant<int, 4>());
+  else go_m(std::integral_constant<int, 2>());
+  return cudaGetLastError();
 }
 
 template <int kMode, int kR, int kWarps, int kLd, int kAct>
@@ -269,6 +386,8 @@ cudaError_t start(const RowArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+bool rows_take32(int64_t rows, int64_t weights) { return rows <= 32 && rows * weights <= 150000000; }
+
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8) {
   const int64_t work = rows * weights;
   if (pitch % 4 != 0) return work <= (q8 ? 60000000 : 70000000);
@@ -277,22 +396,33 @@ bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8) {
   return rows <= 1024 && work <= (q8 ? (whole ? 700000000 : 300000000) : (whole ? 540000000 : 250000000));
 }
 
-cudaError_t rows_gated(const void* x, int64_t ldx, const void* w_gu, int64_t rows, int32_t d, int32_t f, int act, void* h,
-                       int64_t ldh, void* a, void* p, cudaStream_t st) {
-  const RowArgs r{x, w_gu, ldx, (int64_t)f * d, (int32_t)rows, d, f, h, ldh, (__nv_bfloat16*)a, (__nv_bfloat16*)p,
-                  nullptr, nullptr, nullptr, act, 0};
-  if (act == TP_ACT_RELU) return start<kGated, TP_ACT_RELU>(r, st);
-  if (act == TP_ACT_SILU) return start<kGated, TP_ACT_SILU>(r, st);
+cudaError_t rows_gated(const RowsGated& q, cudaStream_t st) {
+  RowArgs r{};
+  r.x = q.x, r.w = q.w_gu, r.ldx = q.ldx, r.up = (int64_t)q.f * q.d, r.rows = (int32_t)q.rows, r.k = q.d, r.n = q.f;
+  r.out = q.h, r.ldo = q.ldh, r.a = q.a, r.p = q.p, r.parts = (__nv_bfloat16*)q.parts, r.ld_keep = q.ld_keep, r.part = q.part;
+  if (q.f32) {
+    if (q.act == TP_ACT_RELU) return start32<true, TP_ACT_RELU>(r, st);
+    if (q.act == TP_ACT_SILU) return start32<true, TP_ACT_SILU>(r, st);
+    return start32<true, TP_ACT_GELU>(r, st);
+  }
+  if (q.act == TP_ACT_RELU) return start<kGated, TP_ACT_RELU>(r, st);
+  if (q.act == TP_ACT_SILU) return start<kGated, TP_ACT_SILU>(r, st);
   return start<kGated, TP_ACT_GELU>(r, st);
 }
 
-cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, void* y, cudaStream_t st) {
-  return start<kPlain, -1>(RowArgs{x, w, ldx, 0, (int32_t)rows, k, n, y, n, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0}, st);
+cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, bool f32, void* y,
+                       cudaStream_t st) {
+  RowArgs r{};
+  r.x = x, r.w = w, r.ldx = ldx, r.rows = (int32_t)rows, r.k = k, r.n = n, r.out = y, r.ldo = n;
+  return f32 ? start32<false, -1>(r, st) : start<kPlain, -1>(r, st);
 }
 
 cudaError_t rows_quant(const int8_t* q, int64_t ldq, const float* sx, const int8_t* w, const float* sw, const float* bias,
                        int64_t rows, int32_t k, int32_t n, bool f32, void* y, cudaStream_t st) {
-  return start<kQuant, -1>(RowArgs{q, w, ldq, 0, (int32_t)rows, k, n, y, n, nullptr, nullptr, sx, sw, bias, 0, f32}, st);
+  RowArgs r{};
+  r.x = q, r.w = w, r.ldx = ldq, r.rows = (int32_t)rows, r.k = k, r.n = n, r.out = y, r.ldo = n;
+  r.sx = sx, r.sw = sw, r.bias = bias, r.f32 = f32;
+  return start<kQuant, -1>(r, st);
 }
 
 }  // namespace tp

@@ -22,9 +22,21 @@ namespace tp {
 // 23.7) or of an element (gated 389, 1001: 32 rows 11.9 / 14.8, 128 rows 17.0 /
 // 15.3; 8-bit 2001 -> 1000: 8 rows 9.5 / 12.1, 32 rows 21.9 / 12.0) pay for less.
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8);
-cudaError_t rows_gated(const void* x, int64_t ldx, const void* w_gu, int64_t rows, int32_t d, int32_t f, int act, void* h,
-                       int64_t ldh, void* a, void* p, cudaStream_t st);
-cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, void* y,
+// The same of a 32-bit block (in fp32 multiply-adds).
+bool rows_take32(int64_t rows, int64_t weights);
+
+struct RowsGated {
+  const void *x, *w_gu;
+  int64_t ldx, rows;
+  int32_t d, f, act;
+  bool f32;
+  void* h;                 // [rows, f] in the block's type, pitch ldh
+  int64_t ldh;
+  void *a, *p, *parts;     // kept for the backward pass (NULL: nothing), pitch ld_keep: act(g), u act'(g) and,
+  int64_t ld_keep, part;   // of a 32-bit block, h as bf16 parts `part` elements apart
+};
+cudaError_t rows_gated(const RowsGated& q, cudaStream_t st);
+cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, bool f32, void* y,
                        cudaStream_t st);
 cudaError_t rows_quant(const int8_t* q, int64_t ldq, const float* sx, const int8_t* w, const float* sw, const float* bias,
                        int64_t rows, int32_t k, int32_t n, bool f32, void* y, cudaStream_t st);
