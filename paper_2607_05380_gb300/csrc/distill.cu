@@ -6,9 +6,10 @@
 //   log softmax(z / tau)_i = ((z_i - zm) c - log2 S) / log2(e)
 //   kd = tau^2 sum_j p_j (log p_j - log softmax(z / tau)[id_j])
 //   dz = [alpha tau (e / S - p) + (1 - alpha) (e1 / S1 - onehot)] / rows
-// (The difference is taken first: z_i c - zm c in one multiply-add would be off
-// by zm c's rounding, whose power of two overflows for a row that a mask left
-// at -10^10 or at the type's lowest value.)  For tau = 1, 2 and 4 e1 is the first, second or fourth power of e, so that a
+// z_i c - o in one multiply-add, o = zm c rounded, is off by that rounding, the
+// same for every class, so it drops out; but for a row that a mask left at
+// -10^10 or at the type's lowest value its power of two overflows: such rows
+// ("far") take the difference first.  For tau = 1, 2 and 4 e1 is the first, second or fourth power of e, so that a
 // class costs one exponential a pass.
 //
 // The gradient's dense part is written for every class; then, after a barrier
@@ -23,15 +24,13 @@
 //   up to 1024          16 or 32 lanes hold a row in registers
 //   above               a block takes a row: running maximum and sums in one
 //                       pass, the gradient in a second that finds the row in
-//                       L2; four 16-byte groups per thread and turn, one
-//                       comparison of maxima for each turn
+//                       L2; one warp more works out the teacher's side meanwhile
 #include <algorithm>
 #include <type_traits>
 
 #include "prod.cuh"
 
-using namespace tp;
-
+namespace tp {
 namespace {
 
 constexpr int kMaxK = 128;
@@ -67,7 +66,8 @@ __device__ __forceinline__ float pow_tau(float e) {
 
 // What a row's threads agree on once its sums are known.
 struct Row {
-  float zm;
+  float zm, o, o1;            // maximum; zm c and zm log2(e), rounded
+  bool far;                   // exponents from z - zm, not from z c - o
   float log_s, log_s1;        // base 2
   float ca, c1;               // alpha tau / (S rows), 0 without a teacher; (1 - alpha) / (S1 rows), 0 without a label
   int label;                  // -1: none
@@ -76,10 +76,12 @@ struct Row {
 
 // (all -inf: zm = -inf, s = 0)
 template <typename T>
-__device__ __forceinline__ Row make_row(const Args<T>& g, float zm, float s, float s1, bool has, int label) {
+__device__ __forceinline__ Row make_row(const Args<T>& g, float zm, bool far, float s, float s1, bool has, int label) {
   Row r;
   r.alive = !(zm == neg_inf() && s == 0.f);
   r.zm = r.alive ? zm : 0.f;
+  r.o = __fmul_rn(r.zm, g.c), r.o1 = __fmul_rn(r.zm, kLog2e);
+  r.far = far;
   r.log_s = log2f(s);
   r.log_s1 = log2f(s1);
   r.ca = has && r.alive ? g.alpha * g.tau * g.inv_rows / s : 0.f;
@@ -88,15 +90,21 @@ __device__ __forceinline__ Row make_row(const Args<T>& g, float zm, float s, flo
   return r;
 }
 
+// log2 of e and of e1 (by an exponential of its own) at a class of logit z
+__device__ __forceinline__ float power(float c, const Row& r, float z) { return r.far ? (z - r.zm) * c : fmaf(z, c, -r.o); }
+__device__ __forceinline__ float power1(const Row& r, float z) {
+  return r.far ? (z - r.zm) * kLog2e : fmaf(z, kLog2e, -r.o1);
+}
+
 // The dense part of the gradient at a class of logit z.
 template <int kHard>
 __device__ __forceinline__ float dense(float c, const Row& r, float z) {
-  const float e = ex2((z - r.zm) * c);
+  const float e = ex2(power(c, r, z));
   if (kHard == kNone) return e * r.ca;
   if (kHard == kPow1) return e * (r.ca + r.c1);
   if (kHard == kPow2) return e * fmaf(r.c1, e, r.ca);
   if (kHard == kPow4) return e * fmaf(r.c1 * e, e * e, r.ca);
-  return fmaf(r.ca, e, r.c1 * ex2((z - r.zm) * kLog2e));
+  return fmaf(r.ca, e, r.c1 * ex2(power1(r, z)));
 }
 template <typename T>
 __device__ __forceinline__ float dense_any(const Args<T>& g, const Row& r, float z) {
@@ -112,11 +120,12 @@ __device__ __forceinline__ float dense_any(const Args<T>& g, const Row& r, float
 // log softmax(z / tau) and -log softmax(z) at a class of logit z
 template <typename T>
 __device__ __forceinline__ float log_q(const Args<T>& g, const Row& r, float z) {
-  return ((z - r.zm) * g.c - r.log_s) * kLn2;
+  return (power(g.c, r, z) - r.log_s) * kLn2;
 }
 template <typename T>
 __device__ __forceinline__ float cross_entropy(const Args<T>& g, const Row& r, float z) {
-  return (r.log_s1 - (z - r.zm) * kLog2e) * kLn2;
+  const float v = g.hard == kOwn ? power1(r, z) : (float)g.hard * power(g.c, r, z);   // (kPow1, 2, 4: tau itself)
+  return (r.log_s1 - v) * kLn2;
 }
 template <typename T>
 __device__ __forceinline__ int label_of(const Args<T>& g, int64_t b) {
@@ -274,7 +283,7 @@ __global__ void __launch_bounds__(kSmallRows) k_distill_thread(const Args<T> g, 
         }
       });
     }
-    const Row r = make_row(g, zm, s, s1, has, label);
+    const Row r = make_row(g, zm, true, s, s1, has, label);
     float kd = 0.f;
     const float inv = 1.f / tot, log_tot = logf(tot);
     if (has && r.alive)
@@ -350,7 +359,7 @@ __global__ void __launch_bounds__(256) k_distill_group(const Args<T> g) {
   }
   s = group_sum<kG>(s);
   s1 = group_sum<kG>(s1);
-  const Row r = make_row(g, zm, s, s1, has, label);
+  const Row r = make_row(g, zm, true, s, s1, has, label);
   T* dz = g.dz && live ? g.dz + row * g.n : nullptr;
   if (dz) {
     by_hard(g.hard, [&](auto h) {
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(256) k_distill_group(const Args<T> g) {
 }
 
 // ------------------------------------------------- many classes: a block a row
-constexpr int kRowThreads = 512, kTurn = 4;
+constexpr int kTurn = 4;   // 16-byte groups that a thread asks for at a time
 
 template <typename T>
 struct Vec;   // 16 bytes of T
@@ -417,192 +426,296 @@ struct Vec<__nv_bfloat16> {
   }
 };
 
-// Two fp32 operations in one instruction.
-struct F2 { float x, y; };
-__device__ __forceinline__ uint64_t pack2(F2 a) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y));
-  return r;
+// 2^(v c - o) of two classes, or 2^((v - o) c), o then being the maximum itself
+template <bool kFar>
+__device__ __forceinline__ float2 exp2_of(float2 v, float o, float c) {
+  const float2 t = kFar ? __fmul2_rn(__fadd2_rn(v, make_float2(-o, -o)), make_float2(c, c))
+                        : __ffma2_rn(v, make_float2(c, c), make_float2(-o, -o));
+  return make_float2(ex2(t.x), ex2(t.y));
 }
-__device__ __forceinline__ F2 unpack2(uint64_t v) {
-  F2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
-  return unpack2(r);
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
-  return unpack2(r);
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)), "l"(pack2(c)));
-  return unpack2(r);
-}
-__device__ __forceinline__ F2 both(float v) { return F2{v, v}; }
-// 2^((v - zm) c) of two
-__device__ __forceinline__ F2 exp2_of(F2 v, float zm, float c) {
-  const F2 t = mul2(add2(v, both(-zm)), both(c));
-  return F2{ex2(t.x), ex2(t.y)};
-}
-template <int kHard>
-__device__ __forceinline__ F2 dense2(float c, const Row& r, F2 v) {
-  const F2 e = exp2_of(v, r.zm, c);
-  if (kHard == kNone) return mul2(e, both(r.ca));
-  if (kHard == kPow1) return mul2(e, both(r.ca + r.c1));
-  if (kHard == kPow2) return mul2(e, fma2(both(r.c1), e, both(r.ca)));
-  if (kHard == kPow4) return mul2(e, fma2(mul2(both(r.c1), e), mul2(e, e), both(r.ca)));
-  return fma2(both(r.ca), e, mul2(both(r.c1), exp2_of(v, r.zm, kLog2e)));
+template <int kHard, bool kFar>
+__device__ __forceinline__ float2 dense2(float c, const Row& r, float2 v) {
+  const float2 e = exp2_of<kFar>(v, kFar ? r.zm : r.o, c);
+  const float2 ca = make_float2(r.ca, r.ca), c1 = make_float2(r.c1, r.c1);
+  if (kHard == kNone) return __fmul2_rn(e, ca);
+  if (kHard == kPow1) return __fmul2_rn(e, __fadd2_rn(ca, c1));
+  if (kHard == kPow2) return __fmul2_rn(e, __ffma2_rn(c1, e, ca));
+  if (kHard == kPow4) return __fmul2_rn(e, __ffma2_rn(__fmul2_rn(c1, e), __fmul2_rn(e, e), ca));
+  return __ffma2_rn(ca, e, __fmul2_rn(c1, exp2_of<kFar>(v, kFar ? r.zm : r.o1, kLog2e)));
 }
 
-// A thread's running maximum and sums (of even and odd classes).
-template <int kHard>
+// m c rounded (not folded into a multiply-add, which would be another offset)
+// and kept finite, so that two equal ones differ by 0.
+__device__ __forceinline__ float offset(float m, float c) {
+  return fminf(fmaxf(__fmul_rn(m, c), -3.402823466e38f), 3.402823466e38f);
+}
+
+// A thread's running maximum m, the offsets its exponents were taken with, and
+// its sums (of even and odd classes).
+template <int kHard, bool kFar>
 struct Running {
-  float m = neg_inf();
-  F2 s{0.f, 0.f}, s1{0.f, 0.f};
+  float m = neg_inf(), o = neg_inf(), o1 = neg_inf();
+  float2 s{0.f, 0.f}, s1{0.f, 0.f};
   __device__ __forceinline__ void raise(float top, float c) {
     if (!(top > m)) return;
-    const float f = ex2((m - top) * c);   // 0 at first
-    s = mul2(s, both(f));
-    s1 = mul2(s1, both(kHard == kOwn ? ex2((m - top) * kLog2e) : pow_tau<kHard>(f)));
     m = top;
+    const float to = kFar ? m : offset(m, c), to1 = kFar ? m : offset(m, kLog2e);
+    const float f = ex2(kFar ? (o - to) * c : o - to);   // 0 at first
+    const float f1 = kHard == kOwn ? ex2(kFar ? (o1 - to1) * kLog2e : o1 - to1) : pow_tau<kHard>(f);
+    s = __fmul2_rn(s, make_float2(f, f));
+    s1 = __fmul2_rn(s1, make_float2(f1, f1));
+    o = to, o1 = to1;
   }
-  __device__ __forceinline__ void add(F2 v, float c) {
-    const F2 e = exp2_of(v, m, c);
-    s = add2(s, e);
-    if (kHard == kOwn) s1 = add2(s1, exp2_of(v, m, kLog2e));
-    else if (kHard == kPow2) s1 = fma2(e, e, s1);
-    else if (kHard == kPow4) s1 = fma2(mul2(e, e), mul2(e, e), s1);
+  __device__ __forceinline__ void add(float2 v, float c) {
+    const float2 e = exp2_of<kFar>(v, o, c);
+    s = __fadd2_rn(s, e);
+    if (kHard == kOwn) s1 = __fadd2_rn(s1, exp2_of<kFar>(v, o1, kLog2e));
+    else if (kHard == kPow2) s1 = __ffma2_rn(e, e, s1);
+    else if (kHard == kPow4) s1 = __ffma2_rn(__fmul2_rn(e, e), __fmul2_rn(e, e), s1);
     else if (kHard == kPow1) s1 = s;
   }
-  // nothing above -inf so far: only a NaN counts
   __device__ __forceinline__ void only_nan(float v) {
     if (v != v) s.x = s1.x = v;
   }
 };
 
-template <typename T, int kHard>
-__global__ void __launch_bounds__(kRowThreads, 3) k_distill_row(const Args<T> g) {
+// |zm c| from which on a row is far: below, the product's rounding is less than 2^3
+constexpr float kFarPower = 67108864.f;
+
+// A row's 16-byte groups and the single classes at its ends.
+template <typename T>
+struct Span {
+  const T* z;
+  const uint4* zv;
+  int head, body, single;
+  bool mine;
+  __device__ __forceinline__ Span(const T* p, int n, int tid) : z(p) {
+    constexpr int kN = Vec<T>::kN;
+    head = min(n, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T));
+    body = (n - head) / kN;
+    const int tail = head + body * kN;
+    zv = reinterpret_cast<const uint4*>(z + head);
+    single = tid < head ? tid : tail + tid - head;   // at most 2 (kN - 1) of them
+    mine = single < n;
+  }
+};
+
+// sums of the offset of maximum m brought to that of maximum `to`
+template <int kHard, bool kFar>
+__device__ __forceinline__ void bring(float& s, float& s1, float m, float to, float c) {
+  if (to == neg_inf()) return;   // no class above -inf: 0 or NaN as it is
+  const float f = ex2(kFar ? (m - to) * c : offset(m, c) - offset(to, c));
+  s *= f;
+  s1 *= kHard == kOwn ? ex2(kFar ? (m - to) * kLog2e : offset(m, kLog2e) - offset(to, kLog2e)) : pow_tau<kHard>(f);
+}
+
+// What a thread sees while its maximum is -inf, or twice as far out as a row
+// that is not far may lie, counts only if it is NaN: either the row's own
+// maximum is so much larger that it adds 0, or the row is far and the sums are
+// taken again.
+template <int kHard, bool kFar>
+__device__ __forceinline__ bool nothing(const Running<kHard, kFar>& q, float c) {
+  return kFar ? q.m == neg_inf() : !(fabsf(q.m) * fmaxf(c, kLog2e) < 2.f * kFarPower);
+}
+// (out of line: predicated into the loop, its comparisons were a quarter of it)
+template <typename T>
+__device__ __noinline__ float find_nan(uint4 u) {
   using V = Vec<T>;
-  constexpr int kWarps = kRowThreads / 32, kN = V::kN;
+  float v[V::kN], s = 0.f;
+  V::get(u, v);
+#pragma unroll
+  for (int e = 0; e < V::kN; ++e) s = v[e] != v[e] ? v[e] : s;
+  return s;
+}
+// kCount groups of a thread into its sums.
+template <typename T, int kHard, bool kFar, int kCount>
+__device__ __forceinline__ void take(Running<kHard, kFar>& q, const uint4 (&u)[kCount], float c) {
+  using V = Vec<T>;
+  float top = V::top(u[0]);
+#pragma unroll
+  for (int k = 1; k < kCount; ++k) top = fmaxf(top, V::top(u[k]));
+  q.raise(top, c);
+  if (nothing(q, c)) {
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) q.only_nan(find_nan<T>(u[k]));
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kCount; ++k) {
+    float v[V::kN];
+    V::get(u[k], v);
+#pragma unroll
+    for (int e = 0; e < V::kN; e += 2) q.add(make_float2(v[e], v[e + 1]), c);
+  }
+}
+// A warp's maximum and sums: the thread's single class, then the lanes joined.
+template <typename T, int kHard, bool kFar, int kWarps>
+__device__ __forceinline__ void finish(Running<kHard, kFar>& q, const Span<T>& sp, float c, float (*red)[kWarps]) {
+  if (sp.mine) {
+    const float v = Elem<T>::to_f(sp.z[sp.single]);
+    q.raise(v, c);
+    if (nothing(q, c)) q.only_nan(v);
+    else q.add(make_float2(v, neg_inf()), c);
+  }
+  float s = q.s.x + q.s.y, s1 = q.s1.x + q.s1.y;
+  const float wm = group_max<32>(q.m);
+  bring<kHard, kFar>(s, s1, q.m, wm, c);
+  s = group_sum<32>(s);
+  s1 = group_sum<32>(s1);
+  if ((threadIdx.x & 31) == 0) {
+    const int w = threadIdx.x >> 5;
+    red[0][w] = wm, red[1][w] = s, red[2][w] = s1;
+  }
+}
+struct Sums { float zm, s, s1; };
+template <int kHard, bool kFar, int kWarps>
+__device__ __forceinline__ Sums row_join(float c, const float (*red)[kWarps]) {
+  Sums t{neg_inf(), 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) t.zm = fmaxf(t.zm, red[0][k]);
+#pragma unroll 4
+  for (int k = 0; k < kWarps; ++k) {
+    float a = red[1][k], a1 = red[2][k];
+    bring<kHard, kFar>(a, a1, red[0][k], t.zm, c);
+    t.s += a;
+    t.s1 += a1;
+  }
+  return t;
+}
+
+// A row's sums by kWarps warps.
+template <typename T, int kHard, bool kFar, int kWarps>
+__device__ __forceinline__ void row_part(const Span<T>& sp, float c, float (*red)[kWarps]) {
+  constexpr int kThreads = 32 * kWarps;
+  Running<kHard, kFar> q;
+  int i = threadIdx.x;
+  for (; i + (kTurn - 1) * kThreads < sp.body; i += kTurn * kThreads) {
+    uint4 u[kTurn];
+#pragma unroll
+    for (int k = 0; k < kTurn; ++k) u[k] = sp.zv[i + k * kThreads];
+    take<T, kHard, kFar, kTurn>(q, u, c);
+  }
+  for (; i < sp.body; i += kThreads) {
+    const uint4 u[1] = {sp.zv[i]};
+    take<T, kHard, kFar, 1>(q, u, c);
+  }
+  finish<T, kHard, kFar, kWarps>(q, sp, c, red);
+}
+
+// A row's dense gradient by kWarps warps; kSame: dz lies as z does in its
+// 16-byte groups.
+template <typename T, int kHard, bool kFar, bool kSame, int kWarps>
+__device__ __forceinline__ void row_dense(const Span<T>& sp, float c, const Row& r, T* dz) {
+  using V = Vec<T>;
+  constexpr int kN = V::kN, kThreads = 32 * kWarps;
+  auto put = [&](int at, const uint4& u) {
+    float v[kN];
+    V::get(u, v);
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+      const float2 d = dense2<kHard, kFar>(c, r, make_float2(v[e], v[e + 1]));
+      v[e] = d.x, v[e + 1] = d.y;
+    }
+    if constexpr (kSame) {
+      reinterpret_cast<uint4*>(dz + sp.head)[at] = V::put(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kN; ++e) dz[sp.head + at * kN + e] = Elem<T>::from_f(v[e]);
+    }
+  };
+  int i = threadIdx.x;
+  for (; i + (kTurn - 1) * kThreads < sp.body; i += kTurn * kThreads) {
+    uint4 u[kTurn];
+#pragma unroll
+    for (int k = 0; k < kTurn; ++k) u[k] = sp.zv[i + k * kThreads];
+#pragma unroll
+    for (int k = 0; k < kTurn; ++k) put(i + k * kThreads, u[k]);
+  }
+  for (; i < sp.body; i += kThreads) put(i, sp.zv[i]);
+  if (sp.mine) dz[sp.single] = Elem<T>::from_f(dense<kHard>(c, r, Elem<T>::to_f(sp.z[sp.single])));
+}
+
+// kWarps warps take the classes; one more works out the teacher's distribution
+// while they take the sums, and the entries' gradients and the loss while they
+// write the dense part; its values go over theirs after the last barrier.
+template <typename T, int kHard, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distill_row(const Args<T> g) {
+  constexpr int kPer = kMaxK / 32;   // entries of a lane
   __shared__ int ids[kMaxK];
   __shared__ float p[kMaxK];
-  __shared__ float rm[kWarps], rs[kWarps], rs1[kWarps];
+  __shared__ float red[2][3][kWarps];
   __shared__ int has_s;
-  __shared__ float hi_s, log_tot_s;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+  const int lane = threadIdx.x & 31;
+  const bool extra = threadIdx.x >= 32 * kWarps;
   pdl_trigger();
   pdl_wait();
   const int64_t row = blockIdx.x, b = row % g.rows;
   const T* z = g.z + row * g.n;
-  const int label = label_of(g, b);
-  if (warp == 0 && g.soft) {
-    float hi = 0.f, log_tot = 0.f;
-    const bool any = teacher<T, 32>(g, b, lane, lane, ids, p, hi, log_tot);
-    if (lane == 0) has_s = any, hi_s = hi, log_tot_s = log_tot;
-  }
-  // single classes up to the first 16-byte boundary, groups, and single ones at the end
-  const int head = min(g.n, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T));
-  const int body = (g.n - head) / kN, tail = head + body * kN;
-  const uint4* zv = reinterpret_cast<const uint4*>(z + head);
-  const int single = tid < head ? tid : tail + tid - head;   // at most 2 (kN - 1) of them
-  const bool mine = single < g.n && (tid < head || single >= tail);
-  Running<kHard> q;
-  for (int i = tid; i < body; i += kTurn * kRowThreads) {
-    uint4 u[kTurn];
-#pragma unroll
-    for (int k = 0; k < kTurn; ++k) u[k] = i + k * kRowThreads < body ? zv[i + k * kRowThreads] : V::none();
-    float top = V::top(u[0]);
-#pragma unroll
-    for (int k = 1; k < kTurn; ++k) top = fmaxf(top, V::top(u[k]));
-    q.raise(top, g.c);
-#pragma unroll
-    for (int k = 0; k < kTurn; ++k) {
-      float v[kN];
-      V::get(u[k], v);
-      if (q.m == neg_inf()) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) q.only_nan(v[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kN; e += 2) q.add(F2{v[e], v[e + 1]}, g.c);
-      }
-    }
-  }
-  if (mine) {
-    const float v = Elem<T>::to_f(z[single]);
-    q.raise(v, g.c);
-    if (q.m == neg_inf()) q.only_nan(v);
-    else q.add(F2{v, neg_inf()}, g.c);
-  }
-  auto join = [&](float& s, float& s1, float m, float to) {
-    if (to == neg_inf()) return;   // no class above -inf: 0 or NaN as it is
-    const float f = ex2((m - to) * g.c);
-    s *= f;
-    s1 *= kHard == kOwn ? ex2((m - to) * kLog2e) : pow_tau<kHard>(f);
-  };
-  float s = q.s.x + q.s.y, s1 = q.s1.x + q.s1.y;
-  const float wm = group_max<32>(q.m);
-  join(s, s1, q.m, wm);
-  s = group_sum<32>(s);
-  s1 = group_sum<32>(s1);
-  if (lane == 0) rm[warp] = wm, rs[warp] = s, rs1[warp] = s1;
-  __syncthreads();
-  float zm = neg_inf();
-  s = s1 = 0.f;
-#pragma unroll
-  for (int k = 0; k < kWarps; ++k) zm = fmaxf(zm, rm[k]);
-#pragma unroll 4
-  for (int k = 0; k < kWarps; ++k) {
-    float a = rs[k], a1 = rs1[k];
-    join(a, a1, rm[k], zm);
-    s += a;
-    s1 += a1;
-  }
-  const bool has = g.soft && has_s;
-  const Row r = make_row(g, zm, s, s1, has, label);
   T* dz = g.dz ? g.dz + row * g.n : nullptr;
-  if (dz) {
-    if ((((uintptr_t)z ^ (uintptr_t)dz) & 15) == 0) {
-      uint4* dv = reinterpret_cast<uint4*>(dz + head);
-      for (int i = tid; i < body; i += kTurn * kRowThreads) {
-        uint4 u[kTurn];
+  const int label = label_of(g, b);
+  const Span<T> sp(z, g.n, threadIdx.x);
+  float hi = 0.f, log_tot = 0.f, z_entry[kPer], z_label = 0.f;
+  if (extra) {
+    bool any = false;
+    if (g.soft) any = teacher<T, 32>(g, b, lane, lane, ids, p, hi, log_tot);
+    if (lane == 0) has_s = any;
 #pragma unroll
-        for (int k = 0; k < kTurn; ++k) u[k] = i + k * kRowThreads < body ? zv[i + k * kRowThreads] : V::none();
-#pragma unroll
-        for (int k = 0; k < kTurn; ++k) {
-          float v[kN];
-          V::get(u[k], v);
-#pragma unroll
-          for (int e = 0; e < kN; e += 2) {
-            const F2 d = dense2<kHard>(g.c, r, F2{v[e], v[e + 1]});
-            v[e] = d.x, v[e + 1] = d.y;
-          }
-          if (i + k * kRowThreads < body) dv[i + k * kRowThreads] = V::put(v);
-        }
-      }
-      if (mine) dz[single] = Elem<T>::from_f(dense<kHard>(g.c, r, Elem<T>::to_f(z[single])));
-    } else {   // dz starts at another place of a 16-byte group than z
-      for (int i = tid; i < g.n; i += kRowThreads) dz[i] = Elem<T>::from_f(dense<kHard>(g.c, r, Elem<T>::to_f(z[i])));
+    for (int i = 0; i < kPer; ++i) {
+      const int j = lane + 32 * i;
+      z_entry[i] = any && j < g.k && ids[j] >= 0 ? Elem<T>::to_f(z[ids[j]]) : 0.f;
     }
+    if (label >= 0) z_label = Elem<T>::to_f(z[label]);
+  } else {
+    row_part<T, kHard, false, kWarps>(sp, g.c, red[0]);
+  }
+  __syncthreads();
+  Sums a = row_join<kHard, false, kWarps>(g.c, red[0]);
+  const bool far = fabsf(a.zm) * fmaxf(g.c, kLog2e) >= kFarPower && a.zm != neg_inf();   // (an infinite maximum: NaN either way)
+  if (far) {
+    if (!extra) row_part<T, kHard, true, kWarps>(sp, g.c, red[1]);
     __syncthreads();
+    a = row_join<kHard, true, kWarps>(g.c, red[1]);
   }
-  if (warp == 0) {
-    float kd = 0.f;
-    if (has && r.alive)
-      for (int j = lane; j < g.k; j += 32)
-        kd += entry(g, r, z, dz, ids, p, (g.top[b * g.k + j] - hi_s) * (g.c * kLn2) - log_tot_s, j);
-    kd = group_sum<32>(kd);
-    if (lane == 0) {
-      label_entry(g, r, z, dz, ids, has);
-      g.row_loss[row] = row_loss(g, r, has, kd, r.label >= 0 ? Elem<T>::to_f(z[r.label]) : 0.f);
-    }
+  const bool has = has_s;
+  const Row r = make_row(g, a.zm, far, a.s, a.s1, has, label);
+  if (!extra) {
+    if (dz == nullptr) return;
+    const bool same = (((uintptr_t)z ^ (uintptr_t)dz) & 15) == 0;
+    if (far) row_dense<T, kHard, true, false, kWarps>(sp, g.c, r, dz);
+    else if (same) row_dense<T, kHard, false, true, kWarps>(sp, g.c, r, dz);
+    else row_dense<T, kHard, false, false, kWarps>(sp, g.c, r, dz);
+    __syncthreads();
+    return;
   }
+  // the entries' gradients and the loss, while the dense part is written
+  float d_entry[kPer], d_label = 0.f, kd = 0.f;
+  const float ones = (1.f - g.alpha) * g.inv_rows;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int j = lane + 32 * i, id = has && r.alive && j < g.k ? ids[j] : -1;
+    d_entry[i] = 0.f;
+    if (id < 0) continue;
+    float same = 0.f;
+    if (dz)
+      for (int q = 0; q < g.k; ++q) same += ids[q] == id ? p[q] : 0.f;
+    d_entry[i] = dense<kHard>(g.c, r, z_entry[i]) - g.alpha * g.tau * g.inv_rows * same;
+    if (id == r.label) d_entry[i] -= ones, found = true;
+    if (p[j] != 0.f)
+      kd += p[j] * ((g.top[b * g.k + j] - hi) * (g.c * kLn2) - log_tot - log_q(g, r, z_entry[i]));
+  }
+  const bool label_apart = !__any_sync(0xffffffffu, found) && r.label >= 0;
+  if (label_apart) d_label = dense<kHard>(g.c, r, z_label) - ones;
+  kd = group_sum<32>(kd);
+  if (lane == 0) g.row_loss[row] = row_loss(g, r, has, kd, z_label);
+  if (dz == nullptr) return;
+  __syncthreads();   // over the dense part
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int j = lane + 32 * i;
+    if (has && r.alive && j < g.k && ids[j] >= 0) dz[ids[j]] = Elem<T>::from_f(d_entry[i]);
+  }
+  if (label_apart && lane == 0) dz[r.label] = Elem<T>::from_f(d_label);
 }
 
 // A student's mean over its rows, in a fixed order.
@@ -629,8 +742,18 @@ void group(const Args<T>& a, cudaStream_t st) {
              (size_t)(256 / kG) * a.k * 8, st, a);
 }
 
+template <typename T, int kWarps>
+void wide(const Args<T>& a, cudaStream_t st) {
+  const dim3 grid((unsigned)a.all), block(32 * kWarps + 32);
+  if (a.hard == kNone) launch_pdl(k_distill_row<T, kNone, kWarps>, grid, block, 0, st, a);
+  else if (a.hard == kPow1) launch_pdl(k_distill_row<T, kPow1, kWarps>, grid, block, 0, st, a);
+  else if (a.hard == kPow2) launch_pdl(k_distill_row<T, kPow2, kWarps>, grid, block, 0, st, a);
+  else if (a.hard == kPow4) launch_pdl(k_distill_row<T, kPow4, kWarps>, grid, block, 0, st, a);
+  else launch_pdl(k_distill_row<T, kOwn, kWarps>, grid, block, 0, st, a);
+}
+
 template <typename T>
-void rows(const Args<T>& a, cudaStream_t st) {
+cudaError_t rows(const Args<T>& a, cudaStream_t st) {
   if (a.n <= kSmallN) {
     const uint32_t div = ((1u << 20) + a.n - 1) / a.n;   // i / n = i div >> 20 for i < 128 * 32
     launch_pdl(k_distill_thread<T>, dim3((unsigned)ceil_div(a.all, kSmallRows)), dim3(kSmallRows),
@@ -645,14 +768,12 @@ void rows(const Args<T>& a, cudaStream_t st) {
     group<T, 32, 16>(a, st);
   } else if (a.n <= 1024) {
     group<T, 32, 32>(a, st);
+  } else if (a.n * (int64_t)sizeof(T) <= 32768) {
+    wide<T, 4>(a, st);
   } else {
-    const dim3 grid((unsigned)a.all), block(kRowThreads);
-    if (a.hard == kNone) launch_pdl(k_distill_row<T, kNone>, grid, block, 0, st, a);
-    else if (a.hard == kPow1) launch_pdl(k_distill_row<T, kPow1>, grid, block, 0, st, a);
-    else if (a.hard == kPow2) launch_pdl(k_distill_row<T, kPow2>, grid, block, 0, st, a);
-    else if (a.hard == kPow4) launch_pdl(k_distill_row<T, kPow4>, grid, block, 0, st, a);
-    else launch_pdl(k_distill_row<T, kOwn>, grid, block, 0, st, a);
+    wide<T, 15>(a, st);
   }
+  return cudaGetLastError();
 }
 
 tp_status check(int64_t m, int64_t rows) {
@@ -663,6 +784,9 @@ tp_status check(int64_t m, int64_t rows) {
 }
 
 }  // namespace
+}  // namespace tp
+
+using namespace tp;
 
 extern "C" {
 
@@ -700,13 +824,15 @@ tp_status pack_distill(const void* z, int64_t m, int64_t n_rows, int32_t n, cons
     const int hard = !(alpha < 1.f && labels) ? kNone : tau == 1.f ? kPow1 : tau == 2.f ? kPow2 : tau == 4.f ? kPow4 : kOwn;
     const float c = kLog2e / tau;
     if (precision == TP_FP32)
-      rows(Args<float>{(const float*)z, ids, labels, top, (float*)dz, rl, m * n_rows, n_rows, n, k, soft, hard, c, tau,
+      e = rows(Args<float>{(const float*)z, ids, labels, top, (float*)dz, rl, m * n_rows, n_rows, n, k, soft, hard, c, tau,
                        alpha, 1.f / (float)n_rows}, st);
     else
-      rows(Args<__nv_bfloat16>{(const __nv_bfloat16*)z, ids, labels, top, (__nv_bfloat16*)dz, rl, m * n_rows, n_rows, n, k,
+      e = rows(Args<__nv_bfloat16>{(const __nv_bfloat16*)z, ids, labels, top, (__nv_bfloat16*)dz, rl, m * n_rows, n_rows, n, k,
                                soft, hard, c, tau, alpha, 1.f / (float)n_rows}, st);
-    launch_pdl(k_distill_mean, dim3((unsigned)m), dim3(256), 0, st, (const float*)rl, n_rows, loss);
-    e = cudaGetLastError();
+    if (e == cudaSuccess) {
+      launch_pdl(k_distill_mean, dim3((unsigned)m), dim3(256), 0, st, (const float*)rl, n_rows, loss);
+      e = cudaGetLastError();
+    }
   }
   if (e == cudaSuccess) return TP_OK;
   cudaGetLastError();   // reported here
