@@ -9,10 +9,9 @@
 // the same block of up columns, so that the epilogue has both factors of h in
 // registers and neither g nor u is written.  For the backward pass it keeps
 // act(g) and u act'(g), the two numbers that dh is multiplied by, instead of g
-// and u: one rounding to bf16 each, where rounding g and u would enter both
-// products through act and act' again, and no exponential in the backward
-// epilogue.  Roundings to bf16 (of bf16 blocks): h, act(g), u act'(g), dg, du,
-// because the tensor cores take them so; every sum is fp32.  32-bit blocks
+// and u, to 24 bits: no exponential in the backward epilogue, and no rounding
+// that shows.  Roundings to bf16 (of bf16 blocks): h, dg and du, because the
+// tensor cores take them so; every sum is fp32.  32-bit blocks
 // keep fp32 and multiply in three bf16 parts each (see prod.cu).
 #include "prod.cuh"
 #include "rows.cuh"
@@ -28,13 +27,14 @@ struct Geo {
   int parts;                     // bf16 parts of an operand
   int64_t ldf;                   // pitch of h, act(g), u act'(g) and their gradients: whole 32-byte sectors
   Geo(int64_t r, int32_t d_, int32_t f_, int32_t o, int32_t prec)
-      : rows(r), d(d_), f(f_), d_out(o), f32(prec == TP_FP32), parts(f32 ? 3 : 1), ldf(round_up(f_, 16)) {}
+      : rows(r), d(d_), f(f_), d_out(o), f32(prec == TP_FP32), parts(f32 ? 3 : 1), ldf(round_up(f_, 32)) {}
 };
 
-// What a forward pass keeps: h as bf16 parts, act(g) and u act'(g) in the
-// block's type; pitch ldf.
+// What a forward pass keeps: h as bf16 parts, act(g) and u act'(g) as fp32 or,
+// of a bf16 block, as 24-bit floats; pitch ldf.
 struct Saved {
   void *h, *a, *p;
+  uint8_t *a_lo, *p_lo;
   int64_t h_bytes, bytes;
   Saved(const Geo& g, void* base) {
     Carver c(base);
@@ -42,6 +42,8 @@ struct Saved {
     h_bytes = c.used;
     a = c.take(g.rows * g.ldf * (g.f32 ? 4 : 2));
     p = c.take(g.rows * g.ldf * (g.f32 ? 4 : 2));
+    a_lo = (uint8_t*)c.take(g.f32 ? 0 : g.rows * g.ldf);
+    p_lo = (uint8_t*)c.take(g.f32 ? 0 : g.rows * g.ldf);
     bytes = c.used;
   }
 };
@@ -116,7 +118,7 @@ void plan_forward(Plans& p, const Geo& g, int act, const ProdOperand& x, const P
   job(p.l[0], g.rows, g.f, g.d, 0, 1, false, false, 1, s.h, g.ldf);
   ProdJob& j = p.l[0].job[0];
   j.up = g.parts, j.part = g.rows * g.ldf;
-  j.a = keep ? s.a : nullptr, j.p = keep ? s.p : nullptr;
+  j.a = keep ? s.a : nullptr, j.p = keep ? s.p : nullptr, j.a_lo = s.a_lo, j.p_lo = s.p_lo;
   start(p.l[1], g, kEpiPlain, 0);
   p.l[1].op[0] = ProdOperand{s.h, g.ldf, g.rows, g.f, g.rows * g.ldf, g.parts}, p.l[1].op[1] = wd;
   job(p.l[1], g.rows, g.d_out, g.f, 0, 1, false, false, 1, y, g.d_out);
@@ -132,6 +134,7 @@ void plan_backward(Plans& p, const Geo& g, const ProdOperand& dy, const ProdOper
   job(p.l[0], g.rows, g.f, g.d_out, 0, 1, false, true, 1, dgu, g.ldf);
   ProdJob& j = p.l[0].job[0];
   j.part = plane, j.half = g.parts * plane, j.a = s.a, j.p = s.p;
+  j.a_lo = s.a_lo, j.p_lo = s.p_lo;
 
   ProdLaunch& l = p.l[1];
   start(l, g, kEpiPlain, 0);
@@ -216,7 +219,8 @@ tp_status pack_gated_forward(const void* x, int64_t ldx, const void* w_gate_up, 
     const int64_t ldh = g.f32 ? f : g.ldf;
     void* h = g.f32 ? own : sv.h;
     cudaError_t e = rows_gated(RowsGated{x, w_gate_up, ldx, rows, d, f, act, g.f32, h, ldh, saved ? sv.a : nullptr,
-                                         saved ? sv.p : nullptr, sv.h, g.ldf, rows * g.ldf}, stream);
+                                         saved ? sv.p : nullptr, sv.h, g.ldf, rows * g.ldf, sv.a_lo,
+                                         sv.p_lo}, stream);
     if (e == cudaSuccess) e = rows_plain(h, ldh, w_down, rows, f, d_out, g.f32, y, stream);
     if (e == cudaSuccess) return TP_OK;
     cudaGetLastError();   // reported here

@@ -405,34 +405,51 @@ __device__ __forceinline__ void add_slot(const float* p, int lane, float (&v)[32
   }
 }
 
+// 24-bit floats: the upper 16 bits of 32 columns as pairs, the next 8 as quads.
+// act(g) and u act'(g) are kept so: as bf16 their rounding is a third one (beside
+// those of dg, du and the outputs), 2.9e-3 of dx instead of 2.4e-3 (norm-wise;
+// rounding the outputs alone 1.7e-3), for a byte more each.
+__device__ __forceinline__ void put_24(const float (&v)[32], __nv_bfloat16* hi, uint8_t* lo, bool live, int n) {
+  uint32_t u[16], b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = round_24(v[4 * e + i]);
+    u[2 * e] = __byte_perm(w[0], w[1], 0x7632), u[2 * e + 1] = __byte_perm(w[2], w[3], 0x7632);
+    b[e] = __byte_perm(__byte_perm(w[0], w[1], 0x0051), __byte_perm(w[2], w[3], 0x0051), 0x5410);
+  }
+  put_bf16(u, hi, live, n);
+  if (live) store32(lo, b);
+}
+
 // What the epilogue reads besides the accumulator: kEpiDgated of a bf16 block,
 // u act'(g) and act(g) of the lane's row, asked for one chunk ahead.
 struct Ahead {
-  uint32_t p[16], a[16];
-  __device__ __forceinline__ void load(const ProdJob& j, int row, int c0) {
+  uint32_t u[16], b[8];
+  __device__ __forceinline__ void load(const ProdJob& j, const void* hi, const uint8_t* lo, int row, int c0) {
     const int64_t at = (int64_t)min(row, j.M - 1) * j.ldo + c0;
-    const __nv_bfloat16 *pp = (const __nv_bfloat16*)j.p + at, *pa = (const __nv_bfloat16*)j.a + at;
-    load32(pp, p);
-    load32(pa, a);
-    if (c0 + 16 < j.N) {   // (a row has room for whole sectors)
-      load32(pp + 16, p + 8);
-      load32(pa + 16, a + 8);
+    const __nv_bfloat16* h = (const __nv_bfloat16*)hi + at;
+    load32(h, u);
+    if (c0 + 16 < j.N) load32(h + 16, u + 8);   // (a row has room for whole sectors)
+    load32(lo + at, b);
+  }
+  // f = these values times acc (what the lowest byte holds is below their rounding)
+  __device__ __forceinline__ void times(float (&f)[32], const float (&acc)[32]) const {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const uint32_t at = e & 3, hw = 4 + 2 * (e & 1);   // byte of b, first byte of the pair's half
+      f[e] = __uint_as_float(__byte_perm(b[e >> 2], u[e >> 1], at | at << 4 | hw << 8 | (hw + 1) << 12)) * acc[e];
     }
   }
 };
-__device__ __forceinline__ void times(float (&f)[32], const uint32_t (&w)[16], const float (&acc)[32]) {
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    f[2 * e] = __uint_as_float(w[e] << 16) * acc[2 * e];
-    f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * acc[2 * e + 1];
-  }
-}
 
 // The epilogue of one 32 x 32 chunk; acc: its accumulator (kEpiGated: the
 // gate product), acc2: the up product.
+// next: the column of the warp's next chunk, or -1.
 template <int kEpi, int kAct, bool kF32>
 __device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lane, float (&acc)[32], float (&acc2)[32],
-                                         const Ahead& ah, int r0, int c0) {
+                                         Ahead& ap, Ahead& aa, int r0, int c0, int next) {
   const int row = r0 + lane, n = j.N - c0;
   const bool live = row < j.M;
   const int64_t at = (int64_t)row * j.ldo + c0;
@@ -451,8 +468,8 @@ __device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lan
         put_f32(acc, (float*)j.a + at, live, n);
         put_f32(da, (float*)j.p + at, live, n);
       } else {
-        put_parts<false>(acc, (__nv_bfloat16*)j.a + at, 0, live, n);
-        put_parts<false>(da, (__nv_bfloat16*)j.p + at, 0, live, n);
+        put_24(acc, (__nv_bfloat16*)j.a + at, j.a_lo + at, live, n);
+        put_24(da, (__nv_bfloat16*)j.p + at, j.p_lo + at, live, n);
       }
     }
     put_parts<kF32>(acc2, (__nv_bfloat16*)j.out + at, j.part, live, n);
@@ -474,9 +491,11 @@ __device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lan
         put_parts<true>(f, out + h * j.half, j.part, live, n);
       }
     } else {
-      times(f, ah.p, acc);
+      ap.times(f, acc);
+      if (next >= 0) ap.load(j, j.p, j.p_lo, row, next);
       put_parts<false>(f, out, 0, live, n);
-      times(f, ah.a, acc);
+      aa.times(f, acc);
+      if (next >= 0) aa.load(j, j.a, j.a_lo, row, next);
       put_parts<false>(f, out + j.half, 0, live, n);
     }
   } else {
@@ -667,11 +686,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     while (walk.next(u)) {
       const ProdJob& j = g.job[u.job];
       const int r0 = u.m0 + rank * 128 + 32 * q;
-      Ahead ahead;
+      Ahead ahead_p, ahead_a;
       constexpr bool kAhead = kEpi == kEpiDgated && !kF32;
       const bool finish = !u.publish && !u.carry_out;
       if constexpr (kAhead)
-        if (finish && r0 < j.M && u.n0 * cols + 32 * half < j.N) ahead.load(j, r0 + lane, u.n0 * cols + 32 * half);
+        if (finish && r0 < j.M && u.n0 * cols + 32 * half < j.N) {
+          ahead_p.load(j, j.p, j.p_lo, r0 + lane, u.n0 * cols + 32 * half);
+          ahead_a.load(j, j.a, j.a_lo, r0 + lane, u.n0 * cols + 32 * half);
+        }
       if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[acc], acc_phase, abort_flag, err, 2 * kWaitNs, 46))) break;
       tc_fence_after();
       bool there = true;
@@ -728,12 +750,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
           add_slot(of + 32 * c, lane, a);
           if constexpr (kEpi == kEpiGated) add_slot(of + 32 * (cols + c), lane, a2);
         }
-        Ahead now;
-        if constexpr (kAhead) {
-          now = ahead;
-          if (c + 64 < cols && c0 + 64 < j.N) ahead.load(j, r0 + lane, c0 + 64);
-        }
-        epilogue<kEpi, kAct, kF32>(j, buf, lane, a, a2, now, r0, c0);
+        epilogue<kEpi, kAct, kF32>(j, buf, lane, a, a2, ahead_p, ahead_a, r0, c0,
+                                   c + 64 < cols && c0 + 64 < j.N ? c0 + 64 : -1);
       }
       tc_fence_before();
       __syncwarp();

@@ -50,7 +50,8 @@ struct ProdJob {
   int64_t ldo;
   int64_t part;                    // elements between the bf16 parts of out
   int64_t half;                    // kEpiDgated: elements from dg to du
-  void *a, *p;                     // kEpiGated / kEpiDgated: act(g), u act'(g) (NULL: not wanted)
+  void *a, *p;                     // kEpiGated / kEpiDgated: act(g), u act'(g) (NULL: not wanted): fp32, or of a
+  uint8_t *a_lo, *p_lo;            // bf16 block the upper 16 bits of a 24-bit float, its lower 8 here
   const float *sx, *sw, *bias;     // kEpiQuant
   // the plan (set by prod_plan): K blocks, tiles, the first one's number
   int32_t kb, tm, tn, tile0;

@@ -36,6 +36,7 @@ struct RowArgs {
   void *a, *p;            // kGated: act(g), u act'(g), pitch ld_keep (NULL: not wanted)
   __nv_bfloat16* parts;   // 32-bit blocks that keep something: h as three bf16 parts, `part` elements apart
   int64_t ld_keep, part;
+  uint8_t *a_lo, *p_lo;   // bf16 blocks: the lower 8 of a's and p's 24 bits
   const float *sx, *sw, *bias;
   int32_t f32;            // kQuant: 32-bit output
 };
@@ -226,8 +227,11 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) k_rows(const RowArgs
         ((__nv_bfloat16*)g.out)[o] = __float2bfloat16_rn(a * u);
         if (g.a) {
           const int64_t at_keep = (int64_t)m * g.ld_keep + n;
-          ((__nv_bfloat16*)g.a)[at_keep] = __float2bfloat16_rn(a);
-          ((__nv_bfloat16*)g.p)[at_keep] = __float2bfloat16_rn(u * d);
+          const uint32_t wa = round_24(a), wp = round_24(u * d);
+          ((uint16_t*)g.a)[at_keep] = (uint16_t)(wa >> 16);
+          ((uint16_t*)g.p)[at_keep] = (uint16_t)(wp >> 16);
+          g.a_lo[at_keep] = (uint8_t)(wa >> 8);
+          g.p_lo[at_keep] = (uint8_t)(wp >> 8);
         }
       } else {
         float v = sum(c >> 4);
@@ -400,6 +404,7 @@ cudaError_t rows_gated(const RowsGated& q, cudaStream_t st) {
   RowArgs r{};
   r.x = q.x, r.w = q.w_gu, r.ldx = q.ldx, r.up = (int64_t)q.f * q.d, r.rows = (int32_t)q.rows, r.k = q.d, r.n = q.f;
   r.out = q.h, r.ldo = q.ldh, r.a = q.a, r.p = q.p, r.parts = (__nv_bfloat16*)q.parts, r.ld_keep = q.ld_keep, r.part = q.part;
+  r.a_lo = q.a_lo, r.p_lo = q.p_lo;
   if (q.f32) {
     if (q.act == TP_ACT_RELU) return start32<true, TP_ACT_RELU>(r, st);
     if (q.act == TP_ACT_SILU) return start32<true, TP_ACT_SILU>(r, st);

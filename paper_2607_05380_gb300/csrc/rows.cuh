@@ -33,13 +33,20 @@ struct RowsGated {
   void* h;                 // [rows, f] in the block's type, pitch ldh
   int64_t ldh;
   void *a, *p, *parts;     // kept for the backward pass (NULL: nothing), pitch ld_keep: act(g), u act'(g) and,
-  int64_t ld_keep, part;   // of a 32-bit block, h as bf16 parts `part` elements apart
+  int64_t ld_keep, part;   // of a 32-bit block, h as bf16 parts `part` elements apart; of a bf16 block 24-bit
+  uint8_t *a_lo, *p_lo;    // floats, their lower 8 bits here
 };
 cudaError_t rows_gated(const RowsGated& q, cudaStream_t st);
 cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, int32_t k, int32_t n, bool f32, void* y,
                        cudaStream_t st);
 cudaError_t rows_quant(const int8_t* q, int64_t ldq, const float* sx, const int8_t* w, const float* sw, const float* bias,
                        int64_t rows, int32_t k, int32_t n, bool f32, void* y, cudaStream_t st);
+
+// The upper 24 bits of a float, rounded to nearest (ties up), in bits 8..31.
+__device__ __forceinline__ uint32_t round_24(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return (u & 0x7F800000u) == 0x7F800000u ? u | (u & 0xFFu ? 0x100u : 0u) : u + 0x80u;   // (a NaN stays one)
+}
 
 // act(g) and act'(g); the exponential and the quotient to 2 ulp where the
 // results are rounded to bf16.  The activation is a template parameter: all
