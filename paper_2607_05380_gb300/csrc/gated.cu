@@ -13,6 +13,8 @@
 // that shows.  Roundings to bf16 (of bf16 blocks): h, dg and du, because the
 // tensor cores take them so; every sum is fp32.  32-bit blocks
 // keep fp32 and multiply in three bf16 parts each (see prod.cu).
+#include <algorithm>
+
 #include "prod.cuh"
 #include "rows.cuh"
 
@@ -54,12 +56,13 @@ bool by_rows(const Geo& g) {
 }
 
 constexpr int32_t kMaxDim = 1 << 17;
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256, kMaxElems = int64_t(1) << 40;   // (tiles are numbered in 32 bits)
 
 tp_status check(int64_t rows, int32_t d, int32_t f, int32_t d_out, int32_t precision) {
   if (rows < 0 || rows > kMaxRows) return ops_fail(TP_EINVAL, "rows %lld out of range", (long long)rows);
   if (d < 1 || f < 1 || d_out < 1 || d > kMaxDim || f > kMaxDim || d_out > kMaxDim)
     return ops_fail(TP_EINVAL, "d %d, f %d and d_out %d must be in 1..%d", d, f, d_out, kMaxDim);
+  if (rows * std::max(d, std::max(f, d_out)) > kMaxElems) return ops_fail(TP_EINVAL, "more than 2^40 elements in a matrix");
   if (precision != TP_BF16 && precision != TP_FP32) return ops_fail(TP_EINVAL, "unknown precision %d", precision);
   return TP_OK;
 }

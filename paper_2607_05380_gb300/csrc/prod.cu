@@ -23,8 +23,9 @@
 // them ends inside a tile, whose first part it takes before all else and whose
 // fp32 sums it leaves in the workspace, and begins inside another, whose last
 // part it takes at the end, adding the sums that the clusters before it have
-// left there long since, in order.  All clusters are resident (grid <= what
-// fits), and a cluster publishes before it waits.
+// left there long since, in order.  A cluster publishes before it waits, and
+// waits only on clusters of lower numbers, which are dispatched no later than
+// it is, so the waits end whatever else holds SMs.
 //
 // Every wait is bounded (2 s): a role that gives up sets the error word that
 // pack_ops_check reads and an abort flag; the others then stop, copies and
@@ -780,67 +781,81 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
 }
 
 // ------------------------------------------------------------------ staging
-// Eight elements per thread: one pass over the source, 16-byte stores.
+// One pass over the source, 16-byte stores; a block takes 256 / 2^shift rows at
+// a time, 2^shift threads a row (a division for every group of eight elements
+// cost more than moving it).
+__device__ __forceinline__ uint4 pack_f16(const int (&v)[8]) {
+  uint32_t h[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    h[e] = __half_as_ushort(__int2half_rn(v[2 * e])) | (uint32_t)__half_as_ushort(__int2half_rn(v[2 * e + 1])) << 16;
+  return make_uint4(h[0], h[1], h[2], h[3]);
+}
 __global__ void __launch_bounds__(256) k_stage(const __grid_constant__ StageLaunch g) {
   pdl_trigger();
   pdl_wait();
   if (blockIdx.x == 0 && blockIdx.y == 0)
     for (int i = threadIdx.x; i < g.n_zero; i += 256) g.zero[i] = 0;
   const StageJob& j = g.job[blockIdx.y];
-  const int groups = (int)(j.ldp >> 3);
-  const int64_t total = j.rows * groups;
+  const int width = 1 << j.shift, tx = threadIdx.x & (width - 1), groups = (int)(j.ldp >> 3);
   const int eb = j.type == kStageF32 ? 4 : j.type == kStageS8 ? 1 : 2;
   const bool vec = ((uintptr_t)j.src & (eb == 1 ? 7 : 15)) == 0 && ((j.ld * eb) & (eb == 1 ? 7 : 15)) == 0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / groups;
-    const int c = (int)(i - r * groups) * 8;
-    const int64_t seg = r / j.rows_seg, rs = r - seg * j.rows_seg;
-    const bool whole = vec && c + 8 <= j.cols;
+  for (int64_t r = (int64_t)blockIdx.x * (256 >> j.shift) + (threadIdx.x >> j.shift); r < j.rows;
+       r += (int64_t)gridDim.x * (256 >> j.shift)) {
+    const int64_t seg = r >= j.rows_seg ? 1 : 0, rs = r - seg * j.rows_seg;   // one or two segments
     if (j.type == kStageF32) {
-      const float* p = (const float*)j.src + r * j.ld + c;
-      float v[8];
-      if (whole) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? p[e] : 0.f;
-      }
-#pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        uint32_t pk[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pk[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-          v[2 * e] -= __uint_as_float(pk[e] << 16);
-          v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
-        }
-        *reinterpret_cast<uint4*>((__nv_bfloat16*)j.dst + ((seg * 3 + q) * j.rows_seg + rs) * j.ldp + c) =
-            make_uint4(pk[0], pk[1], pk[2], pk[3]);
-      }
-    } else {
-      uint16_t h[8];
-      if (j.type == kStageS8) {
-        const int8_t* p = (const int8_t*)j.src + r * j.ld + c;
-        int8_t b[8];
-        if (whole) {
-          const uint2 w = *reinterpret_cast<const uint2*>(p);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) b[e] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+      const float* src = (const float*)j.src + r * j.ld;
+      __nv_bfloat16* dst = (__nv_bfloat16*)j.dst + (seg * 3 * j.rows_seg + rs) * j.ldp;
+#pragma unroll 2
+      for (int q8 = tx; q8 < groups; q8 += width) {
+        const int c = 8 * q8;
+        float v[8];
+        if (vec && c + 8 <= j.cols) {
+          const float4 a = *reinterpret_cast<const float4*>(src + c), b = *reinterpret_cast<const float4*>(src + c + 4);
+          v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) b[e] = c + e < j.cols ? p[e] : (int8_t)0;
+          for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? src[c + e] : 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = __half_as_ushort(__short2half_rn((short)b[e]));
-      } else {
-        const uint16_t* p = (const uint16_t*)j.src + r * j.ld + c;
+        for (int q = 0; q < 3; ++q) {
+          uint32_t pk[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = c + e < j.cols ? p[e] : (uint16_t)0;
+          for (int e = 0; e < 4; ++e) {
+            pk[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+            v[2 * e] -= __uint_as_float(pk[e] << 16);
+            v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
+          }
+          *reinterpret_cast<uint4*>(dst + q * j.rows_seg * j.ldp + c) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        }
       }
-      *reinterpret_cast<uint4*>((uint16_t*)j.dst + (seg * j.rows_seg + rs) * j.ldp + c) =
-          make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                     h[6] | (uint32_t)h[7] << 16);
+    } else {
+      uint16_t* dst = (uint16_t*)j.dst + (seg * j.rows_seg + rs) * j.ldp;
+      const int8_t* s8 = (const int8_t*)j.src + r * j.ld;
+      const uint16_t* s16 = (const uint16_t*)j.src + r * j.ld;
+#pragma unroll 4
+      for (int q8 = tx; q8 < groups; q8 += width) {
+        const int c = 8 * q8;
+        uint4 out;
+        if (j.type == kStageS8) {
+          int v[8];
+          if (vec && c + 8 <= j.cols) {
+            const uint2 w = *reinterpret_cast<const uint2*>(s8 + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? s8[c + e] : 0;
+          }
+          out = pack_f16(v);
+        } else {
+          uint32_t h[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) h[e] = c + e < j.cols ? s16[c + e] : 0u;
+          out = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        }
+        *reinterpret_cast<uint4*>(dst + c) = out;
+      }
     }
   }
 }
@@ -1204,11 +1219,16 @@ cudaError_t prod_run_all(StageLaunch& stage, ProdLaunch* l, int n, void* workspa
   return e;
 }
 
-cudaError_t stage_run(const StageLaunch& s, cudaStream_t st) {
+cudaError_t stage_run(StageLaunch& s, cudaStream_t st) {
   int64_t most = 0;
-  for (int k = 0; k < s.n; ++k) most = std::max<int64_t>(most, s.job[k].rows * (s.job[k].ldp >> 3));
-  if (s.n == 0 || most == 0) return cudaSuccess;
-  launch_pdl(k_stage, dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), kSms * 8), s.n), dim3(256), 0, st, s);
+  for (int k = 0; k < s.n; ++k) {
+    StageJob& j = s.job[k];
+    j.shift = 0;
+    while (j.shift < 8 && (1 << j.shift) < j.ldp >> 3) ++j.shift;
+    most = std::max<int64_t>(most, ceil_div(j.rows, 256 >> j.shift));
+  }
+  if (most == 0) return cudaSuccess;
+  launch_pdl(k_stage, dim3((unsigned)std::min<int64_t>(most, kSms * 8), s.n), dim3(256), 0, st, s);
   return cudaGetLastError();
 }
 

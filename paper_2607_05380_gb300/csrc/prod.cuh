@@ -89,8 +89,8 @@ enum StageType : int32_t { kStageBf16 = 0, kStageF32 = 1, kStageS8 = 2 };
 struct StageJob {
   const void* src;
   void* dst;
-  int64_t ld, rows, rows_seg, ldp;
-  int32_t cols, type;
+  int64_t ld, rows, rows_seg, ldp;   // rows: rows_seg, or twice that
+  int32_t cols, type, shift;         // shift: set by stage_run
 };
 constexpr int kStageJobs = 4;
 struct StageLaunch {
@@ -98,7 +98,7 @@ struct StageLaunch {
   int32_t n, n_zero;
   int* zero;                // n_zero words are set to 0 beside the copies
 };
-cudaError_t stage_run(const StageLaunch& s, cudaStream_t st);
+cudaError_t stage_run(StageLaunch& s, cudaStream_t st);
 
 // Runs the staging copies (none: n = 0) and then n planned launches one after
 // another in a workspace of prod_bytes.

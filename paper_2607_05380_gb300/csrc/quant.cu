@@ -12,12 +12,13 @@ using namespace tp;
 namespace {
 
 constexpr int32_t kMaxDim = 1 << 17;
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256, kMaxElems = int64_t(1) << 40;   // (tiles are numbered in 32 bits)
 
 tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
   if (rows < 0 || rows > kMaxRows) return ops_fail(TP_EINVAL, "rows %lld out of range", (long long)rows);
   if (k < 1 || n < 1 || k > kMaxDim || n > kMaxDim)
     return ops_fail(TP_EINVAL, "k %d and n %d must be in 1..%d", k, n, kMaxDim);
+  if (rows * (k > n ? k : n) > kMaxElems) return ops_fail(TP_EINVAL, "more than 2^40 elements in a matrix");
   if (precision != TP_BF16 && precision != TP_FP32) return ops_fail(TP_EINVAL, "unknown precision %d", precision);
   return TP_OK;
 }

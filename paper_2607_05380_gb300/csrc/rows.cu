@@ -394,7 +394,7 @@ bool rows_take32(int64_t rows, int64_t weights) { return rows <= 32 && rows * we
 
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8) {
   const int64_t work = rows * weights;
-  if (pitch % 4 != 0) return work <= (q8 ? 60000000 : 70000000);
+  if (pitch % 4 != 0) return rows <= 1024 && work <= (q8 ? 60000000 : 70000000);
   const bool whole = pitch % 16 == 0;
   if (rows <= (q8 && whole ? 128 : 32)) return true;
   return rows <= 1024 && work <= (q8 ? (whole ? 700000000 : 300000000) : (whole ? 540000000 : 250000000));

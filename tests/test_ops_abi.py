@@ -93,6 +93,15 @@ def test_rms_norm_backward_refusals(tp, bad):
     assert st == tp.TP_EINVAL
 
 
+def test_sizes_past_the_limits(tp):
+    """2^40 elements a matrix, whatever the workspace."""
+    L = tp.load_library()
+    v = ctypes.c_int64()
+    assert L.pack_gated_bytes(1 << 30, 2048, 64, 64, tp.BF16, ctypes.byref(v), None, None) == tp.TP_EINVAL
+    assert L.pack_product_q8_bytes(1 << 30, 64, 2048, tp.BF16, ctypes.byref(v)) == tp.TP_EINVAL
+    assert L.pack_distill_bytes(2, (1 << 30), ctypes.byref(v)) == tp.TP_EINVAL
+
+
 @pytest.mark.parametrize("bad", [dict(rows=-1), dict(k=0), dict(n=0), dict(k=1 << 18), dict(prec=3), dict(ldq=63),
                                  dict(q=None), dict(s=None), dict(w=None), dict(ws=None), dict(y=None)])
 def test_product_refusals(tp, bad):
