@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import threading
 
 import torch
 
@@ -81,14 +82,36 @@ def _flat(t, name, dtype, *shape):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(t):
     """The current stream's pointer; t has to be on the current device."""
     d = t.get_device()
-    if d != torch.cuda.current_device():
+    if d != _device():
         raise ValueError("the tensors are not on the current device")
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(d)
+
+
+_local = threading.local()
+_SMALL = 1 << 22
+
+
+def _work(n, st, t):
+    """(pointer, owner) of n bytes of workspace on t's device for a call on
+    stream st.  Small ones of the default stream, which outlives every call and
+    is never captured, are kept by the thread that uses them: an allocation is
+    a tenth of a small call's time."""
+    if st or n > _SMALL:
+        w = _empty(n, dtype=torch.uint8, device=t.device)
+        return w.data_ptr(), w
+    space = _local.__dict__
+    d = t.get_device()
+    got = space.get(d)
+    if got is None or got[0] < n:
+        w = _empty(max(n, 1 << 16), dtype=torch.uint8, device=t.device)
+        got = space[d] = (w.numel(), w.data_ptr(), w)
+    return got[1], got[2]
 
 
 @functools.lru_cache(maxsize=1024)
@@ -101,14 +124,15 @@ def _gated_bytes(rows, d, f, d_out, prec):
 
 
 def _gated_shapes(x, w_gate_up, w_down):
-    prec = _precision(x, "x")
-    xp, ldx = _mat(x, "x", x.dtype)
+    prec, dtype = _precision(x, "x"), x.dtype
+    xp, ldx = _mat(x, "x", dtype)
     rows, d = x.shape
-    if w_gate_up.dim() != 2 or w_gate_up.shape[0] % 2 or w_down.dim() != 2:
+    gate, down = w_gate_up.shape, w_down.shape
+    if len(gate) != 2 or gate[0] % 2 or len(down) != 2:
         raise ValueError("w_gate_up must be [2 f, d] and w_down [d_out, f]")
-    f, d_out = w_gate_up.shape[0] // 2, w_down.shape[0]
-    wp = _flat(w_gate_up, "w_gate_up", x.dtype, 2 * f, d)
-    dp = _flat(w_down, "w_down", x.dtype, d_out, f)
+    f, d_out = gate[0] // 2, down[0]
+    wp = _flat(w_gate_up, "w_gate_up", dtype, 2 * f, d)
+    dp = _flat(w_down, "w_down", dtype, d_out, f)
     return prec, xp, ldx, rows, d, f, d_out, wp, dp
 
 
@@ -126,9 +150,9 @@ def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
     st, dev = _stream(x), x.device
     y = _empty((rows, d_out), dtype=x.dtype, device=dev)
     saved = _empty(n_saved, dtype=torch.uint8, device=dev) if save else None
-    work = _empty(n_work, dtype=torch.uint8, device=dev)
+    work, _keep = _work(n_work, st, x)
     status = _lib().pack_gated_forward(xp, ldx, wp, dp, rows, d, f, d_out, code, prec, y.data_ptr(),
-                                       saved.data_ptr() if save else None, work.data_ptr(), n_work, st)
+                                       saved.data_ptr() if save else None, work, n_work, st)
     if status:
         _fail(status)
     return (y, saved) if save else y
@@ -147,9 +171,9 @@ def gated_backward(dy, x, w_gate_up, w_down, saved, stream=None):
     dx = _empty((rows, d), dtype=x.dtype, device=dev)
     dw = _empty((2 * f, d), dtype=x.dtype, device=dev)
     dd = _empty((d_out, f), dtype=x.dtype, device=dev)
-    work = _empty(n_work, dtype=torch.uint8, device=dev)
+    work, _keep = _work(n_work, st, x)
     status = _lib().pack_gated_backward(gp, ldg, xp, ldx, wp, dp, sp, rows, d, f, d_out, prec, dx.data_ptr(),
-                                        dw.data_ptr(), dd.data_ptr(), work.data_ptr(), n_work, st)
+                                        dw.data_ptr(), dd.data_ptr(), work, n_work, st)
     if status:
         _fail(status)
     return dx, dw, dd
@@ -225,9 +249,9 @@ def rms_norm_backward(dy, s, weight, dsum=None, eps=1e-6, stream=None):
     st, dev = _stream(s), s.device
     dx = _empty((rows, d), dtype=dtype, device=dev)
     dw = _empty(d, dtype=torch.float32, device=dev)
-    work = _empty(n, dtype=torch.uint8, device=dev)
+    work, _keep = _work(n, st, s)
     status = _lib().pack_rms_norm_backward(gp, ldg, sp, lds, wp, ap, lda, rows, d, eps, prec, dx.data_ptr(),
-                                           dw.data_ptr(), work.data_ptr(), n, st)
+                                           dw.data_ptr(), work, n, st)
     if status:
         _fail(status)
     return dx, dw
@@ -263,9 +287,9 @@ def product_q8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=Non
     n_work = _product_bytes(rows, k, n, prec)
     st, dev = _stream(q), q.device
     y = _empty((rows, n), dtype=dtype, device=dev)
-    work = _empty(n_work, dtype=torch.uint8, device=dev) if n_work else None
+    work, _keep = _work(n_work, st, q) if n_work else (None, None)
     status = _lib().pack_product_q8(qp, ldq, sp, wp, cp, bp, rows, k, n, prec, y.data_ptr(),
-                                    work.data_ptr() if n_work else None, n_work, st)
+                                    work, n_work, st)
     if status:
         _fail(status)
     return y
@@ -304,9 +328,9 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     st, dev = _stream(z), z.device
     loss = _empty(m, dtype=torch.float32, device=dev)
     dz = torch.empty_like(z) if grad else None
-    work = _empty(n_work, dtype=torch.uint8, device=dev)
+    work, _keep = _work(n_work, st, z)
     status = _lib().pack_distill(z.data_ptr(), m, rows, n, ip, top_p, k, yp, tau, alpha, prec, loss.data_ptr(),
-                                 dz.data_ptr() if grad else None, work.data_ptr(), n_work, st)
+                                 dz.data_ptr() if grad else None, work, n_work, st)
     if status:
         _fail(status)
     return loss, dz
