@@ -1,9 +1,10 @@
 // prod.cu -- single products on tcgen05 with fused epilogues (see prod.cuh).
 //
 // A persistent launch: each CTA (or CTA pair) walks output tiles of 128 (256)
-// rows by n_tile columns with stride gridDim.  Warp 0 stages 64-wide K blocks
-// of both operands by TMA into a ring in shared memory (128-byte swizzle),
-// warp 1 issues tcgen05.mma (K = 16 an instruction) into one of two TMEM
+// rows by n_tile columns with stride gridDim.  Warps 0 and 10 stage 64-wide K
+// blocks of A and B by TMA into a ring in shared memory (128-byte swizzle; one
+// warp for both: 324 ns a K block of a pair's 256 columns, MN-major, against
+// 287), warp 1 issues tcgen05.mma (K = 16 an instruction) into one of two TMEM
 // accumulators, warps 2-9 read the other and run the epilogue.  K-major and
 // MN-major operands are read straight from their row-major arrays.
 //
@@ -1022,15 +1023,19 @@ void prod_pairs(ProdJob& j, bool f32, int halves) {
 
 namespace {
 
+// Time of a whole tile among others, ns: its K blocks or, where that is longer,
+// its epilogue.
+double tile_ns(const ProdJob& j, const Shape& s) { return std::max(j.n_pairs * j.kb * s.kb, s.epi); }
+
 // Shares out the tiles from p.whole on: runs of K blocks that end all clusters
-// at about the same time.  ns: time of a K block of a segment pair.
-void share_out(ProdLaunch& p, double ns) {
+// at about the same time.
+void share_out(ProdLaunch& p, const Shape& s) {
   const int C = p.clusters;
   double load[kSms] = {}, total = 0;
   for (int k = 0; k < p.n_jobs; ++k) {
     const ProdJob& j = p.job[k];
     const int first = j.tile0, end = first + j.tm * j.tn;
-    const double t = j.n_pairs * j.kb * ns;
+    const double t = tile_ns(j, s);
     for (int c = 0; c < C; ++c) {   // whole tiles first .. min(end, whole) - 1 with number c modulo C
       const int last = std::min(end, p.whole);
       if (last > first) load[c] += t * ((last - 1 - c + C) / C - (first - 1 - c + C) / C);
@@ -1061,7 +1066,7 @@ void share_out(ProdLaunch& p, double ns) {
     want += std::max(0.0, level - load[c]);
     while (tile < p.n_tiles) {
       const ProdJob& j = p.job[job];
-      const double t = j.n_pairs * j.kb * ns;
+      const double t = tile_ns(j, s);
       if (c + 1 < C && done + t > want) break;
       done += t;
       pos += j.kb;
@@ -1071,7 +1076,7 @@ void share_out(ProdLaunch& p, double ns) {
     int in = 0;
     if (tile < p.n_tiles) {
       const ProdJob& j = p.job[job];
-      in = (int)((want - done) / (j.n_pairs * ns));
+      in = (int)((want - done) / tile_ns(j, s) * j.kb);
       if (in < 2) in = 0;
       else if (j.kb - in < 2) in = j.kb;
     }
@@ -1113,7 +1118,7 @@ void prod_plan(ProdLaunch& l) {
     double work = 0, longest = 0, blocks = 0;
     for (int k = 0; k < l.n_jobs; ++k) {
       const ProdJob& j = l.job[k];
-      const double tiles = (double)j.tm * j.tn, t = std::max(j.n_pairs * j.kb * s.kb, s.epi) + 100.0;
+      const double tiles = (double)j.tm * j.tn, t = tile_ns(j, s) + 100.0;
       work += t * tiles;
       blocks += tiles * j.n_pairs * j.kb;
       longest = std::max(longest, t);
@@ -1124,12 +1129,14 @@ void prod_plan(ProdLaunch& l) {
     if (even < best) best = even, pick = &s, pick_whole = l.n_tiles, pick_clusters = C;
     // the last one to two rounds shared out: runs of at least four K blocks, at most sixteen clusters a tile.
     // (Of many rounds the last ones' tiles, cut, no longer share operands in L2 with their neighbours: 16384 rows,
-    // 1024 -> 4096, backward, 631 us against 555 us whole.)
+    // 1024 -> 4096, backward, 680 us against 595 us whole.  Where one tile alone takes longer than a cluster's
+    // share, cutting it gains more than that: 80 rows, 2048 -> 4096, backward, 47 us against 62 us.  32-bit
+    // products gain less from it than their two chains' additions cost: 120 rows, 1024 -> 2048, 68 us against 61 us.)
     const int whole = std::max(0, l.n_tiles / C - 1) * C;
     const int clusters = (int)std::min<double>(std::min<double>(C, std::max(1.0, blocks / 4)), 16.0 * work / longest);
     const double share = work / clusters, adds = std::max(1.0, longest / share);
     const double shared = s.fixed + share + 6000.0 + (1.0 + adds) * s.epi;
-    if (clusters > 1 && (clusters == C || whole == 0) && shared < (l.n_tiles <= 3 * C ? 0.93 : 0.8) * best)
+    if (clusters > 1 && (clusters == C || whole == 0) && shared < (l.n_tiles <= 3 * C || (longest > share && !parts) ? 0.93 : 0.8) * best)
       best = shared, pick = &s, pick_whole = whole, pick_clusters = clusters;
   }
   lay(l, *pick);
@@ -1142,7 +1149,7 @@ void prod_plan(ProdLaunch& l) {
   const int64_t slot = (int64_t)l.clusters * l.cta * 128 * l.n_tile * 4;
   l.slot_bytes = l.flag_bytes = 0;
   if (l.whole < l.n_tiles) {
-    share_out(l, pick->kb);
+    share_out(l, *pick);
     l.slot_bytes = slot;
     l.flag_bytes = (int64_t)l.clusters * l.cta * kEpiWarps * 4;
   }
