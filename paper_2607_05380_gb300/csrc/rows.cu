@@ -335,8 +335,8 @@ template <bool kGate, int kAct>
 cudaError_t start32(const RowArgs& a, cudaStream_t st) {
   const bool vec = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)(a.ldx * 4) | (uintptr_t)((int64_t)a.k * 4)) & 15) == 0;
   const dim3 block(256);
-  // four weight rows a warp where that leaves a block for every SM
-  const bool four = ceil_div(a.n, kGate ? 16 : 32) >= kSms;
+  // eight rows of x share four weight rows a warp; one row takes two, for twice the warps (gated block of 512
+  // and 2048, four / two, us: one row 9.7 / 8.3, 8 rows 15.8 / 22.8)
   auto go = [&](auto c, auto m, auto v) {
     const int cols = 8 * (kGate ? c.value / 2 : c.value);
     launch_pdl(k_rows32<c.value, m.value, kGate, v.value, kAct>,
@@ -346,12 +346,8 @@ cudaError_t start32(const RowArgs& a, cudaStream_t st) {
     if (vec) go(c, m, std::true_type());
     else go(c, m, std::false_type());
   };
-  auto go_m = [&](auto c) {
-    if (a.rows == 1) go_v(c, std::integral_constant<int, 1>());
-    else go_v(c, std::integral_constant<int, 8>());
-  };
-  if (four) go_m(std::integral_constant<int, 4>());
-  else go_m(std::integral_constant<int, 2>());
+  if (a.rows == 1) go_v(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+  else go_v(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
   return cudaGetLastError();
 }
 
@@ -366,17 +362,20 @@ template <int kMode, int kAct>
 cudaError_t start(const RowArgs& a, cudaStream_t st) {
   constexpr int kBytes = kMode == kQuant ? 1 : 2, kR = kMode == kGated ? 2 : 1;
   const uintptr_t low = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)(a.ldx * kBytes) | (uintptr_t)((int64_t)a.k * kBytes);
-  // sixteen warps a CTA where there is about one CTA per SM and a warp of eight
-  // would take its loads in several turns
+  // sixteen warps a CTA where a warp of eight would take its loads in several turns and there is about one CTA
+  // per SM, or two of few rows (sixteen / eight, us): 8-bit 2048 -> 4096, one row 3.2 / 3.9, 32 rows 6.4 / 4.9;
+  // 2048 -> 2048, 32 rows 4.1 / 4.6, 64 rows 7.0 / 5.1; 1024 -> 4096, 8 rows 3.2 / 3.1; gated block of 512 and
+  // 2048, 8 rows 4.6 / 5.8; of 1024 and 2048, 8 rows 5.1 / 6.3, 64 rows 10.9 / 10.2
   const int64_t few = ceil_div(a.n, 16) * ceil_div(a.rows, 32);
-  const bool deep = few <= 2 * kSms && a.k > 512;
+  const bool deep = few <= (a.rows <= (kMode == kQuant ? 8 : 32) ? 2 : 1) * kSms && a.k * kBytes > 1024;
   if ((low & 15) == 0) {
     if (deep) {
       launch<kMode, kR, 16, 16, kAct>(a, st);
     } else if constexpr (kMode == kGated) {
       launch<kMode, kR, 8, 16, kAct>(a, st);
     } else {
-      // many columns: 32 a CTA, so that x comes from L2 half as often
+      // many columns: 32 a CTA, so that x comes from L2 half as often (8-bit, 512 -> 16000, 128 rows 24 -> 20 us;
+      // one row 3.1 -> 3.4)
       if (few > 2 * kSms) launch<kMode, 2, 8, 16, kAct>(a, st);
       else launch<kMode, 1, 8, 16, kAct>(a, st);
     }
@@ -390,7 +389,7 @@ cudaError_t start(const RowArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-bool rows_take32(int64_t rows, int64_t weights) { return rows <= 32 && rows * weights <= 150000000; }
+bool rows_take32(int64_t rows, int64_t weights) { return rows <= 16 || (rows <= 64 && rows * weights <= 220000000); }
 
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8) {
   const int64_t work = rows * weights;

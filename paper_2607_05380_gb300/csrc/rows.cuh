@@ -22,7 +22,11 @@ namespace tp {
 // 23.7) or of an element (gated 389, 1001: 32 rows 11.9 / 14.8, 128 rows 17.0 /
 // 15.3; 8-bit 2001 -> 1000: 8 rows 9.5 / 12.1, 32 rows 21.9 / 12.0) pay for less.
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8);
-// The same of a 32-bit block (in fp32 multiply-adds).
+// The same of a 32-bit block, in fp32 multiply-adds (rows / tcgen05):
+//   d = d_out = 512, f = 2048: 8 rows 15.8 / 42, 64 rows 32 / 40
+//   1024, 2048: 32 rows 31 / 44, 48 rows 50 / 44
+//   2048, 4096: one row 27 / 131, 16 rows 72 / 100, 24 rows 106 / 100
+//   389, 1001: 64 rows 26 / 40
 bool rows_take32(int64_t rows, int64_t weights);
 
 struct RowsGated {
