@@ -19,9 +19,9 @@
 // the result does not depend on any order.
 //
 // Bound by HBM (z read, dz written) for many classes, by latency for few.
-//   up to 32 classes    a thread takes a row, which blocks of 128 rows stage in
-//                       shared memory: no exchanges between lanes at all
-//   up to 1024          16 or 32 lanes hold a row in registers
+//   up to 32 classes    of many rows, few entries: a thread takes a row, which blocks of 128
+//                       rows stage in shared memory: no exchanges between lanes
+//   up to 1024          8 to 32 lanes hold a row in registers
 //   above               a block takes a row: running maximum and sums in one
 //                       pass, the gradient in a second that finds the row in
 //                       L2; one warp more works out the teacher's side meanwhile
@@ -140,32 +140,24 @@ __device__ __forceinline__ float row_loss(const Args<T>& g, const Row& r, bool h
   return loss;
 }
 
-// Entry j's share of kd / tau^2; its class's gradient, and by the first entry's
-// thread that of a label no entry has.
+// Entry j's share of kd / tau^2 and its class's gradient; twice: entries of the
+// row may have the same class, whose shares each of them then adds up.
 template <typename T>
 __device__ __forceinline__ float entry(const Args<T>& g, const Row& r, const T* z, T* dz, const int* ids, const float* p,
-                                       float log_p, int j) {
+                                       bool twice, float log_p, int j) {
   const int id = ids[j];
   if (id < 0) return 0.f;
   const float zi = Elem<T>::to_f(z[id]), pj = p[j];
   if (dz) {
-    float same = 0.f;
-    for (int i = 0; i < g.k; ++i) same += ids[i] == id ? p[i] : 0.f;
+    float same = twice ? 0.f : pj;
+    if (twice)
+      for (int i = 0; i < g.k; ++i) same += ids[i] == id ? p[i] : 0.f;
     float d = dense_any(g, r, zi) - g.alpha * g.tau * g.inv_rows * same;
     if (id == r.label) d -= (1.f - g.alpha) * g.inv_rows;
     dz[id] = Elem<T>::from_f(d);
   }
   return pj == 0.f ? 0.f : pj * (log_p - log_q(g, r, zi));
 }
-template <typename T>
-__device__ __forceinline__ void label_entry(const Args<T>& g, const Row& r, const T* z, T* dz, const int* ids, bool has) {
-  if (dz == nullptr || r.label < 0) return;
-  if (has)
-    for (int i = 0; i < g.k; ++i)
-      if (ids[i] == r.label) return;
-  dz[r.label] = Elem<T>::from_f(dense_any(g, r, Elem<T>::to_f(z[r.label])) - (1.f - g.alpha) * g.inv_rows);
-}
-
 template <int kG>
 __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -223,6 +215,24 @@ __device__ __forceinline__ bool teacher(const Args<T>& g, int64_t b, int gl, int
   log_tot = logf(tot);
   __syncwarp();
   return any;
+}
+
+// Marks the classes that have an entry, a bit each (class modulo the bits, a
+// power of two or more than the classes).  Returns whether two entries have
+// the same bit: with that question answered in k steps, the k^2 comparisons
+// are left to rows that need them.
+template <int kG>
+__device__ __forceinline__ bool mark(const int* ids, int k, uint32_t* bits, int mask, int gl, int lane) {
+  bool twice = false;
+  for (int j = gl; j < k; j += kG) {
+    const int id = ids[j];
+    if (id < 0) continue;
+    const uint32_t bit = 1u << (id & 31);
+    twice |= (atomicOr(bits + ((id & mask) >> 5), bit) & bit) != 0;
+  }
+  twice = group_any<kG>(twice, lane);
+  __syncwarp();
+  return twice;
 }
 
 // f(the row's Hard as a constant)
@@ -322,6 +332,9 @@ __global__ void __launch_bounds__(256) k_distill_group(const Args<T> g) {
   const int lane = threadIdx.x & 31, gl = threadIdx.x & (kG - 1), grp = threadIdx.x / kG;
   int* ids = (int*)raw + grp * g.k;
   float* p = (float*)raw + (kGroups + grp) * g.k;
+  constexpr int kWords = kG * kV / 32;
+  uint32_t* bits = (uint32_t*)raw + 2 * kGroups * g.k + grp * kWords;
+  for (int i = gl; i < kWords; i += kG) bits[i] = 0;
   pdl_trigger();
   pdl_wait();
   const int64_t rr = (int64_t)blockIdx.x * kGroups + grp;
@@ -337,6 +350,7 @@ __global__ void __launch_bounds__(256) k_distill_group(const Args<T> g) {
   }
   float hi = 0.f, log_tot = 0.f;
   const bool has = g.soft && teacher<T, kG>(g, b, gl, lane, ids, p, hi, log_tot);
+  const bool twice = g.soft && g.dz && mark<kG>(ids, g.k, bits, ~0, gl, lane);
   const int label = label_of(g, b);
 #pragma unroll
   for (int i = 0; i < kV; ++i) zm = fmaxf(zm, v[i]);
@@ -374,15 +388,18 @@ __global__ void __launch_bounds__(256) k_distill_group(const Args<T> g) {
   float kd = 0.f;
   if (has && r.alive)
     for (int j = gl; j < g.k; j += kG)
-      kd += entry(g, r, z, dz, ids, p, (g.top[b * g.k + j] - hi) * (g.c * kLn2) - log_tot, j);
+      kd += entry(g, r, z, dz, ids, p, twice, (g.top[b * g.k + j] - hi) * (g.c * kLn2) - log_tot, j);
   kd = group_sum<kG>(kd);
   if (gl == 0) {
-    label_entry(g, r, z, dz, ids, has);
-    if (live) g.row_loss[row] = row_loss(g, r, has, kd, r.label >= 0 ? Elem<T>::to_f(z[r.label]) : 0.f);
+    const float zl = r.label >= 0 ? Elem<T>::to_f(z[r.label]) : 0.f;
+    if (dz && r.label >= 0 && !(has && (bits[r.label >> 5] >> (r.label & 31) & 1)))   // a label no entry has
+      dz[r.label] = Elem<T>::from_f(dense_any(g, r, zl) - (1.f - g.alpha) * g.inv_rows);
+    if (live) g.row_loss[row] = row_loss(g, r, has, kd, zl);
   }
 }
 
 // ------------------------------------------------- many classes: a block a row
+constexpr int kMarks = 32768;   // bits for classes that have an entry
 constexpr int kTurn = 4;   // 16-byte groups that a thread asks for at a time
 
 template <typename T>
@@ -644,6 +661,7 @@ __global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distil
   __shared__ int ids[kMaxK];
   __shared__ float p[kMaxK];
   __shared__ float red[2][3][kWarps];
+  __shared__ uint32_t bits[kMarks / 32];   // (of the extra warp)
   __shared__ int has_s;
   const int lane = threadIdx.x & 31;
   const bool extra = threadIdx.x >= 32 * kWarps;
@@ -655,9 +673,14 @@ __global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distil
   const int label = label_of(g, b);
   const Span<T> sp(z, g.n, threadIdx.x);
   float hi = 0.f, log_tot = 0.f, z_entry[kPer], z_label = 0.f;
+  bool twice = true;
   if (extra) {
     bool any = false;
+    const bool marks = dz && g.k > 16;   // fewer entries are compared as fast
+    if (marks)
+      for (int i = lane; 32 * i < min(g.n, kMarks); i += 32) bits[i] = 0;
     if (g.soft) any = teacher<T, 32>(g, b, lane, lane, ids, p, hi, log_tot);
+    if (marks && g.soft) twice = mark<32>(ids, g.k, bits, kMarks - 1, lane, lane);
     if (lane == 0) has_s = any;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -696,8 +719,8 @@ __global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distil
     const int j = lane + 32 * i, id = has && r.alive && j < g.k ? ids[j] : -1;
     d_entry[i] = 0.f;
     if (id < 0) continue;
-    float same = 0.f;
-    if (dz)
+    float same = twice ? 0.f : p[j];
+    if (dz && twice)
       for (int q = 0; q < g.k; ++q) same += ids[q] == id ? p[q] : 0.f;
     d_entry[i] = dense<kHard>(g.c, r, z_entry[i]) - g.alpha * g.tau * g.inv_rows * same;
     if (id == r.label) d_entry[i] -= ones, found = true;
@@ -739,7 +762,7 @@ __global__ void __launch_bounds__(256) k_distill_mean(const float* row_loss, int
 template <typename T, int kG, int kV>
 void group(const Args<T>& a, cudaStream_t st) {
   launch_pdl(k_distill_group<T, kG, kV>, dim3((unsigned)ceil_div(a.all, 256 / kG)), dim3(256),
-             (size_t)(256 / kG) * a.k * 8, st, a);
+             (size_t)(256 / kG) * (a.k * 8 + kG * kV / 8), st, a);
 }
 
 template <typename T, int kWarps>
@@ -754,19 +777,31 @@ void wide(const Args<T>& a, cudaStream_t st) {
 
 template <typename T>
 cudaError_t rows(const Args<T>& a, cudaStream_t st) {
-  if (a.n <= kSmallN) {
+  // Launches of many rows want few lanes a row, launches of few rows short
+  // chains a lane (us; the other way in brackets): 10 classes, 80000 rows, 8
+  // entries 22 (eight lanes 30), 16 entries of 32 classes 51 (34), 4096 rows 6.2
+  // (a thread 8.7); 64 classes, 80000 rows 33 (sixteen lanes 45); 128, 80000
+  // rows 48 (72); 256, 80000 rows 58 (79), 128 rows 5.7 (6.1); 512, 80000 rows
+  // 94 (117), 128 rows 6.2 (7.0); 1000, 16384 rows 31 (a block a row 52), 128
+  // rows 5.3 (6.9).
+  const bool few = a.all <= 4096;
+  if (a.n <= kSmallN && a.k <= 8 && a.all > 24576) {
     const uint32_t div = ((1u << 20) + a.n - 1) / a.n;   // i / n = i div >> 20 for i < 128 * 32
     launch_pdl(k_distill_thread<T>, dim3((unsigned)ceil_div(a.all, kSmallRows)), dim3(kSmallRows),
                (size_t)kSmallRows * (a.n | 1) * 4, st, a, div);
+  } else if (a.n <= 32) {
+    group<T, 8, 4>(a, st);
   } else if (a.n <= 64) {
-    group<T, 16, 4>(a, st);
+    group<T, 8, 8>(a, st);
   } else if (a.n <= 128) {
-    group<T, 32, 4>(a, st);
+    group<T, 16, 8>(a, st);
   } else if (a.n <= 256) {
-    group<T, 32, 8>(a, st);
+    if (few) group<T, 32, 8>(a, st);
+    else group<T, 16, 16>(a, st);
   } else if (a.n <= 512) {
-    group<T, 32, 16>(a, st);
-  } else if (a.n <= 1024) {
+    if (few) group<T, 32, 16>(a, st);
+    else group<T, 16, 32>(a, st);
+  } else if (a.n <= 1024 && a.all > 1024) {
     group<T, 32, 32>(a, st);
   } else if (a.n * (int64_t)sizeof(T) <= 32768) {
     wide<T, 4>(a, st);
