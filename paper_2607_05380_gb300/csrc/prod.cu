@@ -801,6 +801,28 @@ __global__ void __launch_bounds__(256) k_stage(const __grid_constant__ StageLaun
   const int width = 1 << j.shift, tx = threadIdx.x & (width - 1), groups = (int)(j.ldp >> 3);
   const int eb = j.type == kStageF32 ? 4 : j.type == kStageS8 ? 1 : 2;
   const bool vec = ((uintptr_t)j.src & (eb == 1 ? 7 : 15)) == 0 && ((j.ld * eb) & (eb == 1 ? 7 : 15)) == 0;
+  if (j.type == kStageS8 && j.cols % 16 == 0 && j.ld % 16 == 0 && ((uintptr_t)j.src & 15) == 0) {
+    // 16 elements a thread, of four rows at a time (8192 x 2048 -> 4096 in all: 90 us with one load of 8 in flight, 85 so)
+    const int sh = max(j.shift - 1, 0), t16 = threadIdx.x & ((1 << sh) - 1);
+    const int64_t step = (int64_t)gridDim.x * (256 >> sh);
+    for (int64_t r = (int64_t)blockIdx.x * (256 >> sh) + (threadIdx.x >> sh); r < j.rows; r += 4 * step)
+      for (int c = 16 * t16; c < j.cols; c += 16 << sh) {
+        uint4 w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (r + u * step < j.rows) w[u] = *reinterpret_cast<const uint4*>((const int8_t*)j.src + (r + u * step) * j.ld + c);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (r + u * step >= j.rows) break;
+          uint4* dst = reinterpret_cast<uint4*>((uint16_t*)j.dst + (r + u * step) * j.ldp + c);
+          uint4 h[2];
+          s8_to_f16(w[u].x, h[0].x, h[0].y), s8_to_f16(w[u].y, h[0].z, h[0].w);
+          s8_to_f16(w[u].z, h[1].x, h[1].y), s8_to_f16(w[u].w, h[1].z, h[1].w);
+          dst[0] = h[0], dst[1] = h[1];
+        }
+      }
+    return;
+  }
   for (int64_t r = (int64_t)blockIdx.x * (256 >> j.shift) + (threadIdx.x >> j.shift); r < j.rows;
        r += (int64_t)gridDim.x * (256 >> j.shift)) {
     const int64_t seg = r >= j.rows_seg ? 1 : 0, rs = r - seg * j.rows_seg;   // one or two segments

@@ -56,16 +56,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Four int8 as two pairs of fp16: 1024 + (v + 128) has v + 128 in its low bits.
-__device__ __forceinline__ void s8_to_f16(uint32_t v, uint32_t& lo, uint32_t& hi) {
-  v ^= 0x80808080u;
-  const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
-  uint32_t a = __byte_perm(v, 0x64646464u, 0x4140), b = __byte_perm(v, 0x64646464u, 0x4342);
-  __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
-  lo = *reinterpret_cast<uint32_t*>(&x);
-  hi = *reinterpret_cast<uint32_t*>(&y);
-}
-
 // 16 bytes, `left` of which lie inside the row, by loads of kLd bytes that the
 // address is a multiple of; zeros past the row.
 template <int kLd>

@@ -46,6 +46,16 @@ cudaError_t rows_plain(const void* x, int64_t ldx, const void* w, int64_t rows, 
 cudaError_t rows_quant(const int8_t* q, int64_t ldq, const float* sx, const int8_t* w, const float* sw, const float* bias,
                        int64_t rows, int32_t k, int32_t n, bool f32, void* y, cudaStream_t st);
 
+// Four int8 as two pairs of fp16: 1024 + (v + 128) has v + 128 in its low bits.
+__device__ __forceinline__ void s8_to_f16(uint32_t v, uint32_t& lo, uint32_t& hi) {
+  v ^= 0x80808080u;
+  const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+  uint32_t a = __byte_perm(v, 0x64646464u, 0x4140), b = __byte_perm(v, 0x64646464u, 0x4342);
+  __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+  lo = *reinterpret_cast<uint32_t*>(&x);
+  hi = *reinterpret_cast<uint32_t*>(&y);
+}
+
 // The upper 24 bits of a float, rounded to nearest (ties up), in bits 8..31.
 __device__ __forceinline__ uint32_t round_24(float v) {
   const uint32_t u = __float_as_uint(v);
