@@ -55,6 +55,10 @@ constexpr int kABytes = 128 * 128;       // 128 rows of a K block
 constexpr int kBox = 64 * 128;           // a 64 x 64 MN-major box
 constexpr int kMaxStages = 8;
 constexpr int kBufBytes = 32 * 32 * 4;   // per epilogue warp
+// kEpiDgated of a bf16 block: an epilogue warp's 32 x 32 values of u act'(g) and of act(g) as they come in by TMA,
+// the upper 16 bits, then the lower 8
+constexpr int kKeptHi = 32 * 32 * 2, kKeptLo = 32 * 32, kKeptBytes = 2 * (kKeptHi + kKeptLo);
+constexpr int kMapHi = 2, kMapLo = 3, kMapOut = 4;   // its maps: act(g) and u act'(g), two segments; dg and du
 constexpr int kSmemMax = 232448;
 constexpr int kTmemCols = 512, kAccCols = 256;
 constexpr uint64_t kWaitNs = 2000000000ull;
@@ -64,6 +68,7 @@ __device__ int g_prod_err;
 
 struct Tail {
   uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2], done;
+  uint64_t kept[kEpiWarps][2];
   uint32_t tmem_base;
   int abort;
 };
@@ -425,33 +430,76 @@ __device__ __forceinline__ void put_24(const float (&v)[32], __nv_bfloat16* hi, 
   if (live) store32(lo, b);
 }
 
-// What the epilogue reads besides the accumulator: kEpiDgated of a bf16 block,
-// u act'(g) and act(g) of the lane's row, asked for one chunk ahead.
-struct Ahead {
-  uint32_t u[16], b[8];
-  __device__ __forceinline__ void load(const ProdJob& j, const void* hi, const uint8_t* lo, int row, int c0) {
-    const int64_t at = (int64_t)min(row, j.M - 1) * j.ldo + c0;
-    const __nv_bfloat16* h = (const __nv_bfloat16*)hi + at;
-    load32(h, u);
-    if (c0 + 16 < j.N) load32(h + 16, u + 8);   // (a row has room for whole sectors)
-    load32(lo + at, b);
+// kEpiDgated of a bf16 block: what the epilogue reads besides the accumulator
+// comes in, and what it writes goes out, by TMA through the warp's own shared
+// memory, one chunk ahead.  (By loads and stores of the lanes' own rows, a
+// 32-byte sector in 32 different lines each, the loads and stores alone took
+// 6 us of a pair's 256-column tile: 16384 x 1024 -> 4096, 223 us; 133 us so,
+// of which the bytes take 105.)
+struct Kept {
+  uint8_t* in;                // [2][32 rows][64 B], [2][32 rows][32 B]; first u act'(g), then act(g)
+  uint8_t* out;               // [2][32 rows][64 B]: dg, du
+  uint64_t* bar;
+  uint32_t phase = 0, asked = 0;   // a bit each
+  __device__ __forceinline__ void ask(const ProdArgs& g, int h, int c0, int r0) {
+    const uint32_t b = smem_u32(bar + h);
+    expect_elect(b, kKeptHi + kKeptLo);
+    tma_elect<1>(smem_u32(in) + h * kKeptHi, &g.map[kMapHi], b, c0, r0, 1 - h);
+    tma_elect<1>(smem_u32(in) + 2 * kKeptHi + h * kKeptLo, &g.map[kMapLo], b, c0, r0, 1 - h);
+    asked |= 1u << h;
   }
-  // f = these values times acc (what the lowest byte holds is below their rounding)
-  __device__ __forceinline__ void times(float (&f)[32], const float (&acc)[32]) const {
+  __device__ __forceinline__ bool wait(int h, volatile int* abort_flag, int* err) {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar + h, phase >> h & 1, abort_flag, err, kWaitNs, 48));
+    if (ok) phase ^= 1u << h, asked &= ~(1u << h);
+    return ok;
+  }
+  // f = what has come in times acc (what the lowest byte holds is below their rounding)
+  __device__ __forceinline__ void times(int h, int lane, float (&f)[32], const float (&acc)[32]) const {
+    const uint8_t* hi = in + h * kKeptHi + lane * 64;
+    const uint8_t* lo = in + 2 * kKeptHi + h * kKeptLo + lane * 32;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const uint32_t at = e & 3, hw = 4 + 2 * (e & 1);   // byte of b, first byte of the pair's half
-      f[e] = __uint_as_float(__byte_perm(b[e >> 2], u[e >> 1], at | at << 4 | hw << 8 | (hw + 1) << 12)) * acc[e];
+    for (int s = 0; s < 2; ++s) {
+      const uint4 bq = *reinterpret_cast<const uint4*>(lo + ((s ^ ((lane >> 2) & 1)) << 4));
+      const uint32_t b[4] = {bq.x, bq.y, bq.z, bq.w};
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint4 uq = *reinterpret_cast<const uint4*>(hi + (((2 * s + t) ^ ((lane >> 1) & 3)) << 4));
+        const uint32_t u[4] = {uq.x, uq.y, uq.z, uq.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t at = e & 3, hw = 4 + 2 * (e & 1);   // byte of b, first byte of the pair's half
+          const int i = 16 * s + 8 * t + e;
+          f[i] = __uint_as_float(__byte_perm(b[2 * t + (e >> 2)], u[e >> 1], at | at << 4 | hw << 8 | (hw + 1) << 12)) * acc[i];
+        }
+      }
     }
+  }
+  __device__ __forceinline__ void put(const ProdArgs& g, int h, int lane, const float (&f)[32], int c0, int r0) {
+    uint32_t pk[16];
+    pack32(f, pk);
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // the buffer's last store has read it
+    __syncwarp();
+    uint8_t* to = out + h * kKeptHi + lane * 64;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      *reinterpret_cast<uint4*>(to + ((s ^ ((lane >> 1) & 3)) << 4)) =
+          make_uint4(pk[4 * s], pk[4 * s + 1], pk[4 * s + 2], pk[4 * s + 3]);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0)
+      asm volatile(
+          "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n cp.async.bulk.commit_group;" ::"l"(
+              &g.map[kMapOut]),
+          "r"(smem_u32(out + h * kKeptHi)), "r"(c0), "r"(r0), "r"(h)
+          : "memory");
   }
 };
 
 // The epilogue of one 32 x 32 chunk; acc: its accumulator (kEpiGated: the
 // gate product), acc2: the up product.
-// next: the column of the warp's next chunk, or -1.
 template <int kEpi, int kAct, bool kF32>
 __device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lane, float (&acc)[32], float (&acc2)[32],
-                                         Ahead& ap, Ahead& aa, int r0, int c0, int next) {
+                                         int r0, int c0) {
   const int row = r0 + lane, n = j.N - c0;
   const bool live = row < j.M;
   const int64_t at = (int64_t)row * j.ldo + c0;
@@ -475,30 +523,21 @@ __device__ __forceinline__ void epilogue(const ProdJob& j, uint8_t* buf, int lan
       }
     }
     put_parts<kF32>(acc2, (__nv_bfloat16*)j.out + at, j.part, live, n);
-  } else if constexpr (kEpi == kEpiDgated) {
+  } else if constexpr (kEpi == kEpiDgated) {   // of a 32-bit block
     float f[32];
     __nv_bfloat16* out = (__nv_bfloat16*)j.out + at;
-    if constexpr (kF32) {
-      const int64_t from = (int64_t)min(row, j.M - 1) * j.ldo + c0;
+    const int64_t from = (int64_t)min(row, j.M - 1) * j.ldo + c0;
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
-        const float* src = (const float*)(h ? j.a : j.p) + from;
+    for (int h = 0; h < 2; ++h) {
+      const float* src = (const float*)(h ? j.a : j.p) + from;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          uint32_t w[8] = {};
-          if (n > 8 * s) load32(src + 8 * s, w);
+      for (int s = 0; s < 4; ++s) {
+        uint32_t w[8] = {};
+        if (n > 8 * s) load32(src + 8 * s, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[8 * s + e] = __uint_as_float(w[e]) * acc[8 * s + e];
-        }
-        put_parts<true>(f, out + h * j.half, j.part, live, n);
+        for (int e = 0; e < 8; ++e) f[8 * s + e] = __uint_as_float(w[e]) * acc[8 * s + e];
       }
-    } else {
-      ap.times(f, acc);
-      if (next >= 0) ap.load(j, j.p, j.p_lo, row, next);
-      put_parts<false>(f, out, 0, live, n);
-      aa.times(f, acc);
-      if (next >= 0) aa.load(j, j.a, j.a_lo, row, next);
-      put_parts<false>(f, out + j.half, 0, live, n);
+      put_parts<true>(f, out + h * j.half, j.part, live, n);
     }
   } else {
     if constexpr (kEpi == kEpiQuant) {
@@ -530,7 +569,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
   const uint32_t stage_bytes = kABytes + (uint32_t)nh * 128;
   const int stages = g.stages;
   uint8_t* bufs = smem + stages * stage_bytes;
-  Tail* tl = (Tail*)(bufs + kEpiWarps * kBufBytes);
+  constexpr bool kStaged = kEpi == kEpiDgated && !kF32;
+  uint8_t* kept_in = bufs + kEpiWarps * kBufBytes;
+  Tail* tl = (Tail*)(kept_in + (kStaged ? kEpiWarps * kKeptBytes : 0));
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int rank = kCta == 2 ? (int)uniform(cluster_rank()) : 0;
   const bool leader = rank == 0;
@@ -546,6 +587,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
       mbar_init(&tl->tempty[b], kEpiWarps * kCta);
     }
     mbar_init(&tl->done, 1);
+    if constexpr (kStaged)
+      for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(&tl->kept[0][w], 1);
     tl->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -685,16 +728,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     float* own = g.slots + (int64_t)n_clu * kCta * slot + mine;
     Walk<kCta> walk(g, clu, n_clu);
     Item u;
-    while (walk.next(u)) {
+    Kept kept{kept_in + (warp - 2) * kKeptBytes, buf, tl->kept[warp - 2]};
+    bool ok = true;
+    while (ok && walk.next(u)) {
       const ProdJob& j = g.job[u.job];
       const int r0 = u.m0 + rank * 128 + 32 * q;
-      Ahead ahead_p, ahead_a;
-      constexpr bool kAhead = kEpi == kEpiDgated && !kF32;
       const bool finish = !u.publish && !u.carry_out;
-      if constexpr (kAhead)
+      if constexpr (kStaged)
         if (finish && r0 < j.M && u.n0 * cols + 32 * half < j.N) {
-          ahead_p.load(j, j.p, j.p_lo, r0 + lane, u.n0 * cols + 32 * half);
-          ahead_a.load(j, j.a, j.a_lo, r0 + lane, u.n0 * cols + 32 * half);
+          kept.ask(g, 0, u.n0 * cols + 32 * half, r0);
+          kept.ask(g, 1, u.n0 * cols + 32 * half, r0);
         }
       if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[acc], acc_phase, abort_flag, err, 2 * kWaitNs, 46))) break;
       tc_fence_after();
@@ -752,9 +795,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
           add_slot(of + 32 * c, lane, a);
           if constexpr (kEpi == kEpiGated) add_slot(of + 32 * (cols + c), lane, a2);
         }
-        epilogue<kEpi, kAct, kF32>(j, buf, lane, a, a2, ahead_p, ahead_a, r0, c0,
-                                   c + 64 < cols && c0 + 64 < j.N ? c0 + 64 : -1);
+        if constexpr (kStaged) {   // dg = dh u act'(g), du = dh act(g)
+          const bool more = c + 64 < cols && c0 + 64 < j.N;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            ok = ok && kept.wait(h, abort_flag, err);
+            if (!ok) break;
+            kept.times(h, lane, a2, a);
+            __syncwarp();
+            if (more) kept.ask(g, h, c0 + 64, r0);
+            kept.put(g, h, lane, a2, c0, r0);
+          }
+          if (!ok) break;
+        } else {
+          epilogue<kEpi, kAct, kF32>(j, buf, lane, a, a2, r0, c0);
+        }
       }
+      if (!ok) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {   // the loads above have completed
@@ -765,6 +822,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
         red_release_add(g.flags + (clu * kCta + rank) * kEpiWarps + warp - 2, 1);
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
+    }
+    if constexpr (kStaged) {   // copies in flight: of a role that gave up, and the stores
+      int dummy = 0;
+      for (int h = 0; h < 2; ++h)
+        if (kept.asked >> h & 1) mbar_wait(kept.bar + h, kept.phase >> h & 1, &dummy, err, kWaitNs, 49);
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   }
 
@@ -896,21 +959,28 @@ PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
   return fn;
 }
 
-bool encode(CUtensorMap* m, const ProdOperand& o, bool fp16, int box_rows) {
+// [segs][rows][cols] of eb bytes, ld bytes from row to row
+bool encode(CUtensorMap* m, CUtensorMapDataType type, const void* base, int64_t cols, int64_t rows, int64_t ld, int64_t seg,
+            int n_seg, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
   auto fn = get_encode();
   if (!fn) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.n_seg};
-  cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(o.n_seg > 1 ? o.seg : o.ld * 8) * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)n_seg};
+  cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(n_seg > 1 ? seg : ld * 8)};
+  cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
   cuuint32_t es[3] = {1, 1, 1};
-  return fn(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base),
-            dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return fn(m, type, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool encode(CUtensorMap* m, const ProdOperand& o, bool fp16, int box_rows) {
+  return encode(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, o.base, o.cols, o.rows,
+                o.ld * 2, o.seg * 2, o.n_seg, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
 
-int stage_count(int cta, int n_tile) {
+// Shared memory beside the ring's stages, and how many of them fit.
+int smem_rest(bool kept) { return 1024 + kEpiWarps * (kBufBytes + (kept ? kKeptBytes : 0)) + (int)sizeof(Tail); }
+int stage_count(int cta, int n_tile, bool kept) {
   const int bytes = kABytes + n_tile / cta * 128;
-  return std::min<int>(kMaxStages, (kSmemMax - 1024 - kEpiWarps * kBufBytes - (int)sizeof(Tail)) / bytes);
+  return std::min<int>(kMaxStages, (kSmemMax - smem_rest(kept)) / bytes);
 }
 
 // A tile's shape and its times in ns, measured (bf16, operands in L2): a K
@@ -926,7 +996,7 @@ constexpr Shape kShapes[] = {{2, 256, 287, 7000, 2800}, {2, 128, 195, 5600, 1400
 template <int kCta, int kEpi, int kAct, bool kF32>
 cudaError_t launch(const ProdArgs& a, int clusters, cudaStream_t st) {
   const int stage_bytes = kABytes + a.n_tile / kCta * 128;
-  const int smem = a.stages * stage_bytes + kEpiWarps * kBufBytes + (int)sizeof(Tail) + 1024;
+  const int smem = a.stages * stage_bytes + smem_rest(kEpi == kEpiDgated && !kF32);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kCta * clusters);
   cfg.blockDim = dim3(kThreads);
@@ -993,7 +1063,7 @@ cudaError_t device_state(DeviceState* out) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * d.sms);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = stage_count(2, 256) * (kABytes + 128 * 128) + kEpiWarps * kBufBytes + (int)sizeof(Tail) + 1024;
+    cfg.dynamicSmemBytes = stage_count(2, 256, false) * (kABytes + 128 * 128) + smem_rest(false);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -1193,7 +1263,8 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, c
   const int clusters = std::min(fit, l.clusters);
   ProdArgs a;
   a.n_jobs = l.n_jobs, a.n_tiles = l.n_tiles, a.n_maps = 0, a.fp16 = l.fp16, a.n_tile = l.n_tile;
-  a.chains = l.chains, a.stages = stage_count(l.cta, l.n_tile);
+  const bool kept = l.epi == kEpiDgated && !l.f32;
+  a.chains = l.chains, a.stages = stage_count(l.cta, l.n_tile, kept);
   a.whole = l.whole, a.part_kb = l.f32 && !l.fp16 ? 2 * kChainKb : 1 << 30;
   a.slots = (float*)slots, a.flags = (int*)flags;
   for (int c = 0; c <= kSms; ++c) a.cut[c] = c <= l.clusters && l.whole < l.n_tiles ? l.cut[c] : 0;
@@ -1208,6 +1279,16 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, c
     if (!done[j.map_b] && !encode(&a.map[j.map_b], l.op[j.map_b], l.fp16, j.b_mn ? 64 : nh)) return cudaErrorInvalidValue;
     done[j.map_a] = done[j.map_b] = true;
     a.n_maps = std::max(a.n_maps, std::max(j.map_a, j.map_b) + 1);
+  }
+  if (kept) {
+    const ProdJob& j = l.job[0];   // (one product; its columns fill whole sectors of a row)
+    const int64_t hi = (const char*)j.p - (const char*)j.a, lo = j.p_lo - j.a_lo;
+    if (!encode(&a.map[kMapHi], CU_TENSOR_MAP_DATA_TYPE_UINT16, j.a, j.ldo, j.M, j.ldo * 2, hi, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !encode(&a.map[kMapLo], CU_TENSOR_MAP_DATA_TYPE_UINT8, j.a_lo, j.ldo, j.M, j.ldo, lo, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_32B) ||
+        !encode(&a.map[kMapOut], CU_TENSOR_MAP_DATA_TYPE_UINT16, j.out, j.ldo, j.M, j.ldo * 2, j.half * 2, 2, 32, 32,
+                CU_TENSOR_MAP_SWIZZLE_64B))
+      return cudaErrorInvalidValue;
+    a.n_maps = kMapOut + 1;
   }
   *what = "product launch";
   return with_kernel(l.cta, l.epi, l.act, l.f32, [&](auto c, auto k, auto a_, auto t) {
