@@ -14,6 +14,9 @@
 //
 // The weights' first steps are asked for (into L2) before the previous kernel
 // of the stream has finished.
+//
+// Gated block of 1024 and 2048, its 12.6 MB of weights in L2: one row 4.3 us in
+// two launches, 32 rows 7.6; 8-bit product 2048 -> 4096, one row 2.9 us.
 #include <type_traits>
 
 #include "kernels.cuh"
