@@ -743,21 +743,22 @@ __global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distil
   if (label_apart && lane == 0) dz[r.label] = Elem<T>::from_f(d_label);
 }
 
-// A student's mean over its rows, in a fixed order.
-__global__ void __launch_bounds__(256) k_distill_mean(const float* row_loss, int64_t rows, float* loss) {
-  __shared__ float s[8];
+// A student's mean over its rows, in a fixed order: 256 to 1024 threads with four
+// loads in flight (a whole call of 100000 rows, 256 threads: 55 us; 1024: 37).
+__global__ void __launch_bounds__(1024) k_distill_mean(const float* row_loss, int64_t rows, float* loss) {
+  __shared__ float s[32];
   pdl_trigger();
   pdl_wait();
   const float* p = row_loss + blockIdx.x * rows;
   float a = 0.f;
 #pragma unroll 4
-  for (int64_t i = threadIdx.x; i < rows; i += 256) a += p[i];
+  for (int64_t i = threadIdx.x; i < rows; i += blockDim.x) a += p[i];
   a = group_sum<32>(a);
   if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int k = 1; k < 8; ++k) a += s[k];
-    loss[blockIdx.x] = a / (float)rows;
+  if (threadIdx.x < 32) {
+    a = group_sum<32>(32 * threadIdx.x < blockDim.x ? s[threadIdx.x] : 0.f);   // (warps that there are)
+    if (threadIdx.x == 0) loss[blockIdx.x] = a / (float)rows;
   }
 }
 
@@ -867,7 +868,8 @@ tp_status pack_distill(const void* z, int64_t m, int64_t n_rows, int32_t n, cons
       e = rows(Args<__nv_bfloat16>{(const __nv_bfloat16*)z, ids, labels, top, (__nv_bfloat16*)dz, rl, m * n_rows, n_rows, n, k,
                                soft, hard, c, tau, alpha, 1.f / (float)n_rows}, st);
     if (e == cudaSuccess) {
-      launch_pdl(k_distill_mean, dim3((unsigned)m), dim3(256), 0, st, (const float*)rl, n_rows, loss);
+      const int64_t threads = std::min<int64_t>(1024, std::max<int64_t>(256, round_up(ceil_div(n_rows, 4), 32)));
+      launch_pdl(k_distill_mean, dim3((unsigned)m), dim3((unsigned)threads), 0, st, (const float*)rl, n_rows, loss);
       e = cudaGetLastError();
     }
   }

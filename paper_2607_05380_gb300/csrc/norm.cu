@@ -8,12 +8,12 @@
 // One pass: a row's elements stay in registers between the sums and the
 // outputs.  Bound by HBM (8192 rows of 2048, bf16, forward: 22 us, 0.90 of the
 // measured copy rate) and, in the backward pass, by its two sums per row,
-// which the next row's loads do not quite cover (26.5 us, 0.56).
+// which the next row's loads do not quite cover (23.6 us, 0.63).
 //
 // A row takes one to sixteen warps, so that a lane holds at most 16 of its
-// elements, 32 above 8192 (forward / backward, us: 8192 rows of 2048, two warps
-// 24 / 31, four 22 / 26.5, eight 22 / 31; 16384 of 1024, one warp 23.5 / 40, two
-// 21 / 25, four 25 / 30).  dw is summed per block over the rows it takes (at
+// elements, 32 above 8192 (forward / backward, us, when adding up dw took 2.7
+// more: 8192 rows of 2048, two warps 24 / 31, four 22 / 26.5, eight 22 / 31;
+// 16384 of 1024, one warp 23.5 / 40, two 21 / 25, four 25 / 30).  dw is summed per block over the rows it takes (at
 // most kBwdBlocks blocks), then over the blocks, both in a fixed order.
 #include <algorithm>
 
@@ -328,21 +328,27 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 ? 1 : 2) k_rms_bwd(const B
   }
 }
 
-// dw = the blocks' sums: 32 columns a block, eight runs of blocks each.
-__global__ void __launch_bounds__(256) k_rms_dw(const float* part, int n, int d, float* dw) {
-  __shared__ float s[8][33];
+// dw = the blocks' sums: 32 columns a block, a run of blocks for each of its 32
+// warps, whose loads are all in flight at once (the backward pass of 8192 rows
+// of 2048: with eight warps a block 26.3 us, so 23.6).
+__global__ void __launch_bounds__(1024) k_rms_dw(const float* part, int n, int d, float* dw) {
+  __shared__ float s[32][33];
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-  float a = 0.f;
-  if (c < d)
-#pragma unroll 4
-    for (int b = k; b < n; b += 8) a += part[(int64_t)b * d + c];
+  float v[(kBwdBlocks + 31) / 32], a = 0.f;
+#pragma unroll
+  for (int i = 0; i < (kBwdBlocks + 31) / 32; ++i) {
+    const int b = k + 32 * i;
+    v[i] = c < d && b < n ? part[(int64_t)b * d + c] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < (kBwdBlocks + 31) / 32; ++i) a += v[i];
   s[k][lane] = a;
   __syncthreads();
   if (k == 0 && c < d) {
 #pragma unroll
-    for (int q = 1; q < 8; ++q) a += s[q][lane];
+    for (int q = 1; q < 32; ++q) a += s[q][lane];
     dw[c] = a;
   }
 }
@@ -459,7 +465,7 @@ tp_status pack_rms_norm_backward(const void* dy, int64_t lddy, const void* sum, 
   else
     backward(BwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)dy, (const __nv_bfloat16*)sum, (const __nv_bfloat16*)dsum, w,
                                     (__nv_bfloat16*)dx, part, lddy, lds, lddsum, rows, d, eps}, st);
-  if (dw) launch_pdl(k_rms_dw, dim3((unsigned)ceil_div(d, 32)), dim3(256), 0, st, (const float*)part, blocks, d, dw);
+  if (dw) launch_pdl(k_rms_dw, dim3((unsigned)ceil_div(d, 32)), dim3(1024), 0, st, (const float*)part, blocks, d, dw);
   return done(cudaGetLastError(), "pack_rms_norm_backward");
 }
 
