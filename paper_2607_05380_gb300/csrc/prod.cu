@@ -82,6 +82,8 @@ struct ProdArgs {
   int32_t whole, part_kb;   // part_kb: longest reduction between two additions in fp32
   float* slots;             // [2][clusters][CTA][128 n_tile]: published sums; a cluster's own
   int* flags;               // [clusters][CTA][epilogue warp]
+  int* zero;                // n_zero words are set to 0: the next launch's flags
+  int32_t n_zero;
   int32_t cut[kSms + 1];
 };
 static_assert(sizeof(ProdArgs) <= 4096, "kernel parameters");
@@ -728,6 +730,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     // this warp's 32 lanes x n_tile columns in the slots, a chunk of 32 columns after another
     const int64_t slot = (int64_t)128 * g.n_tile, mine = (int64_t)(clu * kCta + rank) * slot + (int64_t)32 * q * g.n_tile;
     float* own = g.slots + (int64_t)n_clu * kCta * slot + mine;
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x - 64; i < g.n_zero; i += 32 * kEpiWarps) g.zero[i] = 0;
     Walk<kCta> walk(g, clu, n_clu);
     Item u;
     Kept kept{kept_in + (warp - 2) * kKeptBytes, buf, tl->kept[warp - 2]};
@@ -1252,7 +1256,10 @@ void prod_plan(ProdLaunch& l) {
       if (l.job[k].kb > 2 * kChainKb) l.slot_bytes = 2 * slot;
 }
 
-cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, const char** what) {
+namespace {
+// Runs a planned launch; slots: at least slot_bytes, flags: flag_bytes of zeros (256-byte aligned); zero: n_zero
+// words that it clears.
+cudaError_t prod_run(ProdLaunch& l, void* slots, int* flags, int* zero, int n_zero, cudaStream_t st, const char** what) {
   DeviceState dev;
   *what = "kernel attributes";
   cudaError_t e = device_state(&dev);
@@ -1268,7 +1275,7 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, c
   const bool kept = l.epi == kEpiDgated && !l.f32;
   a.chains = l.chains, a.stages = stage_count(l.cta, l.n_tile, kept);
   a.whole = l.whole, a.part_kb = l.f32 && !l.fp16 ? 2 * kChainKb : 1 << 30;
-  a.slots = (float*)slots, a.flags = (int*)flags;
+  a.slots = (float*)slots, a.flags = flags, a.zero = zero, a.n_zero = n_zero;
   for (int c = 0; c <= kSms; ++c) a.cut[c] = c <= l.clusters && l.whole < l.n_tiles ? l.cut[c] : 0;
   bool done[kProdMaps] = {};
   *what = "cuTensorMapEncodeTiled";
@@ -1298,7 +1305,6 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, c
   });
 }
 
-namespace {
 void sizes(const ProdLaunch* l, int n, int64_t& slots, int64_t& flags) {
   slots = flags = 0;
   for (int k = 0; k < n; ++k) slots = std::max(slots, round_up(l[k].slot_bytes, 256)), flags += l[k].flag_bytes;
@@ -1314,19 +1320,23 @@ int64_t prod_bytes(const ProdLaunch* l, int n) {
 cudaError_t prod_run_all(StageLaunch& stage, ProdLaunch* l, int n, void* workspace, cudaStream_t st, const char** what) {
   int64_t slots, flags;
   sizes(l, n, slots, flags);
-  char* at = (char*)workspace + slots;
+  int* at = (int*)((char*)workspace + slots);
   cudaError_t e = cudaSuccess;
-  stage.zero = (int*)at, stage.n_zero = (int)(flags / 4);   // the flags, by the staging launch if there is one
-  if (flags && stage.n == 0) {
-    *what = "clearing flags";
-    e = cudaMemsetAsync(at, 0, flags, st);
-  } else {
+  // flags are cleared by the staging launch or, where there is none, the first product's apart, the others' by the
+  // product before them (a memset of its own keeps the next launch's set-up from overlapping: 3 us)
+  const bool staged = stage.n > 0;
+  stage.zero = at, stage.n_zero = (int)(flags / 4);
+  if (staged) {
     *what = "staging launch";
     e = stage_run(stage, st);
+  } else if (l[0].flag_bytes) {
+    *what = "clearing flags";
+    e = cudaMemsetAsync(at, 0, l[0].flag_bytes, st);
   }
   for (int k = 0; e == cudaSuccess && k < n; ++k) {
-    e = prod_run(l[k], workspace, at, st, what);
-    at += l[k].flag_bytes;
+    int* next = at + l[k].flag_bytes / 4;
+    e = prod_run(l[k], workspace, at, next, staged || k + 1 == n ? 0 : (int)(l[k + 1].flag_bytes / 4), st, what);
+    at = next;
   }
   return e;
 }

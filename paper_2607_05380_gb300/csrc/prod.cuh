@@ -78,9 +78,6 @@ void prod_pairs(ProdJob& j, bool f32, int halves);
 
 // Chooses tiles and shares them out.
 void prod_plan(ProdLaunch& l);
-// Runs a planned launch; slots: at least slot_bytes, flags: flag_bytes of zeros
-// (256-byte aligned).
-cudaError_t prod_run(ProdLaunch& l, void* slots, void* flags, cudaStream_t st, const char** what);
 // Copies operands into a layout that TMA takes: rows of `cols` elements to
 // rows of pitch ldp (a multiple of 8), in segments of rows_seg rows; fp32
 // elements become three bf16 parts (segments s * 3 .. s * 3 + 2 of segment s),
