@@ -614,9 +614,20 @@ __device__ __forceinline__ void row_part(const Span<T>& sp, float c, float (*red
     for (int k = 0; k < kTurn; ++k) u[k] = sp.zv[i + k * kThreads];
     take<T, kHard, kFar, kTurn>(q, u, c);
   }
-  for (; i < sp.body; i += kThreads) {
-    const uint4 u[1] = {sp.zv[i]};
-    take<T, kHard, kFar, 1>(q, u, c);
+  // the last turn: at once, past the row's end -inf, which adds 0; group by group in a row of many turns, which
+  // wants the registers (2048 rows of 50021 bf16: 80 us, at once 81.6; 16384 of 4000: 95 us, at once 82)
+  if constexpr (kWarps <= 4) {
+    if (i < sp.body) {
+      uint4 u[kTurn];
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) u[k] = i + k * kThreads < sp.body ? sp.zv[i + k * kThreads] : Vec<T>::none();
+      take<T, kHard, kFar, kTurn>(q, u, c);
+    }
+  } else {
+    for (; i < sp.body; i += kThreads) {
+      const uint4 u[1] = {sp.zv[i]};
+      take<T, kHard, kFar, 1>(q, u, c);
+    }
   }
   finish<T, kHard, kFar, kWarps>(q, sp, c, red);
 }
@@ -650,7 +661,18 @@ __device__ __forceinline__ void row_dense(const Span<T>& sp, float c, const Row&
 #pragma unroll
     for (int k = 0; k < kTurn; ++k) put(i + k * kThreads, u[k]);
   }
-  for (; i < sp.body; i += kThreads) put(i, sp.zv[i]);
+  if constexpr (kWarps <= 4) {   // (as in row_part)
+    if (i < sp.body) {
+      uint4 u[kTurn];
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) u[k] = i + k * kThreads < sp.body ? sp.zv[i + k * kThreads] : V::none();
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k)
+        if (i + k * kThreads < sp.body) put(i + k * kThreads, u[k]);
+    }
+  } else {
+    for (; i < sp.body; i += kThreads) put(i, sp.zv[i]);
+  }
   if (sp.mine) dz[sp.single] = Elem<T>::from_f(dense<kHard>(c, r, Elem<T>::to_f(sp.z[sp.single])));
 }
 
@@ -658,7 +680,7 @@ __device__ __forceinline__ void row_dense(const Span<T>& sp, float c, const Row&
 // while they take the sums, and the entries' gradients and the loss while they
 // write the dense part; its values go over theirs after the last barrier.
 template <typename T, int kHard, int kWarps>
-__global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 8) k_distill_row(const Args<T> g) {
+__global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 32 / kWarps) k_distill_row(const Args<T> g) {
   constexpr int kPer = kMaxK / 32;   // entries of a lane
   __shared__ int ids[kMaxK];
   __shared__ float p[kMaxK];
@@ -785,8 +807,8 @@ cudaError_t rows(const Args<T>& a, cudaStream_t st) {
   // entries 22 (eight lanes 30), 16 entries of 32 classes 51 (34), 4096 rows 6.2
   // (a thread 8.7); 64 classes, 80000 rows 33 (sixteen lanes 45); 128, 80000
   // rows 48 (72); 256, 80000 rows 58 (79), 128 rows 5.7 (6.1); 512, 80000 rows
-  // 94 (117), 128 rows 6.2 (7.0); 1000, 16384 rows 31 (a block a row 52), 128
-  // rows 5.3 (6.9).
+  // 94 (117), 128 rows 6.2 (7.0); 1000, 16384 rows 29 (a block a row 38), 128
+  // rows 5.8 (6.9).
   const bool few = a.all <= 4096;
   if (a.n <= kSmallN && a.k <= 8 && a.all > 24576) {
     const uint32_t div = ((1u << 20) + a.n - 1) / a.n;   // i / n = i div >> 20 for i < 128 * 32
@@ -806,7 +828,9 @@ cudaError_t rows(const Args<T>& a, cudaStream_t st) {
     else group<T, 16, 32>(a, st);
   } else if (a.n <= 1024 && a.all > 1024) {
     group<T, 32, 32>(a, st);
-  } else if (a.n * (int64_t)sizeof(T) <= 32768) {
+  } else if (a.n * (int64_t)sizeof(T) <= 16384) {   // two warps a row: 16384 rows of 2000 bf16, 48 us (four 63)
+    wide<T, 2>(a, st);
+  } else if (a.n * (int64_t)sizeof(T) <= 32768) {   // four: of 16000, 181 us (two 229, fifteen 270)
     wide<T, 4>(a, st);
   } else {
     wide<T, 15>(a, st);
