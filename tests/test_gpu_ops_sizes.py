@@ -63,3 +63,17 @@ def test_product_few_rows(tp, rows, k, n):  # noqa: F811
     ref = s * a.double()[:, None] * b.double() + bias.double()
     tol = 2.0 ** -24 * (3 * (s * a.double()[:, None] * b.double()).abs() + ref.abs()) + 1e-30
     _within(y, ref, 1.01 * tol, (rows, k, n))
+
+
+@pytest.mark.parametrize("rows,d,f,o", [(2048, 64, 2048, 512), (2048, 256, 2048, 1024)])
+def test_gated_backward_many_times(tp, rows, d, f, o):  # noqa: F811
+    """The same bits in 15000 passes: what comes into shared memory for a chunk
+    does not overtake the reading of the one before."""
+    x, wgu, wd, dy = _gated_case(torch.bfloat16, rows, d, f, o, 5)
+    _, saved = tp.gated_forward(x, wgu, wd, "gelu", save=True)
+    ref = tp.gated_backward(dy, x, wgu, wd, saved)[1]
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(15000):
+        bad += (tp.gated_backward(dy, x, wgu, wd, saved)[1] != ref).any()
+    assert int(bad) == 0
+    tp.ops_check()
