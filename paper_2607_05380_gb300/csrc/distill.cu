@@ -9,7 +9,8 @@
 // z_i c - o in one multiply-add, o = zm c rounded, is off by that rounding, the
 // same for every class, so it drops out; but for a row that a mask left at
 // -10^10 or at the type's lowest value its power of two overflows: such rows
-// ("far") take the difference first.  For tau = 1, 2 and 4 e1 is the first, second or fourth power of e, so that a
+// ("far"), and all rows of a tau beyond 2^-18 .. 2^18, take the difference
+// first.  For tau = 1, 2 and 4 e1 is the first, second or fourth power of e, so that a
 // class costs one exponential a pass.
 //
 // The gradient's dense part is written for every class; then, after a barrier
@@ -500,6 +501,10 @@ struct Running {
 
 // |zm c| from which on a row is far: below, the product's rounding is less than 2^3
 constexpr float kFarPower = 67108864.f;
+// Of temperatures further than this from 1 every row is far: a gap of 2^26 in
+// the larger of the two exponents (see nothing()) leaves at least 2^8 in the
+// other one up to here, and may leave less beyond.
+constexpr float kFarTau = 262144.f;
 
 // A row's 16-byte groups and the single classes at its ends.
 template <typename T>
@@ -530,8 +535,9 @@ __device__ __forceinline__ void bring(float& s, float& s1, float m, float to, fl
 
 // What a thread sees while its maximum is -inf, or twice as far out as a row
 // that is not far may lie, counts only if it is NaN: either the row's own
-// maximum is so much larger that it adds 0, or the row is far and the sums are
-// taken again.
+// maximum is 2^26 or more above it in the larger of the two exponents, so that
+// it adds 0 to both sums (see kFarTau), or the row is far and the sums are taken
+// again.
 template <int kHard, bool kFar>
 __device__ __forceinline__ bool nothing(const Running<kHard, kFar>& q, float c) {
   return kFar ? q.m == neg_inf() : !(fabsf(q.m) * fmaxf(c, kLog2e) < 2.f * kFarPower);
@@ -717,7 +723,9 @@ __global__ void __launch_bounds__(32 * kWarps + 32, kWarps > 4 ? 3 : 32 / kWarps
   }
   __syncthreads();
   Sums a = row_join<kHard, false, kWarps>(g.c, red[0]);
-  const bool far = fabsf(a.zm) * fmaxf(g.c, kLog2e) >= kFarPower && a.zm != neg_inf();   // (an infinite maximum: NaN either way)
+  const float wide = fmaxf(g.c, kLog2e), narrow = fminf(g.c, kLog2e);
+  // (an infinite maximum: NaN either way)
+  const bool far = (fabsf(a.zm) * wide >= kFarPower || wide > kFarTau * narrow) && a.zm != neg_inf();
   if (far) {
     if (!extra) row_part<T, kHard, true, kWarps>(sp, g.c, red[1]);
     __syncthreads();

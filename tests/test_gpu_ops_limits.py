@@ -1,0 +1,59 @@
+"""The student operators at the edges of what they take."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_ops import TYPES, U, _act64, _distill64, _gated64, _gated_case, _gen, _within, tp  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------- distillation: temperatures
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [700, 4096, 20001])
+@pytest.mark.parametrize("tau,low", [(1e8, -1e8), (2.0 ** 20, -2.0 ** 21), (2.0 ** 18, -2.0 ** 27), (2.0 ** -18, -2.0 ** 9),
+                                     (2.0 ** -26, -2.0)])
+def test_distill_far_temperatures(tp, dtype, n, tau, low):  # noqa: F811
+    """Classes far below the maximum count by the exponent of each softmax: a
+    gap that leaves nothing of exp(z) may leave exp(z / tau) almost one (tau >
+    1), and the other way round (tau < 1).  Bounds on the gradient: an exponential
+    of a gap x is off by 2 ulp and its exponent's two roundings, 2^-20 (1 + |x|)
+    in all, its softmax by twice that, the teacher's weights likewise."""
+    rows, k, alpha = 6, 3, 0.5
+    g = _gen(n)
+    z = torch.zeros(2, rows, n, device="cuda")
+    z[:, 0, : n // 2] = low                       # the first classes that a thread sees
+    z[:, 1, n // 2:] = low
+    z[:, 2, : n - 1] = low
+    z[:, 3] = torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, low, 0.0)
+    z[:, 4] = low
+    z[:, 5, : n // 2] = -math.inf
+    z[1] *= 0.5
+    z = z.to(dtype)
+    ids = torch.tensor([[n - 1, 0, 5]], dtype=torch.int32, device="cuda").repeat(rows, 1)
+    ids[5] = n - 1
+    top = torch.tensor([[0.0, 0.5 * tau, -tau]], device="cuda").repeat(rows, 1)
+    labels = torch.full((rows,), n - 1, dtype=torch.int32, device="cuda")
+    for lab in (labels, None):
+        loss, dz = tp.distill(z, ids, top, lab, tau=tau, alpha=alpha)
+        (want, _), (ref, _) = _distill64(z, ids, top, lab, tau, alpha)
+        zd = z.double()
+        gap = zd.amax(2, keepdim=True) - zd
+        err = lambda x: 2.0 ** -19 * (2 + x.clamp(max=200.0))  # noqa: E731
+        e = alpha * tau * (torch.softmax(zd / tau, 2) * err(gap / tau))
+        there = torch.zeros(rows, n, dtype=torch.float64, device="cuda").scatter_(1, ids.long(), 1.0)
+        e = e + alpha * tau * there * 2.0 ** -18
+        if lab is not None:
+            e = e + (1 - alpha) * (torch.softmax(zd, 2) * err(gap) + 2.0 ** -22)
+        _within(dz, ref, e / rows + U[dtype] * ref.abs() + 1e-30, (n, tau, low))
+        # the loss is tau^2 times a difference of logarithms, each off by its size's rounding
+        p = torch.softmax(top.double() / tau, 1)
+        size = (p * (4 + torch.gather(gap / tau, 2, ids.long()[None].expand(2, -1, -1)))).sum(2) + math.log(n)
+        tol = alpha * tau ** 2 * size
+        if lab is not None:
+            tol = tol + (1 - alpha) * (gap[:, :, n - 1] + math.log(n) + 4)
+        _within(loss, want, 2.0 ** -18 * tol.mean(1), (n, tau, low))
+        only, none = tp.distill(z, ids, top, lab, tau=tau, alpha=alpha, grad=False)
+        assert none is None and torch.equal(only, loss)
