@@ -126,7 +126,9 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
  * is -inf makes the loss +inf.  Entries of the same class add up.
  *   dz: T [m, rows, n] (may be NULL): the gradient of loss[i] at its logits,
  *   alpha tau (softmax(z / tau) - p) + (1 - alpha) (softmax(z) - onehot),
- *   over rows; loss: float32 [m].  tau > 0, 0 <= alpha <= 1.               */
+ *   over rows; loss: float32 [m].  2^-60 <= tau <= 2^60, 0 <= alpha <= 1.
+ * kd is a difference of fp32 logarithms, whose rounding tau^2 multiplies: above
+ * tau = 100 or so the loss loses its digits, while dz keeps them.           */
 tp_status pack_distill_bytes(int64_t m, int64_t rows, int64_t* workspace);
 tp_status pack_distill(const void* z, int64_t m, int64_t rows, int32_t n, const int32_t* ids, const float* top,
                        int32_t k, const int32_t* labels, float tau, float alpha, int32_t precision, float* loss,

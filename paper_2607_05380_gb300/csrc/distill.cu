@@ -37,6 +37,7 @@ namespace tp {
 namespace {
 
 constexpr int kMaxK = 128;
+constexpr float kMinTau = 8.67361738e-19f;   // 2^-60: tau^2, log2(e) / tau and their like stay normal numbers
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
 __device__ __forceinline__ float ex2(float v) {   // 2^v to 2 ulp; results below 2^-126 are 0
@@ -875,7 +876,7 @@ tp_status pack_distill(const void* z, int64_t m, int64_t n_rows, int32_t n, cons
   if (s != TP_OK) return s;
   if (n < 2) return ops_fail(TP_EINVAL, "n %d must be at least 2", n);
   if (k < 1 || k > kMaxK) return ops_fail(TP_EINVAL, "k %d must be in 1..%d", k, kMaxK);
-  if (!(tau > 0.f) || !(tau <= 3.4e38f)) return ops_fail(TP_EINVAL, "tau must be positive and finite");
+  if (!(tau >= kMinTau && tau <= 1.f / kMinTau)) return ops_fail(TP_EINVAL, "tau must be in 2^-60..2^60");
   if (!(alpha >= 0.f && alpha <= 1.f)) return ops_fail(TP_EINVAL, "alpha must be in 0..1");
   if (precision != TP_BF16 && precision != TP_FP32) return ops_fail(TP_EINVAL, "unknown precision %d", precision);
   if (!loss) return ops_fail(TP_EINVAL, "null argument");
