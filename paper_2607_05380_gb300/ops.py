@@ -45,10 +45,24 @@ def _precision(t, name):
     return p
 
 
-def _mat(t, name, dtype, rows=None, cols=None):
-    """(pointer, row stride) of a matrix with contiguous rows."""
-    if not t.is_cuda:
+def _device_of(t, name):
+    """The device that a call works on: that of its first tensor, which has to
+    be the current one when the call is made (_stream)."""
+    d = t.get_device()
+    if d < 0:
         raise ValueError(f"{name}: expected a CUDA tensor")
+    return d
+
+
+def _elsewhere(t, name, device):
+    return ValueError(f"{name}: expected a CUDA tensor" if t.get_device() < 0 else
+                      f"{name}: on device {t.get_device()}, expected {device}")
+
+
+def _mat(t, name, device, dtype, rows=None, cols=None):
+    """(pointer, row stride) of a matrix with contiguous rows."""
+    if t.get_device() != device:
+        raise _elsewhere(t, name, device)
     if t.dtype is not dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
     shape = t.shape
@@ -66,12 +80,12 @@ def _mat(t, name, dtype, rows=None, cols=None):
     return t.data_ptr(), ld
 
 
-def _flat(t, name, dtype, *shape):
+def _flat(t, name, device, dtype, *shape):
     """Pointer of a contiguous tensor of the given shape (None for None)."""
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError(f"{name}: expected a CUDA tensor")
+    if t.get_device() != device:
+        raise _elsewhere(t, name, device)
     if t.dtype is not dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
     if t.shape != shape:
@@ -85,12 +99,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(t):
-    """The current stream's pointer; t has to be on the current device."""
-    d = t.get_device()
-    if d != _device():
+def _stream(device):
+    """The current stream's pointer; the call's device has to be the current one."""
+    if device != _device():
         raise ValueError("the tensors are not on the current device")
-    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(d)
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
 _local = threading.local()
@@ -124,16 +137,16 @@ def _gated_bytes(rows, d, f, d_out, prec):
 
 
 def _gated_shapes(x, w_gate_up, w_down):
-    prec, dtype = _precision(x, "x"), x.dtype
-    xp, ldx = _mat(x, "x", dtype)
+    prec, dtype, on = _precision(x, "x"), x.dtype, _device_of(x, "x")
+    xp, ldx = _mat(x, "x", on, dtype)
     rows, d = x.shape
     gate, down = w_gate_up.shape, w_down.shape
     if len(gate) != 2 or gate[0] % 2 or len(down) != 2:
         raise ValueError("w_gate_up must be [2 f, d] and w_down [d_out, f]")
     f, d_out = gate[0] // 2, down[0]
-    wp = _flat(w_gate_up, "w_gate_up", dtype, 2 * f, d)
-    dp = _flat(w_down, "w_down", dtype, d_out, f)
-    return prec, xp, ldx, rows, d, f, d_out, wp, dp
+    wp = _flat(w_gate_up, "w_gate_up", on, dtype, 2 * f, d)
+    dp = _flat(w_down, "w_down", on, dtype, d_out, f)
+    return prec, on, xp, ldx, rows, d, f, d_out, wp, dp
 
 
 def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
@@ -145,9 +158,9 @@ def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
     code = ACTIVATIONS.get(act)
     if code is None:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
-    prec, xp, ldx, rows, d, f, d_out, wp, dp = _gated_shapes(x, w_gate_up, w_down)
+    prec, on, xp, ldx, rows, d, f, d_out, wp, dp = _gated_shapes(x, w_gate_up, w_down)
     n_saved, n_work, _ = _gated_bytes(rows, d, f, d_out, prec)
-    st, dev = _stream(x), x.device
+    st, dev = _stream(on), x.device
     y = _empty((rows, d_out), dtype=x.dtype, device=dev)
     saved = _empty(n_saved, dtype=torch.uint8, device=dev) if save else None
     work, _keep = _work(n_work, st, x)
@@ -163,11 +176,11 @@ def gated_backward(dy, x, w_gate_up, w_down, saved, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return gated_backward(dy, x, w_gate_up, w_down, saved)
-    prec, xp, ldx, rows, d, f, d_out, wp, dp = _gated_shapes(x, w_gate_up, w_down)
-    gp, ldg = _mat(dy, "dy", x.dtype, rows, d_out)
+    prec, on, xp, ldx, rows, d, f, d_out, wp, dp = _gated_shapes(x, w_gate_up, w_down)
+    gp, ldg = _mat(dy, "dy", on, x.dtype, rows, d_out)
     n_saved, _, n_work = _gated_bytes(rows, d, f, d_out, prec)
-    sp = _flat(saved, "saved", torch.uint8, n_saved)
-    st, dev = _stream(x), x.device
+    sp = _flat(saved, "saved", on, torch.uint8, n_saved)
+    st, dev = _stream(on), x.device
     dx = _empty((rows, d), dtype=x.dtype, device=dev)
     dw = _empty((2 * f, d), dtype=x.dtype, device=dev)
     dd = _empty((d_out, f), dtype=x.dtype, device=dev)
@@ -180,15 +193,15 @@ def gated_backward(dy, x, w_gate_up, w_down, saved, stream=None):
 
 
 def _norm(x, weight, residual, eps, q8):
-    prec, dtype = _precision(x, "x"), x.dtype
-    xp, ldx = _mat(x, "x", dtype)
+    prec, dtype, on = _precision(x, "x"), x.dtype, _device_of(x, "x")
+    xp, ldx = _mat(x, "x", on, dtype)
     rows, d = x.shape
-    wp = _flat(weight, "weight", torch.float32, d)
-    st, dev = _stream(x), x.device
+    wp = _flat(weight, "weight", on, torch.float32, d)
+    rp, ldr = (None, 0) if residual is None else _mat(residual, "residual", on, dtype, rows, d)
+    st, dev = _stream(on), x.device
     if residual is None:
-        rp, ldr, total, tp = None, 0, x, None
+        total, tp = x, None
     else:
-        rp, ldr = _mat(residual, "residual", dtype, rows, d)
         total = _empty((rows, d), dtype=dtype, device=dev)
         tp = total.data_ptr()
     if q8:
@@ -239,14 +252,14 @@ def rms_norm_backward(dy, s, weight, dsum=None, eps=1e-6, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return rms_norm_backward(dy, s, weight, dsum, eps)
-    prec, dtype = _precision(s, "s"), s.dtype
-    sp, lds = _mat(s, "s", dtype)
+    prec, dtype, on = _precision(s, "s"), s.dtype, _device_of(s, "s")
+    sp, lds = _mat(s, "s", on, dtype)
     rows, d = s.shape
-    gp, ldg = _mat(dy, "dy", dtype, rows, d)
-    wp = _flat(weight, "weight", torch.float32, d)
-    ap, lda = _mat(dsum, "dsum", dtype, rows, d) if dsum is not None else (None, 0)
+    gp, ldg = _mat(dy, "dy", on, dtype, rows, d)
+    wp = _flat(weight, "weight", on, torch.float32, d)
+    ap, lda = _mat(dsum, "dsum", on, dtype, rows, d) if dsum is not None else (None, 0)
     n = _norm_bytes(rows, d)
-    st, dev = _stream(s), s.device
+    st, dev = _stream(on), s.device
     dx = _empty((rows, d), dtype=dtype, device=dev)
     dw = _empty(d, dtype=torch.float32, device=dev)
     work, _keep = _work(n, st, s)
@@ -275,17 +288,18 @@ def product_q8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=Non
     prec = _PRECISION.get(dtype)
     if prec is None:
         raise ValueError(f"dtype: expected bfloat16 or float32, got {dtype}")
-    qp, ldq = _mat(q, "q", torch.int8)
+    on = _device_of(q, "q")
+    qp, ldq = _mat(q, "q", on, torch.int8)
     rows, k = q.shape
     if w.dim() != 2:
         raise ValueError("w must be [n, k]")
     n = w.shape[0]
-    wp = _flat(w, "w", torch.int8, n, k)
-    sp = _flat(scale, "scale", torch.float32, rows)
-    cp = _flat(w_scale, "w_scale", torch.float32, n)
-    bp = _flat(bias, "bias", torch.float32, n)
+    wp = _flat(w, "w", on, torch.int8, n, k)
+    sp = _flat(scale, "scale", on, torch.float32, rows)
+    cp = _flat(w_scale, "w_scale", on, torch.float32, n)
+    bp = _flat(bias, "bias", on, torch.float32, n)
     n_work = _product_bytes(rows, k, n, prec)
-    st, dev = _stream(q), q.device
+    st, dev = _stream(on), q.device
     y = _empty((rows, n), dtype=dtype, device=dev)
     work, _keep = _work(n_work, st, q) if n_work else (None, None)
     status = _lib().pack_product_q8(qp, ldq, sp, wp, cp, bp, rows, k, n, prec, y.data_ptr(),
@@ -314,18 +328,18 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
         with torch.cuda.stream(stream):
             return distill(z, ids, top, labels, tau, alpha, grad)
     prec = _precision(z, "z")
-    shape = z.shape
-    if len(shape) not in (2, 3) or not z.is_cuda or not z.is_contiguous():
+    shape, on = z.shape, _device_of(z, "z")
+    if len(shape) not in (2, 3) or not z.is_contiguous():
         raise ValueError("z must be a contiguous CUDA tensor [m, rows, n] or [rows, n]")
     m, rows, n = (1, *shape) if len(shape) == 2 else shape
     if ids.dim() != 2:
         raise ValueError("ids must be [rows, k]")
     k = ids.shape[1]
-    ip = _flat(ids, "ids", torch.int32, rows, k)
-    top_p = _flat(top, "top", torch.float32, rows, k)
-    yp = _flat(labels, "labels", torch.int32, rows)
+    ip = _flat(ids, "ids", on, torch.int32, rows, k)
+    top_p = _flat(top, "top", on, torch.float32, rows, k)
+    yp = _flat(labels, "labels", on, torch.int32, rows)
     n_work = _distill_bytes(m, rows)
-    st, dev = _stream(z), z.device
+    st, dev = _stream(on), z.device
     loss = _empty(m, dtype=torch.float32, device=dev)
     dz = torch.empty_like(z) if grad else None
     work, _keep = _work(n_work, st, z)

@@ -21,3 +21,58 @@ def test_distill_temperature_range(tp, tau):
     """Beyond 2^-60..2^60, tau^2 or 1 / tau leaves fp32's range and the loss would be no number."""
     st = tp.load_library().pack_distill(SOME, 2, 5, 10, SOME, SOME, 4, None, tau, 0.5, 1, SOME, SOME, SOME, 1 << 30, None)
     assert st == tp.TP_EINVAL and b"tau" in tp.load_library().pack_last_error(None)
+
+
+class Fake:
+    """Stands in for a CUDA tensor where only its description is looked at."""
+
+    def __init__(self, *shape, dtype=torch.float32, device=0):
+        self.shape, self.dtype, self._device, self.is_cuda = torch.Size(shape), dtype, device, True
+
+    def stride(self):
+        return tuple(torch.Size(self.shape[i + 1:]).numel() for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self._device
+
+    def data_ptr(self):
+        return 4096
+
+
+I8, I32, U8 = torch.int8, torch.int32, torch.uint8
+
+
+def _calls(tp):
+    """Each entry point with the descriptions of right arguments."""
+    n_saved = ctypes.c_int64()
+    assert tp.load_library().pack_gated_bytes(5, 16, 24, 8, 1, ctypes.byref(n_saved), None, None) == tp.TP_OK
+    x, w = lambda **k: Fake(5, 16, **k), lambda **k: Fake(16, **k)  # noqa: E731
+    gu, down = lambda **k: Fake(48, 16, **k), lambda **k: Fake(8, 24, **k)  # noqa: E731
+    return {"gated_forward": (tp.gated_forward, [x, gu, down]),
+            "gated_backward": (tp.gated_backward, [lambda **k: Fake(5, 8, **k), x, gu, down,
+                                                   lambda **k: Fake(n_saved.value, dtype=U8, **k)]),
+            "rms_norm": (tp.rms_norm, [x, w, x]), "rms_norm_q8": (tp.rms_norm_q8, [x, w, x]),
+            "rms_norm_backward": (tp.rms_norm_backward, [x, x, w, x]),
+            "product_q8": (tp.product_q8, [lambda **k: Fake(5, 16, dtype=I8, **k), lambda **k: Fake(5, **k),
+                                           lambda **k: Fake(9, 16, dtype=I8, **k), lambda **k: Fake(9, **k),
+                                           lambda **k: Fake(9, **k)]),
+            "distill": (tp.distill, [lambda **k: Fake(2, 5, 10, **k), lambda **k: Fake(5, 3, dtype=I32, **k),
+                                     lambda **k: Fake(5, 3, **k), lambda **k: Fake(5, dtype=I32, **k)])}
+
+
+@pytest.mark.parametrize("name", ["gated_forward", "gated_backward", "rms_norm", "rms_norm_q8", "rms_norm_backward",
+                                  "product_q8", "distill"])
+def test_tensors_of_another_device(tp, name):
+    """A kernel reads every tensor on the device it runs on: one of another
+    device, whichever it is, is refused before anything is allocated or launched."""
+    fn, args = _calls(tp)[name]
+    for other in range(len(args)):
+        for there in (1, -1):
+            with pytest.raises(ValueError, match="device|CUDA"):
+                fn(*(a(device=there if i == other else 0) for i, a in enumerate(args)))
