@@ -5,7 +5,10 @@ Argument checks and marshalling only.  Tensors are CUDA tensors, bf16 or
 float32; rows may be spaced (any stride of the first dimension that is at
 least the row's length), the last dimension is contiguous.  Work runs on
 ``stream`` (a torch stream; None: the current one), where outputs and
-workspaces are also allocated, and is not waited for.
+workspaces are also allocated, and is not waited for.  With ``stream`` the
+inputs' memory is kept until that stream has read them, so that the caller may
+let go of them at once; that they are written before it reads them, and
+outputs before another stream does, is the caller's to order.
 """
 from __future__ import annotations
 
@@ -106,6 +109,16 @@ def _stream(device):
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
+def _on(stream, fn, tensors, *args):
+    """fn(*tensors, *args) on another stream, which the allocator is told of."""
+    with torch.cuda.stream(stream):
+        out = fn(*tensors, *args)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return out
+
+
 _local = threading.local()
 _SMALL = 1 << 22
 
@@ -153,8 +166,7 @@ def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
     """y = (act(x Wg^T) * (x Wu^T)) Wd^T with w_gate_up = [Wg; Wu] [2 f, d] and
     w_down [d_out, f].  save=True returns (y, saved) for gated_backward."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return gated_forward(x, w_gate_up, w_down, act, save)
+        return _on(stream, gated_forward, (x, w_gate_up, w_down), act, save)
     code = ACTIVATIONS.get(act)
     if code is None:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
@@ -174,8 +186,7 @@ def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
 def gated_backward(dy, x, w_gate_up, w_down, saved, stream=None):
     """(dx, dw_gate_up, dw_down) of the gated_forward call that saved."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return gated_backward(dy, x, w_gate_up, w_down, saved)
+        return _on(stream, gated_backward, (dy, x, w_gate_up, w_down, saved))
     prec, on, xp, ldx, rows, d, f, d_out, wp, dp = _gated_shapes(x, w_gate_up, w_down)
     gp, ldg = _mat(dy, "dy", on, x.dtype, rows, d_out)
     n_saved, _, n_work = _gated_bytes(rows, d, f, d_out, prec)
@@ -223,8 +234,7 @@ def rms_norm(x, weight, residual=None, eps=1e-6, stream=None):
     """(y, s): the RMS norm y of s = x + residual (x itself without one) times
     weight [d] (float32), and s for the next residual and rms_norm_backward."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return rms_norm(x, weight, residual, eps)
+        return _on(stream, rms_norm, (x, weight, residual), eps)
     return _norm(x, weight, residual, eps, False)
 
 
@@ -232,8 +242,7 @@ def rms_norm_q8(x, weight, residual=None, eps=1e-6, stream=None):
     """(q, scale, s): rms_norm with its output as int8 q [rows, d] and a scale
     per row, y = q * scale[:, None]."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return rms_norm_q8(x, weight, residual, eps)
+        return _on(stream, rms_norm_q8, (x, weight, residual), eps)
     return _norm(x, weight, residual, eps, True)
 
 
@@ -250,8 +259,7 @@ def rms_norm_backward(dy, s, weight, dsum=None, eps=1e-6, stream=None):
     """(dx, dweight): gradients at s (= at x and at residual) and at weight;
     dsum: the gradient that reaches s from elsewhere, added to dx."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return rms_norm_backward(dy, s, weight, dsum, eps)
+        return _on(stream, rms_norm_backward, (dy, s, weight, dsum), eps)
     prec, dtype, on = _precision(s, "s"), s.dtype, _device_of(s, "s")
     sp, lds = _mat(s, "s", on, dtype)
     rows, d = s.shape
@@ -283,8 +291,7 @@ def product_q8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=Non
     """y[r, c] = (sum_k q[r, k] w[c, k]) scale[r] w_scale[c] + bias[c]: q int8
     [rows, k], w int8 [n, k], scales and bias float32, y of type dtype."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return product_q8(q, scale, w, w_scale, bias, dtype)
+        return _on(stream, product_q8, (q, scale, w, w_scale, bias), dtype)
     prec = _PRECISION.get(dtype)
     if prec is None:
         raise ValueError(f"dtype: expected bfloat16 or float32, got {dtype}")
@@ -325,8 +332,7 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     [rows, n] for one student); ids int32 and top float32 [rows, k]: classes
     (-1: none) and logits of the teacher's entries; labels int32 [rows]."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return distill(z, ids, top, labels, tau, alpha, grad)
+        return _on(stream, distill, (z, ids, top, labels), tau, alpha, grad)
     prec = _precision(z, "z")
     shape, on = z.shape, _device_of(z, "z")
     if len(shape) not in (2, 3) or not z.is_contiguous():

@@ -57,3 +57,46 @@ def test_distill_far_temperatures(tp, dtype, n, tau, low):  # noqa: F811
         _within(loss, want, 2.0 ** -18 * tol.mean(1), (n, tau, low))
         only, none = tp.distill(z, ids, top, lab, tau=tau, alpha=alpha, grad=False)
         assert none is None and torch.equal(only, loss)
+
+
+# ------------------------------------------------------------------ streams
+def test_inputs_of_calls_on_another_stream(tp):  # noqa: F811
+    """Inputs that the caller lets go of at once stay whole until a call with
+    stream= has read them: their memory is not given to the caller's own stream
+    before that."""
+    side = torch.cuda.Stream()
+    g = _gen(5)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    rows, d, f, n, k = 300, 256, 512, 1000, 4
+    x, w, wd, dy = (t.bfloat16() for t in (r(rows, d), r(2 * f, d) / 16, r(d, f) / 22, r(rows, d)))
+    v, res = r(d), r(rows, d).bfloat16()
+    q = torch.randint(-127, 128, (rows, d), generator=g, device="cuda").to(torch.int8)
+    qw = torch.randint(-127, 128, (n, d), generator=g, device="cuda").to(torch.int8)
+    s, sw, b, z, top = r(rows).abs(), r(n).abs(), r(n), r(2, rows, n), r(rows, k)
+    ids = torch.randint(0, n, (rows, k), generator=g, device="cuda").int()
+    y = torch.randint(0, n, (rows,), generator=g, device="cuda").int()
+    saved = tp.gated_forward(x, w, wd, save=True)[1]
+    calls = [(tp.gated_forward, (x, w, wd)), (tp.gated_backward, (dy, x, w, wd, saved)), (tp.rms_norm, (x, v, res)),
+             (tp.rms_norm_q8, (x, v, res)), (tp.rms_norm_backward, (dy, x, v, res)), (tp.product_q8, (q, s, qw, sw, b)),
+             (tp.distill, (z, ids, top, y))]
+    flat = lambda o: list(o) if isinstance(o, tuple) else [o]  # noqa: E731
+    want = [flat(fn(*a)) for fn, a in calls]
+    for fn, a in calls:      # what is loaded or allocated for the first time may wait for the device
+        fn(*a, stream=side)
+        spare = [torch.zeros_like(t) for t in a + a]
+        del spare
+    torch.cuda.synchronize()
+    for (fn, a), ref in zip(calls, want):
+        copies = [t.clone() for t in a]
+        where = [t.data_ptr() for t in copies]
+        shapes = [(t.shape, t.dtype) for t in copies]
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)            # about 50 ms
+        got = flat(fn(*copies, stream=side))
+        del copies
+        again = [torch.zeros(sh, dtype=dt, device="cuda") for sh, dt in shapes]
+        assert not set(where) & {t.data_ptr() for t in again}, fn.__name__
+        torch.cuda.synchronize()
+        for p, t in zip(got, ref):
+            assert torch.equal(p, t), fn.__name__
