@@ -48,6 +48,13 @@ def _precision(t, name):
     return p
 
 
+_MAX_SIZE = (1 << 31) - 1   # of the library's 32-bit sizes, which ctypes would cut
+
+
+def _too_wide(name, n):
+    return ValueError(f"{name}: a width of {n} is not below 2^31")
+
+
 def _device_of(t, name):
     """The device that a call works on: that of its first tensor, which has to
     be the current one when the call is made (_stream)."""
@@ -74,6 +81,8 @@ def _mat(t, name, device, dtype, rows=None, cols=None):
                          f"{'columns' if cols is None else cols})")
     ld, one = t.stride()
     n = shape[1]
+    if n > _MAX_SIZE:
+        raise _too_wide(name, n)
     if one != 1 and n > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
     if ld < n or shape[0] <= 1:
@@ -157,6 +166,8 @@ def _gated_shapes(x, w_gate_up, w_down):
     if len(gate) != 2 or gate[0] % 2 or len(down) != 2:
         raise ValueError("w_gate_up must be [2 f, d] and w_down [d_out, f]")
     f, d_out = gate[0] // 2, down[0]
+    if f > _MAX_SIZE or d_out > _MAX_SIZE:
+        raise _too_wide("w_gate_up or w_down", max(f, d_out))
     wp = _flat(w_gate_up, "w_gate_up", on, dtype, 2 * f, d)
     dp = _flat(w_down, "w_down", on, dtype, d_out, f)
     return prec, on, xp, ldx, rows, d, f, d_out, wp, dp
@@ -301,6 +312,8 @@ def product_q8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=Non
     if w.dim() != 2:
         raise ValueError("w must be [n, k]")
     n = w.shape[0]
+    if n > _MAX_SIZE:
+        raise _too_wide("w", n)
     wp = _flat(w, "w", on, torch.int8, n, k)
     sp = _flat(scale, "scale", on, torch.float32, rows)
     cp = _flat(w_scale, "w_scale", on, torch.float32, n)
@@ -341,6 +354,8 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     if ids.dim() != 2:
         raise ValueError("ids must be [rows, k]")
     k = ids.shape[1]
+    if n > _MAX_SIZE or k > _MAX_SIZE:
+        raise _too_wide("z or ids", max(n, k))
     ip = _flat(ids, "ids", on, torch.int32, rows, k)
     top_p = _flat(top, "top", on, torch.float32, rows, k)
     yp = _flat(labels, "labels", on, torch.int32, rows)

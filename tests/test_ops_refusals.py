@@ -76,3 +76,21 @@ def test_tensors_of_another_device(tp, name):
         for there in (1, -1):
             with pytest.raises(ValueError, match="device|CUDA"):
                 fn(*(a(device=there if i == other else 0) for i, a in enumerate(args)))
+
+
+BIG = 1 << 32
+
+
+@pytest.mark.parametrize("name,shapes", [
+    ("gated_forward", [(5, BIG + 16), (48, BIG + 16), (8, 24)]), ("gated_forward", [(5, 16), (2 * BIG + 48, 16), (8, BIG + 24)]),
+    ("gated_forward", [(5, 16), (48, 16), (BIG + 8, 24)]),
+    ("gated_backward", [(5, BIG + 8), (5, 16), (48, 16), (BIG + 8, 24), (1 << 20,)]),
+    ("rms_norm", [(5, BIG + 16), (BIG + 16,)]), ("rms_norm_q8", [(5, BIG + 16), (BIG + 16,)]),
+    ("rms_norm_backward", [(5, BIG + 16), (5, BIG + 16), (BIG + 16,)]),
+    ("product_q8", [(5, BIG + 16), (5,), (9, BIG + 16), (9,)]), ("product_q8", [(5, 16), (5,), (BIG + 9, 16), (BIG + 9,)]),
+    ("distill", [(5, BIG + 10), (5, 3), (5, 3)]), ("distill", [(5, 10), (5, BIG + 3), (5, BIG + 3)])])
+def test_sizes_past_32_bits(tp, name, shapes):
+    """A width of 2^32 + 10 is no width of 10."""
+    types = {"product_q8": {0: I8, 2: I8}, "distill": {1: I32}, "gated_backward": {4: U8}}.get(name, {})
+    with pytest.raises(ValueError, match="2\\^31"):
+        getattr(tp, name)(*(Fake(*s, dtype=types.get(i, torch.float32)) for i, s in enumerate(shapes)))
