@@ -114,8 +114,9 @@ tp_status pack_product_q8(const int8_t* q, int64_t ldq, const float* scale, cons
  * gradient in one call.
  *   z: T [m, rows, n], the students' logits; ids: int32 [rows, k] and top:
  *   float32 [rows, k], the classes and logits of the teacher's k entries of
- *   a row, 1 <= k <= 128, 2 <= n.  An id outside 0..n-1 (such as -1) or a logit of -inf is no
- *   entry.  labels: int32 [rows] or NULL; a label outside 0..n-1 is none.
+ *   a row, 1 <= k <= 128, 2 <= n <= 2^31 - 1024.  An id outside 0..n-1 (such
+ *   as -1) or a logit of -inf is no entry.  labels: int32 [rows] or NULL; a
+ *   label outside 0..n-1 is none.
  * For a row of student i with p = softmax(top / tau) over the row's entries:
  *   kd = tau^2 sum_j p_j (log p_j - log softmax(z / tau)[id_j]),
  *   ce = -log softmax(z)[label],

@@ -37,6 +37,7 @@ namespace tp {
 namespace {
 
 constexpr int kMaxK = 128;
+constexpr int kMaxN = 2147482624;   // 2^31 - 1024: a thread's number past a row's last class (Span) is still an int
 constexpr float kMinTau = 8.67361738e-19f;   // 2^-60: tau^2, log2(e) / tau and their like stay normal numbers
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
@@ -874,7 +875,7 @@ tp_status pack_distill(const void* z, int64_t m, int64_t n_rows, int32_t n, cons
                        void* dz, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
   tp_status s = check(m, n_rows);
   if (s != TP_OK) return s;
-  if (n < 2) return ops_fail(TP_EINVAL, "n %d must be at least 2", n);
+  if (n < 2 || n > kMaxN) return ops_fail(TP_EINVAL, "n %d must be in 2..%d", n, kMaxN);
   if (k < 1 || k > kMaxK) return ops_fail(TP_EINVAL, "k %d must be in 1..%d", k, kMaxK);
   if (!(tau >= kMinTau && tau <= 1.f / kMinTau)) return ops_fail(TP_EINVAL, "tau must be in 2^-60..2^60");
   if (!(alpha >= 0.f && alpha <= 1.f)) return ops_fail(TP_EINVAL, "alpha must be in 0..1");

@@ -94,3 +94,11 @@ def test_sizes_past_32_bits(tp, name, shapes):
     types = {"product_q8": {0: I8, 2: I8}, "distill": {1: I32}, "gated_backward": {4: U8}}.get(name, {})
     with pytest.raises(ValueError, match="2\\^31"):
         getattr(tp, name)(*(Fake(*s, dtype=types.get(i, torch.float32)) for i, s in enumerate(shapes)))
+
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 512, 2 ** 31 - 1023])
+def test_distill_classes_past_the_limit(tp, n):
+    """A thread's class number, up to 512 past a row's last, has 32 bits."""
+    L = tp.load_library()
+    assert L.pack_distill(SOME, 1, 0, n, None, None, 4, None, 2.0, 0.5, 0, SOME, None, None, 0, None) == tp.TP_EINVAL
+    assert b"n " in L.pack_last_error(None)
