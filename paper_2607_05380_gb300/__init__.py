@@ -8,6 +8,7 @@ without it raises, there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 
 import numpy as np
@@ -511,5 +512,19 @@ class OnlineEnsemble:
         return out
 
 
-from .ops import (ACTIVATIONS, distill, gated_backward, gated_forward, ops_check, product_q8,  # noqa: E402,F401
-                  rms_norm, rms_norm_backward, rms_norm_q8)
+# The student operators' binding (ops.py) needs torch, which nothing else here
+# loads before a call does: it is loaded when one of its names is asked for.
+_OPS = ("ACTIVATIONS", "distill", "gated_backward", "gated_forward", "ops_check", "product_q8", "rms_norm",
+        "rms_norm_backward", "rms_norm_q8")
+
+
+def __getattr__(name):
+    if name != "ops" and name not in _OPS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    ops = importlib.import_module(".ops", __name__)
+    globals().update({n: getattr(ops, n) for n in _OPS})
+    return globals()[name]
+
+
+def __dir__():
+    return sorted({*globals(), *_OPS, "ops"})
