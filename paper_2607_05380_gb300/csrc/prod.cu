@@ -388,16 +388,21 @@ __device__ __forceinline__ void pack32(const float (&v)[32], uint32_t (&pk)[16])
 template <bool kThree>
 __device__ __forceinline__ void put_parts(float (&v)[32], __nv_bfloat16* out, int64_t part, bool live, int n) {
   uint32_t pk[16];
-#pragma unroll 1
-  for (int q = 0; q < (kThree ? 3 : 1); ++q) {
+  if constexpr (!kThree) {
     pack32(v, pk);
-    put_bf16(pk, out + q * part, live, n);
-    if constexpr (kThree) {
+    put_bf16(pk, out, live, n);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pk[e] = first_parts(v[2 * e], v[2 * e + 1]);
+#pragma unroll 1
+    for (int q = 0; q < 3; ++q) {
+      put_bf16(pk, out + q * part, live, n);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         v[2 * e] -= __uint_as_float(pk[e] << 16);
         v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
       }
+      pack32(v, pk);   // (the last time for nothing)
     }
   }
 }
@@ -924,7 +929,7 @@ __global__ void __launch_bounds__(256) k_stage(const __grid_constant__ StageLaun
           uint32_t pk[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            pk[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+            pk[e] = q == 0 ? first_parts(v[2 * e], v[2 * e + 1]) : pack_bf16x2(v[2 * e], v[2 * e + 1]);
             v[2 * e] -= __uint_as_float(pk[e] << 16);
             v[2 * e + 1] -= __uint_as_float(pk[e] & 0xFFFF0000u);
           }

@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(256) k_rows32(const RowArgs g) {
       ((float*)g.p)[at_keep] = u * d;
 #pragma unroll
       for (int q = 0; q < 3; ++q) {
-        const __nv_bfloat16 b = __float2bfloat16_rn(h);
+        const __nv_bfloat16 b = q == 0 ? __ushort_as_bfloat16((uint16_t)first_parts(h, 0.f)) : __float2bfloat16_rn(h);
         g.parts[q * g.part + at_keep] = b;
         h -= __bfloat162float(b);
       }

@@ -56,6 +56,16 @@ __device__ __forceinline__ void s8_to_f16(uint32_t v, uint32_t& lo, uint32_t& hi
   hi = *reinterpret_cast<uint32_t*>(&y);
 }
 
+// Two 32-bit values' first bf16 parts (a's in the lower half): finite ones stay
+// finite, where rounding to nearest makes an infinity of what is above bf16's
+// largest number (3.39e38); the parts after it hold the rest, and an infinity or
+// a NaN again.
+__device__ __forceinline__ uint32_t first_parts(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
 // The upper 24 bits of a float, rounded to nearest (ties up), in bits 8..31.
 __device__ __forceinline__ uint32_t round_24(float v) {
   const uint32_t u = __float_as_uint(v);

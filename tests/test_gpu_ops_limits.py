@@ -100,3 +100,32 @@ def test_inputs_of_calls_on_another_stream(tp):  # noqa: F811
         torch.cuda.synchronize()
         for p, t in zip(got, ref):
             assert torch.equal(p, t), fn.__name__
+
+
+@pytest.mark.parametrize("rows", [5, 40, 100, 300])
+@pytest.mark.parametrize("where", ["x", "h"])
+def test_gated_fp32_largest_values(tp, rows, where):  # noqa: F811
+    """Finite fp32 values above bf16's largest (3.39e38), among the inputs or as
+    weights and h: their parts are finite and sum up to them."""
+    big = 3.4e38
+    g = _gen(rows)
+    d, f, o = 24, 40, 16
+    x = torch.randn(rows, d, generator=g, device="cuda")
+    x[:, 0] = 1.0
+    wgu = torch.randn(2 * f, d, generator=g, device="cuda")
+    wgu[:f] = 0
+    wgu[:f, 0] = 1.0                                   # relu(g) = 1
+    wd, dy = torch.randn(o, f, generator=g, device="cuda"), torch.randn(rows, o, generator=g, device="cuda")
+    sign = 1.0 - 2.0 * (torch.arange(rows, device="cuda") % 2)
+    if where == "x":                                   # u about 10^8
+        x[:, 1] = torch.where(torch.arange(rows, device="cuda") % 3 == 0, x[:, 1], big * sign)
+        wgu[f:, 1] = 1e-30
+        dy = 1e-12 * dy
+    else:                                              # u and h of +-3.4e38 in every other column
+        x[:, 1] = sign
+        wgu[f::2, 1] = big
+        wd, dy = 1e-30 * wd, 1e-3 * dy
+    y, saved = tp.gated_forward(x, wgu, wd, "relu", save=True)
+    got = [y, *tp.gated_backward(dy, x, wgu, wd, saved)]
+    for name, v, (ref, tol) in zip(("y", "dx", "dw_gate_up", "dw_down"), got, _gated64(x, wgu, wd, "relu", dy, torch.float32)):
+        _within(v, ref, tol, (name, rows))
