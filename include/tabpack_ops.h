@@ -79,8 +79,9 @@ tp_status pack_gated_backward(const void* dy, int64_t lddy, const void* x, int64
  *   y: T [rows, d], n rounded once (may be NULL);
  *   q, scale: int8 [rows, d] and float32 [rows] (may both be NULL): scale =
  *   max |n| / 127 over the row, q = n / scale rounded to the nearest integer,
- *   ties to even; a row with scale 0 has q = 0.  A row with an infinite or NaN n has
- *   q = 0 and scale NaN.                                                    */
+ *   ties to even, and at most 127 in magnitude (a scale below 2^-126 may be
+ *   too small by its own rounding); a row with scale 0 has q = 0.  A row with an
+ *   infinite or NaN n has q = 0 and scale NaN.                              */
 tp_status pack_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* w, int64_t rows,
                         int32_t d, float eps, int32_t precision, void* sum, void* y, int8_t* q, float* scale,
                         void* cuda_stream);

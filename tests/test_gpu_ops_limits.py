@@ -129,3 +129,28 @@ def test_gated_fp32_largest_values(tp, rows, where):  # noqa: F811
     got = [y, *tp.gated_backward(dy, x, wgu, wd, saved)]
     for name, v, (ref, tol) in zip(("y", "dx", "dw_gate_up", "dw_down"), got, _gated64(x, wgu, wd, "relu", dy, torch.float32)):
         _within(v, ref, tol, (name, rows))
+
+
+# ------------------------------------------------------------ norm into 8 bits
+@pytest.mark.parametrize("d", [200, 203, 1024, 5000])
+@pytest.mark.parametrize("size", [1.0, 1e-37, 3e-42, 1e30])
+def test_rms_norm_q8_rounds_the_quotient(tp, d, size):  # noqa: F811
+    """q is n / scale of the n and the scale that the same call gives, to the
+    nearest integer, ties to even, at most 127 (a scale below the normal
+    numbers is off by up to half of itself).  The quotient of two fp32 numbers is
+    no closer to a tie than 2^-26 of itself unless it is one, so 64 bits decide."""
+    rows = 4_000_000 // d
+    g = _gen(d)
+    x = torch.randn(rows, d, generator=g, device="cuda")
+    x[:2] = torch.randint(-253, 254, (2, d), generator=g, device="cuda") / 4     # n / scale at and beside k / 2
+    x[:2, 0] = 63.5
+    w = (torch.ones(d, device="cuda") if size == 1.0 else 1 + 0.3 * torch.randn(d, generator=g, device="cuda")) * size
+    y, q = torch.empty_like(x), torch.empty(rows, d, dtype=torch.int8, device="cuda")
+    scale = torch.empty(rows, device="cuda")
+    st = tp.load_library().pack_rms_norm(x.data_ptr(), d, None, 0, w.data_ptr(), rows, d, 1e-6, tp.FP32, None, y.data_ptr(),
+                                         q.data_ptr(), scale.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == tp.TP_OK
+    assert torch.equal(scale, (y.abs().amax(1).double() / 127).float())
+    ratio = torch.where(scale[:, None] > 0, y.double() / scale.double()[:, None], 0.0)
+    want = ratio.round().clamp(-127, 127)
+    assert int((q.double() != want).sum()) == 0, float((q.double() - ratio).abs().max())
