@@ -46,8 +46,9 @@ tp_status pack_ops_check(void* cuda_stream);
  * x: T [rows, d]; w_gate_up: T [2 f, d], Wg above Wu; w_down: T [d_out, f];
  * y: T [rows, d_out].  act: relu(v), silu(v) = v / (1 + exp(-v)), or gelu(v)
  * = v Phi(v).  1 <= d, f, d_out <= 131072; rows < 2^31 - 256; no matrix above 2^40 elements.
- * TP_BF16: fp32 sums; h is rounded to bf16 once.  TP_FP32: operands as three
- * bf16 parts each, whose products above 2^-24 are summed in fp32.          */
+ * TP_BF16: fp32 sums; h is rounded to bf16 once (act to 2^-16 of itself before
+ * that; below 2^-119 it may be 0).  TP_FP32: operands as three bf16 parts
+ * each, whose products above 2^-24 are summed in fp32.                      */
 typedef enum { TP_ACT_RELU = 0, TP_ACT_SILU = 1, TP_ACT_GELU = 2 } tp_act;
 
 /* Bytes of `saved` and of the workspaces of a forward and a backward call

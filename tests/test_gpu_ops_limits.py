@@ -154,3 +154,23 @@ def test_rms_norm_q8_rounds_the_quotient(tp, d, size):  # noqa: F811
     ratio = torch.where(scale[:, None] > 0, y.double() / scale.double()[:, None], 0.0)
     want = ratio.round().clamp(-127, 127)
     assert int((q.double() != want).sum()) == 0, float((q.double() - ratio).abs().max())
+
+
+# ------------------------------------------------------------ gated block
+@pytest.mark.parametrize("rows", [60, 2000])
+def test_gelu_tail(tp, rows):  # noqa: F811
+    """y = GELU(v) exactly once rounded (one pair, u = 1, Wd = 1), out to where
+    it leaves the normal numbers: half a step of bf16, and 2^-15 of the value for
+    an exponential of up to -84 in fp32.  Then its gradient at u, dh act(v)."""
+    v = torch.linspace(-12.9, 12.9, rows, device="cuda").to(torch.bfloat16)
+    x = torch.stack([v, torch.ones_like(v)], 1).contiguous()
+    wgu = torch.eye(2, device="cuda", dtype=torch.bfloat16)
+    wd = torch.ones(1, 1, device="cuda", dtype=torch.bfloat16)
+    y, saved = tp.gated_forward(x, wgu, wd, "gelu", save=True)
+    z = v.double()
+    ref = z * 0.5 * torch.special.erfc(-z / math.sqrt(2.0))
+    step = lambda r: torch.exp2(torch.floor(torch.log2(r.abs().clamp(min=1e-300))) - 8)  # noqa: E731
+    _within(y[:, 0], ref, step(ref) + 2.0 ** -15 * ref.abs(), "gelu")
+    dy = torch.full((rows, 1), 1.5, device="cuda", dtype=torch.bfloat16)
+    dx = tp.gated_backward(dy, x, wgu, wd, saved)[0]
+    _within(dx[:, 1], 1.5 * ref, step(1.5 * ref) + 2.0 ** -15 * 1.5 * ref.abs(), "du")
