@@ -174,3 +174,37 @@ def test_gelu_tail(tp, rows):  # noqa: F811
     dy = torch.full((rows, 1), 1.5, device="cuda", dtype=torch.bfloat16)
     dx = tp.gated_backward(dy, x, wgu, wd, saved)[0]
     _within(dx[:, 1], 1.5 * ref, step(1.5 * ref) + 2.0 ** -15 * 1.5 * ref.abs(), "du")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,at", [(1, 0), (24, 23), (1100, 0), (1100, 37), (1100, 1099)])
+def test_kept_values_have_24_bits(tp, act, rows, at):  # noqa: F811
+    """act(g) and u act'(g) are kept to 16 significant bits: one row has a
+    gradient, so that dW_gu = [dg du]^T x has one term and is rounded only where
+    dg and du are, half a step of bf16; 2^-15 more for what was kept and
+    for the activation.  Kept as bf16 they would be off by up to a step (that
+    more than one value in ten shows it is checked with the oracle).  By both kernels that
+    keep them: up to 1024 rows of odd widths and above."""
+    f = 999
+    g = _gen(rows + at)
+    x = torch.exp2(torch.randint(-1, 2, (rows, 1), generator=g, device="cuda").float()).to(torch.bfloat16)
+    wgu = (1.5 * torch.randn(2 * f, 1, generator=g, device="cuda")).to(torch.bfloat16)
+    wd = torch.randn(1, f, generator=g, device="cuda").to(torch.bfloat16)
+    dy = torch.zeros(rows, 1, device="cuda", dtype=torch.bfloat16)
+    dy[at] = 1.5
+    _, saved = tp.gated_forward(x, wgu, wd, act, save=True)
+    _, dw, _ = tp.gated_backward(dy, x, wgu, wd, saved)
+    xr = float(x[at, 0])
+    gate, up = wgu[:f, 0].double() * xr, wgu[f:, 0].double() * xr
+    a, d = _act64(act, gate)
+    dh = 1.5 * wd[0].double()
+    ref = torch.cat([dh * up * d, dh * a]) * xr
+    step = torch.exp2(torch.floor(torch.log2(ref.abs().clamp(min=1e-30))) - 8)
+    # act' is 1 + ...: a difference near its zero, good to 2^-20 of its terms
+    slack = 2.0 ** -15 * ref.abs() + torch.cat([(dh * up).abs() * 2.0 ** -18, torch.zeros_like(dh)]) * xr
+    _within(dw[:, 0], ref, step + slack, (act, rows))
+    coarse = torch.cat([dh.float() * (up * d).to(torch.bfloat16).float(), dh.float() * a.to(torch.bfloat16).float()])
+    coarse = coarse.to(torch.bfloat16).double() * xr
+    for half in (slice(0, f), slice(f, 2 * f)):
+        over = ((coarse - ref).abs() > step + slack)[half]
+        assert float(over.double().mean()) > 0.1, (act, half)
