@@ -36,9 +36,18 @@ extern "C" {
 #endif
 
 /* Waits for the stream; TP_ETIMEOUT if a bounded wait of a tensor-core
- * product has given up since the last check on this device (its outputs are
- * then undefined).                                                          */
+ * product has given up on this device since the calling thread's last check
+ * of this stream (the first one: ever), whichever stream the product ran on.
+ * That product's outputs are undefined.                                     */
 tp_status pack_ops_check(void* cuda_stream);
+
+/* Failure detection of the tensor-core products, for tests.  Every wait
+ * inside a product gives up after 2 or 4 s: the CTA lets its own copies and MMAs
+ * finish, frees its tensor memory and exits.  After this call the
+ * process's next launch that shares out a tile's reduction between clusters
+ * spoils one of its flags, so that the cluster that waits for it gives up
+ * after 4 s (site 47).                                                      */
+tp_status pack_debug_ops_withhold(void);
 
 /* ------------------------------------------------------------------------
  * Gated feed-forward block, with weights [out, in] and no biases:

@@ -41,7 +41,7 @@ SYMBOLS = ["pack_create", "pack_destroy", "pack_set_stream", "pack_train_step", 
            # include/tabpack_ops.h
            "pack_ops_check", "pack_gated_bytes", "pack_gated_forward", "pack_gated_backward", "pack_rms_norm",
            "pack_rms_norm_bytes", "pack_rms_norm_backward", "pack_product_q8_bytes", "pack_product_q8",
-           "pack_distill_bytes", "pack_distill"]
+           "pack_distill_bytes", "pack_distill", "pack_debug_ops_withhold"]
 
 
 class TabpackError(RuntimeError):
@@ -127,6 +127,7 @@ def load_library(path: str = LIB_PATH):
         "pack_debug_gemm_timeout": (st, [P, ctypes.c_double, i32]),
         "pack_debug_bias_path": (st, [P, i32]),
         "pack_ops_check": (st, [P]),
+        "pack_debug_ops_withhold": (st, []),
         "pack_gated_bytes": (st, [i64, i32, i32, i32, i32, P, P, P]),
         "pack_gated_forward": (st, [P, i64, P, P, i64, i32, i32, i32, i32, i32, P, P, P, i64, P]),
         "pack_gated_backward": (st, [P, i64, P, i64, P, P, P, i64, i32, i32, i32, i32, P, P, P, P, i64, P]),

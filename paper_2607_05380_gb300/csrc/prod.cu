@@ -66,7 +66,16 @@ constexpr int kTmemCols = 512, kAccCols = 256;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int kChainKb = 16;
 
-__device__ int g_prod_err;
+__device__ int g_prod_err, g_prod_taken;
+// Takes the error word, so that none that comes in meanwhile is erased.
+__global__ void k_take_err() { g_prod_taken = atomicExch(&g_prod_err, 0); }
+
+// What checks have taken, per device: how often, and the last site.
+struct Failures {
+  int count = 0, site = 0;
+};
+// pack_debug_ops_withhold: the next launch that shares out tiles spoils a flag.
+std::atomic<bool> g_withhold{false};
 
 struct Tail {
   uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2], done;
@@ -1062,6 +1071,8 @@ struct DeviceState {
 };
 DeviceState g_dev[kMaxDevices];
 std::mutex g_dev_mu;
+Failures g_failures[kMaxDevices];
+std::mutex g_failures_mu;
 
 // Once per device: shared-memory limits of the kernels, and how many CTA pairs fit.
 cudaError_t device_state(DeviceState* out) {
@@ -1272,6 +1283,20 @@ void prod_plan(ProdLaunch& l) {
 }
 
 namespace {
+// The flags of the first cluster that leaves sums for another one, once: set so low that its announcement does not
+// raise them to what the other waits for.
+cudaError_t withhold_one(const ProdArgs& a, int cta, int clusters, cudaStream_t st) {
+  for (int c = 0; c < clusters; ++c) {
+    Walk<1> walk(a, c, clusters);
+    Item it;
+    while (walk.next(it))
+      if (it.publish)
+        return g_withhold.exchange(false) ? cudaMemsetAsync(a.flags + c * cta * kEpiWarps, 0x80, cta * kEpiWarps * 4, st)
+                                          : cudaSuccess;
+  }
+  return cudaSuccess;
+}
+
 // Runs a planned launch; slots: at least slot_bytes, flags: flag_bytes of zeros (256-byte aligned); zero: n_zero
 // words that it clears.
 cudaError_t prod_run(ProdLaunch& l, void* slots, int* flags, int* zero, int n_zero, cudaStream_t st, const char** what) {
@@ -1314,6 +1339,10 @@ cudaError_t prod_run(ProdLaunch& l, void* slots, int* flags, int* zero, int n_ze
       return cudaErrorInvalidValue;
     a.n_maps = kMapOut + 1;
   }
+  *what = "spoiling a flag";
+  if (l.whole < l.n_tiles && g_withhold.load(std::memory_order_relaxed) &&
+      (e = withhold_one(a, l.cta, clusters, st)) != cudaSuccess)
+    return e;
   *what = "product launch";
   return with_kernel(l.cta, l.epi, l.act, l.f32, [&](auto c, auto k, auto a_, auto t) {
     return launch<c.value, k.value, a_.value, t.value>(a, clusters, st);
@@ -1374,19 +1403,50 @@ cudaError_t stage_run(StageLaunch& s, cudaStream_t st) {
 using namespace tp;
 
 extern "C" tp_status pack_ops_check(void* cuda_stream) {
-  int v = 0;
+  // what this thread's last check of a stream saw, once something has given up; of more streams than that the
+  // oldest entry goes, and its stream is told again
+  struct Seen {
+    int dev, count;
+    void* stream;
+  };
+  constexpr int kSeen = 64;
+  thread_local Seen seen[kSeen];
+  thread_local int n_seen = 0;
+  int v = 0, dev = 0;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_prod_err, sizeof v, 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e == cudaSuccess && v != 0) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_prod_err, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  auto read = [&](const int& from) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, from, sizeof v, 0, cudaMemcpyDeviceToHost, st);
+    return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
+  };
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= kMaxDevices)) e = cudaErrorInvalidDevice;
+  if (e == cudaSuccess) e = read(g_prod_err);
+  Failures f;
+  if (e == cudaSuccess) {
+    // whoever takes the word counts it before another check looks at the count
+    std::lock_guard<std::mutex> lock(g_failures_mu);
+    if (v != 0) {
+      k_take_err<<<1, 1, 0, st>>>();
+      e = cudaGetLastError();
+      if (e == cudaSuccess) e = read(g_prod_taken);
+      if (e == cudaSuccess && v != 0) ++g_failures[dev].count, g_failures[dev].site = v;
+    }
+    f = g_failures[dev];
   }
   if (e != cudaSuccess) {
     cudaGetLastError();   // reported here
     return ops_fail(TP_ECUDA, "pack_ops_check: %s", cudaGetErrorString(e));
   }
-  if (v != 0) return ops_fail(TP_ETIMEOUT, "a wait of a tensor-core product gave up (site %d)", v);
+  if (f.count == 0) return TP_OK;
+  int k = 0;
+  while (k < std::min(n_seen, kSeen) && !(seen[k].dev == dev && seen[k].stream == cuda_stream)) ++k;
+  if (k == std::min(n_seen, kSeen)) k = n_seen++ % kSeen, seen[k] = Seen{dev, 0, cuda_stream};
+  if (f.count == seen[k].count) return TP_OK;
+  seen[k].count = f.count;
+  return ops_fail(TP_ETIMEOUT, "a wait of a tensor-core product gave up (site %d)", f.site);
+}
+
+extern "C" tp_status pack_debug_ops_withhold(void) {
+  g_withhold.store(true);
   return TP_OK;
 }

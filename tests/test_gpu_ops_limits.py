@@ -208,3 +208,30 @@ def test_kept_values_have_24_bits(tp, act, rows, at):  # noqa: F811
     for half in (slice(0, f), slice(f, 2 * f)):
         over = ((coarse - ref).abs() > step + slack)[half]
         assert float(over.double().mean()) > 0.1, (act, half)
+
+
+# ----------------------------------------------------------------- give-up path
+def test_wait_gives_up(tp):  # noqa: F811
+    """A cluster's sums that are never announced: the clusters that wait for
+    them give up after the limit, the launch ends, every stream's check says
+    so once, and the next calls are right."""
+    L = tp.load_library()
+    # dW's few tiles of a long reduction, whose K blocks are shared out
+    x, wgu, wd, dy = _gated_case(torch.bfloat16, 20011, 256, 256, 256, 3)
+    y, saved = tp.gated_forward(x, wgu, wd, save=True)
+    ref = tp.gated_backward(dy, x, wgu, wd, saved)
+    other = torch.cuda.Stream()
+    tp.ops_check()
+    tp.ops_check(other)
+    assert L.pack_debug_ops_withhold() == tp.TP_OK
+    tp.gated_backward(dy, x, wgu, wd, saved)
+    torch.cuda.synchronize()
+    for stream in (other, None):               # neither takes the other's report
+        with pytest.raises(tp.TabpackError) as ei:
+            tp.ops_check(stream)
+        assert ei.value.status == tp.TP_ETIMEOUT and "site 47" in str(ei.value)
+        tp.ops_check(stream)
+    for a, b in zip(tp.gated_backward(dy, x, wgu, wd, saved), ref):
+        assert torch.equal(a, b)
+    tp.ops_check()
+    tp.ops_check(other)
