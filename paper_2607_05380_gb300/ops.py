@@ -55,18 +55,10 @@ def _too_wide(name, n):
     return ValueError(f"{name}: a width of {n} is not below 2^31")
 
 
-def _device_of(t, name):
-    """The device that a call works on: that of its first tensor, which has to
-    be the current one when the call is made (_stream)."""
-    d = t.get_device()
-    if d < 0:
-        raise ValueError(f"{name}: expected a CUDA tensor")
-    return d
-
-
 def _elsewhere(t, name, device):
-    return ValueError(f"{name}: expected a CUDA tensor" if t.get_device() < 0 else
-                      f"{name}: on device {t.get_device()}, expected {device}")
+    """A call works on the device of its first tensor, which has to be the
+    current one (_stream)."""
+    return ValueError(f"{name}: expected a CUDA tensor on the call's device {device}, got device {t.get_device()}")
 
 
 def _mat(t, name, device, dtype, rows=None, cols=None):
@@ -113,8 +105,8 @@ _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 def _stream(device):
     """The current stream's pointer; the call's device has to be the current one."""
-    if device != _device():
-        raise ValueError("the tensors are not on the current device")
+    if device < 0 or device != _device():
+        raise ValueError("expected CUDA tensors on the current device")
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
@@ -159,7 +151,7 @@ def _gated_bytes(rows, d, f, d_out, prec):
 
 
 def _gated_shapes(x, w_gate_up, w_down):
-    prec, dtype, on = _precision(x, "x"), x.dtype, _device_of(x, "x")
+    prec, dtype, on = _precision(x, "x"), x.dtype, x.get_device()
     xp, ldx = _mat(x, "x", on, dtype)
     rows, d = x.shape
     gate, down = w_gate_up.shape, w_down.shape
@@ -215,7 +207,7 @@ def gated_backward(dy, x, w_gate_up, w_down, saved, stream=None):
 
 
 def _norm(x, weight, residual, eps, q8):
-    prec, dtype, on = _precision(x, "x"), x.dtype, _device_of(x, "x")
+    prec, dtype, on = _precision(x, "x"), x.dtype, x.get_device()
     xp, ldx = _mat(x, "x", on, dtype)
     rows, d = x.shape
     wp = _flat(weight, "weight", on, torch.float32, d)
@@ -271,7 +263,7 @@ def rms_norm_backward(dy, s, weight, dsum=None, eps=1e-6, stream=None):
     dsum: the gradient that reaches s from elsewhere, added to dx."""
     if stream is not None:
         return _on(stream, rms_norm_backward, (dy, s, weight, dsum), eps)
-    prec, dtype, on = _precision(s, "s"), s.dtype, _device_of(s, "s")
+    prec, dtype, on = _precision(s, "s"), s.dtype, s.get_device()
     sp, lds = _mat(s, "s", on, dtype)
     rows, d = s.shape
     gp, ldg = _mat(dy, "dy", on, dtype, rows, d)
@@ -306,7 +298,7 @@ def product_q8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=Non
     prec = _PRECISION.get(dtype)
     if prec is None:
         raise ValueError(f"dtype: expected bfloat16 or float32, got {dtype}")
-    on = _device_of(q, "q")
+    on = q.get_device()
     qp, ldq = _mat(q, "q", on, torch.int8)
     rows, k = q.shape
     if w.dim() != 2:
@@ -347,7 +339,7 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     if stream is not None:
         return _on(stream, distill, (z, ids, top, labels), tau, alpha, grad)
     prec = _precision(z, "z")
-    shape, on = z.shape, _device_of(z, "z")
+    shape, on = z.shape, z.get_device()
     if len(shape) not in (2, 3) or not z.is_contiguous():
         raise ValueError("z must be a contiguous CUDA tensor [m, rows, n] or [rows, n]")
     m, rows, n = (1, *shape) if len(shape) == 2 else shape
