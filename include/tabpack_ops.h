@@ -2,7 +2,7 @@
  * tabpack_ops.h -- operators of a student network, beside the packs of
  * tabpack.h: one residual network of gated blocks that a selected ensemble
  * (pack_select_greedy, pack_online_predict) is distilled into and that then
- * answers alone, its layers' weights in 8 bits where that is wanted.  (The
+ * answers alone, its head's weights in 8 bits where that is wanted.  (The
  * paper has no counterpart.)
  *
  * Conventions, beside those of tabpack.h:
@@ -85,7 +85,9 @@ tp_status pack_gated_backward(const void* dy, int64_t lddy, const void* x, int64
  *   s = x + residual (x without one),  n = s / sqrt(mean(s^2) + eps) w
  * x, residual: T [rows, d] (residual may be NULL), w: float32 [d], d in
  * 1..16384, eps >= 0.  sum: T [rows, d], s rounded once (may be NULL); the
- * norm is taken of s before that rounding.  Outputs, either or both:
+ * norm is taken of s before that rounding.  The sum of a row's squares is an
+ * fp32 value: where it overflows (|s| from about 10^19 / sqrt(d) on) n is 0,
+ * and where it and eps are 0 NaN.  Outputs, either or both:
  *   y: T [rows, d], n rounded once (may be NULL);
  *   q, scale: int8 [rows, d] and float32 [rows] (may both be NULL): scale =
  *   max |n| / 127 over the row, q = n / scale rounded to the nearest integer,

@@ -20,8 +20,10 @@
 // the result does not depend on any order.
 //
 // Bound by HBM (z read, dz written) for many classes (2048 rows of 50021, bf16:
-// 81 us, 0.75 of the measured copy rate, issue slots 60 % taken), by latency
-// for few (64 students, 1024 rows of 10: 9 us).
+// 80 us, 0.76 of the measured copy rate, issue slots 60 % taken; fp32 182 us,
+// 0.66; a tau without a shared exponential, bf16: 89 us), by latency for few (64
+// students, 1024 rows of 10: 8.4 us) and by its loads of single elements
+// between (80000 rows of 512, bf16: 85 us, 0.29).
 //   up to 32 classes    of many rows, few entries: a thread takes a row, which blocks of 128
 //                       rows stage in shared memory: no exchanges between lanes
 //   up to 1024          8 to 32 lanes hold a row in registers
@@ -813,12 +815,16 @@ void wide(const Args<T>& a, cudaStream_t st) {
 template <typename T>
 cudaError_t rows(const Args<T>& a, cudaStream_t st) {
   // Launches of many rows want few lanes a row, launches of few rows short
-  // chains a lane (us; the other way in brackets): 10 classes, 80000 rows, 8
-  // entries 22 (eight lanes 30), 16 entries of 32 classes 51 (34), 4096 rows 6.2
-  // (a thread 8.7); 64 classes, 80000 rows 33 (sixteen lanes 45); 128, 80000
-  // rows 48 (72); 256, 80000 rows 58 (79), 128 rows 5.7 (6.1); 512, 80000 rows
-  // 94 (117), 128 rows 6.2 (7.0); 1000, 16384 rows 29 (a block a row 38), 128
-  // rows 5.8 (6.9).
+  // chains a lane (a whole call, us, bf16 / fp32; the other way in brackets):
+  //   10 classes, 80000 rows: 8 entries, a thread 21.7 / 21.1 (eight lanes 24.5 / 24.0), 2 entries 15.1 / 14.9
+  //   (24.7 / 24.2); 32 classes, 16 entries: eight lanes 27.7 / 27.2 (a thread 66.9 / 66.5); 10 classes, 8 entries,
+  //   4096 rows: eight lanes 5.3 / 5.1 (a thread 8.6 / 8.4), 24000 rows 9.6 / 9.4 (10.8 / 10.7)
+  //   64 classes, 80000 rows: eight lanes 26.7 / 26.0 (sixteen 38.6 / 37.8)
+  //   128, 80000 rows: sixteen 41.8 / 41.5 (thirty-two 64.7 / 64.2; eight would take 32.5 / 31.5), 4096 rows 6.5 / 6.5
+  //   (8.2 / 8.1)
+  //   256, 80000 rows: sixteen 53.0 / 55.4 (thirty-two 73.2 / 76.0), 128 rows: thirty-two 5.2 / 4.9 (5.5 / 5.1)
+  //   512, 80000 rows: sixteen 85.2 / 73.6 (thirty-two 108 / 96.7), 128 rows: thirty-two 5.5 / 5.1 (6.5 / 5.7)
+  //   1000, 16384 rows: a warp 28.5 / 32.3 (a block 36.9 / 38.8), 128 rows: a block 4.8 / 5.1 (6.6 / 5.9)
   const bool few = a.all <= 4096;
   if (a.n <= kSmallN && a.k <= 8 && a.all > 24576) {
     const uint32_t div = ((1u << 20) + a.n - 1) / a.n;   // i / n = i div >> 20 for i < 128 * 32
@@ -838,9 +844,11 @@ cudaError_t rows(const Args<T>& a, cudaStream_t st) {
     else group<T, 16, 32>(a, st);
   } else if (a.n <= 1024 && a.all > 1024) {
     group<T, 32, 32>(a, st);
-  } else if (a.n * (int64_t)sizeof(T) <= 16384) {   // two warps a row: 16384 rows of 2000 bf16, 48 us (four 63)
+  } else if (a.n * (int64_t)sizeof(T) <= 16384) {
+    // two warps a row: 16384 rows of 2000, bf16 48 us (four 68), fp32 57 (71); of 4000, 65 (82), 95 (101)
     wide<T, 2>(a, st);
-  } else if (a.n * (int64_t)sizeof(T) <= 32768) {   // four: of 16000, 181 us (two 229, fifteen 270)
+  } else if (a.n * (int64_t)sizeof(T) <= 32768) {
+    // four: 16384 rows of 16000 bf16, 182 us (two 230, fifteen 264); fp32, by fifteen, 349 us (four 433)
     wide<T, 4>(a, st);
   } else {
     wide<T, 15>(a, st);

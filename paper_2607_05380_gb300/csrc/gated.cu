@@ -16,7 +16,8 @@
 //
 // Forward and backward of 2048 rows, d = d_out = 1024, f = 2048, bf16: 85 us,
 // of which the operations at the measured tensor rate take 40; of 16384 rows,
-// f = 4096: 788 us, 1.57 PFLOP/s.
+// f = 4096: 831 us, 1.49 PFLOP/s (power cap; 788 at best); fp32, of 2000 rows,
+// d = d_out = 1024, f = 2048: 392 us, of which the six products take 237.
 #include <algorithm>
 
 #include "prod.cuh"

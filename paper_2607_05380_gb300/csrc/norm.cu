@@ -6,15 +6,20 @@
 //   dx = r (t - s r^2 mean(t s)) + dsum with t = dy w;  dw = sum_rows dy s r
 //
 // One pass: a row's elements stay in registers between the sums and the
-// outputs.  Bound by HBM (8192 rows of 2048, bf16, forward: 22 us, 0.90 of the
-// measured copy rate) and, in the backward pass, by its two sums per row,
-// which the next row's loads do not quite cover (23.6 us, 0.63).
+// outputs.  Bound by HBM (8192 rows of 2048, forward with a residual: bf16 22 us,
+// 0.91 of the measured copy rate, fp32 40 us, 0.98) and, in the backward pass,
+// by its two sums per row, which the next row's loads do not quite cover (bf16
+// without dsum 23.6 us, 0.63, with it 29 us, 0.68; fp32, which asks for no
+// row ahead, 44 and 50 us, 0.67 and 0.80).  Above 8192 columns the backward pass
+// has no registers left (1024 rows of 16384, with dsum: bf16 45 us, 0.44; fp32 75
+// us, 0.53).
 //
 // A row takes one to sixteen warps, so that a lane holds at most 16 of its
-// elements, 32 above 8192 (forward / backward, us, when adding up dw took 2.7
-// more: 8192 rows of 2048, two warps 24 / 31, four 22 / 26.5, eight 22 / 31;
-// 16384 of 1024, one warp 23.5 / 40, two 21 / 25, four 25 / 30).  dw is summed per block over the rows it takes (at
-// most kBwdBlocks blocks), then over the blocks, both in a fixed order.
+// elements, 32 above 8192 (forward / backward without dsum, bf16, us, when adding
+// up dw took 2.7 more: 8192 rows of 2048, two warps 24 / 31, four 22 / 26.5,
+// eight 22 / 31; 16384 of 1024, one warp 23.5 / 40, two 21 / 25, four 25 / 30).
+// dw is summed per block over the rows it takes (at most kBwdBlocks blocks), then
+// over the blocks, both in a fixed order.
 #include <algorithm>
 
 #include "prod.cuh"

@@ -10,7 +10,7 @@
 //
 // Bound by the tensor cores where all three sizes are large: a CTA pair's
 // 256 x 256 tile streams 32 KB per SM and K block (a gated block of 1024 and
-// 4096, 20011 rows, forward, 284 us: 1.77 PFLOP/s, 0.93 of cuBLAS's measured
+// 4096, 20011 rows, forward, 275 us: 1.83 PFLOP/s, 0.96 of cuBLAS's measured
 // 8192^3 burst); by a launch's fill, last epilogues and uneven rounds, 4 to 7
 // us, where they are not (2048 rows, 1024 and 2048, 33 us: 0.78 PFLOP/s).
 //

@@ -20,7 +20,11 @@ namespace tp {
 //   1024 -> 1000: 256 rows 5.0 / 11.0, 768 rows 12.8 / 11.5
 // Loads of four bytes (gated 1022, 2046: 64 rows 19.5 / 22.5, 128 rows 26.1 /
 // 23.7) or of an element (gated 389, 1001: 32 rows 11.9 / 14.8, 128 rows 17.0 /
-// 15.3; 8-bit 2001 -> 1000: 8 rows 9.5 / 12.1, 32 rows 21.9 / 12.0) pay for less.
+// 15.3; 8-bit 2001 -> 1000: 8 rows 8.4 / 12.1, 16 rows 12.0, 28 rows 20.6, 32 rows
+// 21.9 / 14.0) pay for less; the limit for elements lets more rows through than
+// those figures would (up to 29 of 2001 -> 1000).  Only the weights' pitch counts
+// here: rows of x at an odd pitch or address make k_rows load both by elements
+// (gated 1024, 2048: 64 rows 25 instead of 10.5).
 bool rows_take(int64_t rows, int64_t weights, int64_t pitch, bool q8);
 // The same of a 32-bit block, in fp32 multiply-adds (rows / tcgen05):
 //   d = d_out = 512, f = 2048: 8 rows 15.8 / 42, 64 rows 32 / 40

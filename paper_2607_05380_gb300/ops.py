@@ -9,6 +9,11 @@ workspaces are also allocated, and is not waited for.  With ``stream`` the
 inputs' memory is kept until that stream has read them, so that the caller may
 let go of them at once; that they are written before it reads them, and
 outputs before another stream does, is the caller's to order.
+
+Nothing here takes part in autograd: outputs have no graph, whether or not an
+input requires a gradient.  Gradients come from the ``_backward`` calls and from
+``distill``, which returns its own; a caller that wants them in a graph wraps the
+pairs in a ``torch.autograd.Function``.
 """
 from __future__ import annotations
 
@@ -167,7 +172,8 @@ def _gated_shapes(x, w_gate_up, w_down):
 
 def gated_forward(x, w_gate_up, w_down, act="silu", save=False, stream=None):
     """y = (act(x Wg^T) * (x Wu^T)) Wd^T with w_gate_up = [Wg; Wu] [2 f, d] and
-    w_down [d_out, f].  save=True returns (y, saved) for gated_backward."""
+    w_down [d_out, f].  save=True returns (y, saved) for gated_backward, the only
+    way to its gradients (no autograd graph)."""
     if stream is not None:
         return _on(stream, gated_forward, (x, w_gate_up, w_down), act, save)
     code = ACTIVATIONS.get(act)
@@ -235,7 +241,8 @@ def _norm(x, weight, residual, eps, q8):
 
 def rms_norm(x, weight, residual=None, eps=1e-6, stream=None):
     """(y, s): the RMS norm y of s = x + residual (x itself without one) times
-    weight [d] (float32), and s for the next residual and rms_norm_backward."""
+    weight [d] (float32), and s for the next residual and rms_norm_backward, the
+    only way to its gradients (no autograd graph)."""
     if stream is not None:
         return _on(stream, rms_norm, (x, weight, residual), eps)
     return _norm(x, weight, residual, eps, False)
@@ -335,7 +342,8 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     of m students from the teacher's top entries, plus 1 - alpha times the
     cross-entropy with labels, mean over the rows.  z [m, rows, n] (or
     [rows, n] for one student); ids int32 and top float32 [rows, k]: classes
-    (-1: none) and logits of the teacher's entries; labels int32 [rows]."""
+    (-1: none) and logits of the teacher's entries; labels int32 [rows].  dz is the
+    gradient of loss[i] at z[i] (no autograd graph)."""
     if stream is not None:
         return _on(stream, distill, (z, ids, top, labels), tau, alpha, grad)
     prec = _precision(z, "z")
@@ -364,7 +372,8 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
 
 
 def ops_check(stream=None):
-    """Waits for the stream; raises if a bounded wait of a product gave up."""
+    """Waits for the stream; raises if a bounded wait of a product has given up on
+    this device since the calling thread's last check of this stream."""
     status = _lib().pack_ops_check((stream or torch.cuda.current_stream()).cuda_stream)
     if status:
         _fail(status)
