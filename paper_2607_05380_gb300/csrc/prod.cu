@@ -79,7 +79,7 @@ std::atomic<bool> g_withhold{false};
 
 struct Tail {
   uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2], done;
-  uint64_t kept[kEpiWarps][4];   // a warp's two slots: filled, read
+  uint64_t kept[kEpiWarps][2];   // a warp's two slots: filled
   uint32_t tmem_base;
   int abort;
 };
@@ -457,7 +457,7 @@ __device__ __forceinline__ void put_24(const float (&v)[32], __nv_bfloat16* hi, 
 struct Kept {
   uint8_t* in;                // [2][32 rows][64 B], [2][32 rows][32 B]; first u act'(g), then act(g)
   uint8_t* out;               // [2][32 rows][64 B]: dg, du
-  uint64_t* bar;                   // [2] filled, [2] read
+  uint64_t* bar;                   // [2] filled
   uint32_t phase = 0, asked = 0;   // a bit a slot
   __device__ __forceinline__ void ask(const ProdArgs& g, int h, int c0, int r0) {
     const uint32_t b = smem_u32(bar + h);
@@ -470,15 +470,6 @@ struct Kept {
     const bool ok = __all_sync(0xffffffffu, mbar_wait(bar + h, phase >> h & 1, abort_flag, err, kWaitNs, 48));
     if (ok) phase ^= 1u << h, asked &= ~(1u << h);
     return ok;
-  }
-  // The slot has been read: the copy that fills it again must not overtake loads that have been issued but not
-  // served, which an arrival, served after them, shows.  (A barrier of the warp alone does not wait for them: one
-  // pass in 10^4 of 2048 rows, 512 -> 2048, took a few rows' values from the next chunk; of 750000 with it, none.)
-  __device__ __forceinline__ bool release(int h, int lane, volatile int* abort_flag, int* err) {
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar + 2 + h);
-    // (the phase has just gone on to the next filling)
-    return __all_sync(0xffffffffu, mbar_wait(bar + 2 + h, (phase >> h & 1) ^ 1, abort_flag, err, kWaitNs, 50));
   }
   // f = what has come in times acc (what the lowest byte holds is below their rounding)
   __device__ __forceinline__ void times(int h, int lane, float (&f)[32], const float (&acc)[32]) const {
@@ -501,6 +492,11 @@ struct Kept {
       }
     }
   }
+  // f on its way out.  After this the slot that f was made from may be filled again: the copy that does so must not
+  // overtake loads that have been issued but not served, and here every lane has stored what its loads came back
+  // with, before the warp's barrier.  (Neither that barrier alone nor an mbarrier's arrival after the loads waits
+  // for them: 4043 x 477 -> 2354, after a forward pass, had 16-byte pieces of the next chunk in one pass of
+  // seven.)
   __device__ __forceinline__ void put(const ProdArgs& g, int h, int lane, const float (&f)[32], int c0, int r0) {
     uint32_t pk[16];
     pack32(f, pk);
@@ -615,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
     }
     mbar_init(&tl->done, 1);
     if constexpr (kStaged)
-      for (int w = 0; w < 4 * kEpiWarps; ++w) mbar_init(&tl->kept[0][w], 1);
+      for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(&tl->kept[0][w], 1);
     tl->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -831,10 +827,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
             ok = ok && kept.wait(h, abort_flag, err);
             if (!ok) break;
             kept.times(h, lane, a2, a);
-            ok = kept.release(h, lane, abort_flag, err);
-            if (!ok) break;
-            if (more) kept.ask(g, h, c0 + 64, r0);
             kept.put(g, h, lane, a2, c0, r0);
+            if (more) kept.ask(g, h, c0 + 64, r0);   // (after put)
           }
           if (!ok) break;
         } else {

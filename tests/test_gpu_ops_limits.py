@@ -235,3 +235,23 @@ def test_wait_gives_up(tp):  # noqa: F811
         assert torch.equal(a, b)
     tp.ops_check()
     tp.ops_check(other)
+
+
+@pytest.mark.parametrize("rows,d,f,o", [(4043, 5, 2354, 477), (2048, 64, 2048, 512), (4000, 40, 1000, 300)])
+def test_gated_backward_between_forwards(tp, rows, d, f, o):  # noqa: F811
+    """The same bits in 1500 backward passes, each right after two forward ones
+    (one pass in seven of the first shape, otherwise, had pieces of what comes
+    into shared memory for the next chunk)."""
+    x, wgu, wd, dy = _gated_case(torch.bfloat16, rows, d, f, o, 5)
+    _, saved = tp.gated_forward(x, wgu, wd, "gelu", save=True)
+    ref = tp.gated_backward(dy, x, wgu, wd, saved)
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(1500):
+        hold = tp.gated_forward(x, wgu, wd, "gelu", save=True)
+        tp.gated_forward(x, wgu, wd, "gelu")
+        got = tp.gated_backward(dy, x, wgu, wd, saved)
+        for a, b in zip(got, ref):
+            bad += (a != b).any()
+    del hold
+    assert int(bad) == 0
+    tp.ops_check()
