@@ -859,7 +859,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (kCta == 2) cluster_sync();
+  if constexpr (kCta == 2) {
+    // the leader's last commit arrives in both CTAs: its arrival here, too, is over before this memory is another's
+    if (warp == 1 && !leader) {
+      int dummy = 0;
+      mbar_wait(&tl->done, 0, &dummy, err, 4 * kWaitNs, 45);
+    }
+    cluster_sync();
+  }
   if (warp == 1) {
     if constexpr (kCta == 2)
       asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
