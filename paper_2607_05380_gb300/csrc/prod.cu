@@ -635,6 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod(const __grid_constant__ Pr
   if (warp == 0 && lane < kProdMaps && lane < g.n_maps)
     asm volatile("prefetch.tensormap [%0];" ::"l"(&g.map[lane]) : "memory");
   pdl_wait();                      // the set-up above overlaps the previous kernel
+  fence_proxy_async_global();      // what it wrote by plain stores is read by TMA
   const uint32_t tmem = uniform(tl->tmem_base);
   volatile int* abort_flag = &tl->abort;
   int* err = &g_prod_err;
