@@ -148,6 +148,66 @@ tp_status pack_distill(const void* z, int64_t m, int64_t rows, int32_t n, const 
                        int32_t k, const int32_t* labels, float tau, float alpha, int32_t precision, float* loss,
                        void* dz, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------
+ * Embedding lookup with scaling, for category columns: y[i] = scale
+ * table[ids[i]], 0 for an id outside 0..vocab-1 (such as -1).
+ *   ids: n integers of id_bytes (4 or 8); table: [vocab, d], float32 or bf16
+ *   by table_precision, rows ldt elements apart; y: T [n, d], T by precision.
+ *   0 <= n < 2^31 - 4095, 1 <= vocab < 2^31 - 4095, 1 <= d <= 131072, no matrix
+ *   above 2^40 elements.                                                    */
+tp_status pack_embed(const void* ids, int32_t id_bytes, int64_t n, const void* table, int64_t ldt, int32_t vocab, int32_t d,
+                     float scale, int32_t table_precision, int32_t precision, void* y, void* cuda_stream);
+
+/* Its gradient: dtable[v] = scale times the sum of dy[i] over the i with
+ * ids[i] = v, all of dtable written (0 where there is none).  dy: T [n, d] by
+ * precision; dtable: [vocab, d], contiguous, by table_precision.  fp32 sums
+ * of sorted tokens, joined in a fixed order; rounded once.                  */
+tp_status pack_embed_bytes(int64_t n, int32_t vocab, int32_t d, int64_t* backward);
+tp_status pack_embed_backward(const void* dy, int64_t lddy, const void* ids, int32_t id_bytes, int64_t n, int32_t vocab,
+                              int32_t d, float scale, int32_t precision, int32_t table_precision, void* dtable,
+                              void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Dropout whose mask is a function of its arguments and never stored:
+ *   y(r, c) = x(r, c) / (1 - p) where kept, 0 where dropped, + residual(r, c)
+ * Kept iff word c & 3 of Philox4x32-10 at counter (r, c >> 2, step, site) under
+ * key (seed low, seed high) is >= floor(p 2^32): the rule of pack_train_step's
+ * masks, whose site is (member << 4) | layer.  Its gradient at x is the same
+ * call of dy without a residual; at residual it is dy.
+ *   x, residual (may be NULL), y: T [rows, d]; 0 <= p < 1; 1 <= d <= 131072;
+ *   rows < 2^31 - 255, no matrix above 2^40 elements.  What x holds where it is
+ *   dropped does not matter (NaN and infinities included).  Rounded once;
+ *   1 / (1 - p) is an fp32 value.                                           */
+tp_status pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int32_t d, float p,
+                       uint64_t seed, uint32_t step, uint32_t site, int32_t precision, void* y, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm of a residual stream:
+ *   s = x + residual, rounded to T (x without one),
+ *   y = (s - m) r w + b,  m = mean(s),  r = 1 / sqrt(mean((s - m)^2) + eps)
+ * x, residual: T [rows, d] (residual may be NULL), w, b: float32 [d] (b may
+ * be NULL), d in 1..16384, eps >= 0.  Outputs, any of them NULL: sum: T
+ * [rows, d], s; y: T [rows, d], rounded once; stats: float32 [rows, 2], 8-byte
+ * aligned, m and r of every row.  A row's sum and its sum of squares are fp32
+ * values: where the squares overflow r is 0, and where they and eps are 0 it
+ * is infinite and y NaN.                                                    */
+tp_status pack_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* w, const float* b,
+                          int64_t rows, int32_t d, float eps, int32_t precision, void* sum, void* y, float* stats,
+                          void* cuda_stream);
+
+/* Its gradients: with h = (s - m) r and t = dy w, dx = r (t - mean(t) - h
+ * mean(t h)) + dsum, which is the gradient of x and of residual alike; dw and
+ * db = the sums over the rows of dy h and of dy.
+ *   dy, s: T [rows, d], s as it was stored; stats: of the forward call; dsum:
+ *   T [rows, d], the gradient that reaches the stored sum from elsewhere (may
+ *   be NULL); dx: T [rows, d]; dw, db: float32 [d] (either may be NULL; with
+ *   both, no workspace is needed).                                          */
+tp_status pack_layer_norm_bytes(int64_t rows, int32_t d, int64_t* backward);
+tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* s, int64_t lds, const float* w,
+                                   const float* stats, const void* dsum, int64_t lddsum, int64_t rows, int32_t d,
+                                   int32_t precision, void* dx, float* dw, float* db, void* workspace,
+                                   int64_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,7 +41,9 @@ SYMBOLS = ["pack_create", "pack_destroy", "pack_set_stream", "pack_train_step", 
            # include/tabpack_ops.h
            "pack_ops_check", "pack_gated_bytes", "pack_gated_forward", "pack_gated_backward", "pack_rms_norm",
            "pack_rms_norm_bytes", "pack_rms_norm_backward", "pack_product_q8_bytes", "pack_product_q8",
-           "pack_distill_bytes", "pack_distill", "pack_debug_ops_withhold"]
+           "pack_distill_bytes", "pack_distill", "pack_debug_ops_withhold", "pack_embed", "pack_embed_bytes",
+           "pack_embed_backward", "pack_dropout", "pack_layer_norm", "pack_layer_norm_bytes",
+           "pack_layer_norm_backward"]
 
 
 class TabpackError(RuntimeError):
@@ -76,6 +78,7 @@ def load_library(path: str = LIB_PATH):
         raise ImportError(f"libtabpack.so not built at {path}: run paper_2607_05380_gb300.build.build()")
     L = ctypes.CDLL(path)
     P, i32, i64, u32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float
+    u64 = ctypes.c_uint64
     st = ctypes.c_int
     sig = {
         "pack_create": (st, [ctypes.POINTER(Config), P, P, P, P, P, P, ctypes.POINTER(P)]),
@@ -138,6 +141,13 @@ def load_library(path: str = LIB_PATH):
         "pack_product_q8": (st, [P, i64, P, P, P, P, i64, i32, i32, i32, P, P, i64, P]),
         "pack_distill_bytes": (st, [i64, i64, P]),
         "pack_distill": (st, [P, i64, i64, i32, P, P, i32, P, f32, f32, i32, P, P, P, i64, P]),
+        "pack_embed": (st, [P, i32, i64, P, i64, i32, i32, f32, i32, i32, P, P]),
+        "pack_embed_bytes": (st, [i64, i32, i32, P]),
+        "pack_embed_backward": (st, [P, i64, P, i32, i64, i32, i32, f32, i32, i32, P, P, i64, P]),
+        "pack_dropout": (st, [P, i64, P, i64, i64, i32, f32, u64, u32, u32, i32, P, P]),
+        "pack_layer_norm": (st, [P, i64, P, i64, P, P, i64, i32, f32, i32, P, P, P, P]),
+        "pack_layer_norm_bytes": (st, [i64, i32, P]),
+        "pack_layer_norm_backward": (st, [P, i64, P, i64, P, P, P, i64, i64, i32, i32, P, P, P, P, i64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -515,7 +525,8 @@ class OnlineEnsemble:
 
 # The student operators' binding (ops.py) needs torch, which nothing else here
 # loads before a call does: it is loaded when one of its names is asked for.
-_OPS = ("ACTIVATIONS", "distill", "gated_backward", "gated_forward", "ops_check", "product_q8", "rms_norm",
+_OPS = ("ACTIVATIONS", "distill", "dropout", "dropout_backward", "embed", "embed_backward", "gated_backward",
+        "gated_forward", "layer_norm", "layer_norm_backward", "ops_check", "product_q8", "rms_norm",
         "rms_norm_backward", "rms_norm_q8")
 
 

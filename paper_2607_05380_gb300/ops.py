@@ -1,5 +1,6 @@
 """Python binding of the student operators (``include/tabpack_ops.h``): gated
-feed-forward block, RMS norm, 8-bit product, distillation loss.
+feed-forward block, RMS norm and layer norm, 8-bit product, distillation loss,
+embedding lookup, dropout.
 
 Argument checks and marshalling only.  Tensors are CUDA tensors, bf16 or
 float32; rows may be spaced (any stride of the first dimension that is at
@@ -369,6 +370,181 @@ def distill(z, ids, top, labels=None, tau=1.0, alpha=1.0, grad=True, stream=None
     if status:
         _fail(status)
     return loss, dz
+
+
+def _ids(ids, device):
+    """(pointer, bytes an id, their number) of contiguous ids of any shape."""
+    if ids.get_device() != device:
+        raise _elsewhere(ids, "ids", device)
+    size = _ID_BYTES.get(ids.dtype)
+    if size is None:
+        raise ValueError(f"ids: expected int32 or int64, got {ids.dtype}")
+    if not ids.is_contiguous():
+        raise ValueError("ids: expected a contiguous tensor")
+    return ids.data_ptr(), size, ids.shape.numel()
+
+
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def _out_type(dtype, name="dtype"):
+    p = _PRECISION.get(dtype)
+    if p is None:
+        raise ValueError(f"{name}: expected bfloat16 or float32, got {dtype}")
+    return p
+
+
+def embed(ids, table, scale=1.0, dtype=None, stream=None):
+    """scale * table[ids], of shape [*ids.shape, d] and type dtype (None: the
+    table's): ids int32 or int64, table [vocab, d].  An id outside 0..vocab-1
+    (such as -1) gives zeros.  Gradients come from embed_backward (no autograd
+    graph)."""
+    if stream is not None:
+        return _on(stream, embed, (ids, table), scale, dtype)
+    prec, on = _precision(table, "table"), table.get_device()
+    dtype = table.dtype if dtype is None else dtype
+    out = _out_type(dtype)
+    tp, ldt = _mat(table, "table", on, table.dtype)
+    vocab, d = table.shape
+    if vocab > _MAX_SIZE:
+        raise _too_wide("table", vocab)
+    ip, size, n = _ids(ids, on)
+    st = _stream(on)
+    y = _empty((*ids.shape, d), dtype=dtype, device=table.device)
+    status = _lib().pack_embed(ip, size, n, tp, ldt, vocab, d, scale, prec, out, y.data_ptr(), st)
+    if status:
+        _fail(status)
+    return y
+
+
+@functools.lru_cache(maxsize=1024)
+def _embed_bytes(n, vocab, d):
+    v = ctypes.c_int64()
+    status = _lib().pack_embed_bytes(n, vocab, d, ctypes.byref(v))
+    if status:
+        _fail(status)
+    return v.value
+
+
+def embed_backward(dy, ids, vocab, scale=1.0, dtype=torch.float32, stream=None):
+    """The gradient [vocab, d], of type dtype, at the table of embed(ids, table,
+    scale): dy [*ids.shape, d], or [n, d] with spaced rows."""
+    if stream is not None:
+        return _on(stream, embed_backward, (dy, ids), vocab, scale, dtype)
+    prec, on = _precision(dy, "dy"), dy.get_device()
+    out = _out_type(dtype)
+    ip, size, n = _ids(ids, on)
+    if dy.dim() == 2 and dy.shape[0] == n:
+        gp, ldg = _mat(dy, "dy", on, dy.dtype)
+    elif dy.dim() and dy.shape[:-1] == ids.shape:
+        gp, ldg = _flat(dy, "dy", on, dy.dtype, *dy.shape), dy.shape[-1]
+    else:
+        raise ValueError(f"dy: shape {tuple(dy.shape)}, expected (*ids.shape, d) of ids {tuple(ids.shape)}")
+    d = dy.shape[-1]
+    if max(vocab, d) > _MAX_SIZE:
+        raise _too_wide("vocab or dy", max(vocab, d))
+    n_work = _embed_bytes(n, vocab, d)
+    st = _stream(on)
+    dt = _empty((vocab, d), dtype=dtype, device=dy.device)
+    work, _keep = _work(n_work, st, dy)
+    status = _lib().pack_embed_backward(gp, ldg, ip, size, n, vocab, d, scale, prec, out, dt.data_ptr(), work, n_work, st)
+    if status:
+        _fail(status)
+    return dt
+
+
+def dropout(x, p, seed, step=0, site=0, residual=None, stream=None):
+    """x [rows, d] with elements zeroed at rate p and the others over 1 - p, plus
+    residual where one is given.  The mask is a function of (seed, step, site,
+    row, column), as a pack's masks are: other steps and sites, other masks."""
+    if stream is not None:
+        return _on(stream, _dropout, (x, residual), p, seed, step, site)
+    return _dropout(x, residual, p, seed, step, site)
+
+
+def _dropout(x, residual, p, seed, step, site):
+    prec, dtype, on = _precision(x, "x"), x.dtype, x.get_device()
+    xp, ldx = _mat(x, "x", on, dtype)
+    rows, d = x.shape
+    rp, ldr = (None, 0) if residual is None else _mat(residual, "residual", on, dtype, rows, d)
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= site < 1 << 32):
+        raise ValueError("seed must be of 64 bits, step and site of 32")
+    st = _stream(on)
+    y = _empty((rows, d), dtype=dtype, device=x.device)
+    status = _lib().pack_dropout(xp, ldx, rp, ldr, rows, d, p, seed, step, site, prec, y.data_ptr(), st)
+    if status:
+        _fail(status)
+    return y
+
+
+def dropout_backward(dy, p, seed, step=0, site=0, stream=None):
+    """The gradient at x of dropout(x, p, seed, step, site): the same elements of
+    dy over 1 - p.  (The gradient at residual is dy.)"""
+    return dropout(dy, p, seed, step, site, None, stream)
+
+
+def layer_norm(x, weight, bias=None, residual=None, eps=1e-5, save=False, stream=None):
+    """(y, s): the layer norm y of s = x + residual (rounded to their type; x
+    itself without one) times weight [d], plus bias [d] (float32), and s for the
+    next residual.  save=True returns (y, s, stats) with what
+    layer_norm_backward needs, the only way to its gradients (no autograd
+    graph)."""
+    if stream is not None:
+        return _on(stream, layer_norm, (x, weight, bias, residual), eps, save)
+    prec, dtype, on = _precision(x, "x"), x.dtype, x.get_device()
+    xp, ldx = _mat(x, "x", on, dtype)
+    rows, d = x.shape
+    wp = _flat(weight, "weight", on, torch.float32, d)
+    bp = _flat(bias, "bias", on, torch.float32, d)
+    rp, ldr = (None, 0) if residual is None else _mat(residual, "residual", on, dtype, rows, d)
+    st, dev = _stream(on), x.device
+    if residual is None:
+        total, tp = x, None
+    else:
+        total = _empty((rows, d), dtype=dtype, device=dev)
+        tp = total.data_ptr()
+    y = _empty((rows, d), dtype=dtype, device=dev)
+    stats = _empty((rows, 2), dtype=torch.float32, device=dev) if save else None
+    status = _lib().pack_layer_norm(xp, ldx, rp, ldr, wp, bp, rows, d, eps, prec, tp, y.data_ptr(),
+                                    stats.data_ptr() if save else None, st)
+    if status:
+        _fail(status)
+    return (y, total, stats) if save else (y, total)
+
+
+@functools.lru_cache(maxsize=1024)
+def _layer_norm_bytes(rows, d):
+    v = ctypes.c_int64()
+    status = _lib().pack_layer_norm_bytes(rows, d, ctypes.byref(v))
+    if status:
+        _fail(status)
+    return v.value
+
+
+def layer_norm_backward(dy, s, weight, stats, dsum=None, stream=None):
+    """(dx, dweight, dbias) of the layer_norm call that returned s and stats: dx
+    is the gradient at s (= at x and at residual); dsum: the gradient that
+    reaches s from elsewhere, added to dx."""
+    if stream is not None:
+        return _on(stream, layer_norm_backward, (dy, s, weight, stats, dsum))
+    prec, dtype, on = _precision(s, "s"), s.dtype, s.get_device()
+    sp, lds = _mat(s, "s", on, dtype)
+    rows, d = s.shape
+    gp, ldg = _mat(dy, "dy", on, dtype, rows, d)
+    wp = _flat(weight, "weight", on, torch.float32, d)
+    mp = _flat(stats, "stats", on, torch.float32, rows, 2)
+    ap, lda = _mat(dsum, "dsum", on, dtype, rows, d) if dsum is not None else (None, 0)
+    n = _layer_norm_bytes(rows, d)
+    st, dev = _stream(on), s.device
+    dx = _empty((rows, d), dtype=dtype, device=dev)
+    dw = _empty(d, dtype=torch.float32, device=dev)
+    db = _empty(d, dtype=torch.float32, device=dev)
+    work, _keep = _work(n, st, s)
+    status = _lib().pack_layer_norm_backward(gp, ldg, sp, lds, wp, mp, ap, lda, rows, d, prec, dx.data_ptr(), dw.data_ptr(),
+                                             db.data_ptr(), work, n, st)
+    if status:
+        _fail(status)
+    return dx, dw, db
 
 
 def ops_check(stream=None):
