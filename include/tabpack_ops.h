@@ -208,6 +208,32 @@ tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* s, 
                                    int32_t precision, void* dx, float* dw, float* db, void* workspace,
                                    int64_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------
+ * 8-bit floating point (e4m3) with a scale for each block of 128.
+ * Quantisation: a block is 128 columns of one row (block_rows 1: activations)
+ * or of 128 rows (block_rows 128: weights); the last ones are shorter.
+ *   scale = max |x| / 448 over the block, as a float32; q = the e4m3 number
+ *   nearest to x / scale (ties to even, at most 448 in magnitude); q = 0 where
+ *   scale is 0.  A block with an infinity or a NaN has q = 0 and scale NaN.
+ *   x: T [rows, k]; q: [rows, k] bytes, ldq apart; scale: float32
+ *   [ceil(rows / block_rows), ceil(k / 128)].  1 <= k <= 131072, rows <
+ *   2^31 - 255 (2^23 - 128 in blocks of 128 rows).                          */
+tp_status pack_quantise_f8(const void* x, int64_t ldx, int64_t rows, int32_t k, int32_t block_rows, int32_t precision,
+                           void* q, int64_t ldq, float* scale, void* cuda_stream);
+
+/* The product of such operands:
+ *   y[r, c] = sum_b scale[r, b] w_scale[c / 128, b] sum_{k in block b}
+ *             q[r, k] w[c, k] + bias[c]
+ * q: e4m3 [rows, k], scale: float32 [rows, ceil(k / 128)]; w: e4m3 [n, k],
+ * w_scale: float32 [ceil(n / 128), ceil(k / 128)]; bias: float32 [n] or NULL; y:
+ * T [rows, n].  1 <= k, n <= 131072.  fp32 sums; rounded once.
+ * aligned: whether q and w start at multiples of 16 bytes, as their rows do
+ * (ldq and ldw): others are copied into the workspace first.                */
+tp_status pack_product_f8_bytes(int64_t rows, int32_t k, int32_t n, int32_t aligned, int64_t* workspace);
+tp_status pack_product_f8(const void* q, int64_t ldq, const float* scale, const void* w, int64_t ldw, const float* w_scale,
+                          const float* bias, int64_t rows, int32_t k, int32_t n, int32_t precision, void* y,
+                          void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

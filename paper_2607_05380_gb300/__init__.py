@@ -43,7 +43,7 @@ SYMBOLS = ["pack_create", "pack_destroy", "pack_set_stream", "pack_train_step", 
            "pack_rms_norm_bytes", "pack_rms_norm_backward", "pack_product_q8_bytes", "pack_product_q8",
            "pack_distill_bytes", "pack_distill", "pack_debug_ops_withhold", "pack_embed", "pack_embed_bytes",
            "pack_embed_backward", "pack_dropout", "pack_layer_norm", "pack_layer_norm_bytes",
-           "pack_layer_norm_backward"]
+           "pack_layer_norm_backward", "pack_quantise_f8", "pack_product_f8_bytes", "pack_product_f8"]
 
 
 class TabpackError(RuntimeError):
@@ -146,6 +146,9 @@ def load_library(path: str = LIB_PATH):
         "pack_embed_backward": (st, [P, i64, P, i32, i64, i32, i32, f32, i32, i32, P, P, i64, P]),
         "pack_dropout": (st, [P, i64, P, i64, i64, i32, f32, u64, u32, u32, i32, P, P]),
         "pack_layer_norm": (st, [P, i64, P, i64, P, P, i64, i32, f32, i32, P, P, P, P]),
+        "pack_quantise_f8": (st, [P, i64, i64, i32, i32, i32, P, i64, P, P]),
+        "pack_product_f8_bytes": (st, [i64, i32, i32, i32, P]),
+        "pack_product_f8": (st, [P, i64, P, P, i64, P, P, i64, i32, i32, i32, P, P, i64, P]),
         "pack_layer_norm_bytes": (st, [i64, i32, P]),
         "pack_layer_norm_backward": (st, [P, i64, P, i64, P, P, P, i64, i64, i32, i32, P, P, P, P, i64, P]),
     }
@@ -526,8 +529,8 @@ class OnlineEnsemble:
 # The student operators' binding (ops.py) needs torch, which nothing else here
 # loads before a call does: it is loaded when one of its names is asked for.
 _OPS = ("ACTIVATIONS", "distill", "dropout", "dropout_backward", "embed", "embed_backward", "gated_backward",
-        "gated_forward", "layer_norm", "layer_norm_backward", "ops_check", "product_q8", "rms_norm",
-        "rms_norm_backward", "rms_norm_q8")
+        "gated_forward", "layer_norm", "layer_norm_backward", "ops_check", "product_f8", "product_q8",
+        "quantise_f8", "rms_norm", "rms_norm_backward", "rms_norm_q8")
 
 
 def __getattr__(name):

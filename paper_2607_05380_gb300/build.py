@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libtabpack.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["tabpack.cu", "kernels.cu", "select.cu", "select_static.cu", "tc_gemm.cu", "head_tc.cu", "online.cu",
            "prod.cu", "rows.cu", "gated.cu", "norm.cu", "quant.cu", "distill.cu",
-           "embed.cu", "dropout.cu", "lnorm.cu"]
+           "embed.cu", "dropout.cu", "lnorm.cu", "f8.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

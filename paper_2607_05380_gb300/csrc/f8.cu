@@ -1,0 +1,589 @@
+// f8.cu -- products in 8-bit floating point (e4m3) with a scale for each block of
+// 128, and the quantisation that makes such operands (entry points in
+// tabpack_ops.h).
+//
+//   scale = max |x| / 448 of a block, q = the e4m3 number nearest to x / scale
+//   y[r, c] = sum_b scale[r, b] w_scale[c / 128, b] sum_{k in block b} q[r, k] w[c, k] + bias[c]
+//
+// The product: a persistent tcgen05 launch (kind::f8f6f4).  A scale block is a K
+// block: its 128 bytes a row are one swizzled line of shared memory and four
+// MMAs.  Every K block has an accumulator of its own in TMEM, of two to four in
+// turn; the epilogue warps read it while the next ones are made, and add it, times
+// its row's and its column block's scale, to their fp32 sums in registers.  So the
+// scales cost a multiply-add an element and K block beside the MMAs, and the
+// tensor cores' own chains are four instructions long.
+//
+// Waits are bounded as in prod.cu, and set the same error word.
+#include <algorithm>
+
+#include "lanes.cuh"
+#include "prod.cuh"
+#include "tc_ptx.cuh"
+#include "tc_warp.cuh"
+
+namespace tp {
+namespace {
+
+constexpr int kBlock = 128;                // of a scale
+constexpr int32_t kMaxDim = 1 << 17;
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256, kMaxElems = int64_t(1) << 40;
+
+// ----------------------------------------------------------------- quantise
+// A block's scale and what its elements are divided by.  Below 2^-64 both sides
+// of the quotient are taken 2^64 times, so that no step of it leaves the normal
+// numbers.
+struct BlockScale {
+  float scale, up, unit, inv;
+  __device__ __forceinline__ explicit BlockScale(uint32_t top) {
+    const float t = __uint_as_float(top);
+    const bool finite = top < 0x7F800000u;
+    scale = finite ? t / 448.f : __uint_as_float(0x7FC00000u);
+    up = t < 5.4e-20f ? 18446744073709551616.f : 1.f;
+    unit = scale * up;
+    inv = finite && scale > 0.f ? 1.f / unit : 0.f;   // 0: the block's q are 0
+  }
+};
+
+// The float whose nearest e4m3 number is that of x / scale: the quotient, or
+// near a border between two numbers (20 bits below the last one kept: 5 places
+// of a million; and below 2^-6, where fewer are kept) the quotient rounded to odd,
+// which lies on the border only if the exact one does.
+__device__ __forceinline__ float quotient(float x, const BlockScale& s) {
+  float t = x * s.up * s.inv;
+  const uint32_t b = __float_as_uint(t);
+  if ((b & 0xFFFFFu) - 0x7FFFCu <= 8u || (b & 0x7FFFFFFFu) - 1u < 0x3C7FFFFFu) {
+    if (s.inv == 0.f) return 0.f;
+    const float v = x * s.up;
+    t = __fdiv_rn(v, s.unit);
+    const float r = fmaf(-t, s.unit, v);
+    if (r != 0.f) {
+      uint32_t u = __float_as_uint(t);
+      if ((r < 0.f) == (t > 0.f)) --u;   // beyond the exact quotient: back towards zero
+      t = __uint_as_float(u | 1u);
+    }
+  }
+  return t;
+}
+// Two numbers as e4m3 (the first one in the lower byte), to the nearest, ties to even, at most 448.
+__device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+template <typename T>
+struct QuantArgs {
+  const T* x;
+  uint8_t* q;
+  float* scale;
+  int64_t ldx, ldq, rows;
+  int32_t k, blocks;      // blocks of 128 columns
+};
+
+// Scales per row and block: sixteen lanes a block, eight elements each.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_rows(const QuantArgs<T> g) {
+  using L = Lane<T, 1, 1, 8>;
+  const int lane = threadIdx.x & 15;
+  const int64_t total = g.rows * g.blocks, step = (int64_t)gridDim.x * 16;
+  pdl_trigger();
+  pdl_wait();
+  for (int64_t base = (int64_t)blockIdx.x * 16 + ((threadIdx.x >> 5) << 1); base < total; base += step) {
+    const int64_t at = base + ((threadIdx.x >> 4) & 1);   // (both halves of a warp stay in the loop together)
+    const int64_t row = at / g.blocks;
+    const int b = (int)(at - row * g.blocks), c = b * kBlock + lane * 8;
+    const bool live = at < total && c < g.k;
+    L x;
+    x.load(g.x + (live ? row * g.ldx + c : 0), 0, live ? 8 : 0);
+    float v[8];
+    x.get(0, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const BlockScale s(top);
+    if (at < total && lane == 0) g.scale[at] = s.scale;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = s.inv == 0.f ? 0.f : quotient(v[e], s);
+    if (live)
+      *reinterpret_cast<uint2*>(g.q + row * g.ldq + c) =
+          make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+  }
+}
+
+// Any alignment: a warp a block, its lanes side by side.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_rows1(const QuantArgs<T> g) {
+  const int lane = threadIdx.x & 31;
+  const int64_t total = g.rows * g.blocks;
+  pdl_trigger();
+  pdl_wait();
+  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < total; at += (int64_t)gridDim.x * 8) {
+    const int64_t row = at / g.blocks;
+    const int c0 = (int)(at - row * g.blocks) * kBlock + lane;
+    float v[4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = c0 + 32 * i < g.k ? Elem<T>::to_f(g.x[row * g.ldx + c0 + 32 * i]) : 0.f;
+      top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    }
+    top = warp_max(top);
+    const BlockScale s(top);
+    if (lane == 0) g.scale[at] = s.scale;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c0 + 32 * i < g.k) g.q[row * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(s.inv == 0.f ? 0.f : quotient(v[i], s), 0.f);
+  }
+}
+
+// Scales per 128 x 128 block: a CTA a block, a warp sixteen rows.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_blocks(const QuantArgs<T> g) {
+  __shared__ uint32_t tops[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t r0 = (int64_t)blockIdx.y * kBlock + warp * 16;
+  const int c0 = blockIdx.x * kBlock + lane;
+  pdl_trigger();
+  pdl_wait();
+  float v[16][4];
+  uint32_t top = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[r][i] = r0 + r < g.rows && c0 + 32 * i < g.k ? Elem<T>::to_f(g.x[(r0 + r) * g.ldx + c0 + 32 * i]) : 0.f;
+      top = max(top, __float_as_uint(v[r][i]) & 0x7FFFFFFFu);
+    }
+  top = warp_max(top);
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = max(top, tops[w]);
+  const BlockScale s(top);
+  if (threadIdx.x == 0) g.scale[(int64_t)blockIdx.y * g.blocks + blockIdx.x] = s.scale;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r0 + r < g.rows && c0 + 32 * i < g.k)
+        g.q[(r0 + r) * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(s.inv == 0.f ? 0.f : quotient(v[r][i], s), 0.f);
+}
+
+template <typename T>
+void quantise(const QuantArgs<T>& a, int block_rows, cudaStream_t st) {
+  if (block_rows != 1) {
+    launch_pdl(k_quant_blocks<T>, dim3((unsigned)a.blocks, (unsigned)ceil_div(a.rows, kBlock)), dim3(256), 0, st, a);
+    return;
+  }
+  const int64_t total = a.rows * a.blocks;
+  const bool vec = a.k % 8 == 0 && aligned16(a.x, a.ldx, sizeof(T)) && ((uintptr_t)a.q & 7) == 0 && a.ldq % 8 == 0;
+  if (vec) launch_pdl(k_quant_rows<T>, dim3((unsigned)std::min<int64_t>(ceil_div(total, 16), 16 * kSms)), dim3(256), 0, st, a);
+  else launch_pdl(k_quant_rows1<T>, dim3((unsigned)std::min<int64_t>(ceil_div(total, 8), 16 * kSms)), dim3(256), 0, st, a);
+}
+
+// ------------------------------------------------------------------ staging
+// Rows of k bytes at any address into rows that TMA takes.
+struct CopyArgs {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t ld, ldp, rows;
+  int32_t k;
+};
+__global__ void __launch_bounds__(256) k_copy_rows(const CopyArgs a, const CopyArgs b) {
+  const CopyArgs& g = blockIdx.y ? b : a;
+  const int groups = (int)(g.ldp >> 4);
+  pdl_trigger();
+  pdl_wait();
+  const int64_t total = g.rows * groups;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / groups;
+    const int c = (int)(i - row * groups) * 16;
+    const uint8_t* p = g.src + row * g.ld + c;
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < g.k) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+    *reinterpret_cast<uint4*>(g.dst + row * g.ldp + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// ------------------------------------------------------------------ product
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;   // a producer, the MMA issuer
+constexpr int kABytes = 128 * kBlock;
+constexpr int kStages = 6, kMaxBufs = 4;
+constexpr int kTmemCols = 512;
+constexpr int kBufBytes = 32 * 32 * 4;   // per epilogue warp
+
+struct Tail {
+  uint64_t full[kStages], empty[kStages], tfull[kMaxBufs], tempty[kMaxBufs], done;
+  uint32_t tmem_base;
+  int abort;
+};
+
+struct F8Args {
+  CUtensorMap a, b;
+  const float *sx, *sw, *bias;
+  void* y;
+  int* err;
+  int32_t M, N, kb, tm, tn, f32;   // kb: K blocks; tiles
+};
+
+// One K block: four MMAs (K = 32 each, 32 bytes apart) into an accumulator of
+// its own; then `bar` and `bar2` (in every CTA of the tile) are told.
+#define TP_F8_MMA4(GROUP, COMMIT)                                                                                     \
+  "{\n .reg .pred e, p, t;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n elect.sync _|e, 0xffffffff;\n"                        \
+  " setp.ne.b32 p, 0, 0;\n setp.eq.b32 t, 0, 0;\n"                                                                    \
+  " add.s64 a1, %1, 2;\n add.s64 a2, %1, 4;\n add.s64 a3, %1, 6;\n"                                                   \
+  " add.s64 b1, %2, 2;\n add.s64 b2, %2, 4;\n add.s64 b3, %2, 6;\n"                                                   \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], %1, %2, %3, p;\n"                                          \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a1, b1, %3, t;\n"                                          \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a2, b2, %3, t;\n"                                          \
+  " @e tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a3, b3, %3, t;\n" COMMIT "}\n"
+#define TP_F8_COMMIT1                                                                        \
+  " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n"        \
+  " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n"
+#define TP_F8_COMMIT2                                                                                                 \
+  " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], %6;\n"          \
+  " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %6;\n"
+template <int kCta>
+__device__ __forceinline__ void mma_block(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t bar, uint32_t bar2) {
+  if constexpr (kCta == 2)
+    asm volatile(TP_F8_MMA4("2", TP_F8_COMMIT2)::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(bar), "r"(bar2), "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile(TP_F8_MMA4("1", TP_F8_COMMIT1)::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(bar), "r"(bar2) : "memory");
+}
+
+// Eight row blocks at a time walk the columns, so that tiles that run at once share operands in L2.
+__device__ __forceinline__ void tile_at(const F8Args& g, int t, int& m, int& n) {
+  const int group = t / (8 * g.tn), rows = min(8, g.tm - 8 * group), local = t - group * 8 * g.tn;
+  m = 8 * group + local % rows;
+  n = local / rows;
+}
+
+// kN: columns of a tile, kCta * 128 its rows.
+template <int kCta, int kN>
+__global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__ F8Args g) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  constexpr int kNh = kN / kCta;                        // rows of B that this CTA stages
+  constexpr uint32_t kStageBytes = kABytes + kNh * kBlock;
+  constexpr int kBufs = kTmemCols / kN < kMaxBufs ? kTmemCols / kN : kMaxBufs;
+  constexpr int kCols = kN / 2;                         // of an epilogue warp
+  uint8_t* bufs = smem + kStages * kStageBytes;
+  Tail* tl = (Tail*)(bufs + kEpiWarps * kBufBytes);
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int rank = kCta == 2 ? (int)uniform(cluster_rank()) : 0;
+  const bool leader = rank == 0;
+  const int clu = blockIdx.x / kCta, n_clu = gridDim.x / kCta, n_tiles = g.tm * g.tn;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&tl->full[s], 1);
+      mbar_init(&tl->empty[s], 1);
+    }
+    for (int b = 0; b < kBufs; ++b) {
+      mbar_init(&tl->tfull[b], 1);
+      mbar_init(&tl->tempty[b], kEpiWarps * kCta);
+    }
+    mbar_init(&tl->done, 1);
+    tl->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if constexpr (kCta == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tl->tmem_base)),
+                   "r"(kTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tl->tmem_base)),
+                   "r"(kTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (kCta == 2) cluster_sync();   // the peer's barriers exist before any copy or arrival targets them
+  if (warp == 0 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &g.b : &g.a) : "memory");
+  pdl_wait();                      // the set-up above overlaps the previous kernel
+  fence_proxy_async_global();      // what it wrote by plain stores is read by TMA
+  const uint32_t tmem = uniform(tl->tmem_base);
+  volatile int* abort_flag = &tl->abort;
+  int* err = g.err;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------- producer
+    uint32_t stage = 0, phase = 0, issued = 0;
+    bool ok = true;
+    const uint32_t s0 = smem_u32(smem), full0 = smem_u32(&tl->full[0]);
+    const uint32_t lead0 = kCta == 2 ? mapa(full0, 0) : full0;   // the barriers that copies complete on
+    for (int t = clu; ok && t < n_tiles; t += n_clu) {
+      int m, n;
+      tile_at(g, t, m, n);
+      const int ya = (m * kCta + rank) * 128, yb = n * kN + rank * kNh;
+      for (int kb = 0; kb < g.kb; ++kb) {
+        if (!wait_all(&tl->empty[stage], phase ^ 1u, abort_flag, err, kWaitNs, 61)) {
+          ok = false;
+          break;
+        }
+        const uint32_t dst = s0 + stage * kStageBytes, bar = lead0 + 8 * stage;
+        if (leader) expect_elect(full0 + 8 * stage, kCta * kStageBytes);
+        tma_elect<kCta>(dst, &g.a, bar, kBlock * kb, ya, 0);
+        tma_elect<kCta>(dst + kABytes, &g.b, bar, kBlock * kb, yb, 0);
+        issued |= 1u << stage;
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    // every copy has landed before the CTA leaves: a stage's last one is of this
+    // turn of the ring below `stage`, of the one before from there on
+    if (leader)
+      for (int s = 0; s < kStages; ++s)
+        if (issued & (1u << s)) {
+          int dummy = 0;
+          mbar_wait(&tl->full[s], s < (int)stage ? phase : phase ^ 1u, &dummy, err, kWaitNs, 62);
+        }
+  } else if (warp == 1) {
+    if (leader) {
+      // --------------------------------------------------------------- MMA
+      const uint32_t s0 = smem_u32(smem), empty0 = smem_u32(&tl->empty[0]), tfull0 = smem_u32(&tl->tfull[0]);
+      const uint64_t da = smem_desc(s0, 16, 1024), db = smem_desc(s0 + kABytes, 16, 1024);
+      // fp32 accumulators, e4m3 operands (format 0), both K-major
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(128 * kCta >> 4) << 24);
+      uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+      bool ok = true;
+      for (int t = clu; ok && t < n_tiles; t += n_clu)
+        for (int kb = 0; kb < g.kb; ++kb) {
+          if (!wait_all(&tl->tempty[buf], buf_phase ^ 1u, abort_flag, err, 2 * kWaitNs, 63) ||
+              !wait_all(&tl->full[stage], phase, abort_flag, err, 2 * kWaitNs, 64)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          mma_block<kCta>(tmem + buf * kN, da + stage * (kStageBytes >> 4), db + stage * (kStageBytes >> 4), idesc,
+                          empty0 + 8 * stage, tfull0 + 8 * buf);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+          if (++buf == kBufs) {
+            buf = 0;
+            buf_phase ^= 1u;
+          }
+        }
+      commit_elect<kCta>(smem_u32(&tl->done));   // all MMAs are over before TMEM is freed
+      int dummy = 0;
+      mbar_wait(&tl->done, 0, &dummy, err, kWaitNs, 65);
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* out_buf = bufs + (warp - 2) * kBufBytes;
+    uint32_t buf = 0, buf_phase = 0;
+    const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + half * kCols;
+    bool ok = true;
+    for (int t = clu; ok && t < n_tiles; t += n_clu) {
+      int m, n;
+      tile_at(g, t, m, n);
+      const int r0 = (m * kCta + rank) * 128 + 32 * q, c0 = n * kN + half * kCols;
+      const int row = min(r0 + lane, g.M - 1);
+      const float* sx = g.sx + (int64_t)row * g.kb;
+      const float* sw = g.sw + (int64_t)(min(c0, g.N - 1) / kBlock) * g.kb;
+      float acc[kCols];
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
+      float ax = sx[0], aw = sw[0];
+      for (int kb = 0; kb < g.kb; ++kb) {
+        const float f = ax * aw;
+        if (kb + 1 < g.kb) ax = sx[kb + 1], aw = sw[kb + 1];
+        if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[buf], buf_phase, abort_flag, err, 2 * kWaitNs, 66))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < kCols; c += 32) {
+          uint32_t v[32];
+          tmem_ask32(t0 + buf * kN + c, v);
+          tmem_wait();
+          tmem_got(v);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[c + e] = fmaf(__uint_as_float(v[e]), f, acc[c + e]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {   // the loads above have completed
+          if constexpr (kCta == 2) mbar_arrive_cluster_relaxed(mapa(smem_u32(&tl->tempty[buf]), 0));
+          else mbar_arrive_relaxed(&tl->tempty[buf]);
+        }
+        if (++buf == kBufs) {
+          buf = 0;
+          buf_phase ^= 1u;
+        }
+      }
+      if (!ok) break;
+      const bool live = r0 + lane < g.M;
+#pragma unroll
+      for (int c = 0; c < kCols; c += 32) {
+        const int col = c0 + c, left = g.N - col;
+        if (left <= 0) break;
+        const float b = g.bias && col + lane < g.N ? g.bias[col + lane] : 0.f;
+        float v[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = acc[c + e] + __shfl_sync(0xffffffffu, b, e);
+        const int64_t at = (int64_t)(r0 + lane) * g.N + col;
+        if (g.f32) {
+          if (left >= 32 && ((uintptr_t)g.y & 31) == 0 && (g.N & 7) == 0) put_f32(v, (float*)g.y + at, live, 32);
+          else emit_f32(out_buf, lane, v, (float*)g.y, g.N, r0, g.M, col, g.N, vec_ok(g.y, g.N, 4));
+        } else {
+          uint32_t pk[16];
+          pack32(v, pk);
+          if (left >= 32 && ((uintptr_t)g.y & 31) == 0 && (g.N & 15) == 0) put_bf16(pk, (__nv_bfloat16*)g.y + at, live, 32);
+          else emit_bf16(out_buf, lane, pk, (__nv_bfloat16*)g.y, g.N, r0, g.M, col, g.N, vec_ok(g.y, g.N, 2));
+        }
+      }
+    }
+  }
+
+  pdl_trigger();   // not earlier: CTAs of the next kernel parked beside a running product slow it down
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if constexpr (kCta == 2) {
+    // the leader's last commit arrives in both CTAs: its arrival here, too, is over before this memory is another's
+    if (warp == 1 && !leader) {
+      int dummy = 0;
+      mbar_wait(&tl->done, 0, &dummy, err, 4 * kWaitNs, 65);
+    }
+    cluster_sync();
+  }
+  if (warp == 1) {
+    if constexpr (kCta == 2)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+template <int kCta, int kN>
+cudaError_t launch_f8(F8Args& g, const void* q, int64_t ldq, const void* w, int64_t ldw, int64_t k, cudaStream_t st) {
+  g.tm = (int32_t)ceil_div(g.M, 128 * kCta), g.tn = (int32_t)ceil_div(g.N, kN);
+  if (!tma_map_bytes(&g.a, q, k, g.M, ldq, kBlock, 128) || !tma_map_bytes(&g.b, w, k, g.N, ldw, kBlock, kN / kCta))
+    return cudaErrorInvalidValue;
+  const int smem = 1024 + kStages * (kABytes + kN / kCta * kBlock) + kEpiWarps * kBufBytes + (int)sizeof(Tail);
+  cudaError_t e = cudaFuncSetAttribute(k_prod_f8<kCta, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCta * (unsigned)std::min<int64_t>((int64_t)g.tm * g.tn, kSms / kCta));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCta;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = kCta == 2 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_prod_f8<kCta, kN>, g);
+}
+
+tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
+  if (rows < 0 || rows > kMaxRows) return ops_fail(TP_EINVAL, "rows %lld out of range", (long long)rows);
+  if (k < 1 || n < 1 || k > kMaxDim || n > kMaxDim)
+    return ops_fail(TP_EINVAL, "k %d and n %d must be in 1..%d", k, n, kMaxDim);
+  if (rows * (k > n ? k : n) > kMaxElems) return ops_fail(TP_EINVAL, "more than 2^40 elements in a matrix");
+  if (precision != TP_BF16 && precision != TP_FP32) return ops_fail(TP_EINVAL, "unknown precision %d", precision);
+  return TP_OK;
+}
+
+// An operand's rows as TMA takes them, staged where they lie otherwise.
+int64_t staged_bytes(int64_t rows, int32_t k) { return round_up(rows * round_up(k, 16), 256); }
+
+tp_status done(cudaError_t e, const char* who) {
+  if (e == cudaSuccess) return TP_OK;
+  cudaGetLastError();   // reported here
+  return ops_fail(TP_ECUDA, "%s: %s", who, cudaGetErrorString(e));
+}
+
+}  // namespace
+}  // namespace tp
+
+using namespace tp;
+
+extern "C" {
+
+tp_status pack_quantise_f8(const void* x, int64_t ldx, int64_t rows, int32_t k, int32_t block_rows, int32_t precision,
+                           void* q, int64_t ldq, float* scale, void* cuda_stream) {
+  tp_status s = check(rows, k, 1, precision);
+  if (s != TP_OK) return s;
+  if (block_rows != 1 && block_rows != kBlock) return ops_fail(TP_EINVAL, "block_rows %d must be 1 or %d", block_rows, kBlock);
+  if (ldx < k || ldq < k) return ops_fail(TP_EINVAL, "ldx and ldq must not be less than k %d", k);
+  if (block_rows != 1 && rows > int64_t(kBlock) * 65535)
+    return ops_fail(TP_EINVAL, "at most %d rows in blocks of %d", kBlock * 65535, kBlock);
+  if (rows == 0) return TP_OK;
+  if (!x || !q || !scale) return ops_fail(TP_EINVAL, "null argument");
+  if ((s = ops_device()) != TP_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int32_t blocks = (int32_t)ceil_div(k, kBlock);
+  if (precision == TP_FP32)
+    quantise(QuantArgs<float>{(const float*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks}, block_rows, st);
+  else
+    quantise(QuantArgs<__nv_bfloat16>{(const __nv_bfloat16*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks}, block_rows, st);
+  return done(cudaGetLastError(), "pack_quantise_f8");
+}
+
+tp_status pack_product_f8_bytes(int64_t rows, int32_t k, int32_t n, int32_t aligned, int64_t* workspace) {
+  const tp_status s = check(rows, k, n, TP_BF16);
+  if (s != TP_OK) return s;
+  if (!workspace) return ops_fail(TP_EINVAL, "null argument");
+  *workspace = rows == 0 || aligned ? 0 : staged_bytes(rows, k) + staged_bytes(n, k);
+  return TP_OK;
+}
+
+tp_status pack_product_f8(const void* q, int64_t ldq, const float* scale, const void* w, int64_t ldw, const float* w_scale,
+                          const float* bias, int64_t rows, int32_t k, int32_t n, int32_t precision, void* y,
+                          void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+  tp_status s = check(rows, k, n, precision);
+  if (s != TP_OK) return s;
+  if (ldq < k || ldw < k) return ops_fail(TP_EINVAL, "ldq and ldw must not be less than k %d", k);
+  if (rows == 0) return TP_OK;
+  if (!q || !scale || !w || !w_scale || !y) return ops_fail(TP_EINVAL, "null argument");
+  if (rows == 1) ldq = round_up(k, 16);   // (one row has no distance to the next)
+  if (n == 1) ldw = round_up(k, 16);
+  const bool q_ok = aligned16(q, ldq, 1), w_ok = aligned16(w, ldw, 1);
+  const int64_t need = q_ok && w_ok ? 0 : staged_bytes(rows, k) + staged_bytes(n, k);
+  if (need && (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255)))
+    return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
+  if ((s = ops_device()) != TP_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  F8Args g{};
+  cudaError_t e = prod_err_word(&g.err);
+  if (e != cudaSuccess) return done(e, "pack_product_f8");
+  if (need) {
+    const int64_t ldp = round_up(k, 16);
+    uint8_t* qs = (uint8_t*)workspace;
+    uint8_t* ws = qs + staged_bytes(rows, k);
+    const CopyArgs cq{(const uint8_t*)q, qs, ldq, ldp, rows, k}, cw{(const uint8_t*)w, ws, ldw, ldp, n, k};
+    const int64_t blocks = std::min<int64_t>(ceil_div(std::max<int64_t>(rows, n) * (ldp / 16), 256), 8 * kSms);
+    launch_pdl(k_copy_rows, dim3((unsigned)blocks, !q_ok && !w_ok ? 2 : 1), dim3(256), 0, st, q_ok ? cw : cq, cw);
+    if ((e = cudaGetLastError()) != cudaSuccess) return done(e, "pack_product_f8");
+    if (!q_ok) q = qs, ldq = ldp;
+    if (!w_ok) w = ws, ldw = ldp;
+  }
+  g.sx = scale, g.sw = w_scale, g.bias = bias, g.y = y;
+  g.M = (int32_t)rows, g.N = n, g.kb = (int32_t)ceil_div(k, kBlock), g.f32 = precision == TP_FP32;
+  if (ceil_div(rows, 256) * ceil_div(n, 256) >= kSms / 4) e = launch_f8<2, 256>(g, q, ldq, w, ldw, k, st);
+  else e = launch_f8<1, 128>(g, q, ldq, w, ldw, k, st);
+  return done(e, "pack_product_f8");
+}
+
+}  // extern "C"

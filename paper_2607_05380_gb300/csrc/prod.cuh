@@ -105,6 +105,11 @@ cudaError_t prod_run_all(StageLaunch& stage, ProdLaunch* l, int n, void* workspa
 // Is a 16-bit operand fit for TMA as it lies there?
 inline bool tma_ready(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
+// The device's word that a bounded wait of a product which gives up sets, and pack_ops_check reads.
+cudaError_t prod_err_word(int** word);
+// A TMA map of [rows][cols] bytes, ld from row to row, 128-byte swizzle; base and ld are multiples of 16.
+bool tma_map_bytes(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_cols, int box_rows);
+
 // Error reporting of the entry points without a handle.
 tp_status ops_fail(tp_status s, const char* fmt, ...);
 // Is a CUDA device there that the library runs on (an error status if not)?

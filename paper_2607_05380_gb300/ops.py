@@ -547,6 +547,69 @@ def layer_norm_backward(dy, s, weight, stats, dsum=None, stream=None):
     return dx, dw, db
 
 
+def quantise_f8(x, block_rows=1, stream=None):
+    """(q, scale): x [rows, k] as float8_e4m3fn with a float32 scale [ceil(rows /
+    block_rows), ceil(k / 128)] for every 128 columns of a row (block_rows=1:
+    activations) or of 128 rows (block_rows=128: weights).  q's rows are padded to
+    multiples of 16 bytes, as product_f8 takes them best."""
+    if stream is not None:
+        return _on(stream, quantise_f8, (x,), block_rows)
+    prec, on = _precision(x, "x"), x.get_device()
+    xp, ldx = _mat(x, "x", on, x.dtype)
+    if block_rows not in (1, 128):
+        raise ValueError(f"block_rows must be 1 or 128, not {block_rows}")
+    rows, k = x.shape
+    st, dev = _stream(on), x.device
+    ldq = (k + 15) // 16 * 16
+    q = _empty((rows, ldq), dtype=torch.float8_e4m3fn, device=dev)
+    scale = _empty(((rows + block_rows - 1) // block_rows, (k + 127) // 128), dtype=torch.float32, device=dev)
+    status = _lib().pack_quantise_f8(xp, ldx, rows, k, block_rows, prec, q.data_ptr(), ldq, scale.data_ptr(), st)
+    if status:
+        _fail(status)
+    return q if ldq == k else q[:, :k], scale
+
+
+@functools.lru_cache(maxsize=1024)
+def _f8_bytes(rows, k, n, aligned):
+    v = ctypes.c_int64()
+    status = _lib().pack_product_f8_bytes(rows, k, n, aligned, ctypes.byref(v))
+    if status:
+        _fail(status)
+    return v.value
+
+
+def product_f8(q, scale, w, w_scale, bias=None, dtype=torch.bfloat16, stream=None):
+    """y[r, c] = sum_b scale[r, b] w_scale[c // 128, b] sum_{k in block b} q[r, k]
+    w[c, k] + bias[c], of type dtype: q [rows, k] and scale of quantise_f8, w
+    [n, k] and w_scale of quantise_f8(weights, 128), bias float32 [n].  Operands
+    whose rows do not start at multiples of 16 bytes are copied first."""
+    if stream is not None:
+        return _on(stream, product_f8, (q, scale, w, w_scale, bias), dtype)
+    prec = _out_type(dtype)
+    on = q.get_device()
+    qp, ldq = _mat(q, "q", on, torch.float8_e4m3fn)
+    rows, k = q.shape
+    if w.dim() != 2:
+        raise ValueError("w must be [n, k]")
+    n = w.shape[0]
+    if n > _MAX_SIZE:
+        raise _too_wide("w", n)
+    wp, ldw = _mat(w, "w", on, torch.float8_e4m3fn, n, k)
+    blocks = (k + 127) // 128
+    sp = _flat(scale, "scale", on, torch.float32, rows, blocks)
+    cp = _flat(w_scale, "w_scale", on, torch.float32, (n + 127) // 128, blocks)
+    bp = _flat(bias, "bias", on, torch.float32, n)
+    odd = qp | wp | (ldq if rows > 1 else 0) | (ldw if n > 1 else 0)   # (one row has no distance to the next)
+    n_work = _f8_bytes(rows, k, n, odd & 15 == 0)
+    st, dev = _stream(on), q.device
+    y = _empty((rows, n), dtype=dtype, device=dev)
+    work, _keep = _work(n_work, st, q) if n_work else (None, None)
+    status = _lib().pack_product_f8(qp, ldq, sp, wp, ldw, cp, bp, rows, k, n, prec, y.data_ptr(), work, n_work, st)
+    if status:
+        _fail(status)
+    return y
+
+
 def ops_check(stream=None):
     """Waits for the stream; raises if a bounded wait of a product has given up on
     this device since the calling thread's last check of this stream."""
