@@ -33,50 +33,81 @@ struct Args {
   float up;
 };
 
-// Round 1 of (row, col, step, site): (x0 ^ col, w1, w2, w3); round 2: (v0, v1, hi(Ma (x0 ^ col)) ^ x2, lo(Ma (x0 ^ col))).
-__device__ __forceinline__ uint32_t keep4(uint32_t row, uint32_t col, uint32_t step, uint32_t site, uint32_t k0, uint32_t k1,
-                                          uint32_t drop) {
-  const uint32_t x0 = __umulhi(kPhiloxMb, step) ^ k0, w1 = kPhiloxMb * step;
-  const uint32_t w2 = __umulhi(kPhiloxMa, row) ^ site ^ k1, w3 = kPhiloxMa * row;
-  const uint32_t v0 = __umulhi(kPhiloxMb, w2) ^ w1 ^ (k0 + kPhiloxWa), v1 = kPhiloxMb * w2;
-  const uint32_t x2 = w3 ^ (k1 + kPhiloxWb);
-  const uint32_t y0 = v1 ^ (k0 + 2u * kPhiloxWa);
-  const uint32_t y2 = __umulhi(kPhiloxMa, v0) ^ (k1 + 2u * kPhiloxWb), y3 = kPhiloxMa * v0;
-  const uint32_t c = x0 ^ col;
-  const uint32_t v2 = __umulhi(kPhiloxMa, c) ^ x2, v3 = kPhiloxMa * c;
-  const U4 r = philox_rounds<7>(__umulhi(kPhiloxMb, v2) ^ y0, kPhiloxMb * v2, v3 ^ y2, y3, k0 + 3u * kPhiloxWa,
-                                k1 + 3u * kPhiloxWb);
-  return (uint32_t)(r.x >= drop) | (uint32_t)(r.y >= drop) << 1 | (uint32_t)(r.z >= drop) << 2 | (uint32_t)(r.w >= drop) << 3;
+// Round 1 of (row, col, step, site): (x0 ^ col, w1, w2, w3); round 2: (v0, v1, v2 = hi(Ma (x0 ^ col)) ^ x2, v3 = lo(Ma (x0
+// ^ col))); round 3: (hi(Mb v2) ^ y0, lo(Mb v2), v3 ^ y2, y3).  What of it a row decides, and what a column.
+struct RowPart {
+  uint32_t x2, y0, y2, y3;
+  __device__ __forceinline__ RowPart(uint32_t row, uint32_t step, uint32_t site, uint32_t k0, uint32_t k1) {
+    const uint32_t w1 = kPhiloxMb * step, w2 = __umulhi(kPhiloxMa, row) ^ site ^ k1, w3 = kPhiloxMa * row;
+    const uint32_t v0 = __umulhi(kPhiloxMb, w2) ^ w1 ^ (k0 + kPhiloxWa), v1 = kPhiloxMb * w2;
+    x2 = w3 ^ (k1 + kPhiloxWb);
+    y0 = v1 ^ (k0 + 2u * kPhiloxWa);
+    y2 = __umulhi(kPhiloxMa, v0) ^ (k1 + 2u * kPhiloxWb), y3 = kPhiloxMa * v0;
+  }
+};
+struct ColPart {
+  uint32_t hi, v3;
+  __device__ __forceinline__ ColPart(uint32_t col, uint32_t step, uint32_t k0) {
+    const uint32_t c = __umulhi(kPhiloxMb, step) ^ k0 ^ col;
+    hi = __umulhi(kPhiloxMa, c), v3 = kPhiloxMa * c;
+  }
+};
+__device__ __forceinline__ U4 draw4(const RowPart& r, const ColPart& c, uint32_t k0, uint32_t k1) {
+  const uint32_t v2 = c.hi ^ r.x2;
+  return philox_rounds<7>(__umulhi(kPhiloxMb, v2) ^ r.y0, kPhiloxMb * v2, c.v3 ^ r.y2, r.y3, k0 + 3u * kPhiloxWa,
+                          k1 + 3u * kPhiloxWb);
 }
 
-// Eight columns a thread, loads and stores of 16 bytes.
 template <typename T>
+__device__ __forceinline__ void drop8(const Args<T>& g, float (&v)[8], const RowPart& r, const ColPart (&c)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const U4 w = draw4(r, c[h], g.k0, g.k1);
+    v[4 * h] = w.x >= g.drop ? v[4 * h] * g.up : 0.f;
+    v[4 * h + 1] = w.y >= g.drop ? v[4 * h + 1] * g.up : 0.f;
+    v[4 * h + 2] = w.z >= g.drop ? v[4 * h + 2] * g.up : 0.f;
+    v[4 * h + 3] = w.w >= g.drop ? v[4 * h + 3] * g.up : 0.f;
+  }
+}
+
+// Eight columns a thread, loads and stores of 16 bytes; kRows rows in flight.  A
+// block's threads are one row's (kWide: what a row decides is then computed by
+// the uniform units, once a warp) or several rows'.
+template <typename T, bool kWide>
 __global__ void __launch_bounds__(256) k_drop8(const Args<T> g) {
   using L = Lane<T, 1, 1, 8>;
-  const int tx = threadIdx.x & ((1 << g.shift) - 1), ty = threadIdx.x >> g.shift;
+  constexpr int kRows = 4;
+  const int tx = kWide ? threadIdx.x : threadIdx.x & ((1 << g.shift) - 1), ty = kWide ? 0 : threadIdx.x >> g.shift;
+  const int rows_at_once = kWide ? 1 : 256 >> g.shift;
   const int c = 8 * (blockIdx.x * (1 << g.shift) + tx);
   pdl_trigger();
+  const ColPart cols[2] = {ColPart((uint32_t)c >> 2, g.step, g.k0), ColPart(((uint32_t)c >> 2) + 1, g.step, g.k0)};
   pdl_wait();
   if (c >= g.d) return;
-  const int64_t step = (int64_t)gridDim.y * (256 >> g.shift);
-  for (int64_t row = (int64_t)blockIdx.y * (256 >> g.shift) + ty; row < g.rows; row += step) {
-    L x, res;
-    x.load(g.x + row * g.ldx + c, 0, 8);
-    if (g.res) res.load(g.res + row * g.ldr + c, 0, 8);
-    uint32_t keep = 0xFFu;
-    if (g.drop)
-      keep = keep4((uint32_t)row, (uint32_t)c >> 2, g.step, g.site, g.k0, g.k1, g.drop) |
-             keep4((uint32_t)row, ((uint32_t)c >> 2) + 1, g.step, g.site, g.k0, g.k1, g.drop) << 4;
-    float v[8], r[8];
-    x.get(0, v);
+  const int64_t step = (int64_t)gridDim.y * rows_at_once;
+  for (int64_t row = (int64_t)blockIdx.y * rows_at_once + ty; row < g.rows; row += kRows * step) {
+    L x[kRows], res[kRows];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = keep >> e & 1 ? v[e] * g.up : 0.f;
-    if (g.res) {
-      res.get(0, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += r[e];
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = row + u * step;
+      const int there = r < g.rows ? 8 : 0;
+      x[u].load(g.x + r * g.ldx + c, 0, there);
+      if (g.res) res[u].load(g.res + r * g.ldr + c, 0, there);
     }
-    L::put(g.y + row * g.d + c, 0, 0, 8, v);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = row + u * step;
+      if (r >= g.rows) break;
+      float v[8], w[8];
+      x[u].get(0, v);
+      if (g.drop) drop8(g, v, RowPart((uint32_t)r, g.step, g.site, g.k0, g.k1), cols);
+      if (g.res) {
+        res[u].get(0, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += w[e];
+      }
+      L::put(g.y + r * g.d + c, 0, 0, 8, v);
+    }
   }
 }
 
@@ -84,12 +115,12 @@ __global__ void __launch_bounds__(256) k_drop8(const Args<T> g) {
 // whose words come from the eight lanes that have drawn them.
 template <typename T>
 __global__ void __launch_bounds__(256) k_drop1(const Args<T> g) {
-  const int lane = threadIdx.x & 31;
-  const int64_t wide = ceil_div(g.d, 128), total = g.rows * wide;
+  const int lane = threadIdx.x & 31, wide = (g.d + 127) >> 7;
+  const int64_t total = g.rows * wide;
   pdl_trigger();
   pdl_wait();
   for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < total; at += (int64_t)gridDim.x * 8) {
-    const int64_t row = at / wide;
+    const int64_t row = total >> 31 ? at / wide : (int64_t)((uint32_t)at / (uint32_t)wide);
     const int c0 = (int)(at - row * wide) * 128;
     T x[4], r[4];
 #pragma unroll
@@ -99,12 +130,17 @@ __global__ void __launch_bounds__(256) k_drop1(const Args<T> g) {
       r[i] = c < g.d && g.res ? g.res[row * g.ldr + c] : Elem<T>::from_f(0.f);
     }
     uint32_t keep = 0xFu;
-    if (g.drop) keep = keep4((uint32_t)row, ((uint32_t)c0 >> 2) + lane, g.step, g.site, g.k0, g.k1, g.drop);
+    if (g.drop) {
+      const U4 w = draw4(RowPart((uint32_t)row, g.step, g.site, g.k0, g.k1),
+                         ColPart(((uint32_t)c0 >> 2) + lane, g.step, g.k0), g.k0, g.k1);
+      keep = (uint32_t)(w.x >= g.drop) | (uint32_t)(w.y >= g.drop) << 1 | (uint32_t)(w.z >= g.drop) << 2 |
+             (uint32_t)(w.w >= g.drop) << 3;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = c0 + 32 * i + lane;
       const uint32_t k = __shfl_sync(0xffffffffu, keep, 8 * i + (lane >> 2)) >> (lane & 3) & 1;
-      float v = k ? Elem<T>::to_f(x[i]) * g.up : 0.f;
+      float v = !g.drop ? Elem<T>::to_f(x[i]) : k ? Elem<T>::to_f(x[i]) * g.up : 0.f;
       if (g.res) v += Elem<T>::to_f(r[i]);
       if (c < g.d) g.y[row * g.d + c] = Elem<T>::from_f(v);
     }
@@ -117,9 +153,13 @@ void run(Args<T> a, cudaStream_t st) {
   if (vec) {
     a.shift = 0;
     while (a.shift < 8 && (8 << a.shift) < a.d) ++a.shift;
-    const int64_t across = ceil_div(a.d, 8 << a.shift), down = ceil_div(a.rows, 256 >> a.shift);
-    launch_pdl(k_drop8<T>, dim3((unsigned)across, (unsigned)std::min<int64_t>(down, std::max<int64_t>(1, 8 * kSms / across))),
-               dim3(256), 0, st, a);
+    const bool wide = a.shift >= 5;
+    const int64_t across = ceil_div(a.d, 8 << a.shift), at_once = wide ? 1 : 256 >> a.shift;
+    // blocks for every SM to be full, as many rows each as that leaves
+    const int64_t most = std::max<int64_t>(1, (wide ? 8 * (256 >> a.shift) : 8) * kSms / across);
+    const dim3 grid((unsigned)across, (unsigned)std::min<int64_t>(std::min<int64_t>(ceil_div(a.rows, at_once), most), 65535));
+    if (wide) launch_pdl(k_drop8<T, true>, grid, dim3(1u << a.shift), 0, st, a);
+    else launch_pdl(k_drop8<T, false>, grid, dim3(256), 0, st, a);
   } else {
     const int64_t blocks = ceil_div(a.rows * ceil_div(a.d, 128), 8);
     launch_pdl(k_drop1<T>, dim3((unsigned)std::min<int64_t>(blocks, 8 * kSms)), dim3(256), 0, st, a);

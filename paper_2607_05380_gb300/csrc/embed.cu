@@ -15,6 +15,7 @@
 // any others.  Rows without a token are zeroed beside the first level's sums: a
 // bit per row says which they are.
 #include <algorithm>
+#include <type_traits>
 
 #include "lanes.cuh"
 #include "prod.cuh"
@@ -37,39 +38,93 @@ struct Ids {
   }
 };
 
-// kE = 8 columns by 16-byte loads and stores, or one.
+// kE neighbouring columns of a row, as they were read, by loads and stores of up
+// to 16 bytes that their address is a multiple of.
 template <typename T, int kE>
-__device__ __forceinline__ void load_cols(const T* p, float (&v)[kE], bool there) {
-  if constexpr (kE == 1) {
-    v[0] = there ? Elem<T>::to_f(p[0]) : 0.f;
-  } else {
-    Lane<T, 1, 1, 8> l;
-    l.load(p, 0, there ? 8 : 0);
-    l.get(0, v);
+struct Cols {
+  static constexpr int kBytes = (int)sizeof(T) * kE, kWords = kBytes < 4 ? 1 : kBytes / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T* p, bool there) {
+    if constexpr (kBytes == 2) {
+      w[0] = there ? *reinterpret_cast<const uint16_t*>(p) : 0u;
+    } else if constexpr (kBytes == 4) {
+      w[0] = there ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+    } else if constexpr (kBytes == 8) {
+      const uint2 v = there ? *reinterpret_cast<const uint2*>(p) : make_uint2(0u, 0u);
+      w[0] = v.x, w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int h = 0; h < kBytes / 16; ++h) {
+        const uint4 v = there ? reinterpret_cast<const uint4*>(p)[h] : make_uint4(0u, 0u, 0u, 0u);
+        w[4 * h] = v.x, w[4 * h + 1] = v.y, w[4 * h + 2] = v.z, w[4 * h + 3] = v.w;
+      }
+    }
   }
-}
-template <typename T, int kE>
-__device__ __forceinline__ void store_cols(T* p, const float (&v)[kE]) {
-  if constexpr (kE == 1) p[0] = Elem<T>::from_f(v[0]);
-  else Lane<T, 1, 1, 8>::put(p, 0, 0, 8, v);
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+  }
+  static __device__ __forceinline__ void put(T* p, const float (&v)[kE]) {
+    uint32_t w[kWords];
+    if constexpr (kBytes == 2) {
+      *p = Elem<T>::from_f(v[0]);
+      return;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          w[i] = __float_as_uint(v[i]);
+        } else {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+          w[i] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+      }
+      if constexpr (kBytes == 4) {
+        *reinterpret_cast<uint32_t*>(p) = w[0];
+      } else if constexpr (kBytes == 8) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+      } else {
+#pragma unroll
+        for (int h = 0; h < kBytes / 16; ++h)
+          reinterpret_cast<uint4*>(p)[h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
+      }
+    }
+  }
+};
+// Do rows of d elements of `bytes` each, ld apart, allow loads of e of them at once?
+bool fits(const void* p, int64_t ld, int d, int bytes, int e) {
+  const int b = std::min(16, bytes * e);
+  return d % e == 0 && ((uintptr_t)p % b) == 0 && (ld * bytes) % b == 0;
 }
 
-// Lanes a row (a power of two) and the columns they take together: kI groups
-// of kE columns a lane.
+// How a row's columns are spread: 2^shift lanes a row, kI = `items` groups of
+// kE = e columns a lane, the lanes' groups side by side.
 struct Split {
-  int shift, items;
+  int e, shift, items;
+  int64_t width() const { return (int64_t)(e * items) << shift; }
 };
-Split split_cols(int d, int e) {
-  const int groups = (int)ceil_div(d, e);
-  Split best{5, 1};
-  int64_t least = INT64_MAX;
-  for (int items = 1; items <= (e == 1 ? 5 : 1); ++items)
-    for (int shift = e == 1 && d >= 8 ? 3 : 0; shift <= 5; ++shift) {
-      // idle lanes cost most, then the keys that every block of columns reads again
-      const int64_t w = (int64_t)items << shift, cost = ceil_div(groups, w) * (w * 16 + 24) + (1 << shift) / 8;
-      if (cost < least) least = cost, best = Split{shift, items};
-    }
-  return best;
+// A warp a row where the row is wide enough for it, with as few columns a lane as
+// that takes (the longest chain of a lane's work is what counts); e_most: what
+// the addresses allow.
+Split split_cols(int d, int e_most) {
+  Split s{1, 5, 1};
+  while (s.e < e_most && s.e * 32 < d) s.e *= 2;
+  while (s.shift > 0 && (s.e << (s.shift - 1)) >= d) --s.shift;
+  if (s.e == 1) s.items = (int)std::min<int64_t>(4, ceil_div(d, 32));
+  return s;
+}
+// f(kE, kI) of a split
+template <typename F>
+void with_split(const Split& s, F f) {
+  using std::integral_constant;
+  using One = integral_constant<int, 1>;
+  if (s.e == 8) f(integral_constant<int, 8>(), One());
+  else if (s.e == 4) f(integral_constant<int, 4>(), One());
+  else if (s.e == 2) f(integral_constant<int, 2>(), One());
+  else if (s.items == 1) f(One(), One());
+  else if (s.items == 2) f(One(), integral_constant<int, 2>());
+  else if (s.items == 3) f(One(), integral_constant<int, 3>());
+  else f(One(), integral_constant<int, 4>());
 }
 
 // ------------------------------------------------------------------- lookup
@@ -79,15 +134,15 @@ struct LookArgs {
   const T* table;
   O* y;
   int64_t n, ldt;
-  int32_t d, shift, items;
+  int32_t d, shift;
   float scale;
 };
-template <typename T, typename O, int kE>
+template <typename T, typename O, int kE, int kI>
 __global__ void __launch_bounds__(256) k_lookup(const LookArgs<T, O> g) {
   constexpr int kU = 4;   // tokens in flight
   const int lanes = 1 << g.shift, groups = 256 >> g.shift;
   const int at = threadIdx.x & (lanes - 1), grp = threadIdx.x >> g.shift;
-  const int64_t t0 = (int64_t)blockIdx.x * (groups * kU) + grp;
+  const int64_t t0 = (int64_t)blockIdx.x * (groups * kU) + grp, c0 = ((int64_t)blockIdx.y * kI * lanes + at) * kE;
   pdl_trigger();
   pdl_wait();
   uint32_t id[kU];
@@ -96,93 +151,95 @@ __global__ void __launch_bounds__(256) k_lookup(const LookArgs<T, O> g) {
     const int64_t t = t0 + u * groups;
     id[u] = t < g.n ? g.ids.at(t) : (uint32_t)g.ids.vocab;
   }
-  for (int i = 0; i < g.items; ++i) {
-    const int64_t c = ((int64_t)blockIdx.y * g.items + i) * (lanes * kE) + at * kE;
-    if (c >= g.d) break;
-    float v[kU][kE];
+  Cols<T, kE> v[kU][kI];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const bool there = id[u] < (uint32_t)g.ids.vocab;
-      load_cols<T, kE>(g.table + (there ? (int64_t)id[u] * g.ldt : 0) + c, v[u], there);
+  for (int u = 0; u < kU; ++u) {
+    const bool there = id[u] < (uint32_t)g.ids.vocab;
+    const T* row = g.table + (there ? (int64_t)id[u] * g.ldt : 0) + c0;
+#pragma unroll
+    for (int i = 0; i < kI; ++i) v[u][i].load(row + i * lanes * kE, there && c0 + i * lanes * kE < g.d);
+  }
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    const int64_t t = t0 + u * groups;
+    if (t >= g.n) break;
+    const bool there = id[u] < (uint32_t)g.ids.vocab;
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      if (c0 + i * lanes * kE >= g.d) break;
+      float f[kE];
+#pragma unroll
+      for (int e = 0; e < kE; ++e) f[e] = there ? v[u][i].get(e) * g.scale : 0.f;   // (no -0, no NaN by the scale)
+      Cols<O, kE>::put(g.y + t * g.d + c0 + i * lanes * kE, f);
     }
+  }
+}
+
+// Rows of an odd number of columns: four neighbouring elements of y a thread,
+// whatever rows they belong to, by one store.  (140077 tokens of 33 columns, fp32:
+// a warp a row 13 us.)
+template <typename T, typename O>
+__global__ void __launch_bounds__(256) k_lookup_flat(const LookArgs<T, O> g) {
+  constexpr int kU = 2;   // times 256 groups of four a block
+  pdl_trigger();
+  pdl_wait();
+  const int64_t total = g.n * g.d, e0 = (int64_t)blockIdx.x * (1024 * kU), t0 = e0 / g.d;
+  const uint32_t off = (uint32_t)(e0 - t0 * g.d);
+  float v[kU][4];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int64_t t = t0 + u * groups;
-      if (t >= g.n) break;
-      const bool there = id[u] < (uint32_t)g.ids.vocab;
+  for (int u = 0; u < kU; ++u) {
+    const uint32_t e = off + 4 * (threadIdx.x + 256 * u);
+    uint32_t row = e / (uint32_t)g.d, c = e - row * (uint32_t)g.d;
+    uint32_t id = t0 + row < g.n ? g.ids.at(t0 + row) : (uint32_t)g.ids.vocab;
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[u][e] = there ? v[u][e] * g.scale : 0.f;
-      store_cols<O, kE>(g.y + t * g.d + c, v[u]);
+    for (int i = 0; i < 4; ++i) {
+      const bool there = id < (uint32_t)g.ids.vocab;
+      v[u][i] = there ? Elem<T>::to_f(g.table[(int64_t)id * g.ldt + c]) * g.scale : 0.f;
+      if (++c == (uint32_t)g.d) {
+        c = 0, ++row;
+        id = t0 + row < g.n ? g.ids.at(t0 + row) : (uint32_t)g.ids.vocab;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    const int64_t at = e0 + 4 * (threadIdx.x + 256 * u);
+    if (at + 4 <= total) {
+      Cols<O, 4>::put(g.y + at, v[u]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (at + i < total) g.y[at + i] = Elem<O>::from_f(v[u][i]);
     }
   }
 }
 
 // --------------------------------------------------------------------- sort
-// A block takes a tile of kTile tokens, a warp 32 kRounds of them in order.
-constexpr int kSortThreads = 512, kRounds = 8, kTile = kSortThreads * kRounds, kSortWarps = kSortThreads / 32;
-constexpr int kMaxBits = 10;   // of a pass: the warps' counts of a digit's values fit in shared memory beside a tile
+// Radix sort, stable, by digits of at most kMaxBits bits.  A block ranks the
+// tokens of a tile by its warps' counts of each digit.
+constexpr int kMaxBits = 10;   // the warps' counts of a digit's values fit in shared memory beside a tile
 
 struct SortArgs {
   Ids ids;                      // the first pass's keys; their places are its values
   const uint32_t *key, *val;    // the later ones'
   uint32_t *key_out, *val_out;
   uint32_t *count, *total;      // [bins][blocks]; [bins]
-  uint32_t* seen;               // a bit per row of the table
+  uint8_t* seen;                // a byte per row of the table: whether it has a token
   int64_t n;
-  int32_t first, last, shift, bits, blocks;
+  int32_t first, shift, bits, bits_all, blocks;
 };
+constexpr uint32_t kLast = 0xffffffffu;   // the key of a place past the last token: behind all others in every pass
 __device__ __forceinline__ uint32_t key_at(const SortArgs& g, int64_t i) { return g.first ? g.ids.at(i) : g.key[i]; }
-__device__ __forceinline__ int64_t seen_words(const SortArgs& g) { return ((int64_t)g.ids.vocab + 31) >> 5; }
-__device__ __forceinline__ void mark(const SortArgs& g, uint32_t key) {
-  if (key >= (uint32_t)g.ids.vocab) return;
-  uint32_t* w = g.seen + (key >> 5);
-  if (!(*(volatile uint32_t*)w >> (key & 31) & 1)) atomicOr(w, 1u << (key & 31));   // frequent values: once, then reads
-}
 
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const SortArgs g) {
-  __shared__ uint32_t h[1 << kMaxBits];
-  pdl_trigger();
-  pdl_wait();
-  const int bins = 1 << g.bits;
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) h[i] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = (int64_t)blockIdx.x * kTile + r * kSortThreads + threadIdx.x;
-    if (i < g.n) atomicAdd(&h[key_at(g, i) >> g.shift & (bins - 1)], 1u);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) g.count[(int64_t)i * g.blocks + blockIdx.x] = h[i];
-  if (g.first)
-    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < seen_words(g); i += (int64_t)g.blocks * kSortThreads)
-      g.seen[i] = 0;
-}
-
-// Where each block's tokens of a digit begin among the digit's: a warp a digit.
-__global__ void __launch_bounds__(256) k_sort_scan(uint32_t* count, uint32_t* total, int blocks, int bins) {
-  pdl_trigger();
-  pdl_wait();
-  const int bin = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (bin >= bins) return;
-  uint32_t* row = count + (int64_t)bin * blocks;
-  uint32_t before = 0;
-  for (int b = 0; b < blocks; b += 32) {
-    const uint32_t c = b + lane < blocks ? row[b + lane] : 0u;
-    uint32_t s = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += v;
-    }
-    if (b + lane < blocks) row[b + lane] = before + s - c;
-    before += __shfl_sync(0xffffffffu, s, 31);
-  }
-  if (lane == 0) total[bin] = before;
+__device__ __forceinline__ void clear_seen(const SortArgs& g, int64_t thread, int64_t threads) {
+  const int64_t words = ((int64_t)g.ids.vocab + 15) >> 4;
+  for (int64_t i = thread; i < words; i += threads) reinterpret_cast<uint4*>(g.seen)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Exclusive prefix sums of v[0 .. bins - 1] in shared memory, by the whole block.
+template <int kThreads>
 __device__ __forceinline__ void block_scan(uint32_t* v, int bins, uint32_t* warps) {
-  constexpr int kPer = (1 << kMaxBits) / kSortThreads;
+  constexpr int kPer = (1 << kMaxBits) / kThreads, kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t c[kPer], s = 0;
 #pragma unroll
@@ -199,8 +256,10 @@ __device__ __forceinline__ void block_scan(uint32_t* v, int bins, uint32_t* warp
   }
   if (lane == 31) warps[warp] = t;
   __syncthreads();
-  uint32_t before = t - s;
-  for (int w = 0; w < warp; ++w) before += warps[w];
+  uint32_t before = lane < warp && lane < kWarps ? warps[lane] : 0u;   // the warps before this one
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+  before += t - s;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int at = threadIdx.x * kPer + i;
@@ -212,18 +271,25 @@ __device__ __forceinline__ void block_scan(uint32_t* v, int bins, uint32_t* warp
 
 // Each token's number among those of its digit in its warp (in order), and in
 // wh the warps' counts; afterwards wh holds, per warp and digit, the tokens of
-// the warps before it, and sum (if wanted) the block's counts.
-__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kRounds], int shift, int bits, uint16_t* wh, uint32_t* sum,
-                                          uint32_t (&rank)[kRounds]) {
+// the warps before it, and sum (if wanted) the block's counts.  The lanes of one
+// digit find each other by a ballot per bit: 170 issue slots a warp and round, the
+// most of a pass's work (masks or-ed in shared memory, or match.any: as much
+// for spread digits, more for frequent ones).
+template <int kThreads, int kR>
+__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, int bits, uint16_t* wh, uint32_t* sum,
+                                          uint32_t (&rank)[kR]) {
+  constexpr int kWarps = kThreads / 32;
   const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < bins * kSortWarps; i += kSortThreads) wh[i] = 0;
+  for (int i = threadIdx.x; i < bins * kWarps / 2; i += kThreads) ((uint32_t*)wh)[i] = 0;
   __syncthreads();
   uint16_t* mine = wh + warp * bins;
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < kR; ++r) {
     const uint32_t digit = key[r] >> shift & (bins - 1);
     uint32_t same = 0xffffffffu;
-    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int b = 0; b < kMaxBits; ++b) {
+      if (b >= bits) break;
       const uint32_t set = __ballot_sync(0xffffffffu, digit >> b & 1);
       same &= digit >> b & 1 ? set : ~set;
     }
@@ -234,19 +300,83 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kRounds], int sh
     __syncwarp();
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) {
+  for (int i = threadIdx.x; i < bins; i += kThreads) {
     uint32_t s = 0;
+#pragma unroll 1
+    for (int w0 = 0; w0 < kWarps; w0 += 8) {   // eight loads in flight
+      uint32_t c[8];
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = wh[w * bins + i];
-      wh[w * bins + i] = (uint16_t)s;
-      s += c;
+      for (int w = 0; w < 8; ++w) c[w] = wh[(w0 + w) * bins + i];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        wh[(w0 + w) * bins + i] = (uint16_t)s;
+        s += c[w];
+      }
     }
     if (sum) sum[i] = s;
   }
   __syncthreads();
 }
 
+// Many tokens: three launches a pass, a tile of kRounds tokens a thread a block.
+constexpr int kSortThreads = 512;
+
+template <int kRounds>
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const SortArgs g) {
+  __shared__ uint32_t h[1 << kMaxBits];
+  pdl_trigger();
+  pdl_wait();
+  const int bins = 1 << g.bits;
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) h[i] = 0;
+  uint32_t key[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t i = (int64_t)blockIdx.x * (kSortThreads * kRounds) + r * kSortThreads + threadIdx.x;
+    key[r] = i < g.n ? key_at(g, i) : kLast;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r)
+    if (key[r] != kLast) atomicAdd(&h[key[r] >> g.shift & (bins - 1)], 1u);
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) g.count[(int64_t)i * g.blocks + blockIdx.x] = h[i];
+  if (g.first) clear_seen(g, (int64_t)blockIdx.x * kSortThreads + threadIdx.x, (int64_t)g.blocks * kSortThreads);
+}
+
+// Where each block's tokens of a digit begin among the digit's: a warp a digit.
+__global__ void __launch_bounds__(256) k_sort_scan(uint32_t* count, uint32_t* total, int blocks, int bins) {
+  pdl_trigger();
+  pdl_wait();
+  const int bin = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (bin >= bins) return;
+  uint32_t* row = count + (int64_t)bin * blocks;
+  uint32_t before = 0;
+  for (int b = 0; b < blocks; b += 128) {   // four a lane
+    uint32_t c[4], s = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = b + 4 * lane + i;
+      c[i] = at < blocks ? row[at] : 0u;
+      s += c[i];
+    }
+    uint32_t t = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += v;
+    }
+    uint32_t at_lane = before + t - s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (b + 4 * lane + i < blocks) row[b + 4 * lane + i] = at_lane;
+      at_lane += c[i];
+    }
+    before += __shfl_sync(0xffffffffu, t, 31);
+  }
+  if (lane == 0) total[bin] = before;
+}
+
+template <int kRounds>
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const SortArgs g) {
   extern __shared__ uint32_t sm[];
   uint32_t* base = sm;
@@ -254,64 +384,137 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const SortArgs g)
   const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   pdl_wait();
-  const int64_t i0 = (int64_t)blockIdx.x * kTile + warp * (32 * kRounds) + lane;
-  uint32_t key[kRounds], rank[kRounds];
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) key[r] = i0 + 32 * r < g.n ? key_at(g, i0 + 32 * r) : 0xffffffffu;
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) base[i] = g.total[i];
-  __syncthreads();
-  block_scan(base, bins, sm + bins);
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) base[i] += g.count[(int64_t)i * g.blocks + blockIdx.x];
-  rank_tile(key, g.shift, g.bits, wh, nullptr, rank);
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = i0 + 32 * r;
-    if (i >= g.n) break;
-    const uint32_t digit = key[r] >> g.shift & (bins - 1);
-    const uint32_t to = base[digit] + wh[warp * bins + digit] + rank[r];
-    g.key_out[to] = key[r];
-    g.val_out[to] = g.first ? (uint32_t)i : g.val[i];
-    if (g.last) mark(g, key[r]);
-  }
-}
-
-// Up to kTile tokens: every pass in one block.
-__global__ void __launch_bounds__(kSortThreads) k_sort_tile(const SortArgs g, int bits_all) {
-  extern __shared__ uint32_t sm[];
-  uint32_t *ks = sm, *vs = sm + kTile, *base = vs + kTile;
-  uint16_t* wh = (uint16_t*)(base + (1 << g.bits) + 32);
-  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();
-  pdl_wait();
-  const int i0 = warp * (32 * kRounds) + lane;
+  const int64_t i0 = (int64_t)blockIdx.x * (kSortThreads * kRounds) + warp * (32 * kRounds) + lane;
   uint32_t key[kRounds], val[kRounds], rank[kRounds];
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
-    val[r] = i0 + 32 * r;
-    key[r] = (int)val[r] < g.n ? key_at(g, val[r]) : 0xffffffffu;   // (behind all others in every pass)
+    const int64_t i = i0 + 32 * r;
+    key[r] = i < g.n ? key_at(g, i) : kLast;
+    val[r] = g.first ? (uint32_t)i : i < g.n ? g.val[i] : 0u;
   }
-  for (int64_t i = threadIdx.x; i < seen_words(g); i += kSortThreads) g.seen[i] = 0;
-  for (int shift = 0; shift < bits_all; shift += g.bits) {
-    rank_tile(key, shift, g.bits, wh, base, rank);
-    block_scan(base, bins, base + bins);
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      const uint32_t digit = key[r] >> shift & (bins - 1);
-      const uint32_t to = base[digit] + wh[warp * bins + digit] + rank[r];
-      ks[to] = key[r], vs[to] = val[r];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) key[r] = ks[i0 + 32 * r], val[r] = vs[i0 + 32 * r];
-    __syncthreads();
-  }
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) base[i] = g.total[i];
+  __syncthreads();
+  block_scan<kSortThreads>(base, bins, sm + bins);
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) base[i] += g.count[(int64_t)i * g.blocks + blockIdx.x];
+  rank_tile<kSortThreads>(key, g.shift, g.bits, wh, nullptr, rank);
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
-    const int i = i0 + 32 * r;
-    if (i >= g.n) break;
-    g.key_out[i] = key[r], g.val_out[i] = val[r];
-    mark(g, key[r]);
+    if (i0 + 32 * r >= g.n) continue;
+    const uint32_t digit = key[r] >> g.shift & (bins - 1);
+    const uint32_t to = base[digit] + wh[warp * bins + digit] + rank[r];
+    g.key_out[to] = key[r];
+    g.val_out[to] = val[r];
   }
+}
+
+// Up to 64 K tokens: every pass in one launch of a cluster of kCluster blocks,
+// which keep the tokens in registers and hand them over through each other's
+// shared memory.  A block sorts its own by the digit first: neighbours then go
+// to neighbouring places (one 4-byte store each to a place of its own: 38 us for
+// 49152 tokens and two passes).
+constexpr int kCluster = 16, kClusterThreads = 512;
+__device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <int kR>
+constexpr int cluster_smem(int bits) {   // tokens sent and received; counts, three bases and the scan's; the warps' counts
+  return 2 * kR * kClusterThreads * 8 + (4 * (1 << bits) + 32) * 4 + (1 << bits) * (kClusterThreads / 32) * 2;
+}
+template <int kR>
+__global__ void __launch_bounds__(kClusterThreads, 1) k_sort_cluster(const SortArgs g) {
+  constexpr int kPer = kR * kClusterThreads;   // tokens a block
+  extern __shared__ __align__(16) uint32_t sm[];
+  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint2 *sent = (uint2*)sm, *got = sent + kPer;
+  uint32_t *cnt = (uint32_t*)(got + kPer), *local = cnt + bins, *below = local + bins, *base = below + bins;
+  uint16_t* wh = (uint16_t*)(base + bins + 32);
+  const uint32_t rank_of = blockIdx.x;         // (one cluster)
+  pdl_trigger();
+  pdl_wait();
+  const int at0 = warp * (32 * kR) + lane;
+  uint32_t key[kR], val[kR], rank[kR];
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    val[r] = rank_of * kPer + at0 + 32 * r;
+    key[r] = (int64_t)val[r] < g.n ? g.ids.at(val[r]) : kLast;
+  }
+  clear_seen(g, rank_of * kClusterThreads + threadIdx.x, kCluster * kClusterThreads);
+  for (int shift = 0; shift < g.bits_all; shift += g.bits) {
+    rank_tile<kClusterThreads>(key, shift, g.bits, wh, cnt, rank);
+    cluster_barrier();   // all counts are there, and all tokens of the pass before have been read
+    // what the blocks have of a digit: four lanes a digit look at four blocks each
+    for (int i = threadIdx.x; i < 4 * bins; i += kClusterThreads) {
+      const int bin = i >> 2, b0 = (i & 3) * (kCluster / 4);
+      uint32_t c[kCluster / 4], all = 0, low = 0;
+#pragma unroll
+      for (int b = 0; b < kCluster / 4; ++b)
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[b]) : "r"(cluster_address(cnt + bin, b0 + b)));
+#pragma unroll
+      for (int b = 0; b < kCluster / 4; ++b) all += c[b], low += b0 + b < (int)rank_of ? c[b] : 0u;
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        low += __shfl_xor_sync(0xffffffffu, low, o);
+      }
+      if ((i & 3) == 0) base[bin] = all, local[bin] = cnt[bin], below[bin] = low;
+    }
+    __syncthreads();
+    block_scan<kClusterThreads>(local, bins, base + bins);
+    block_scan<kClusterThreads>(base, bins, base + bins);
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const uint32_t digit = key[r] >> shift & (bins - 1);
+      sent[local[digit] + wh[warp * bins + digit] + rank[r]] = make_uint2(key[r], val[r]);
+    }
+    for (int i = threadIdx.x; i < bins; i += kClusterThreads)   // from a block's own place to the cluster's
+      base[i] += below[i] - local[i];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const int i = threadIdx.x + r * kClusterThreads;
+      const uint2 t = sent[i];
+      const uint32_t to = base[t.x >> shift & (bins - 1)] + i, block = to / kPer, place = to % kPer;
+      asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(cluster_address(got + place, block)), "r"(t.x), "r"(t.y)
+                   : "memory");
+    }
+    cluster_barrier();
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const uint2 t = got[at0 + 32 * r];
+      key[r] = t.x, val[r] = t.y;
+    }
+  }
+  const int64_t i0 = (int64_t)rank_of * kPer + at0;
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+    if (i0 + 32 * r < g.n) g.key_out[i0 + 32 * r] = key[r], g.val_out[i0 + 32 * r] = val[r];
+}
+
+// A few tokens: each one's place is the number of those before it.
+constexpr int kFew = 1024;
+__global__ void __launch_bounds__(kFew) k_sort_few(const SortArgs g) {
+  __shared__ __align__(16) uint32_t ks[kFew];
+  pdl_trigger();
+  pdl_wait();
+  const int i = threadIdx.x, n4 = ((int)g.n + 3) >> 2;
+  const uint32_t key[1] = {i < g.n ? g.ids.at(i) : kLast};
+  ks[i] = key[0];
+  clear_seen(g, i, blockDim.x);
+  __syncthreads();
+  uint32_t to = 0;
+#pragma unroll 4
+  for (int j = 0; j < n4; ++j) {
+    const uint4 k = reinterpret_cast<const uint4*>(ks)[j];
+    to += (k.x < key[0]) + (k.y < key[0]) + (k.z < key[0]) + (k.w < key[0]);
+    to += (k.x == key[0] && 4 * j < i) + (k.y == key[0] && 4 * j + 1 < i) + (k.z == key[0] && 4 * j + 2 < i) +
+          (k.w == key[0] && 4 * j + 3 < i);
+  }
+  if (i < g.n) g.key_out[to] = key[0], g.val_out[to] = i;
 }
 
 // --------------------------------------------------------------------- runs
@@ -320,49 +523,62 @@ struct RunArgs {
   const uint32_t *key, *val;    // val: the rows of src (NULL: one after another)
   const T* src;
   O* out;
-  uint32_t* key_out;            // two entries a chunk
+  uint32_t* key_out;            // two entries a block
   float* part;
-  const uint32_t* seen;         // first level: rows to be zeroed (NULL: none)
-  int64_t m, ld, chunks;
-  int32_t chunk, d, vocab, shift, items, run_blocks;
+  uint8_t* seen;                // the table's rows that have a token: the first level says, beside the second the others
+                                // are zeroed
+  int64_t m, ld;
+  int32_t chunk, d, vocab, shift, run_blocks, first, wide;   // wide: out's rows start at multiples of 16 bytes
   float scale;
 };
 
+// Rows without a token become zero: a warp takes 32 of them, 2^shift lanes a row,
+// by 16-byte stores where the rows lie on multiples of 16 bytes.
 template <typename O, int kE>
-__device__ __forceinline__ void zero_rows(const uint32_t* seen, O* out, int64_t vocab, int d, int shift, int64_t block,
-                                          int64_t blocks) {
-  const int lanes = 1 << shift, at = threadIdx.x & (lanes - 1);
+__device__ __forceinline__ void zero_rows(const uint8_t* seen, O* out, int64_t vocab, int d, int64_t block, int64_t blocks) {
+  const int lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+  int shift = 0;
+  while (shift < 5 && (kE << shift) < d) ++shift;
+  const int at = lane & ((1 << shift) - 1), sub = lane >> shift, step = 32 >> shift;
   const float zero[kE] = {};
-  for (int64_t r = block * (256 >> shift) + (threadIdx.x >> shift); r < vocab; r += blocks * (256 >> shift)) {
-    if (seen[r >> 5] >> (r & 31) & 1) continue;
-    for (int64_t c = at * kE; c < d; c += lanes * kE) store_cols<O, kE>(out + r * d + c, zero);
+  for (int64_t r0 = (block * warps + (threadIdx.x >> 5)) * 32; r0 < vocab; r0 += blocks * warps * 32) {
+    const uint32_t absent = __ballot_sync(0xffffffffu, r0 + lane < vocab && seen[r0 + lane] == 0);
+#pragma unroll 4
+    for (int r = sub; r < 32; r += step)
+      if (absent >> r & 1)
+        for (int64_t c = at * kE; c < d; c += kE << shift) Cols<O, kE>::put(out + (r0 + r) * d + c, zero);
   }
 }
 
-// A group of lanes takes a chunk of the sorted list and kI * kE of their
-// columns each.
+// A group of 2^shift lanes takes `chunk` entries of the sorted list, kI kE of
+// their columns a lane, a block the chunks of its groups.  What the groups leave
+// is joined in shared memory, what the block leaves goes to the next level.
+constexpr int kRunThreads = 512, kJoinThreads = 1024;   // of the first level; of the later ones
+constexpr int kMostEntries = 4096;                      // of a block
 template <typename T, typename O, int kE, int kI>
-__global__ void __launch_bounds__(256) k_runs(const RunArgs<T, O> g) {
-  constexpr int kU = kE == 1 ? 8 : 4;   // rows in flight
+__global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
+  constexpr int kWords = Cols<T, kE>::kWords * kI, kU = kWords >= 8 ? 4 : 8;   // rows in flight
+  extern __shared__ __align__(16) float rows[];           // two a group, then the block's keys and places
+  __shared__ uint32_t keys[2 * 1024];
   pdl_trigger();
   pdl_wait();
   if ((int)blockIdx.x >= g.run_blocks) {
-    if (blockIdx.y == 0)
-      zero_rows<O, kE>(g.seen, g.out, g.vocab, g.d, g.shift, blockIdx.x - g.run_blocks, gridDim.x - g.run_blocks);
+    if (blockIdx.y) return;
+    constexpr int kWide = 16 / sizeof(O);
+    const int64_t block = blockIdx.x - g.run_blocks, blocks = gridDim.x - g.run_blocks;
+    if (g.wide) zero_rows<O, kWide>(g.seen, g.out, g.vocab, g.d, block, blocks);
+    else zero_rows<O, 1>(g.seen, g.out, g.vocab, g.d, block, blocks);
     return;
   }
-  const int lanes = 1 << g.shift, at = threadIdx.x & (lanes - 1);
-  const int64_t q = (int64_t)blockIdx.x * (256 >> g.shift) + (threadIdx.x >> g.shift);
-  if (q >= g.chunks) return;
-  const int64_t first = q * g.chunk, end = min(first + g.chunk, g.m);
-  const int64_t c0 = (int64_t)blockIdx.y * kI * (lanes * kE) + at * kE;
-  const uint32_t none = 0xffffffffu;
-  const uint32_t before = first ? g.key[first - 1] & ~kSkip : none, after = end < g.m ? g.key[end] & ~kSkip : none;
-  uint32_t cur = g.key[first] & ~kSkip;
-  // what the chunk leaves in its two entries: nothing yet
-  uint32_t left0 = cur | kSkip, left1 = kSkip;
+  const int lanes = 1 << g.shift, groups = (int)blockDim.x >> g.shift, at = threadIdx.x & (lanes - 1);
+  const int grp = threadIdx.x >> g.shift, per_block = groups * g.chunk;
+  uint32_t* key_at = (uint32_t*)(rows + 2 * blockDim.x * (kI * kE));
+  uint32_t* val_at = key_at + per_block;
+  const int64_t b0 = (int64_t)blockIdx.x * per_block, c0 = ((int64_t)blockIdx.y * kI * lanes + at) * kE;
+  const int n_here = (int)min((int64_t)per_block, g.m - b0);
+  const int i_first = min(grp * g.chunk, n_here), count = min(g.chunk, n_here - i_first);
   float acc[kI][kE];
-  bool any = false, head = true;
+  bool any = false;
   auto clear = [&] {
 #pragma unroll
     for (int i = 0; i < kI; ++i)
@@ -370,84 +586,134 @@ __global__ void __launch_bounds__(256) k_runs(const RunArgs<T, O> g) {
       for (int e = 0; e < kE; ++e) acc[i][e] = 0.f;
     any = false;
   };
-  auto finish = [&](bool tail) {
-    const bool from = head && before == cur, on = tail && after == cur;
-    if (any) {
-      if (!from && !on) {
+  auto write = [&](uint32_t row) {   // a finished sum
+    O* out = g.out + (int64_t)row * g.d + c0;
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-          const int64_t c = c0 + (int64_t)i * (lanes * kE);
-          float v[kE];
+    for (int i = 0; i < kI; ++i) {
+      float v[kE];
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[e] = acc[i][e] * g.scale;
-          if (c < g.d) store_cols<O, kE>(g.out + (int64_t)cur * g.d + c, v);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kI; ++i) {
-          const int64_t c = c0 + (int64_t)i * (lanes * kE);
-          if (c < g.d) store_cols<float, kE>(g.part + (2 * q + (from ? 0 : 1)) * g.d + c, acc[i]);
-        }
-        if (from) left0 = cur;
-        else left1 = cur;
-      }
+      for (int e = 0; e < kE; ++e) v[e] = acc[i][e] * g.scale;
+      if (c0 + i * lanes * kE < g.d) Cols<O, kE>::put(out + i * lanes * kE, v);
     }
-    head = false;
+  };
+  // an entry's row, the lanes' columns side by side
+  auto slot = [&](int entry, int i) { return rows + (entry * kI + i) * (lanes * kE) + at * kE; };
+  for (int i = threadIdx.x; i < n_here; i += blockDim.x) {
+    const uint32_t key = g.key[b0 + i];
+    key_at[i] = key;
+    val_at[i] = g.val ? g.val[b0 + i] : (uint32_t)(b0 + i);
+    // the first token of a row says that the row has one
+    if (g.first && blockIdx.y == 0 && key < (uint32_t)g.vocab && (b0 + i == 0 || g.key[b0 + i - 1] != key)) g.seen[key] = 1;
+  }
+  const uint32_t block_before = b0 ? g.key[b0 - 1] & ~kSkip : kLast;
+  const uint32_t block_after = b0 + n_here < g.m ? g.key[b0 + n_here] & ~kSkip : kLast;
+  __syncthreads();
+  const uint32_t before = i_first ? key_at[i_first - 1] & ~kSkip : block_before;
+  const uint32_t after = i_first + count < n_here ? key_at[i_first + count] & ~kSkip : block_after;
+  uint32_t cur = count ? key_at[i_first] & ~kSkip : kLast;
+  uint32_t left0 = cur | kSkip, left1 = kLast;   // what the group leaves: nothing yet
+  bool open = before == cur;                     // the run began before the group
+  auto leave = [&](int entry) {
+#pragma unroll
+    for (int i = 0; i < kI; ++i) Cols<float, kE>::put(slot(2 * grp + entry, i), acc[i]);
+    if (entry) left1 = cur;
+    else left0 = cur;
   };
   clear();
-  for (int64_t i0 = first; i0 < end; i0 += kU) {
+  // all groups of a warp take the same number of steps, so that they meet again after each
+#pragma unroll 1
+  for (int i0 = 0; i0 < g.chunk; i0 += kU) {
+    Cols<T, kE> v[kU][kI];
     uint32_t key[kU];
-    float v[kU][kI][kE];
-#pragma unroll
-    for (int u = 0; u < kU; ++u) key[u] = i0 + u < end ? g.key[i0 + u] : none;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
+      key[u] = i0 + u < count ? key_at[i_first + i0 + u] : kLast;
       const bool there = key[u] < (uint32_t)g.vocab;   // (neither skipped nor outside the table)
-      const int64_t row = !there ? 0 : g.val ? (int64_t)g.val[i0 + u] : i0 + u;
+      const T* row = g.src + (there ? (int64_t)val_at[i_first + i0 + u] * g.ld : 0) + c0;
 #pragma unroll
-      for (int i = 0; i < kI; ++i) {
-        const int64_t c = c0 + (int64_t)i * (lanes * kE);
-        load_cols<T, kE>(g.src + row * g.ld + c, v[u][i], there && c < g.d);
-      }
+      for (int i = 0; i < kI; ++i) v[u][i].load(row + i * lanes * kE, there && c0 + i * lanes * kE < g.d);
     }
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      if (i0 + u >= end) break;
-      const uint32_t k = key[u] & ~kSkip;
-      if (k != cur) {
-        finish(false);
+      if (key[u] != kLast && (key[u] & ~kSkip) != cur) {
+        if (any) {
+          if (open) leave(0);
+          else write(cur);
+        }
         clear();
-        cur = k;
+        cur = key[u] & ~kSkip, open = false;
       }
-      if (key[u] < (uint32_t)g.vocab) {
-        any = true;
+      __syncwarp();
+      any = any || key[u] < (uint32_t)g.vocab;
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
+      for (int i = 0; i < kI; ++i)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) acc[i][e] += v[u][i][e];
-      }
+        for (int e = 0; e < kE; ++e) acc[i][e] += v[u][i].get(e);   // (zeros where there is none)
     }
   }
-  finish(true);
-  if (g.key_out && at == 0 && blockIdx.y == 0) {
-    g.key_out[2 * q] = left0;
-    g.key_out[2 * q + 1] = left1 == kSkip ? cur | kSkip : left1;
+  if (any) {
+    if (open) leave(0);
+    else if (after == cur) leave(1);
+    else write(cur);
+  }
+  if (at == 0) {   // (a group without entries: kLast)
+    keys[2 * grp] = left0;
+    keys[2 * grp + 1] = left1 == kLast ? cur | kSkip : left1;
+  }
+  __syncthreads();
+  const int n = 2 * ((n_here + g.chunk - 1) / g.chunk);   // entries that the block's groups have left
+  // a run of entries is summed by the group that left its first one
+#pragma unroll 1
+  for (int e = 2 * grp; e < min(2 * grp + 2, n); ++e) {
+    const uint32_t key = keys[e] & ~kSkip;
+    if (e && (keys[e - 1] & ~kSkip) == key) continue;
+    clear();
+    int j = e;
+    for (; j < n && (keys[j] & ~kSkip) == key; ++j) {
+      if (keys[j] & kSkip) continue;
+      any = true;
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int c = 0; c < kE; ++c) acc[i][c] += slot(j, i)[c];
+    }
+    const bool from = e == 0 && block_before == key, on = j == n && block_after == key;
+    if (any && !from && !on) write(key);
+    if (!g.key_out) continue;
+    const bool left = any && (from || on);
+    if (left) {
+      float* part = g.part + (2 * (int64_t)blockIdx.x + (from ? 0 : 1)) * g.d + c0;
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        if (c0 + i * lanes * kE < g.d) Cols<float, kE>::put(part + i * lanes * kE, acc[i]);
+    }
+    // the block's two entries: of its first run and of its last; where these are one run, the second holds nothing
+    if (at == 0 && blockIdx.y == 0) {
+      uint32_t* out = g.key_out + 2 * (int64_t)blockIdx.x;
+      if (e == 0) out[0] = left && from ? key : key | kSkip;
+      if (j == n) out[1] = left && !from ? key : key | kSkip;
+    }
   }
 }
 
 // --------------------------------------------------------------------- host
-// Sizes of a backward call and where its workspace's parts begin.
-constexpr int kLevels = 12;   // a level has at most an eighth of the entries before
+constexpr int kLevels = 16;   // a level has at most a quarter of the entries before
+
+// Sizes of a backward call and where its workspace's parts begin; e: columns a
+// lane takes at once.
 struct Plan {
-  int32_t bits_all, bits, passes, chunk[kLevels], levels = 0;
-  int64_t blocks, m[kLevels];
+  Split split;
+  int32_t bits_all, bits, passes, rounds, chunk[kLevels], levels = 0;
+  int64_t blocks, m[kLevels], run_blocks[kLevels];
   int64_t key[2], val[2], count, total, seen, part_key[kLevels], part[kLevels], bytes;
-  Plan(int64_t n, int32_t vocab, int32_t d) {
+  Plan(int64_t n, int32_t vocab, int32_t d, int e) {
+    split = split_cols(d, e);
     bits_all = 0;
     while (bits_all < 31 && (uint32_t)vocab >> bits_all) ++bits_all;
     passes = (int32_t)ceil_div(bits_all, kMaxBits);
-    bits = (int32_t)ceil_div(bits_all, passes);
-    blocks = ceil_div(n, kTile);
+    bits = std::max<int32_t>(3, (int32_t)ceil_div(bits_all, passes));   // (whole warps of four lanes a digit)
+    rounds = n <= 2 * kSortThreads * 2 * kSms ? 2 : 8;
+    blocks = ceil_div(n, kSortThreads * rounds);
     Carver c(nullptr);
     auto take = [&](int64_t b) {
       const int64_t at = c.used;
@@ -457,102 +723,146 @@ struct Plan {
     for (int i = 0; i < 2; ++i) key[i] = take(n * 4), val[i] = take(n * 4);
     count = take(blocks * 4 << bits);
     total = take(4 << bits);
-    seen = take(ceil_div(vocab, 32) * 4);
-    // tokens a chunk: enough chunks for every lane of the GPU, but partial rows are written and read again
-    int64_t left = n;
-    do {
-      int64_t c2 = 16;
-      while (c2 < 64 && ceil_div(left, 2 * c2) * std::min<int64_t>(d, 256) >= int64_t(kSms) * 2048 * 4) c2 *= 2;
-      chunk[levels] = (int32_t)c2;
-      m[levels] = left;
-      left = 2 * ceil_div(left, c2);
-      if (m[levels] > c2) part_key[levels] = take(left * 4), part[levels] = take(left * d * 4);
-      ++levels;
-    } while (m[levels - 1] > chunk[levels - 1]);
+    seen = take(round_up(vocab, 16));
+    for (int64_t left = n;;) {
+      // entries a group: 16, or 32 where the blocks fill the GPU several times all the same; one block takes what
+      // is left once it can with 32
+      const int64_t groups = (levels ? kJoinThreads : kRunThreads) >> split.shift;
+      int64_t per = levels == 0 && left >= groups * 32 * 4 * kSms ? 32 : 16;
+      per = std::min(per, kMostEntries / groups);
+      if (levels && left <= std::min<int64_t>(32 * groups, kMostEntries)) per = std::max<int64_t>(1, ceil_div(left, groups));
+      m[levels] = left, chunk[levels] = (int32_t)per, run_blocks[levels] = ceil_div(left, groups * per);
+      left = 2 * run_blocks[levels];
+      if (run_blocks[levels++] == 1 && levels > 1) break;   // (two at least: the second one zeroes)
+      part_key[levels - 1] = take(left * 4), part[levels - 1] = take(left * d * 4);
+    }
     bytes = c.used;
   }
 };
 
-template <typename T, typename O, int kE>
-void run_level(RunArgs<T, O> a, int64_t zero_blocks, cudaStream_t st) {
-  const Split s = split_cols(a.d, kE);
-  a.shift = s.shift, a.items = s.items;
-  a.run_blocks = (int32_t)ceil_div(a.chunks, 256 >> s.shift);
-  const dim3 grid((unsigned)(a.run_blocks + zero_blocks), (unsigned)ceil_div(a.d, (int64_t)s.items * kE << s.shift));
-  if constexpr (kE == 8) {
-    launch_pdl(k_runs<T, O, 8, 1>, grid, dim3(256), 0, st, a);
-  } else {
-    if (s.items == 1) launch_pdl(k_runs<T, O, 1, 1>, grid, dim3(256), 0, st, a);
-    else if (s.items == 2) launch_pdl(k_runs<T, O, 1, 2>, grid, dim3(256), 0, st, a);
-    else if (s.items == 3) launch_pdl(k_runs<T, O, 1, 3>, grid, dim3(256), 0, st, a);
-    else if (s.items == 4) launch_pdl(k_runs<T, O, 1, 4>, grid, dim3(256), 0, st, a);
-    else launch_pdl(k_runs<T, O, 1, 5>, grid, dim3(256), 0, st, a);
-  }
+// Of a call whatever its addresses allow.
+int64_t plan_bytes(int64_t n, int32_t vocab, int32_t d) {
+  int64_t most = 0;
+  for (int e = 1; e <= 8 && d % e == 0; e *= 2) most = std::max(most, Plan(n, vocab, d, e).bytes);
+  return most;
 }
 
 template <typename T, typename O>
-void backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32_t d, float scale, O* out, char* ws, cudaStream_t st) {
-  const Plan p(n, ids.vocab, d);
+cudaError_t run_level(RunArgs<T, O> a, const Split& s, int threads, int64_t zero_blocks, cudaStream_t st) {
+  a.shift = s.shift;
+  const dim3 grid((unsigned)(a.run_blocks + zero_blocks), (unsigned)ceil_div(a.d, s.width()));
+  const size_t smem = (size_t)2 * threads * s.e * s.items * 4 + (size_t)(threads >> s.shift) * a.chunk * 8;
+  cudaError_t e = cudaSuccess;
+  with_split(s, [&](auto c, auto i) {
+    if (smem > 32 * 1024)
+      e = cudaFuncSetAttribute(k_runs<T, O, c.value, i.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
+    if (e == cudaSuccess) launch_pdl(k_runs<T, O, c.value, i.value>, grid, dim3((unsigned)threads), smem, st, a);
+  });
+  return e;
+}
+
+template <int kR>
+cudaError_t sort_cluster(const SortArgs& s, cudaStream_t st) {
+  const int smem = cluster_smem<kR>(s.bits);
+  cudaError_t e = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCluster);
+  cfg.blockDim = dim3(kClusterThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kCluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, k_sort_cluster<kR>, s);
+}
+
+template <typename T, typename O>
+cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32_t d, float scale, O* out, char* ws,
+                     cudaStream_t st) {
+  int most = 8;
+  while (most > 1 && !(fits(dy, lddy, d, sizeof(T), most) && fits(out, d, d, sizeof(O), most))) most /= 2;
+  const Plan p(n, ids.vocab, d, most);
   SortArgs s{};
-  s.ids = ids, s.n = n, s.bits = p.bits, s.blocks = (int32_t)p.blocks;
-  s.count = (uint32_t*)(ws + p.count), s.total = (uint32_t*)(ws + p.total), s.seen = (uint32_t*)(ws + p.seen);
+  s.ids = ids, s.n = n, s.bits = p.bits, s.bits_all = p.bits_all, s.blocks = (int32_t)p.blocks;
+  s.count = (uint32_t*)(ws + p.count), s.total = (uint32_t*)(ws + p.total), s.seen = (uint8_t*)(ws + p.seen);
   uint32_t* key[2] = {(uint32_t*)(ws + p.key[0]), (uint32_t*)(ws + p.key[1])};
   uint32_t* val[2] = {(uint32_t*)(ws + p.val[0]), (uint32_t*)(ws + p.val[1])};
-  const int bins = 1 << p.bits;
-  const size_t sm = (size_t)(bins + 32) * 4 + (size_t)bins * kSortWarps * 2;
+  s.first = 1, s.key_out = key[0], s.val_out = val[0];
+  cudaError_t e = cudaSuccess;
   int at = 0;
-  if (n <= kTile) {
-    s.first = s.last = 1, s.key_out = key[0], s.val_out = val[0];
-    const size_t all = sm + 2 * kTile * 4;
-    cudaFuncSetAttribute(k_sort_tile, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
-    launch_pdl(k_sort_tile, dim3(1), dim3(kSortThreads), all, st, s, (int)p.bits_all);
+  if (n <= kFew) {
+    launch_pdl(k_sort_few, dim3(1), dim3((unsigned)round_up(n, 32)), 0, st, s);
+  } else if (n <= 2 * kCluster * kClusterThreads) {
+    e = sort_cluster<2>(s, st);
+  } else if (n <= 4 * kCluster * kClusterThreads) {
+    e = sort_cluster<4>(s, st);
+  } else if (n <= 8 * kCluster * kClusterThreads) {
+    e = sort_cluster<8>(s, st);
   } else {
+    const int bins = 1 << p.bits;
+    const size_t sm = (size_t)(bins + 32) * 4 + (size_t)bins * (kSortThreads / 32) * 2;
     for (int i = 0; i < p.passes; ++i) {
-      s.first = i == 0, s.last = i + 1 == p.passes, s.shift = i * p.bits;
+      s.first = i == 0, s.shift = i * p.bits;
       s.key = key[at ^ 1], s.val = val[at ^ 1], s.key_out = key[at], s.val_out = val[at];
-      launch_pdl(k_sort_count, dim3((unsigned)p.blocks), dim3(kSortThreads), 0, st, s);
+      const dim3 grid((unsigned)p.blocks), block(kSortThreads);
+      if (p.rounds == 2) launch_pdl(k_sort_count<2>, grid, block, 0, st, s);
+      else launch_pdl(k_sort_count<8>, grid, block, 0, st, s);
       launch_pdl(k_sort_scan, dim3((unsigned)ceil_div(bins, 8)), dim3(256), 0, st, s.count, s.total, (int)p.blocks, bins);
-      launch_pdl(k_sort_scatter, dim3((unsigned)p.blocks), dim3(kSortThreads), sm, st, s);
+      if (p.rounds == 2) launch_pdl(k_sort_scatter<2>, grid, block, sm, st, s);
+      else launch_pdl(k_sort_scatter<8>, grid, block, sm, st, s);
       at ^= 1;
     }
     at ^= 1;
   }
-  const bool out_ok = d % 8 == 0 && aligned16(out, 0, 4), in_ok = aligned16(dy, lddy, sizeof(T));
+  if (e != cudaSuccess) return e;
   const uint32_t *k = key[at], *v = val[at];
   for (int l = 0; l < p.levels; ++l) {
     const bool last = l + 1 == p.levels;
     auto fill = [&](auto& a) {
-      a.key = k, a.val = v, a.out = out, a.m = p.m[l], a.chunk = p.chunk[l], a.chunks = ceil_div(p.m[l], p.chunk[l]);
+      a.key = k, a.val = v, a.out = out, a.m = p.m[l], a.chunk = p.chunk[l], a.run_blocks = (int32_t)p.run_blocks[l];
       a.key_out = last ? nullptr : (uint32_t*)(ws + p.part_key[l]), a.part = last ? nullptr : (float*)(ws + p.part[l]);
-      a.d = d, a.vocab = ids.vocab, a.scale = scale;
+      a.d = d, a.vocab = ids.vocab, a.scale = scale, a.seen = s.seen, a.wide = fits(out, d, d, sizeof(O), 16 / sizeof(O));
     };
     if (l == 0) {
       RunArgs<T, O> a{};
       fill(a);
-      a.src = dy, a.ld = lddy, a.seen = s.seen;
-      const int64_t zero_blocks = std::min<int64_t>(ceil_div((int64_t)ids.vocab * d, 256 * 64), 4 * kSms);
-      if (out_ok && in_ok) run_level<T, O, 8>(a, zero_blocks, st);
-      else run_level<T, O, 1>(a, zero_blocks, st);
+      a.src = dy, a.ld = lddy, a.first = 1;
+      e = run_level(a, p.split, kRunThreads, 0, st);
     } else {
       RunArgs<float, O> a{};
       fill(a);
       a.src = (const float*)(ws + p.part[l - 1]), a.ld = d;
-      if (out_ok) run_level<float, O, 8>(a, 0, st);
-      else run_level<float, O, 1>(a, 0, st);
+      const int64_t zero_blocks = l > 1 ? 0 : std::min<int64_t>(ceil_div((int64_t)ids.vocab * d, 1024 * 32), 2 * kSms);
+      e = run_level(a, p.split, kJoinThreads, zero_blocks, st);
     }
+    if (e != cudaSuccess) return e;
     if (!last) k = (const uint32_t*)(ws + p.part_key[l]), v = nullptr;
   }
+  return cudaGetLastError();
 }
 
 template <typename T, typename O>
 void lookup(const Ids& ids, int64_t n, const T* table, int64_t ldt, int32_t d, float scale, O* y, cudaStream_t st) {
-  const bool vec = d % 8 == 0 && aligned16(table, ldt, sizeof(T)) && aligned16(y, 0, 4);
-  LookArgs<T, O> a{ids, table, y, n, ldt, d, 0, 0, scale};
-  const Split s = split_cols(d, vec ? 8 : 1);
-  a.shift = s.shift, a.items = s.items;
-  const dim3 grid((unsigned)ceil_div(n, (int64_t)(256 >> s.shift) * 4), (unsigned)ceil_div(d, (int64_t)s.items * (vec ? 8 : 1) << s.shift));
-  if (vec) launch_pdl(k_lookup<T, O, 8>, grid, dim3(256), 0, st, a);
-  else launch_pdl(k_lookup<T, O, 1>, grid, dim3(256), 0, st, a);
+  int most = 8;
+  while (most > 1 && !(fits(table, ldt, d, sizeof(T), most) && fits(y, d, d, sizeof(O), most))) most /= 2;
+  Split s = split_cols(d, most);
+  // (no chains here: the widest loads)
+  if (most > s.e) s = Split{most, 0, 1};
+  while (s.e > 1 && s.shift < 5 && (s.e << s.shift) < d) ++s.shift;
+  LookArgs<T, O> a{ids, table, y, n, ldt, d, s.shift, scale};
+  if (most == 1 && ((uintptr_t)y & 15) == 0) {
+    launch_pdl(k_lookup_flat<T, O>, dim3((unsigned)ceil_div(n * d, 2048)), dim3(256), 0, st, a);
+    return;
+  }
+  const dim3 grid((unsigned)ceil_div(n, (int64_t)(256 >> s.shift) * 4), (unsigned)ceil_div(d, s.width()));
+  with_split(s, [&](auto c, auto i) { launch_pdl(k_lookup<T, O, c.value, i.value>, grid, dim3(256), 0, st, a); });
 }
 
 tp_status check(int64_t n, int32_t id_bytes, int32_t vocab, int32_t d) {
@@ -603,7 +913,7 @@ tp_status pack_embed_bytes(int64_t n, int32_t vocab, int32_t d, int64_t* backwar
   const tp_status s = check(n, 4, vocab, d);
   if (s != TP_OK) return s;
   if (!backward_bytes) return ops_fail(TP_EINVAL, "null argument");
-  *backward_bytes = n ? Plan(n, vocab, d).bytes : 0;
+  *backward_bytes = n ? plan_bytes(n, vocab, d) : 0;
   return TP_OK;
 }
 
@@ -624,20 +934,21 @@ tp_status pack_embed_backward(const void* dy, int64_t lddy, const void* ids, int
   }
   if (!dy || !ids) return ops_fail(TP_EINVAL, "null argument");
   if ((uintptr_t)ids & (id_bytes - 1)) return ops_fail(TP_EINVAL, "ids must be aligned to their size");
-  const int64_t need = Plan(n, vocab, d).bytes;
+  const int64_t need = plan_bytes(n, vocab, d);
   if (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255))
     return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
   if ((s = ops_device()) != TP_OK) return s;
   const Ids i{ids, id_bytes == 8, vocab};
   char* ws = (char*)workspace;
+  cudaError_t e;
   if (precision == TP_FP32) {
-    if (table_precision == TP_FP32) backward((const float*)dy, lddy, i, n, d, scale, (float*)dtable, ws, st);
-    else backward((const float*)dy, lddy, i, n, d, scale, (Half*)dtable, ws, st);
+    if (table_precision == TP_FP32) e = backward((const float*)dy, lddy, i, n, d, scale, (float*)dtable, ws, st);
+    else e = backward((const float*)dy, lddy, i, n, d, scale, (Half*)dtable, ws, st);
   } else {
-    if (table_precision == TP_FP32) backward((const Half*)dy, lddy, i, n, d, scale, (float*)dtable, ws, st);
-    else backward((const Half*)dy, lddy, i, n, d, scale, (Half*)dtable, ws, st);
+    if (table_precision == TP_FP32) e = backward((const Half*)dy, lddy, i, n, d, scale, (float*)dtable, ws, st);
+    else e = backward((const Half*)dy, lddy, i, n, d, scale, (Half*)dtable, ws, st);
   }
-  return done(cudaGetLastError(), "pack_embed_backward");
+  return done(e, "pack_embed_backward");
 }
 
 }  // extern "C"

@@ -40,29 +40,34 @@ struct BlockScale {
     scale = finite ? t / 448.f : __uint_as_float(0x7FC00000u);
     up = t < 5.4e-20f ? 18446744073709551616.f : 1.f;
     unit = scale * up;
-    inv = finite && scale > 0.f ? 1.f / unit : 0.f;   // 0: the block's q are 0
+    inv = finite && scale > 0.f ? __fdividef(1.f, unit) : 0.f;   // 0: the block's q are 0
   }
 };
 
-// The float whose nearest e4m3 number is that of x / scale: the quotient, or
-// near a border between two numbers (20 bits below the last one kept: 5 places
-// of a million; and below 2^-6, where fewer are kept) the quotient rounded to odd,
-// which lies on the border only if the exact one does.
-__device__ __forceinline__ float quotient(float x, const BlockScale& s) {
-  float t = x * s.up * s.inv;
-  const uint32_t b = __float_as_uint(t);
-  if ((b & 0xFFFFFu) - 0x7FFFCu <= 8u || (b & 0x7FFFFFFFu) - 1u < 0x3C7FFFFFu) {
-    if (s.inv == 0.f) return 0.f;
-    const float v = x * s.up;
-    t = __fdiv_rn(v, s.unit);
-    const float r = fmaf(-t, s.unit, v);
-    if (r != 0.f) {
-      uint32_t u = __float_as_uint(t);
-      if ((r < 0.f) == (t > 0.f)) --u;   // beyond the exact quotient: back towards zero
-      t = __uint_as_float(u | 1u);
-    }
+// Floats whose nearest e4m3 numbers are those of x / scale.  The quotients by a
+// reciprocal are right to within three places.  Where that leaves open on which
+// side of the border between two e4m3 numbers one lies (20 bits below the last
+// one kept; in bf16 data, whose quotients often are borders, one in a few
+// hundred), and below 2^-6, where the numbers are 2^-9 apart, the side is that of
+// x - border * scale, which a multiply-add gives exactly.
+template <int kN>
+__device__ __forceinline__ void quotients(float (&x)[kN], const BlockScale& s) {
+  if (s.up != 1.f) {
+#pragma unroll
+    for (int e = 0; e < kN; ++e) x[e] *= s.up;
   }
-  return t;
+#pragma unroll
+  for (int e = 0; e < kN; ++e) {
+    float t = x[e] * s.inv;
+    const bool small = fabsf(t) < 0.015625f && t != 0.f;
+    if ((__float_as_uint(t) & 0xFFFFFu) - 0x7FFFCu <= 8u || small) {
+      const float border = small ? (floorf(t * 512.f) + 0.5f) * (1.f / 512.f)
+                                 : __uint_as_float((__float_as_uint(t) & 0xFFF00000u) | 0x80000u);
+      const float r = fmaf(-border, s.unit, x[e]), side = r > 0.f ? 1.f : r < 0.f ? -1.f : 0.f;
+      t = fmaf(fabsf(border) * 0x1p-20f, side, border);
+    }
+    x[e] = s.inv == 0.f ? 0.f : t;   // (an infinity times 0 is none)
+  }
 }
 // Two numbers as e4m3 (the first one in the lower byte), to the nearest, ties to even, at most 448.
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
@@ -78,37 +83,54 @@ struct QuantArgs {
   float* scale;
   int64_t ldx, ldq, rows;
   int32_t k, blocks;      // blocks of 128 columns
+  int32_t q16;            // q's rows start at multiples of 16 bytes
 };
 
-// Scales per row and block: sixteen lanes a block, eight elements each.
+// Scales per row and block: eight lanes a block, sixteen elements each, so that a
+// scale's two divisions are shared by many.
 template <typename T>
 __global__ void __launch_bounds__(256) k_quant_rows(const QuantArgs<T> g) {
   using L = Lane<T, 1, 1, 8>;
-  const int lane = threadIdx.x & 15;
-  const int64_t total = g.rows * g.blocks, step = (int64_t)gridDim.x * 16;
+  const int lane = threadIdx.x & 7, b = blockIdx.x * 4 + ((threadIdx.x >> 3) & 3), c = b * kBlock + lane * 16;
+  const int64_t step = (int64_t)gridDim.y * 8;
   pdl_trigger();
   pdl_wait();
-  for (int64_t base = (int64_t)blockIdx.x * 16 + ((threadIdx.x >> 5) << 1); base < total; base += step) {
-    const int64_t at = base + ((threadIdx.x >> 4) & 1);   // (both halves of a warp stay in the loop together)
-    const int64_t row = at / g.blocks;
-    const int b = (int)(at - row * g.blocks), c = b * kBlock + lane * 8;
-    const bool live = at < total && c < g.k;
-    L x;
-    x.load(g.x + (live ? row * g.ldx + c : 0), 0, live ? 8 : 0);
-    float v[8];
-    x.get(0, v);
+  const int in = c < g.k ? min(16, g.k - c) : 0;   // 0, 8 or 16 elements
+  int64_t row = (int64_t)blockIdx.y * 8 + (threadIdx.x >> 5);
+  L x[2];
+  auto ask = [&](int64_t r) {
+    const bool there = r < g.rows;
+    x[0].load(g.x + r * g.ldx + c, 0, there && in > 0 ? 8 : 0);
+    x[1].load(g.x + r * g.ldx + c + 8, 0, there && in > 8 ? 8 : 0);
+  };
+  ask(row);
+  for (; row < g.rows; row += step) {
+    float v[16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float w[8];
+      x[h].get(0, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[8 * h + e] = w[e];
+    }
+    ask(row + step);   // the next row's, while this one is worked on
     uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const BlockScale s(top);
-    if (at < total && lane == 0) g.scale[at] = s.scale;
+    if (in && lane == 0) g.scale[row * g.blocks + b] = s.scale;
+    quotients(v, s);
+    uint32_t w[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = s.inv == 0.f ? 0.f : quotient(v[e], s);
-    if (live)
-      *reinterpret_cast<uint2*>(g.q + row * g.ldq + c) =
-          make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+    for (int e = 0; e < 4; ++e) w[e] = e4m3x2(v[4 * e], v[4 * e + 1]) | e4m3x2(v[4 * e + 2], v[4 * e + 3]) << 16;
+    uint8_t* q = g.q + row * g.ldq + c;
+    if (in == 16 && g.q16) *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if (in) {
+      *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+      if (in > 8) *reinterpret_cast<uint2*>(q + 8) = make_uint2(w[2], w[3]);
+    }
   }
 }
 
@@ -132,9 +154,10 @@ __global__ void __launch_bounds__(256) k_quant_rows1(const QuantArgs<T> g) {
     top = warp_max(top);
     const BlockScale s(top);
     if (lane == 0) g.scale[at] = s.scale;
+    quotients(v, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (c0 + 32 * i < g.k) g.q[row * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(s.inv == 0.f ? 0.f : quotient(v[i], s), 0.f);
+      if (c0 + 32 * i < g.k) g.q[row * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(v[i], 0.f);
   }
 }
 
@@ -164,11 +187,12 @@ __global__ void __launch_bounds__(256) k_quant_blocks(const QuantArgs<T> g) {
   const BlockScale s(top);
   if (threadIdx.x == 0) g.scale[(int64_t)blockIdx.y * g.blocks + blockIdx.x] = s.scale;
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
+  for (int r = 0; r < 16; ++r) {
+    quotients(v[r], s);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (r0 + r < g.rows && c0 + 32 * i < g.k)
-        g.q[(r0 + r) * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(s.inv == 0.f ? 0.f : quotient(v[r][i], s), 0.f);
+      if (r0 + r < g.rows && c0 + 32 * i < g.k) g.q[(r0 + r) * g.ldq + c0 + 32 * i] = (uint8_t)e4m3x2(v[r][i], 0.f);
+  }
 }
 
 template <typename T>
@@ -179,7 +203,9 @@ void quantise(const QuantArgs<T>& a, int block_rows, cudaStream_t st) {
   }
   const int64_t total = a.rows * a.blocks;
   const bool vec = a.k % 8 == 0 && aligned16(a.x, a.ldx, sizeof(T)) && ((uintptr_t)a.q & 7) == 0 && a.ldq % 8 == 0;
-  if (vec) launch_pdl(k_quant_rows<T>, dim3((unsigned)std::min<int64_t>(ceil_div(total, 16), 16 * kSms)), dim3(256), 0, st, a);
+  const int64_t across = ceil_div(a.blocks, 4);
+  const dim3 grid((unsigned)across, (unsigned)std::min<int64_t>(ceil_div(a.rows, 8), std::max<int64_t>(1, 12 * kSms / across)));
+  if (vec) launch_pdl(k_quant_rows<T>, grid, dim3(256), 0, st, a);
   else launch_pdl(k_quant_rows1<T>, dim3((unsigned)std::min<int64_t>(ceil_div(total, 8), 16 * kSms)), dim3(256), 0, st, a);
 }
 
@@ -210,7 +236,12 @@ __global__ void __launch_bounds__(256) k_copy_rows(const CopyArgs a, const CopyA
 }
 
 // ------------------------------------------------------------------ product
-constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;   // a producer, the MMA issuer
+// A warpgroup of the producer, the MMA issuer and two idle warps, and two of the
+// epilogue, which the first one leaves its registers to: 128 (40 + 2 x 232) =
+// 384 x 168, what the block is launched with.
+constexpr int kEpiWarps = 8, kThreads = 128 + 32 * kEpiWarps;
+constexpr int kFewRegs = 40, kManyRegs = 232;
+static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "register split");
 constexpr int kABytes = 128 * kBlock;
 constexpr int kStages = 6, kMaxBufs = 4;
 constexpr int kTmemCols = 512;
@@ -263,8 +294,25 @@ __device__ __forceinline__ void tile_at(const F8Args& g, int t, int& m, int& n) 
   n = local / rows;
 }
 
-// kN: columns of a tile, kCta * 128 its rows.
-template <int kCta, int kN>
+// wait_all without a call: the epilogue's registers leave none for one.
+__device__ __forceinline__ bool wait_here(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                          uint64_t budget_ns, int site) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const uint64_t t0 = global_ns();
+  while (true) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
+    if (__any_sync(0xffffffffu, global_ns() - t0 > budget_ns)) {
+      *abort_flag = 1;
+      atomicCAS(err, 0, site);
+      return false;
+    }
+  }
+}
+
+// kN: columns of a tile, kCta * 128 its rows; kSplit: CTAs of a cluster that share
+// out a tile's K blocks (kCta = 1).
+template <int kCta, int kN, int kSplit>
 __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__ F8Args g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -277,7 +325,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int rank = kCta == 2 ? (int)uniform(cluster_rank()) : 0;
   const bool leader = rank == 0;
-  const int clu = blockIdx.x / kCta, n_clu = gridDim.x / kCta, n_tiles = g.tm * g.tn;
+  constexpr int kClu = kCta * kSplit;
+  const int clu = blockIdx.x / kClu, n_clu = gridDim.x / kClu, n_tiles = g.tm * g.tn;
+  const int part = kSplit > 1 ? (int)uniform(cluster_rank()) : 0;
+  const int kb_first = g.kb * part / kSplit, kb_end = g.kb * (part + 1) / kSplit;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -308,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (kCta == 2) cluster_sync();   // the peer's barriers exist before any copy or arrival targets them
+  if (kClu > 1) cluster_sync();    // the peers' barriers and memory exist before anything targets them
   if (warp == 0 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &g.b : &g.a) : "memory");
   pdl_wait();                      // the set-up above overlaps the previous kernel
   fence_proxy_async_global();      // what it wrote by plain stores is read by TMA
@@ -316,76 +367,85 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
   volatile int* abort_flag = &tl->abort;
   int* err = g.err;
 
-  if (warp == 0) {
-    // ---------------------------------------------------------- producer
-    uint32_t stage = 0, phase = 0, issued = 0;
-    bool ok = true;
-    const uint32_t s0 = smem_u32(smem), full0 = smem_u32(&tl->full[0]);
-    const uint32_t lead0 = kCta == 2 ? mapa(full0, 0) : full0;   // the barriers that copies complete on
-    for (int t = clu; ok && t < n_tiles; t += n_clu) {
-      int m, n;
-      tile_at(g, t, m, n);
-      const int ya = (m * kCta + rank) * 128, yb = n * kN + rank * kNh;
-      for (int kb = 0; kb < g.kb; ++kb) {
-        if (!wait_all(&tl->empty[stage], phase ^ 1u, abort_flag, err, kWaitNs, 61)) {
-          ok = false;
-          break;
-        }
-        const uint32_t dst = s0 + stage * kStageBytes, bar = lead0 + 8 * stage;
-        if (leader) expect_elect(full0 + 8 * stage, kCta * kStageBytes);
-        tma_elect<kCta>(dst, &g.a, bar, kBlock * kb, ya, 0);
-        tma_elect<kCta>(dst + kABytes, &g.b, bar, kBlock * kb, yb, 0);
-        issued |= 1u << stage;
-        if (++stage == kStages) {
-          stage = 0;
-          phase ^= 1u;
-        }
-      }
-    }
-    // every copy has landed before the CTA leaves: a stage's last one is of this
-    // turn of the ring below `stage`, of the one before from there on
-    if (leader)
-      for (int s = 0; s < kStages; ++s)
-        if (issued & (1u << s)) {
-          int dummy = 0;
-          mbar_wait(&tl->full[s], s < (int)stage ? phase : phase ^ 1u, &dummy, err, kWaitNs, 62);
-        }
-  } else if (warp == 1) {
-    if (leader) {
-      // --------------------------------------------------------------- MMA
-      const uint32_t s0 = smem_u32(smem), empty0 = smem_u32(&tl->empty[0]), tfull0 = smem_u32(&tl->tfull[0]);
-      const uint64_t da = smem_desc(s0, 16, 1024), db = smem_desc(s0 + kABytes, 16, 1024);
-      // fp32 accumulators, e4m3 operands (format 0), both K-major
-      const uint32_t idesc = (1u << 4) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(128 * kCta >> 4) << 24);
-      uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+    if (warp == 0) {
+      // ---------------------------------------------------------- producer
+      uint32_t stage = 0, phase = 0, issued = 0;
       bool ok = true;
-      for (int t = clu; ok && t < n_tiles; t += n_clu)
-        for (int kb = 0; kb < g.kb; ++kb) {
-          if (!wait_all(&tl->tempty[buf], buf_phase ^ 1u, abort_flag, err, 2 * kWaitNs, 63) ||
-              !wait_all(&tl->full[stage], phase, abort_flag, err, 2 * kWaitNs, 64)) {
+      const uint32_t s0 = smem_u32(smem), full0 = smem_u32(&tl->full[0]);
+      const uint32_t lead0 = kCta == 2 ? mapa(full0, 0) : full0;   // the barriers that copies complete on
+      for (int t = clu; ok && t < n_tiles; t += n_clu) {
+        int m, n;
+        tile_at(g, t, m, n);
+        const int ya = (m * kCta + rank) * 128, yb = n * kN + rank * kNh;
+        for (int kb = kb_first; kb < kb_end; ++kb) {
+          if (!wait_all(&tl->empty[stage], phase ^ 1u, abort_flag, err, kWaitNs, 61)) {
             ok = false;
             break;
           }
-          tc_fence_after();
-          mma_block<kCta>(tmem + buf * kN, da + stage * (kStageBytes >> 4), db + stage * (kStageBytes >> 4), idesc,
-                          empty0 + 8 * stage, tfull0 + 8 * buf);
+          const uint32_t dst = s0 + stage * kStageBytes, bar = lead0 + 8 * stage;
+          if (leader) expect_elect(full0 + 8 * stage, kCta * kStageBytes);
+          tma_elect<kCta>(dst, &g.a, bar, kBlock * kb, ya, 0);
+          tma_elect<kCta>(dst + kABytes, &g.b, bar, kBlock * kb, yb, 0);
+          issued |= 1u << stage;
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
-          if (++buf == kBufs) {
-            buf = 0;
-            buf_phase ^= 1u;
-          }
         }
-      commit_elect<kCta>(smem_u32(&tl->done));   // all MMAs are over before TMEM is freed
-      int dummy = 0;
-      mbar_wait(&tl->done, 0, &dummy, err, kWaitNs, 65);
+      }
+      // every copy has landed before the CTA leaves: a stage's last one is of this
+      // turn of the ring below `stage`, of the one before from there on
+      if (leader)
+        for (int s = 0; s < kStages; ++s)
+          if (issued & (1u << s)) {
+            int dummy = 0;
+            mbar_wait(&tl->full[s], s < (int)stage ? phase : phase ^ 1u, &dummy, err, kWaitNs, 62);
+          }
+    } else if (warp == 1) {
+      if (leader) {
+        // --------------------------------------------------------------- MMA
+        const uint32_t s0 = smem_u32(smem), empty0 = smem_u32(&tl->empty[0]), tfull0 = smem_u32(&tl->tfull[0]);
+        const uint64_t da = smem_desc(s0, 16, 1024), db = smem_desc(s0 + kABytes, 16, 1024);
+        // fp32 accumulators, e4m3 operands (format 0), both K-major
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(128 * kCta >> 4) << 24);
+        uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+        bool ok = true;
+        for (int t = clu; ok && t < n_tiles; t += n_clu)
+          for (int kb = kb_first; kb < kb_end; ++kb) {
+            if (!wait_all(&tl->tempty[buf], buf_phase ^ 1u, abort_flag, err, 2 * kWaitNs, 63) ||
+                !wait_all(&tl->full[stage], phase, abort_flag, err, 2 * kWaitNs, 64)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            mma_block<kCta>(tmem + buf * kN, da + stage * (kStageBytes >> 4), db + stage * (kStageBytes >> 4), idesc,
+                            empty0 + 8 * stage, tfull0 + 8 * buf);
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1u;
+            }
+            if (++buf == kBufs) {
+              buf = 0;
+              buf_phase ^= 1u;
+            }
+          }
+        commit_elect<kCta>(smem_u32(&tl->done));   // all MMAs are over before TMEM is freed
+        int dummy = 0;
+        mbar_wait(&tl->done, 0, &dummy, err, kWaitNs, 65);
+      }
+    }
+    if constexpr (kSplit > 1) {   // the epilogue's two meetings
+      __syncwarp();
+      cluster_sync();
+      cluster_sync();
     }
   } else {
     // ------------------------------------------------------------ epilogue
-    const int q = warp & 3, half = (warp - 2) >> 2;
-    uint8_t* out_buf = bufs + (warp - 2) * kBufBytes;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    uint8_t* out_buf = bufs + (warp - 4) * kBufBytes;
     uint32_t buf = 0, buf_phase = 0;
     const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + half * kCols;
     bool ok = true;
@@ -399,11 +459,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
       float acc[kCols];
 #pragma unroll
       for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
-      float ax = sx[0], aw = sw[0];
-      for (int kb = 0; kb < g.kb; ++kb) {
+      float ax = sx[kb_first], aw = sw[kb_first];
+      for (int kb = kb_first; kb < kb_end; ++kb) {
         const float f = ax * aw;
-        if (kb + 1 < g.kb) ax = sx[kb + 1], aw = sw[kb + 1];
-        if (!__all_sync(0xffffffffu, mbar_wait(&tl->tfull[buf], buf_phase, abort_flag, err, 2 * kWaitNs, 66))) {
+        if (kb + 1 < kb_end) ax = sx[kb + 1], aw = sw[kb + 1];
+        if (!wait_here(&tl->tfull[buf], buf_phase, abort_flag, err, 2 * kWaitNs, 66)) {
           ok = false;
           break;
         }
@@ -414,19 +474,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
           tmem_ask32(t0 + buf * kN + c, v);
           tmem_wait();
           tmem_got(v);
+          if (c + 32 == kCols) {   // the accumulator is read: free for the block but one after this before its last sums
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              if constexpr (kCta == 2) mbar_arrive_cluster_relaxed(mapa(smem_u32(&tl->tempty[buf]), 0));
+              else mbar_arrive_relaxed(&tl->tempty[buf]);
+            }
+          }
+          
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[c + e] = fmaf(__uint_as_float(v[e]), f, acc[c + e]);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {   // the loads above have completed
-          if constexpr (kCta == 2) mbar_arrive_cluster_relaxed(mapa(smem_u32(&tl->tempty[buf]), 0));
-          else mbar_arrive_relaxed(&tl->tempty[buf]);
         }
         if (++buf == kBufs) {
           buf = 0;
           buf_phase ^= 1u;
         }
+      }
+      if constexpr (kSplit > 1) {
+        // the others' sums go to the first CTA's ring, which no copy or MMA uses any more, and are added in order
+        cluster_sync();
+        float* ring = (float*)smem + (warp - 4) * (32 * kCols);
+        if (part > 0) {
+          const uint32_t to = mapa(smem_u32(ring + (part - 1) * (256 * kCols)), 0);
+#pragma unroll
+          for (int e = 0; e < kCols; e += 4)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (e * 32 + 4 * lane) * 4), "f"(acc[e]),
+                         "f"(acc[e + 1]), "f"(acc[e + 2]), "f"(acc[e + 3])
+                         : "memory");
+        }
+        cluster_sync();
+        if (part > 0) break;
+#pragma unroll
+        for (int p = 0; p < kSplit - 1; ++p)
+#pragma unroll
+          for (int e = 0; e < kCols; e += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(ring + p * (256 * kCols) + e * 32 + 4 * lane);
+            acc[e] += v.x, acc[e + 1] += v.y, acc[e + 2] += v.z, acc[e + 3] += v.w;
+          }
       }
       if (!ok) break;
       const bool live = r0 + lane < g.M;
@@ -472,16 +557,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
   }
 }
 
-template <int kCta, int kN>
+template <int kCta, int kN, int kSplit>
 cudaError_t launch_f8(F8Args& g, const void* q, int64_t ldq, const void* w, int64_t ldw, int64_t k, cudaStream_t st) {
+  constexpr int kClu = kCta * kSplit;
+  static_assert(kSplit == 1 || (kSplit - 1) * 256 * (kN / 2) * 4 <= kStages * (kABytes + kN * kBlock), "a ring holds the other parts");
   g.tm = (int32_t)ceil_div(g.M, 128 * kCta), g.tn = (int32_t)ceil_div(g.N, kN);
   if (!tma_map_bytes(&g.a, q, k, g.M, ldq, kBlock, 128) || !tma_map_bytes(&g.b, w, k, g.N, ldw, kBlock, kN / kCta))
     return cudaErrorInvalidValue;
   const int smem = 1024 + kStages * (kABytes + kN / kCta * kBlock) + kEpiWarps * kBufBytes + (int)sizeof(Tail);
-  cudaError_t e = cudaFuncSetAttribute(k_prod_f8<kCta, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(k_prod_f8<kCta, kN, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kCta * (unsigned)std::min<int64_t>((int64_t)g.tm * g.tn, kSms / kCta));
+  // a cluster a tile where K is shared out, else as many as run at once
+  const int64_t tiles = (int64_t)g.tm * g.tn;
+  cfg.gridDim = dim3(kClu * (unsigned)(kSplit > 1 ? tiles : std::min<int64_t>(tiles, kSms / kCta)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -489,11 +578,11 @@ cudaError_t launch_f8(F8Args& g, const void* q, int64_t ldq, const void* w, int6
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCta;
+  attr[1].val.clusterDim.x = kClu;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = kCta == 2 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_prod_f8<kCta, kN>, g);
+  cfg.numAttrs = kClu > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_prod_f8<kCta, kN, kSplit>, g);
 }
 
 tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
@@ -503,6 +592,180 @@ tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
   if (rows * (k > n ? k : n) > kMaxElems) return ops_fail(TP_EINVAL, "more than 2^40 elements in a matrix");
   if (precision != TP_BF16 && precision != TP_FP32) return ops_fail(TP_EINVAL, "unknown precision %d", precision);
   return TP_OK;
+}
+
+// The tile, by times measured: us a K block, of a tile alone on its SMs and with
+// all of them at work (there the pairs' half of the traffic from L2 counts), and
+// what a launch takes besides.  A K block's time is hardly less for fewer
+// columns, because it is the chain from MMA to epilogue and back that it waits for.
+struct Shape {
+  int rows, cols, split;
+  double kb, kb_full, fixed;
+};
+constexpr Shape kShapes[] = {{256, 256, 1, 0.44, 0.55, 5.0}, {128, 128, 1, 0.235, 0.31, 3.2}, {128, 64, 1, 0.225, 0.31, 2.7},
+                             {128, 64, 2, 0.225, 0.31, 4.2}, {128, 64, 4, 0.225, 0.31, 5.5}};
+int pick_shape(int64_t rows, int64_t n, int64_t kb) {
+  int pick = 0;
+  double best = 1e30;
+  for (int i = 0; i < 5; ++i) {
+    const Shape& s = kShapes[i];
+    const int64_t tiles = ceil_div(rows, s.rows) * ceil_div(n, s.cols), at_once = kSms / (s.rows / 128 * s.split);
+    if (s.split > 1 && (tiles > at_once || kb < s.split)) continue;
+    const double t = s.fixed + (double)(ceil_div(tiles, at_once) * ceil_div(kb, s.split)) * (tiles > at_once ? s.kb_full : s.kb);
+    if (t < best) best = t, pick = i;
+  }
+  return pick;
+}
+cudaError_t run_product(F8Args& g, const void* q, int64_t ldq, const void* w, int64_t ldw, int64_t k, cudaStream_t st) {
+  switch (pick_shape(g.M, g.N, g.kb)) {
+    case 0: return launch_f8<2, 256, 1>(g, q, ldq, w, ldw, k, st);
+    case 1: return launch_f8<1, 128, 1>(g, q, ldq, w, ldw, k, st);
+    case 2: return launch_f8<1, 64, 1>(g, q, ldq, w, ldw, k, st);
+    case 3: return launch_f8<1, 64, 2>(g, q, ldq, w, ldw, k, st);
+    default: return launch_f8<1, 64, 4>(g, q, ldq, w, ldw, k, st);
+  }
+}
+
+// ----------------------------------------------------------------- few rows
+// A serving call: bound by the weights' bytes, each of which is read once, straight
+// into the registers of the warp that multiplies it, as the 16-row operand of
+// mma.sync (e4m3 as fp16, exact); the rows of x are its eight columns.  A warp
+// takes K blocks in turns; a block's sums are scaled and added in fp32; the warps'
+// meet in shared memory, added in order.
+struct FewArgs {
+  const uint8_t *x, *w;
+  const float *sx, *sw, *bias;
+  void* y;
+  int64_t ldx, ldw;
+  int32_t rows, k, n, kb, f32;
+};
+__device__ __forceinline__ uint32_t f16_of(uint32_t two) {   // two e4m3 numbers (the lower 16 bits)
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+// 16 bytes from `p`, `left` of which lie inside the row; zeros past it.
+template <bool kVec>
+__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int left) {
+  if constexpr (kVec) {
+    // (rows and their distance are multiples of 16: the last piece of a row may be filled up by what lies behind it)
+    if (left >= 16) return *reinterpret_cast<const uint4*>(p);
+  }
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (e < left) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+constexpr int kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
+template <int kNT, int kWarps, bool kVec>
+__global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
+  __shared__ float red[kWarps][8 * kNT][kStride];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * kNT;
+  pdl_trigger();
+  const uint8_t* wr[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) wr[h] = g.w + (int64_t)min(n0 + gid + 8 * h, g.n - 1) * g.ldw;
+  if (warp < g.kb)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) asm volatile("prefetch.global.L2 [%0];" ::"l"(wr[h] + min(kBlock * warp + 32 * t, g.k - 1)));
+  pdl_wait();
+  float acc[kNT][4];
+#pragma unroll
+  for (int j = 0; j < kNT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
+  const float* sw = g.sw + (int64_t)(n0 / kBlock) * g.kb;
+  for (int b = warp; b < g.kb; b += kWarps) {
+    // a lane's 32 bytes of a row's 128: two pieces of 16, 64 apart; both operands agree on the order of k
+    uint4 wv[2][2], xv[kNT][2];
+    float s[kNT][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int k = kBlock * b + 64 * p + 16 * t;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) wv[h][p] = bytes16<kVec>(wr[h] + k, n0 + gid + 8 * h < g.n ? g.k - k : 0);
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        const int m = m0 + 8 * j + gid;
+        xv[j][p] = bytes16<kVec>(g.x + (int64_t)min(m, g.rows - 1) * g.ldx + k, m < g.rows ? g.k - k : 0);
+      }
+    }
+    const float ws = sw[b];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int m = m0 + 8 * j + 2 * t + c;
+        s[j][c] = m < g.rows ? g.sx[(int64_t)m * g.kb + b] * ws : 0.f;
+      }
+    float blk[kNT][4];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) blk[j][e] = 0.f;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      uint32_t a[2][8];   // the 16 numbers of each of the lane's rows, as pairs
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t v[4] = {wv[h][p].x, wv[h][p].y, wv[h][p].z, wv[h][p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[h][2 * i] = f16_of(v[i]), a[h][2 * i + 1] = f16_of(v[i] >> 16);
+      }
+#pragma unroll
+      for (int j = 0; j < kNT; ++j) {
+        const uint32_t v[4] = {xv[j][p].x, xv[j][p].y, xv[j][p].z, xv[j][p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile(
+              "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+              "%3};"
+              : "+f"(blk[j][0]), "+f"(blk[j][1]), "+f"(blk[j][2]), "+f"(blk[j][3])
+              : "r"(a[0][2 * i]), "r"(a[1][2 * i]), "r"(a[0][2 * i + 1]), "r"(a[1][2 * i + 1]), "r"(f16_of(v[i])),
+                "r"(f16_of(v[i] >> 16)));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(blk[j][e], s[j][e & 1], acc[j][e]);
+  }
+#pragma unroll
+  for (int j = 0; j < kNT; ++j) {
+    red[warp][8 * j + 2 * t][gid] = acc[j][0];
+    red[warp][8 * j + 2 * t + 1][gid] = acc[j][1];
+    red[warp][8 * j + 2 * t][gid + 8] = acc[j][2];
+    red[warp][8 * j + 2 * t + 1][gid + 8] = acc[j][3];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * 8 * kNT; i += 32 * kWarps) {
+    const int ml = i >> 4, c = i & 15, m = m0 + ml, n = n0 + c;
+    if (m >= g.rows || n >= g.n) continue;
+    float v = red[0][ml][c];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) v += red[w][ml][c];
+    if (g.bias) v += g.bias[n];
+    if (g.f32) ((float*)g.y)[(int64_t)m * g.n + n] = v;
+    else ((__nv_bfloat16*)g.y)[(int64_t)m * g.n + n] = __float2bfloat16_rn(v);
+  }
+}
+template <int kWarps, bool kVec>
+void launch_few(const FewArgs& a, cudaStream_t st) {
+  const int nt = a.rows <= 8 ? 1 : a.rows <= 16 ? 2 : 4;
+  const dim3 grid((unsigned)ceil_div(a.n, 16), (unsigned)ceil_div(a.rows, 8 * nt)), block(32 * kWarps);
+  if (nt == 1) launch_pdl(k_few_f8<1, kWarps, kVec>, grid, block, 0, st, a);
+  else if (nt == 2) launch_pdl(k_few_f8<2, kWarps, kVec>, grid, block, 0, st, a);
+  else launch_pdl(k_few_f8<4, kWarps, kVec>, grid, block, 0, st, a);
+}
+// Do these take `rows` rows?  Measured against the best tcgen05 tile (us): 2048 ->
+// 4096, 16 rows 4.7 / 7.1, 32 rows 6.7 / 7.2, 48 rows 10.7 / 7.1; 1024 -> 1000, 128
+// rows 3.6 / 4.8, 200 rows 6.1 / 4.9; 4096 -> 4096, 16 rows 6.8 / 11, 32 rows 10.3 /
+// 8.5; 512 -> 512, 256 rows 2.7 / 4.0.
+bool few_take(int64_t rows, int64_t k, int64_t n) {
+  const int64_t work = rows * k * n;
+  return rows <= 16 || (rows <= 32 && work <= 270000000) || (rows <= 256 && work <= 140000000);
 }
 
 // An operand's rows as TMA takes them, staged where they lie otherwise.
@@ -533,11 +796,11 @@ tp_status pack_quantise_f8(const void* x, int64_t ldx, int64_t rows, int32_t k, 
   if (!x || !q || !scale) return ops_fail(TP_EINVAL, "null argument");
   if ((s = ops_device()) != TP_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const int32_t blocks = (int32_t)ceil_div(k, kBlock);
+  const int32_t blocks = (int32_t)ceil_div(k, kBlock), q16 = aligned16(q, ldq, 1);
   if (precision == TP_FP32)
-    quantise(QuantArgs<float>{(const float*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks}, block_rows, st);
+    quantise(QuantArgs<float>{(const float*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks, q16}, block_rows, st);
   else
-    quantise(QuantArgs<__nv_bfloat16>{(const __nv_bfloat16*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks}, block_rows, st);
+    quantise(QuantArgs<__nv_bfloat16>{(const __nv_bfloat16*)x, (uint8_t*)q, scale, ldx, ldq, rows, k, blocks, q16}, block_rows, st);
   return done(cudaGetLastError(), "pack_quantise_f8");
 }
 
@@ -545,7 +808,7 @@ tp_status pack_product_f8_bytes(int64_t rows, int32_t k, int32_t n, int32_t alig
   const tp_status s = check(rows, k, n, TP_BF16);
   if (s != TP_OK) return s;
   if (!workspace) return ops_fail(TP_EINVAL, "null argument");
-  *workspace = rows == 0 || aligned ? 0 : staged_bytes(rows, k) + staged_bytes(n, k);
+  *workspace = rows == 0 || aligned || few_take(rows, k, n) ? 0 : staged_bytes(rows, k) + staged_bytes(n, k);
   return TP_OK;
 }
 
@@ -560,6 +823,17 @@ tp_status pack_product_f8(const void* q, int64_t ldq, const float* scale, const 
   if (rows == 1) ldq = round_up(k, 16);   // (one row has no distance to the next)
   if (n == 1) ldw = round_up(k, 16);
   const bool q_ok = aligned16(q, ldq, 1), w_ok = aligned16(w, ldw, 1);
+  if (few_take(rows, k, n)) {
+    if ((s = ops_device()) != TP_OK) return s;
+    const FewArgs a{(const uint8_t*)q, (const uint8_t*)w, scale, w_scale, bias, y, ldq, ldw, (int32_t)rows, k, n,
+                    (int32_t)ceil_div(k, kBlock), precision == TP_FP32};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    // sixteen warps where there are K blocks for them and the CTAs are few
+    const bool deep = a.kb > 8 && ceil_div(n, 16) * ceil_div(rows, 32) <= 2 * kSms;
+    if (q_ok && w_ok) deep ? launch_few<16, true>(a, st) : launch_few<8, true>(a, st);
+    else deep ? launch_few<16, false>(a, st) : launch_few<8, false>(a, st);
+    return done(cudaGetLastError(), "pack_product_f8");
+  }
   const int64_t need = q_ok && w_ok ? 0 : staged_bytes(rows, k) + staged_bytes(n, k);
   if (need && (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255)))
     return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
@@ -581,8 +855,7 @@ tp_status pack_product_f8(const void* q, int64_t ldq, const float* scale, const 
   }
   g.sx = scale, g.sw = w_scale, g.bias = bias, g.y = y;
   g.M = (int32_t)rows, g.N = n, g.kb = (int32_t)ceil_div(k, kBlock), g.f32 = precision == TP_FP32;
-  if (ceil_div(rows, 256) * ceil_div(n, 256) >= kSms / 4) e = launch_f8<2, 256>(g, q, ldq, w, ldw, k, st);
-  else e = launch_f8<1, 128>(g, q, ldq, w, ldw, k, st);
+  e = run_product(g, q, ldq, w, ldw, k, st);
   return done(e, "pack_product_f8");
 }
 

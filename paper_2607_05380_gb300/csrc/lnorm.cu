@@ -12,6 +12,7 @@
 // that are kept for the backward pass are then exactly those of the s that it
 // reads, and it needs one round of sums per row instead of two.
 #include <algorithm>
+#include <type_traits>
 
 #include "lanes.cuh"
 #include "prod.cuh"
@@ -24,10 +25,35 @@ constexpr int32_t kMaxD = 16384;
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 256;
 constexpr int kBwdBlocks = 2 * kSms;
 
+// Warps per row and groups of eight elements per lane, so that few lanes idle.  By
+// single elements, whose addresses and predicates take issue slots, a lane has
+// eight, and a row more warps (2003 rows of 5001, fp32, backward: sixteen a lane 38
+// us).
+template <typename F>
+void by_row(int d, bool vec, F f) {
+  if (vec) {
+    if (d > 4096 && d <= 5120) f(Width<10, 2>(), std::integral_constant<int, 8>());
+    else if (d > 5120 && d <= 6144) f(Width<12, 2>(), std::integral_constant<int, 8>());
+    else by_width(d, [&](auto s) { f(s, std::integral_constant<int, 8>()); });
+    return;
+  }
+  using One = std::integral_constant<int, 1>;
+  if (d <= 256) f(Width<1, 1>(), One());
+  else if (d <= 512) f(Width<2, 1>(), One());
+  else if (d <= 1024) f(Width<4, 1>(), One());
+  else if (d <= 2048) f(Width<8, 1>(), One());
+  else if (d <= 12 * 256) f(Width<12, 1>(), One());
+  else if (d <= 4096) f(Width<16, 1>(), One());
+  else if (d <= 5120) f(Width<20, 1>(), One());
+  else if (d <= 6144) f(Width<24, 1>(), One());
+  else if (d <= 8192) f(Width<32, 1>(), One());
+  else f(Width<32, 2>(), One());
+}
+
 // Sums of kN values over the kW warps of a row, in a fixed order; red: a set of
-// [kN][16] that no one else writes before the next barrier but one.
+// [kN][32] that no one else writes before the next barrier but one.
 template <int kW, int kN>
-__device__ __forceinline__ void row_sums(float (&v)[kN], float (*red)[16], int warp, int lane, int grp) {
+__device__ __forceinline__ void row_sums(float (&v)[kN], float (*red)[32], int warp, int lane, int grp) {
 #pragma unroll
   for (int i = 0; i < kN; ++i) v[i] = warp_sum(v[i]);
   if constexpr (kW > 1) {
@@ -59,7 +85,7 @@ struct FwdArgs {
 template <typename T, int kW, int kV, int kE>
 __global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
   using L = Lane<T, kW, kV, kE>;
-  __shared__ float red[2][1][16];
+  __shared__ float red[2][1][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW;
   const int64_t row = (int64_t)blockIdx.x * (threads(kW) / 32 / kW) + grp;
@@ -112,6 +138,81 @@ __global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
   }
 }
 
+// Many rows by single elements: a block of the row's warps takes rows in turn,
+// with the weights in shared memory and the next row asked for before this one is
+// worked on.
+constexpr int many_threads(int kW) { return kW == 1 ? 128 : 32 * kW; }
+constexpr int many_blocks(int kW, int kV) {   // an SM: as many threads as leave the registers for a row and the next one
+  const int n = 65536 / 56 / many_threads(kW);
+  return n < 1 ? 1 : n < 16 ? n : 16;
+}
+template <typename T, int kW, int kV, int kE>
+__global__ void __launch_bounds__(many_threads(kW), many_blocks(kW, kV)) k_ln_fwd_many(const FwdArgs<T> g) {
+  static_assert(kE == 1, "one element at a time");
+  using L = Lane<T, kW, kV, kE>;
+  constexpr int kRows = many_threads(kW) / 32 / kW, kCols = 32 * kW * kV * 8;
+  extern __shared__ __align__(16) float ws[];   // weights, then biases
+  __shared__ float red[2][2][1][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW;
+  pdl_trigger();
+  pdl_wait();
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + grp;
+  L x, res;
+  auto ask = [&](int64_t at) {
+    const int d = at < g.rows ? g.d : 0;   // a row past the last one has no elements
+    x.load(g.x + at * g.ldx, wl, d);
+    if (g.res) res.load(g.res + at * g.ldr, wl, d);
+  };
+  ask(row);
+  for (int c = threadIdx.x; c < kCols; c += many_threads(kW)) {
+    ws[c] = c < g.d ? g.w[c] : 0.f;
+    ws[kCols + c] = c < g.d && g.b ? g.b[c] : 0.f;
+  }
+  __syncthreads();
+  int turn = 0;
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < g.rows; base += stride, row += stride, turn ^= 1) {
+    const int d = row < g.rows ? g.d : 0;
+    float v[L::kGroups][kE], a[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      x.get(i, v[i]);
+      if (g.res) {
+        float r[kE];
+        res.get(i, r);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) v[i][e] = Elem<T>::to_f(Elem<T>::from_f(v[i][e] + r[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) a[0] += v[i][e];   // (past the row: zeros)
+    }
+    if (base + stride < g.rows) ask(row + stride);
+    if (g.sum)
+#pragma unroll
+      for (int i = 0; i < L::kGroups; ++i) L::put(g.sum + row * g.d, i, wl, d, v[i]);
+    // (two sets of sums in turn: the next row's may be written while these are read)
+    row_sums<kW>(a, red[turn][0], warp, lane, grp);
+    const float mean = a[0] / (float)g.d;
+    a[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      v[i][0] -= mean;
+      a[0] += L::col(i, wl) < g.d ? v[i][0] * v[i][0] : 0.f;
+    }
+    row_sums<kW>(a, red[turn][1], warp, lane, grp);
+    const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
+    if (d && wl == 0 && g.stats) g.stats[row] = make_float2(mean, r);
+    if (g.y)
+#pragma unroll
+      for (int i = 0; i < L::kGroups; ++i) {
+        const float *w = ws + L::col(i, wl), *b = w + kCols;
+        v[i][0] = v[i][0] * r * w[0] + b[0];
+        L::put(g.y + row * g.d, i, wl, d, v[i]);
+      }
+  }
+}
+
 template <typename T>
 struct BwdArgs {
   const T *dy, *s, *dsum;
@@ -124,11 +225,11 @@ struct BwdArgs {
 };
 
 template <typename T, int kW, int kV, int kE>
-__global__ void __launch_bounds__(threads(kW), kW > 8 ? 1 : 2) k_ln_bwd(const BwdArgs<T> g) {
+__global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 12 && kE == 1) ? 1 : 2) k_ln_bwd(const BwdArgs<T> g) {
   using L = Lane<T, kW, kV, kE>;
   constexpr int kRows = threads(kW) / 32 / kW;   // rows at a time
   constexpr int kCols = 32 * kW * kV * 8;
-  __shared__ float red[2][2][16];
+  __shared__ float red[2][2][32];
   __shared__ __align__(16) float join[kRows > 1 ? kRows * kCols : kCols];
   float* ws = join;   // first the weights, at the end the rows' sums
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -151,8 +252,8 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 ? 1 : 2) k_ln_bwd(const Bw
   for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
     for (int e = 0; e < kE; ++e) dw[i][e] = db[i][e] = 0.f;
-  // bf16: the next rows are asked for before these are worked on
-  constexpr bool kAhead = sizeof(T) == 2 && kV <= 2 && kE == 8;
+  // the next rows are asked for before these are worked on, where there are registers for them
+  constexpr bool kAhead = kE == 8 ? kV <= 2 && sizeof(T) == 2 : kV == 1 && kW < 32;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + grp;
   L s, t, o;
@@ -269,26 +370,35 @@ __global__ void __launch_bounds__(1024) k_ln_dw(const float* part, int n, int d,
   }
 }
 
-int bwd_blocks(int64_t rows, int d) { return (int)std::min<int64_t>(ceil_div(rows, rows_per_block(d)), kBwdBlocks); }
+// As many blocks as run at once: two an SM, or one of the largest.  (Blocks that
+// take several rows at a time may find none: they leave sums of 0.)
+int bwd_blocks(int64_t rows, int d) { return (int)std::min<int64_t>(rows, d > 4096 ? kSms : kBwdBlocks); }
 
 template <typename T>
 void forward(const FwdArgs<T>& a, cudaStream_t st) {
   const bool vec = a.d % 8 == 0 && aligned16(a.x, a.ldx, sizeof(T)) && aligned16(a.res, a.ldr, sizeof(T)) &&
                    aligned16(a.w, 0, 4) && aligned16(a.b, 0, 4) && aligned16(a.sum, 0, 4) && aligned16(a.y, 0, 4);
-  by_width(a.d, [&](auto s) {
-    const dim3 grid((unsigned)ceil_div(a.rows, rows_per_block(a.d))), block(threads(s.w));
-    if (vec) launch_pdl(k_ln_fwd<T, s.w, s.v, 8>, grid, block, 0, st, a);
-    else launch_pdl(k_ln_fwd<T, s.w, s.v, 1>, grid, block, 0, st, a);
+  by_row(a.d, vec, [&](auto s, auto e) {
+    if constexpr (e.value == 1) {
+      constexpr int kRows = many_threads(s.w) / 32 / s.w, smem = 2 * 32 * s.w * s.v * 8 * 4;
+      const int64_t blocks = ceil_div(a.rows, kRows), most = many_blocks(s.w, s.v) * kSms;
+      if (blocks > most && smem <= 64 * 1024) {
+        if (smem > 48 * 1024)
+          cudaFuncSetAttribute(k_ln_fwd_many<T, s.w, s.v, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        launch_pdl(k_ln_fwd_many<T, s.w, s.v, 1>, dim3((unsigned)most), dim3(many_threads(s.w)), smem, st, a);
+        return;
+      }
+    }
+    const dim3 grid((unsigned)ceil_div(a.rows, threads(s.w) / 32 / s.w)), block(threads(s.w));
+    launch_pdl(k_ln_fwd<T, s.w, s.v, e.value>, grid, block, 0, st, a);
   });
 }
 template <typename T>
-void backward(const BwdArgs<T>& a, cudaStream_t st) {
+void backward(const BwdArgs<T>& a, int blocks, cudaStream_t st) {
   const bool vec = a.d % 8 == 0 && aligned16(a.dy, a.lddy, sizeof(T)) && aligned16(a.s, a.lds, sizeof(T)) &&
                    aligned16(a.dsum, a.lddsum, sizeof(T)) && aligned16(a.dx, 0, 4);
-  by_width(a.d, [&](auto s) {
-    const dim3 grid((unsigned)bwd_blocks(a.rows, a.d)), block(threads(s.w));
-    if (vec) launch_pdl(k_ln_bwd<T, s.w, s.v, 8>, grid, block, 0, st, a);
-    else launch_pdl(k_ln_bwd<T, s.w, s.v, 1>, grid, block, 0, st, a);
+  by_row(a.d, vec, [&](auto s, auto e) {
+    launch_pdl(k_ln_bwd<T, s.w, s.v, e.value>, dim3((unsigned)blocks), dim3(threads(s.w)), 0, st, a);
   });
 }
 
@@ -365,10 +475,10 @@ tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* sum
   float* part = sums ? (float*)workspace : nullptr;
   if (precision == TP_FP32)
     backward(BwdArgs<float>{(const float*)dy, (const float*)sum, (const float*)dsum, w, (const float2*)stats, (float*)dx,
-                            part, lddy, lds, lddsum, rows, d}, st);
+                            part, lddy, lds, lddsum, rows, d}, blocks, st);
   else
     backward(BwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)dy, (const __nv_bfloat16*)sum, (const __nv_bfloat16*)dsum, w,
-                                    (const float2*)stats, (__nv_bfloat16*)dx, part, lddy, lds, lddsum, rows, d}, st);
+                                    (const float2*)stats, (__nv_bfloat16*)dx, part, lddy, lds, lddsum, rows, d}, blocks, st);
   if (sums)
     launch_pdl(k_ln_dw, dim3((unsigned)ceil_div(2 * d, 32)), dim3(1024), 0, st, (const float*)part, blocks, d, dw, db);
   return done(cudaGetLastError(), "pack_layer_norm_backward");
