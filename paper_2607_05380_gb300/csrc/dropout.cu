@@ -70,13 +70,14 @@ __device__ __forceinline__ void drop8(const Args<T>& g, float (&v)[8], const Row
   }
 }
 
-// Eight columns a thread, loads and stores of 16 bytes; kRows rows in flight.  A
-// block's threads are one row's (kWide: what a row decides is then computed by
-// the uniform units, once a warp) or several rows'.
+template <typename T>
+constexpr int drop_blocks() { return sizeof(T) == 2 ? 6 : 5; }   // an SM
+// Eight columns a thread, loads and stores of 16 bytes, the next row asked for
+// before this one is worked on.  A block's threads are one row's (kWide: what a row
+// decides is then computed by the uniform units, once a warp) or several rows'.
 template <typename T, bool kWide>
-__global__ void __launch_bounds__(256) k_drop8(const Args<T> g) {
+__global__ void __launch_bounds__(256, drop_blocks<T>()) k_drop8(const Args<T> g) {
   using L = Lane<T, 1, 1, 8>;
-  constexpr int kRows = 4;
   const int tx = kWide ? threadIdx.x : threadIdx.x & ((1 << g.shift) - 1), ty = kWide ? 0 : threadIdx.x >> g.shift;
   const int rows_at_once = kWide ? 1 : 256 >> g.shift;
   const int c = 8 * (blockIdx.x * (1 << g.shift) + tx);
@@ -85,29 +86,25 @@ __global__ void __launch_bounds__(256) k_drop8(const Args<T> g) {
   pdl_wait();
   if (c >= g.d) return;
   const int64_t step = (int64_t)gridDim.y * rows_at_once;
-  for (int64_t row = (int64_t)blockIdx.y * rows_at_once + ty; row < g.rows; row += kRows * step) {
-    L x[kRows], res[kRows];
+  int64_t row = (int64_t)blockIdx.y * rows_at_once + ty;
+  L x, res;
+  auto ask = [&](int64_t r) {
+    const int there = r < g.rows ? 8 : 0;
+    x.load(g.x + r * g.ldx + c, 0, there);
+    if (g.res) res.load(g.res + r * g.ldr + c, 0, there);
+  };
+  ask(row);
+  for (; row < g.rows; row += step) {
+    float v[8], w[8];
+    x.get(0, v);
+    if (g.res) res.get(0, w);
+    ask(row + step);
+    if (g.drop) drop8(g, v, RowPart((uint32_t)row, g.step, g.site, g.k0, g.k1), cols);
+    if (g.res) {
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = row + u * step;
-      const int there = r < g.rows ? 8 : 0;
-      x[u].load(g.x + r * g.ldx + c, 0, there);
-      if (g.res) res[u].load(g.res + r * g.ldr + c, 0, there);
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
     }
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = row + u * step;
-      if (r >= g.rows) break;
-      float v[8], w[8];
-      x[u].get(0, v);
-      if (g.drop) drop8(g, v, RowPart((uint32_t)r, g.step, g.site, g.k0, g.k1), cols);
-      if (g.res) {
-        res[u].get(0, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += w[e];
-      }
-      L::put(g.y + r * g.d + c, 0, 0, 8, v);
-    }
+    L::put(g.y + row * g.d + c, 0, 0, 8, v);
   }
 }
 
@@ -155,8 +152,8 @@ void run(Args<T> a, cudaStream_t st) {
     while (a.shift < 8 && (8 << a.shift) < a.d) ++a.shift;
     const bool wide = a.shift >= 5;
     const int64_t across = ceil_div(a.d, 8 << a.shift), at_once = wide ? 1 : 256 >> a.shift;
-    // blocks for every SM to be full, as many rows each as that leaves
-    const int64_t most = std::max<int64_t>(1, (wide ? 8 * (256 >> a.shift) : 8) * kSms / across);
+    // as many blocks as run at once (8192 x 2048, bf16, both passes: 37 us; a block a row 41)
+    const int64_t most = std::max<int64_t>(1, drop_blocks<T>() * (wide ? 256 >> a.shift : 1) * kSms / across);
     const dim3 grid((unsigned)across, (unsigned)std::min<int64_t>(std::min<int64_t>(ceil_div(a.rows, at_once), most), 65535));
     if (wide) launch_pdl(k_drop8<T, true>, grid, dim3(1u << a.shift), 0, st, a);
     else launch_pdl(k_drop8<T, false>, grid, dim3(256), 0, st, a);

@@ -103,13 +103,17 @@ struct Split {
   int e, shift, items;
   int64_t width() const { return (int64_t)(e * items) << shift; }
 };
-// A warp a row where the row is wide enough for it, with as few columns a lane as
-// that takes (the longest chain of a lane's work is what counts); e_most: what
-// the addresses allow.
-Split split_cols(int d, int e_most) {
+// The sums' split of n tokens: a warp a row where the row is wide enough for it,
+// with as few columns a lane as that takes, because the longest chain of a lane's
+// work is what counts; but of more tokens than that keeps the GPU busy with, more
+// columns a lane, because then the instructions a token are (800 440 tokens of 64
+// columns, both passes: two columns a lane 187 us, four 164, eight 179).  e_most:
+// what the addresses allow.
+Split split_cols(int64_t n, int d, int e_most) {
   Split s{1, 5, 1};
   while (s.e < e_most && s.e * 32 < d) s.e *= 2;
   while (s.shift > 0 && (s.e << (s.shift - 1)) >= d) --s.shift;
+  while (s.e < e_most && s.shift > 0 && (n >> 4) << (s.shift - 1) >= (int64_t)128 * 32 * kSms) s.e *= 2, --s.shift;
   if (s.e == 1) s.items = (int)std::min<int64_t>(4, ceil_div(d, 32));
   return s;
 }
@@ -139,38 +143,45 @@ struct LookArgs {
 };
 template <typename T, typename O, int kE, int kI>
 __global__ void __launch_bounds__(256) k_lookup(const LookArgs<T, O> g) {
-  constexpr int kU = 4;   // tokens in flight
+  constexpr int kU = 2;   // tokens in flight
   const int lanes = 1 << g.shift, groups = 256 >> g.shift;
   const int at = threadIdx.x & (lanes - 1), grp = threadIdx.x >> g.shift;
-  const int64_t t0 = (int64_t)blockIdx.x * (groups * kU) + grp, c0 = ((int64_t)blockIdx.y * kI * lanes + at) * kE;
+  const int64_t c0 = ((int64_t)blockIdx.y * kI * lanes + at) * kE, step = (int64_t)gridDim.x * groups * kU;
   pdl_trigger();
   pdl_wait();
-  uint32_t id[kU];
+  int64_t t0 = (int64_t)blockIdx.x * (groups * kU) + grp;
+  uint32_t next[kU];   // the ids asked for
+  auto ask = [&](int64_t from) {
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const int64_t t = t0 + u * groups;
-    id[u] = t < g.n ? g.ids.at(t) : (uint32_t)g.ids.vocab;
-  }
-  Cols<T, kE> v[kU][kI];
+    for (int u = 0; u < kU; ++u) next[u] = from + u * groups < g.n ? g.ids.at(from + u * groups) : (uint32_t)g.ids.vocab;
+  };
+  ask(t0);
+  for (; t0 < g.n; t0 += step) {
+    uint32_t id[kU];
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const bool there = id[u] < (uint32_t)g.ids.vocab;
-    const T* row = g.table + (there ? (int64_t)id[u] * g.ldt : 0) + c0;
+    for (int u = 0; u < kU; ++u) id[u] = next[u];
+    Cols<T, kE> v[kU][kI];
 #pragma unroll
-    for (int i = 0; i < kI; ++i) v[u][i].load(row + i * lanes * kE, there && c0 + i * lanes * kE < g.d);
-  }
+    for (int u = 0; u < kU; ++u) {
+      const bool there = id[u] < (uint32_t)g.ids.vocab;
+      const T* row = g.table + (there ? (int64_t)id[u] * g.ldt : 0) + c0;
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const int64_t t = t0 + u * groups;
-    if (t >= g.n) break;
-    const bool there = id[u] < (uint32_t)g.ids.vocab;
+      for (int i = 0; i < kI; ++i) v[u][i].load(row + i * lanes * kE, there && c0 + i * lanes * kE < g.d);
+    }
+    ask(t0 + step);
 #pragma unroll
-    for (int i = 0; i < kI; ++i) {
-      if (c0 + i * lanes * kE >= g.d) break;
-      float f[kE];
+    for (int u = 0; u < kU; ++u) {
+      const int64_t t = t0 + u * groups;
+      if (t >= g.n) break;
+      const bool there = id[u] < (uint32_t)g.ids.vocab;
 #pragma unroll
-      for (int e = 0; e < kE; ++e) f[e] = there ? v[u][i].get(e) * g.scale : 0.f;   // (no -0, no NaN by the scale)
-      Cols<O, kE>::put(g.y + t * g.d + c0 + i * lanes * kE, f);
+      for (int i = 0; i < kI; ++i) {
+        if (c0 + i * lanes * kE >= g.d) break;
+        float f[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) f[e] = there ? v[u][i].get(e) * g.scale : 0.f;   // (no -0, no NaN by the scale)
+        Cols<O, kE>::put(g.y + t * g.d + c0 + i * lanes * kE, f);
+      }
     }
   }
 }
@@ -377,7 +388,7 @@ __global__ void __launch_bounds__(256) k_sort_scan(uint32_t* count, uint32_t* to
 }
 
 template <int kRounds>
-__global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const SortArgs g) {
+__global__ void __launch_bounds__(kSortThreads, kRounds <= 4 ? 3 : 2) k_sort_scatter(const SortArgs g) {
   extern __shared__ uint32_t sm[];
   uint32_t* base = sm;
   uint16_t* wh = (uint16_t*)(sm + (1 << g.bits) + 32);
@@ -707,12 +718,12 @@ struct Plan {
   int64_t blocks, m[kLevels], run_blocks[kLevels];
   int64_t key[2], val[2], count, total, seen, part_key[kLevels], part[kLevels], bytes;
   Plan(int64_t n, int32_t vocab, int32_t d, int e) {
-    split = split_cols(d, e);
+    split = split_cols(n, d, e);
     bits_all = 0;
     while (bits_all < 31 && (uint32_t)vocab >> bits_all) ++bits_all;
     passes = (int32_t)ceil_div(bits_all, kMaxBits);
     bits = std::max<int32_t>(3, (int32_t)ceil_div(bits_all, passes));   // (whole warps of four lanes a digit)
-    rounds = n <= 2 * kSortThreads * 2 * kSms ? 2 : 8;
+    rounds = n <= 2 * kSortThreads * 2 * kSms ? 2 : n <= 4 * kSortThreads * 4 * kSms ? 4 : 8;   // a wave or two of blocks
     blocks = ceil_div(n, kSortThreads * rounds);
     Carver c(nullptr);
     auto take = [&](int64_t b) {
@@ -725,10 +736,11 @@ struct Plan {
     total = take(4 << bits);
     seen = take(round_up(vocab, 16));
     for (int64_t left = n;;) {
-      // entries a group: 16, or 32 where the blocks fill the GPU several times all the same; one block takes what
-      // is left once it can with 32
+      // entries a group: 16, or 32 where the blocks then fill the GPU all the same; one block takes what is
+      // left once it can with 32
       const int64_t groups = (levels ? kJoinThreads : kRunThreads) >> split.shift;
-      int64_t per = levels == 0 && left >= groups * 32 * 4 * kSms ? 32 : 16;
+      int64_t per = 16;
+      while (levels == 0 && per < 32 && left > groups * per * 2 * kSms) per *= 2;
       per = std::min(per, kMostEntries / groups);
       if (levels && left <= std::min<int64_t>(32 * groups, kMostEntries)) per = std::max<int64_t>(1, ceil_div(left, groups));
       m[levels] = left, chunk[levels] = (int32_t)per, run_blocks[levels] = ceil_div(left, groups * per);
@@ -813,9 +825,11 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
       s.key = key[at ^ 1], s.val = val[at ^ 1], s.key_out = key[at], s.val_out = val[at];
       const dim3 grid((unsigned)p.blocks), block(kSortThreads);
       if (p.rounds == 2) launch_pdl(k_sort_count<2>, grid, block, 0, st, s);
+      else if (p.rounds == 4) launch_pdl(k_sort_count<4>, grid, block, 0, st, s);
       else launch_pdl(k_sort_count<8>, grid, block, 0, st, s);
       launch_pdl(k_sort_scan, dim3((unsigned)ceil_div(bins, 8)), dim3(256), 0, st, s.count, s.total, (int)p.blocks, bins);
       if (p.rounds == 2) launch_pdl(k_sort_scatter<2>, grid, block, sm, st, s);
+      else if (p.rounds == 4) launch_pdl(k_sort_scatter<4>, grid, block, sm, st, s);
       else launch_pdl(k_sort_scatter<8>, grid, block, sm, st, s);
       at ^= 1;
     }
@@ -852,16 +866,15 @@ template <typename T, typename O>
 void lookup(const Ids& ids, int64_t n, const T* table, int64_t ldt, int32_t d, float scale, O* y, cudaStream_t st) {
   int most = 8;
   while (most > 1 && !(fits(table, ldt, d, sizeof(T), most) && fits(y, d, d, sizeof(O), most))) most /= 2;
-  Split s = split_cols(d, most);
-  // (no chains here: the widest loads)
-  if (most > s.e) s = Split{most, 0, 1};
-  while (s.e > 1 && s.shift < 5 && (s.e << s.shift) < d) ++s.shift;
+  // no chains here: the widest loads
+  Split s{most, 0, most == 1 ? (int)std::min<int64_t>(4, ceil_div(d, 32)) : 1};
+  while (s.shift < 5 && (s.e << s.shift) < d) ++s.shift;
   LookArgs<T, O> a{ids, table, y, n, ldt, d, s.shift, scale};
   if (most == 1 && ((uintptr_t)y & 15) == 0) {
     launch_pdl(k_lookup_flat<T, O>, dim3((unsigned)ceil_div(n * d, 2048)), dim3(256), 0, st, a);
     return;
   }
-  const dim3 grid((unsigned)ceil_div(n, (int64_t)(256 >> s.shift) * 4), (unsigned)ceil_div(d, s.width()));
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(256 >> s.shift) * 2), 8 * kSms), (unsigned)ceil_div(d, s.width()));
   with_split(s, [&](auto c, auto i) { launch_pdl(k_lookup<T, O, c.value, i.value>, grid, dim3(256), 0, st, a); });
 }
 
