@@ -112,8 +112,8 @@ struct Split {
 Split split_cols(int64_t n, int d, int e_most) {
   Split s{1, 5, 1};
   while (s.e < e_most && s.e * 32 < d) s.e *= 2;
-  while (s.shift > 0 && (s.e << (s.shift - 1)) >= d) --s.shift;
-  while (s.e < e_most && s.shift > 0 && (n >> 4) << (s.shift - 1) >= (int64_t)128 * 32 * kSms) s.e *= 2, --s.shift;
+  while (s.shift > 3 && (s.e << (s.shift - 1)) >= d) --s.shift;   // (lanes idle in rows of less than eight columns: more, shorter lists)
+  while (s.e < e_most && s.shift > 3 && (n >> 4) << (s.shift - 1) >= (int64_t)128 * 32 * kSms) s.e *= 2, --s.shift;
   if (s.e == 1) s.items = (int)std::min<int64_t>(4, ceil_div(d, 32));
   return s;
 }
@@ -245,6 +245,14 @@ __device__ __forceinline__ uint32_t key_at(const SortArgs& g, int64_t i) { retur
 __device__ __forceinline__ void clear_seen(const SortArgs& g, int64_t thread, int64_t threads) {
   const int64_t words = ((int64_t)g.ids.vocab + 15) >> 4;
   for (int64_t i = thread; i < words; i += threads) reinterpret_cast<uint4*>(g.seen)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// Of a launch whose first block sorts alone: the others, where the table is large
+// enough for some, clear its bytes.  Is this one of them?
+__device__ __forceinline__ bool clears(const SortArgs& g) {
+  if (blockIdx.x > 0) clear_seen(g, (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x, (int64_t)(gridDim.x - 1) * blockDim.x);
+  else if (gridDim.x == 1) clear_seen(g, threadIdx.x, blockDim.x);
+  return blockIdx.x > 0;
 }
 
 // Exclusive prefix sums of v[0 .. bins - 1] in shared memory, by the whole block.
@@ -506,26 +514,71 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_sort_cluster(const SortA
     if (i0 + 32 * r < g.n) g.key_out[i0 + 32 * r] = key[r], g.val_out[i0 + 32 * r] = val[r];
 }
 
-// A few tokens: each one's place is the number of those before it.
-constexpr int kFew = 1024;
+// A few tokens: each one's place is the number of those before it (256 tokens 2 us,
+// but 1000 of them 21).
+constexpr int kFew = 256;
 __global__ void __launch_bounds__(kFew) k_sort_few(const SortArgs g) {
   __shared__ __align__(16) uint32_t ks[kFew];
   pdl_trigger();
   pdl_wait();
   const int i = threadIdx.x, n4 = ((int)g.n + 3) >> 2;
-  const uint32_t key[1] = {i < g.n ? g.ids.at(i) : kLast};
-  ks[i] = key[0];
-  clear_seen(g, i, blockDim.x);
+  if (clears(g)) return;
+  const uint32_t key = i < g.n ? g.ids.at(i) : kLast;
+  ks[i] = key;
   __syncthreads();
   uint32_t to = 0;
 #pragma unroll 4
   for (int j = 0; j < n4; ++j) {
     const uint4 k = reinterpret_cast<const uint4*>(ks)[j];
-    to += (k.x < key[0]) + (k.y < key[0]) + (k.z < key[0]) + (k.w < key[0]);
-    to += (k.x == key[0] && 4 * j < i) + (k.y == key[0] && 4 * j + 1 < i) + (k.z == key[0] && 4 * j + 2 < i) +
-          (k.w == key[0] && 4 * j + 3 < i);
+    to += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    to += (k.x == key && 4 * j < i) + (k.y == key && 4 * j + 1 < i) + (k.z == key && 4 * j + 2 < i) +
+          (k.w == key && 4 * j + 3 < i);
   }
-  if (i < g.n) g.key_out[to] = key[0], g.val_out[to] = i;
+  if (i < g.n) g.key_out[to] = key, g.val_out[to] = i;
+}
+
+// Up to 4096 tokens: every pass in one block, digits of at most kTileBits bits (the
+// counts are cleared and added up in every pass).
+constexpr int kTileThreads = 1024, kTileBits = 7;
+template <int kR>
+constexpr int tile_smem(int bits) {
+  return kR * kTileThreads * 8 + (2 * (1 << bits) + 32) * 4 + (1 << bits) * (kTileThreads / 32) * 2;
+}
+template <int kR>
+__global__ void __launch_bounds__(kTileThreads, 1) k_sort_tile(const SortArgs g) {
+  extern __shared__ __align__(16) uint32_t sm[];
+  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint2* sorted = (uint2*)sm;
+  uint32_t *base = (uint32_t*)(sorted + kR * kTileThreads);
+  uint16_t* wh = (uint16_t*)(base + bins + 32);
+  pdl_trigger();
+  pdl_wait();
+  if (clears(g)) return;
+  const int at0 = warp * (32 * kR) + lane;
+  uint32_t key[kR], val[kR], rank[kR];
+#pragma unroll
+  for (int r = 0; r < kR; ++r) {
+    val[r] = at0 + 32 * r;
+    key[r] = (int)val[r] < g.n ? g.ids.at(val[r]) : kLast;
+  }
+  for (int shift = 0; shift < g.bits_all; shift += g.bits) {
+    rank_tile<kTileThreads>(key, shift, g.bits, wh, base, rank);
+    block_scan<kTileThreads>(base, bins, base + bins);
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const uint32_t digit = key[r] >> shift & (bins - 1);
+      sorted[base[digit] + wh[warp * bins + digit] + rank[r]] = make_uint2(key[r], val[r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+      const uint2 t = sorted[at0 + 32 * r];
+      key[r] = t.x, val[r] = t.y;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+    if (at0 + 32 * r < g.n) g.key_out[at0 + 32 * r] = key[r], g.val_out[at0 + 32 * r] = val[r];
 }
 
 // --------------------------------------------------------------------- runs
@@ -543,8 +596,37 @@ struct RunArgs {
   float scale;
 };
 
-// Rows without a token become zero: a warp takes 32 of them, 2^shift lanes a row,
-// by 16-byte stores where the rows lie on multiples of 16 bytes.
+// Rows without a token become zero.  Where they do not lie on multiples of 16 bytes
+// (but the table does), a thread takes 16 bytes whatever rows they belong to.
+template <typename O>
+__device__ __forceinline__ void zero_flat(const uint8_t* seen, O* out, int64_t vocab, int d, int64_t block, int64_t blocks) {
+  constexpr int kE = 16 / sizeof(O);
+  const int64_t total = vocab * d, step = blocks * blockDim.x * kE;
+  for (int64_t base = (block * blockDim.x + (threadIdx.x & ~31)) * kE; base < total; base += step) {
+    const int64_t row0 = base / d;   // of the warp's first element
+    const uint32_t off = (uint32_t)(base - row0 * d) + (threadIdx.x & 31) * kE, row = off / (uint32_t)d;
+    const int64_t at = base + (threadIdx.x & 31) * kE;
+    if (at >= total) continue;
+    uint32_t c = off - row * (uint32_t)d;
+    int64_t r = row0 + row;
+    uint32_t keep = 0, here = seen[r];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      if (at + e < total) keep |= (here ? 1u : 0u) << e;
+      if (++c == (uint32_t)d && e + 1 < kE) c = 0, here = ++r < vocab ? seen[r] : 1u;
+    }
+    const float zero[kE] = {};
+    if (keep == 0 && at + kE <= total) {
+      Cols<O, kE>::put(out + at, zero);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        if (!(keep >> e & 1) && at + e < total) out[at + e] = Elem<O>::from_f(0.f);
+    }
+  }
+}
+// A warp takes 32 rows, 2^shift lanes a row, by 16-byte stores where the rows lie on
+// multiples of 16 bytes.
 template <typename O, int kE>
 __device__ __forceinline__ void zero_rows(const uint8_t* seen, O* out, int64_t vocab, int d, int64_t block, int64_t blocks) {
   const int lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
@@ -578,6 +660,7 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
     constexpr int kWide = 16 / sizeof(O);
     const int64_t block = blockIdx.x - g.run_blocks, blocks = gridDim.x - g.run_blocks;
     if (g.wide) zero_rows<O, kWide>(g.seen, g.out, g.vocab, g.d, block, blocks);
+    else if (((uintptr_t)g.out & 15) == 0) zero_flat(g.seen, g.out, g.vocab, g.d, block, blocks);
     else zero_rows<O, 1>(g.seen, g.out, g.vocab, g.d, block, blocks);
     return;
   }
@@ -680,13 +763,29 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
     if (e && (keys[e - 1] & ~kSkip) == key) continue;
     clear();
     int j = e;
-    for (; j < n && (keys[j] & ~kSkip) == key; ++j) {
-      if (keys[j] & kSkip) continue;
-      any = true;
+    for (bool more = true; more;) {   // four entries at a time
+      uint32_t k[4];
+      float v[4][kI][kE];
 #pragma unroll
-      for (int i = 0; i < kI; ++i)
+      for (int u = 0; u < 4; ++u) {
+        k[u] = j + u < n ? keys[j + u] : kLast;
 #pragma unroll
-        for (int c = 0; c < kE; ++c) acc[i][c] += slot(j, i)[c];
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+          for (int c = 0; c < kE; ++c) v[u][i][c] = k[u] == key ? slot(j + u, i)[c] : 0.f;
+      }
+      int same = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        more = more && (k[u] & ~kSkip) == key && k[u] != kLast;
+        same += more;
+        any = any || (more && k[u] == key);
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+          for (int c = 0; c < kE; ++c) acc[i][c] += v[u][i][c];   // (an entry of the key lies in its run)
+      }
+      j += same;
     }
     const bool from = e == 0 && block_before == key, on = j == n && block_after == key;
     if (any && !from && !on) write(key);
@@ -721,7 +820,7 @@ struct Plan {
     split = split_cols(n, d, e);
     bits_all = 0;
     while (bits_all < 31 && (uint32_t)vocab >> bits_all) ++bits_all;
-    passes = (int32_t)ceil_div(bits_all, kMaxBits);
+    passes = (int32_t)ceil_div(bits_all, n <= 4 * kTileThreads ? kTileBits : kMaxBits);
     bits = std::max<int32_t>(3, (int32_t)ceil_div(bits_all, passes));   // (whole warps of four lanes a digit)
     rounds = n <= 2 * kSortThreads * 2 * kSms ? 2 : n <= 4 * kSortThreads * 4 * kSms ? 4 : 8;   // a wave or two of blocks
     blocks = ceil_div(n, kSortThreads * rounds);
@@ -766,8 +865,13 @@ cudaError_t run_level(RunArgs<T, O> a, const Split& s, int threads, int64_t zero
   const size_t smem = (size_t)2 * threads * s.e * s.items * 4 + (size_t)(threads >> s.shift) * a.chunk * 8;
   cudaError_t e = cudaSuccess;
   with_split(s, [&](auto c, auto i) {
-    if (smem > 32 * 1024)
-      e = cudaFuncSetAttribute(k_runs<T, O, c.value, i.value>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
+    if (smem > 32 * 1024) {
+      static OncePerDevice once;
+      e = once([] {
+        return cudaFuncSetAttribute(k_runs<T, O, decltype(c)::value, decltype(i)::value>,
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
+      });
+    }
     if (e == cudaSuccess) launch_pdl(k_runs<T, O, c.value, i.value>, grid, dim3((unsigned)threads), smem, st, a);
   });
   return e;
@@ -776,8 +880,12 @@ cudaError_t run_level(RunArgs<T, O> a, const Split& s, int threads, int64_t zero
 template <int kR>
 cudaError_t sort_cluster(const SortArgs& s, cudaStream_t st) {
   const int smem = cluster_smem<kR>(s.bits);
-  cudaError_t e = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  static OncePerDevice once;
+  const cudaError_t e = once([] {
+    const cudaError_t a = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               cluster_smem<kR>(kMaxBits));
+    return a == cudaSuccess ? cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : a;
+  });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kCluster);
@@ -809,8 +917,14 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
   s.first = 1, s.key_out = key[0], s.val_out = val[0];
   cudaError_t e = cudaSuccess;
   int at = 0;
+  const dim3 one(1 + (unsigned)std::min<int64_t>(ids.vocab >> 16, kSms));   // the block that sorts, and 64 KB to clear a block
   if (n <= kFew) {
-    launch_pdl(k_sort_few, dim3(1), dim3((unsigned)round_up(n, 32)), 0, st, s);
+    launch_pdl(k_sort_few, one, dim3(one.x > 1 ? kFew : (unsigned)round_up(n, 32)), 0, st, s);
+  } else if (n <= kTileThreads) {
+    launch_pdl(k_sort_tile<1>, one, dim3(kTileThreads), tile_smem<1>(p.bits), st, s);
+  } else if (n <= 4 * kTileThreads) {
+    static_assert(tile_smem<4>(kTileBits) <= 48 * 1024, "a block's shared memory");
+    launch_pdl(k_sort_tile<4>, one, dim3(kTileThreads), tile_smem<4>(p.bits), st, s);
   } else if (n <= 2 * kCluster * kClusterThreads) {
     e = sort_cluster<2>(s, st);
   } else if (n <= 4 * kCluster * kClusterThreads) {

@@ -210,6 +210,39 @@ void quantise(const QuantArgs<T>& a, int block_rows, cudaStream_t st) {
 }
 
 // ------------------------------------------------------------------ staging
+// 16 bytes from `p`, `left` of which lie inside the row; zeros past it.  Elsewhere
+// than at a multiple of 16 by words that lie inside [lo, hi), the whole matrix, and
+// at its ends by bytes.
+template <bool kVec>
+__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int left, const uint8_t* lo, const uint8_t* hi) {
+  if (left <= 0) return make_uint4(0u, 0u, 0u, 0u);
+  if constexpr (kVec) {
+    if (left >= 16) return *reinterpret_cast<const uint4*>(p);
+  }
+  const int shift = (int)((uintptr_t)p & 3);
+  const uint8_t* from = p - shift;
+  uint32_t w[4];
+  if (from >= lo && from + 20 <= hi) {
+    uint32_t v[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = 4 * i < left + shift ? *reinterpret_cast<const uint32_t*>(from + 4 * i) : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 8 * shift);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // nothing of what lies behind the row
+      const int in = left - 4 * i;
+      w[i] = in >= 4 ? w[i] : in <= 0 ? 0u : w[i] & (0xffffffffu >> (8 * (4 - in)));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = 0u;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e < left) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Rows of k bytes at any address into rows that TMA takes.
 struct CopyArgs {
   const uint8_t* src;
@@ -226,12 +259,8 @@ __global__ void __launch_bounds__(256) k_copy_rows(const CopyArgs a, const CopyA
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / groups;
     const int c = (int)(i - row * groups) * 16;
-    const uint8_t* p = g.src + row * g.ld + c;
-    uint32_t w[4] = {};
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (c + e < g.k) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
-    *reinterpret_cast<uint4*>(g.dst + row * g.ldp + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(g.dst + row * g.ldp + c) =
+        bytes16<false>(g.src + row * g.ld + c, g.k - c, g.src, g.src + (g.rows - 1) * g.ld + g.k);
   }
 }
 
@@ -292,6 +321,20 @@ __device__ __forceinline__ void tile_at(const F8Args& g, int t, int& m, int& n) 
   const int group = t / (8 * g.tn), rows = min(8, g.tm - 8 * group), local = t - group * 8 * g.tn;
   m = 8 * group + local % rows;
   n = local / rows;
+}
+
+// A warp's 32 x 32 chunk (lane = row) into rows at any address: a row's 32 columns
+// side by side (20011 x 1024 -> 1001: 102 us by each lane's own eight columns).
+template <typename T>
+__device__ __forceinline__ void emit_rows(float* buf, int lane, const float (&v)[32], T* out, int n, int r0, int m_lim, int c0) {
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < 32; ++e) buf[lane * 32 + (e ^ lane)] = v[e];
+  __syncwarp();
+  if (c0 + lane < n)
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r)
+      if (r0 + r < m_lim) out[(int64_t)(r0 + r) * n + c0 + lane] = Elem<T>::from_f(buf[r * 32 + (lane ^ r)]);
 }
 
 // wait_all without a call: the epilogue's registers leave none for one.
@@ -526,12 +569,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
         const int64_t at = (int64_t)(r0 + lane) * g.N + col;
         if (g.f32) {
           if (left >= 32 && ((uintptr_t)g.y & 31) == 0 && (g.N & 7) == 0) put_f32(v, (float*)g.y + at, live, 32);
-          else emit_f32(out_buf, lane, v, (float*)g.y, g.N, r0, g.M, col, g.N, vec_ok(g.y, g.N, 4));
+          else if (vec_ok(g.y, g.N, 4)) emit_f32(out_buf, lane, v, (float*)g.y, g.N, r0, g.M, col, g.N, true);
+          else emit_rows((float*)out_buf, lane, v, (float*)g.y, g.N, r0, g.M, col);
         } else {
           uint32_t pk[16];
           pack32(v, pk);
           if (left >= 32 && ((uintptr_t)g.y & 31) == 0 && (g.N & 15) == 0) put_bf16(pk, (__nv_bfloat16*)g.y + at, live, 32);
-          else emit_bf16(out_buf, lane, pk, (__nv_bfloat16*)g.y, g.N, r0, g.M, col, g.N, vec_ok(g.y, g.N, 2));
+          else if (vec_ok(g.y, g.N, 2)) emit_bf16(out_buf, lane, pk, (__nv_bfloat16*)g.y, g.N, r0, g.M, col, g.N, true);
+          else emit_rows((float*)out_buf, lane, v, (__nv_bfloat16*)g.y, g.N, r0, g.M, col);
         }
       }
     }
@@ -565,7 +610,9 @@ cudaError_t launch_f8(F8Args& g, const void* q, int64_t ldq, const void* w, int6
   if (!tma_map_bytes(&g.a, q, k, g.M, ldq, kBlock, 128) || !tma_map_bytes(&g.b, w, k, g.N, ldw, kBlock, kN / kCta))
     return cudaErrorInvalidValue;
   const int smem = 1024 + kStages * (kABytes + kN / kCta * kBlock) + kEpiWarps * kBufBytes + (int)sizeof(Tail);
-  cudaError_t e = cudaFuncSetAttribute(k_prod_f8<kCta, kN, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static OncePerDevice once;
+  const cudaError_t e = once(
+      [] { return cudaFuncSetAttribute(k_prod_f8<kCta, kN, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448); });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   // a cluster a tile where K is shared out, else as many as run at once
@@ -596,14 +643,15 @@ tp_status check(int64_t rows, int32_t k, int32_t n, int32_t precision) {
 
 // The tile, by times measured: us a K block, of a tile alone on its SMs and with
 // all of them at work (there the pairs' half of the traffic from L2 counts), and
-// what a launch takes besides.  A K block's time is hardly less for fewer
+// what a launch and a tile's results take besides.  A K block's time is hardly less for fewer
 // columns, because it is the chain from MMA to epilogue and back that it waits for.
 struct Shape {
   int rows, cols, split;
-  double kb, kb_full, fixed;
+  double kb, kb_full, fixed, epi;
 };
-constexpr Shape kShapes[] = {{256, 256, 1, 0.44, 0.55, 5.0}, {128, 128, 1, 0.235, 0.31, 3.2}, {128, 64, 1, 0.225, 0.31, 2.7},
-                             {128, 64, 2, 0.225, 0.31, 4.2}, {128, 64, 4, 0.225, 0.31, 5.5}};
+constexpr Shape kShapes[] = {{256, 256, 1, 0.44, 0.55, 5.0, 3.0}, {128, 128, 1, 0.235, 0.31, 3.2, 1.5},
+                             {128, 64, 1, 0.225, 0.31, 2.7, 1.0}, {128, 64, 2, 0.225, 0.31, 4.2, 1.0},
+                             {128, 64, 4, 0.225, 0.31, 5.5, 1.0}};
 int pick_shape(int64_t rows, int64_t n, int64_t kb) {
   int pick = 0;
   double best = 1e30;
@@ -611,7 +659,8 @@ int pick_shape(int64_t rows, int64_t n, int64_t kb) {
     const Shape& s = kShapes[i];
     const int64_t tiles = ceil_div(rows, s.rows) * ceil_div(n, s.cols), at_once = kSms / (s.rows / 128 * s.split);
     if (s.split > 1 && (tiles > at_once || kb < s.split)) continue;
-    const double t = s.fixed + (double)(ceil_div(tiles, at_once) * ceil_div(kb, s.split)) * (tiles > at_once ? s.kb_full : s.kb);
+    const double waves = (double)ceil_div(tiles, at_once);
+    const double t = s.fixed + waves * (double)ceil_div(kb, s.split) * (tiles > at_once ? s.kb_full : s.kb) + (waves - 1) * s.epi;
     if (t < best) best = t, pick = i;
   }
   return pick;
@@ -644,19 +693,6 @@ __device__ __forceinline__ uint32_t f16_of(uint32_t two) {   // two e4m3 numbers
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
   return r;
 }
-// 16 bytes from `p`, `left` of which lie inside the row; zeros past it.
-template <bool kVec>
-__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int left) {
-  if constexpr (kVec) {
-    // (rows and their distance are multiples of 16: the last piece of a row may be filled up by what lies behind it)
-    if (left >= 16) return *reinterpret_cast<const uint4*>(p);
-  }
-  uint32_t w[4] = {};
-#pragma unroll
-  for (int e = 0; e < 16; ++e)
-    if (e < left) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 constexpr int kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
 template <int kNT, int kWarps, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
@@ -671,6 +707,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) asm volatile("prefetch.global.L2 [%0];" ::"l"(wr[h] + min(kBlock * warp + 32 * t, g.k - 1)));
   pdl_wait();
+  const uint8_t *w_end = g.w + (g.n - 1) * g.ldw + g.k, *x_end = g.x + (g.rows - 1) * g.ldx + g.k;
   float acc[kNT][4];
 #pragma unroll
   for (int j = 0; j < kNT; ++j)
@@ -685,11 +722,11 @@ __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
     for (int p = 0; p < 2; ++p) {
       const int k = kBlock * b + 64 * p + 16 * t;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) wv[h][p] = bytes16<kVec>(wr[h] + k, n0 + gid + 8 * h < g.n ? g.k - k : 0);
+      for (int h = 0; h < 2; ++h) wv[h][p] = bytes16<kVec>(wr[h] + k, n0 + gid + 8 * h < g.n ? g.k - k : 0, g.w, w_end);
 #pragma unroll
       for (int j = 0; j < kNT; ++j) {
         const int m = m0 + 8 * j + gid;
-        xv[j][p] = bytes16<kVec>(g.x + (int64_t)min(m, g.rows - 1) * g.ldx + k, m < g.rows ? g.k - k : 0);
+        xv[j][p] = bytes16<kVec>(g.x + (int64_t)min(m, g.rows - 1) * g.ldx + k, m < g.rows ? g.k - k : 0, g.x, x_end);
       }
     }
     const float ws = sw[b];

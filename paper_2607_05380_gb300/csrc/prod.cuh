@@ -14,6 +14,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "tabpack_ops.h"
 #include "tp_internal.cuh"
 
@@ -109,6 +111,22 @@ inline bool tma_ready(const void* p, int64_t ld) { return ((uintptr_t)p & 15) ==
 cudaError_t prod_err_word(int** word);
 // A TMA map of [rows][cols] bytes, ld from row to row, 128-byte swizzle; base and ld are multiples of 16.
 bool tma_map_bytes(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_cols, int box_rows);
+
+// Runs f (a cudaError_t of no arguments: a kernel's attributes) once per device
+// that succeeds; a failure is tried again by the next call.
+struct OncePerDevice {
+  std::atomic<uint64_t> done{0};
+  template <typename F>
+  cudaError_t operator()(F f) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    if ((e = f()) == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
+};
 
 // Error reporting of the entry points without a handle.
 tp_status ops_fail(tp_status s, const char* fmt, ...);

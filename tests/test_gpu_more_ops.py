@@ -72,7 +72,8 @@ EMBED = [(1, 1, 1), (1, 1000, 64), (7, 3, 5), (13, 1000, 8), (32, 2, 33), (100, 
          (5000, 300, 33), (3000, 20011, 64), (9000, 1025, 40), (20011, 100003, 8), (50000, 5, 12), (70000, 2, 64),
          (40000, 1, 1), (777, 50, 1024), (300, 17, 1000), (65, 9, 4099), (16384, 1 << 20, 4),
          (1024, 1, 8), (1025, 1 << 21, 2), (16385, 700, 40), (32769, 1023, 16), (65536, 1024, 8), (65537, 40000, 8),
-         (65000, 3, 264), (150000, 2047, 33)]
+         (65000, 3, 264), (150000, 2047, 33), (256, 2000, 3), (257, 9, 7), (1000, 3000, 194), (2048, 5, 1),
+         (20000, 49, 1), (13, 70001, 21), (200000, 6, 2), (5, 1000, 1021)]
 
 
 def _ids(g, n, vocab, dtype, missing=0.1):
