@@ -229,6 +229,7 @@ __global__ void __launch_bounds__(256) k_lookup_flat(const LookArgs<T, O> g) {
 // Radix sort, stable, by digits of at most kMaxBits bits.  A block ranks the
 // tokens of a tile by its warps' counts of each digit.
 constexpr int kMaxBits = 10;   // the warps' counts of a digit's values fit in shared memory beside a tile
+constexpr int kFewBits = 8;    // of the sorts in one launch, whose passes clear and add up the counts of fewer tokens
 
 struct SortArgs {
   Ids ids;                      // the first pass's keys; their places are its values
@@ -237,7 +238,7 @@ struct SortArgs {
   uint32_t *count, *total;      // [bins][blocks]; [bins]
   uint8_t* seen;                // a byte per row of the table: whether it has a token
   int64_t n;
-  int32_t first, shift, bits, bits_all, blocks;
+  int32_t first, shift, bits_all, blocks;
 };
 constexpr uint32_t kLast = 0xffffffffu;   // the key of a place past the last token: behind all others in every pass
 __device__ __forceinline__ uint32_t key_at(const SortArgs& g, int64_t i) { return g.first ? g.ids.at(i) : g.key[i]; }
@@ -291,14 +292,13 @@ __device__ __forceinline__ void block_scan(uint32_t* v, int bins, uint32_t* warp
 // Each token's number among those of its digit in its warp (in order), and in
 // wh the warps' counts; afterwards wh holds, per warp and digit, the tokens of
 // the warps before it, and sum (if wanted) the block's counts.  The lanes of one
-// digit find each other by a ballot per bit: 170 issue slots a warp and round, the
-// most of a pass's work (masks or-ed in shared memory, or match.any: as much
-// for spread digits, more for frequent ones).
-template <int kThreads, int kR>
-__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, int bits, uint16_t* wh, uint32_t* sum,
+// digit find each other by a ballot per bit, the most of a pass's work (masks or-ed
+// in shared memory, or match.any: as much for spread digits, more for frequent ones).
+template <int kThreads, int kBits, int kR>
+__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, uint16_t* wh, uint32_t* sum,
                                           uint32_t (&rank)[kR]) {
-  constexpr int kWarps = kThreads / 32;
-  const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kWarps = kThreads / 32, bins = 1 << kBits;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < bins * kWarps / 2; i += kThreads) ((uint32_t*)wh)[i] = 0;
   __syncthreads();
   uint16_t* mine = wh + warp * bins;
@@ -307,10 +307,9 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, 
     const uint32_t digit = key[r] >> shift & (bins - 1);
     uint32_t same = 0xffffffffu;
 #pragma unroll
-    for (int b = 0; b < kMaxBits; ++b) {
-      if (b >= bits) break;
+    for (int b = 0; b < kBits; ++b) {
       const uint32_t set = __ballot_sync(0xffffffffu, digit >> b & 1);
-      same &= digit >> b & 1 ? set : ~set;
+      same &= ~(set ^ (uint32_t)((int32_t)(digit << (31 - b)) >> 31));   // the lanes whose bit is this one's
     }
     const uint32_t before = mine[digit], lower = same & ((1u << lane) - 1);
     rank[r] = before + __popc(lower);
@@ -340,12 +339,12 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, 
 // Many tokens: three launches a pass, a tile of kRounds tokens a thread a block.
 constexpr int kSortThreads = 512;
 
-template <int kRounds>
+template <int kRounds, int kBits>
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(const SortArgs g) {
-  __shared__ uint32_t h[1 << kMaxBits];
+  __shared__ uint32_t h[1 << kBits];
   pdl_trigger();
   pdl_wait();
-  const int bins = 1 << g.bits;
+  constexpr int bins = 1 << kBits;
   for (int i = threadIdx.x; i < bins; i += kSortThreads) h[i] = 0;
   uint32_t key[kRounds];
 #pragma unroll
@@ -395,12 +394,13 @@ __global__ void __launch_bounds__(256) k_sort_scan(uint32_t* count, uint32_t* to
   if (lane == 0) total[bin] = before;
 }
 
-template <int kRounds>
+template <int kRounds, int kBits>
 __global__ void __launch_bounds__(kSortThreads, kRounds <= 4 ? 3 : 2) k_sort_scatter(const SortArgs g) {
   extern __shared__ uint32_t sm[];
+  constexpr int bins = 1 << kBits;
   uint32_t* base = sm;
-  uint16_t* wh = (uint16_t*)(sm + (1 << g.bits) + 32);
-  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint16_t* wh = (uint16_t*)(sm + bins + 32);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   pdl_wait();
   const int64_t i0 = (int64_t)blockIdx.x * (kSortThreads * kRounds) + warp * (32 * kRounds) + lane;
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(kSortThreads, kRounds <= 4 ? 3 : 2) k_sort_sca
   __syncthreads();
   block_scan<kSortThreads>(base, bins, sm + bins);
   for (int i = threadIdx.x; i < bins; i += kSortThreads) base[i] += g.count[(int64_t)i * g.blocks + blockIdx.x];
-  rank_tile<kSortThreads>(key, g.shift, g.bits, wh, nullptr, rank);
+  rank_tile<kSortThreads, kBits>(key, g.shift, wh, nullptr, rank);
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     if (i0 + 32 * r >= g.n) continue;
@@ -441,14 +441,16 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 template <int kR>
-constexpr int cluster_smem(int bits) {   // tokens sent and received; counts, three bases and the scan's; the warps' counts
-  return 2 * kR * kClusterThreads * 8 + (4 * (1 << bits) + 32) * 4 + (1 << bits) * (kClusterThreads / 32) * 2;
+constexpr int cluster_smem() {   // tokens sent and received; counts, three bases and the scan's; the warps' counts
+  return 2 * kR * kClusterThreads * 8 + (4 * (1 << kFewBits) + 32) * 4 +
+         (1 << kFewBits) * (kClusterThreads / 32) * 2;
 }
 template <int kR>
 __global__ void __launch_bounds__(kClusterThreads, 1) k_sort_cluster(const SortArgs g) {
   constexpr int kPer = kR * kClusterThreads;   // tokens a block
   extern __shared__ __align__(16) uint32_t sm[];
-  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int bins = 1 << kFewBits;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint2 *sent = (uint2*)sm, *got = sent + kPer;
   uint32_t *cnt = (uint32_t*)(got + kPer), *local = cnt + bins, *below = local + bins, *base = below + bins;
   uint16_t* wh = (uint16_t*)(base + bins + 32);
@@ -463,8 +465,8 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_sort_cluster(const SortA
     key[r] = (int64_t)val[r] < g.n ? g.ids.at(val[r]) : kLast;
   }
   clear_seen(g, rank_of * kClusterThreads + threadIdx.x, kCluster * kClusterThreads);
-  for (int shift = 0; shift < g.bits_all; shift += g.bits) {
-    rank_tile<kClusterThreads>(key, shift, g.bits, wh, cnt, rank);
+  for (int shift = 0; shift < g.bits_all; shift += kFewBits) {
+    rank_tile<kClusterThreads, kFewBits>(key, shift, wh, cnt, rank);
     cluster_barrier();   // all counts are there, and all tokens of the pass before have been read
     // what the blocks have of a digit: four lanes a digit look at four blocks each
     for (int i = threadIdx.x; i < 4 * bins; i += kClusterThreads) {
@@ -537,17 +539,17 @@ __global__ void __launch_bounds__(kFew) k_sort_few(const SortArgs g) {
   if (i < g.n) g.key_out[to] = key, g.val_out[to] = i;
 }
 
-// Up to 4096 tokens: every pass in one block, digits of at most kTileBits bits (the
-// counts are cleared and added up in every pass).
-constexpr int kTileThreads = 1024, kTileBits = 7;
+// Up to 4096 tokens: every pass in one block.
+constexpr int kTileThreads = 1024;
 template <int kR>
-constexpr int tile_smem(int bits) {
-  return kR * kTileThreads * 8 + (2 * (1 << bits) + 32) * 4 + (1 << bits) * (kTileThreads / 32) * 2;
+constexpr int tile_smem() {
+  return kR * kTileThreads * 8 + ((1 << kFewBits) + 32) * 4 + (1 << kFewBits) * (kTileThreads / 32) * 2;
 }
 template <int kR>
 __global__ void __launch_bounds__(kTileThreads, 1) k_sort_tile(const SortArgs g) {
   extern __shared__ __align__(16) uint32_t sm[];
-  const int bins = 1 << g.bits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int bins = 1 << kFewBits;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint2* sorted = (uint2*)sm;
   uint32_t *base = (uint32_t*)(sorted + kR * kTileThreads);
   uint16_t* wh = (uint16_t*)(base + bins + 32);
@@ -561,8 +563,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_sort_tile(const SortArgs g)
     val[r] = at0 + 32 * r;
     key[r] = (int)val[r] < g.n ? g.ids.at(val[r]) : kLast;
   }
-  for (int shift = 0; shift < g.bits_all; shift += g.bits) {
-    rank_tile<kTileThreads>(key, shift, g.bits, wh, base, rank);
+  for (int shift = 0; shift < g.bits_all; shift += kFewBits) {
+    rank_tile<kTileThreads, kFewBits>(key, shift, wh, base, rank);
     block_scan<kTileThreads>(base, bins, base + bins);
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
@@ -820,8 +822,8 @@ struct Plan {
     split = split_cols(n, d, e);
     bits_all = 0;
     while (bits_all < 31 && (uint32_t)vocab >> bits_all) ++bits_all;
-    passes = (int32_t)ceil_div(bits_all, n <= 4 * kTileThreads ? kTileBits : kMaxBits);
-    bits = std::max<int32_t>(3, (int32_t)ceil_div(bits_all, passes));   // (whole warps of four lanes a digit)
+    passes = (int32_t)ceil_div(bits_all, kMaxBits);   // of the sort in many launches
+    bits = std::max<int32_t>(8, (int32_t)ceil_div(bits_all, passes));
     rounds = n <= 2 * kSortThreads * 2 * kSms ? 2 : n <= 4 * kSortThreads * 4 * kSms ? 4 : 8;   // a wave or two of blocks
     blocks = ceil_div(n, kSortThreads * rounds);
     Carver c(nullptr);
@@ -877,20 +879,21 @@ cudaError_t run_level(RunArgs<T, O> a, const Split& s, int threads, int64_t zero
   return e;
 }
 
+template <int kRounds, int kBits>
+void sort_pass(const SortArgs& s, cudaStream_t st) {
+  constexpr int bins = 1 << kBits;
+  const dim3 grid((unsigned)s.blocks), block(kSortThreads);
+  launch_pdl(k_sort_count<kRounds, kBits>, grid, block, 0, st, s);
+  launch_pdl(k_sort_scan, dim3((unsigned)ceil_div(bins, 8)), dim3(256), 0, st, s.count, s.total, (int)s.blocks, bins);
+  launch_pdl(k_sort_scatter<kRounds, kBits>, grid, block, (bins + 32) * 4 + bins * (kSortThreads / 32) * 2, st, s);
+}
+
 template <int kR>
 cudaError_t sort_cluster(const SortArgs& s, cudaStream_t st) {
-  const int smem = cluster_smem<kR>(s.bits);
-  static OncePerDevice once;
-  const cudaError_t e = once([] {
-    const cudaError_t a = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               cluster_smem<kR>(kMaxBits));
-    return a == cudaSuccess ? cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : a;
-  });
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kCluster);
   cfg.blockDim = dim3(kClusterThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = cluster_smem<kR>();
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -900,7 +903,15 @@ cudaError_t sort_cluster(const SortArgs& s, cudaStream_t st) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_sort_cluster<kR>, s);
+  static OncePerDevice once;
+  const cudaError_t e = once([&] {
+    cudaError_t a = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, cluster_smem<kR>());
+    if (a == cudaSuccess) a = cudaFuncSetAttribute(k_sort_cluster<kR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    int fit = 0;
+    if (a == cudaSuccess) a = cudaOccupancyMaxActiveClusters(&fit, k_sort_cluster<kR>, &cfg);
+    return a == cudaSuccess && fit < 1 ? cudaErrorNotSupported : a;
+  });
+  return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_sort_cluster<kR>, s) : e;
 }
 
 template <typename T, typename O>
@@ -910,7 +921,7 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
   while (most > 1 && !(fits(dy, lddy, d, sizeof(T), most) && fits(out, d, d, sizeof(O), most))) most /= 2;
   const Plan p(n, ids.vocab, d, most);
   SortArgs s{};
-  s.ids = ids, s.n = n, s.bits = p.bits, s.bits_all = p.bits_all, s.blocks = (int32_t)p.blocks;
+  s.ids = ids, s.n = n, s.bits_all = p.bits_all, s.blocks = (int32_t)p.blocks;
   s.count = (uint32_t*)(ws + p.count), s.total = (uint32_t*)(ws + p.total), s.seen = (uint8_t*)(ws + p.seen);
   uint32_t* key[2] = {(uint32_t*)(ws + p.key[0]), (uint32_t*)(ws + p.key[1])};
   uint32_t* val[2] = {(uint32_t*)(ws + p.val[0]), (uint32_t*)(ws + p.val[1])};
@@ -921,35 +932,42 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
   if (n <= kFew) {
     launch_pdl(k_sort_few, one, dim3(one.x > 1 ? kFew : (unsigned)round_up(n, 32)), 0, st, s);
   } else if (n <= kTileThreads) {
-    launch_pdl(k_sort_tile<1>, one, dim3(kTileThreads), tile_smem<1>(p.bits), st, s);
+    launch_pdl(k_sort_tile<1>, one, dim3(kTileThreads), tile_smem<1>(), st, s);
   } else if (n <= 4 * kTileThreads) {
-    static_assert(tile_smem<4>(kTileBits) <= 48 * 1024, "a block's shared memory");
-    launch_pdl(k_sort_tile<4>, one, dim3(kTileThreads), tile_smem<4>(p.bits), st, s);
-  } else if (n <= 2 * kCluster * kClusterThreads) {
-    e = sort_cluster<2>(s, st);
-  } else if (n <= 4 * kCluster * kClusterThreads) {
-    e = sort_cluster<4>(s, st);
-  } else if (n <= 8 * kCluster * kClusterThreads) {
-    e = sort_cluster<8>(s, st);
+    static_assert(tile_smem<4>() <= 64 * 1024, "a block's shared memory");
+    static OncePerDevice once;
+    e = once([] { return cudaFuncSetAttribute(k_sort_tile<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024); });
+    if (e != cudaSuccess) return e;
+    launch_pdl(k_sort_tile<4>, one, dim3(kTileThreads), tile_smem<4>(), st, s);
   } else {
-    const int bins = 1 << p.bits;
-    const size_t sm = (size_t)(bins + 32) * 4 + (size_t)bins * (kSortThreads / 32) * 2;
+    e = n <= 2 * kCluster * kClusterThreads   ? sort_cluster<2>(s, st)
+        : n <= 4 * kCluster * kClusterThreads ? sort_cluster<4>(s, st)
+        : n <= 8 * kCluster * kClusterThreads ? sort_cluster<8>(s, st)
+                                              : cudaErrorNotSupported;
+    if (e == cudaErrorNotSupported) {   // too many, or a part of a GPU that no such cluster fits on
+      cudaGetLastError();
+      e = cudaSuccess;
+      at = -1;
+    }
+  }
+  if (e != cudaSuccess) return e;
+  if (at < 0) {
+    at = 0;
     for (int i = 0; i < p.passes; ++i) {
       s.first = i == 0, s.shift = i * p.bits;
       s.key = key[at ^ 1], s.val = val[at ^ 1], s.key_out = key[at], s.val_out = val[at];
-      const dim3 grid((unsigned)p.blocks), block(kSortThreads);
-      if (p.rounds == 2) launch_pdl(k_sort_count<2>, grid, block, 0, st, s);
-      else if (p.rounds == 4) launch_pdl(k_sort_count<4>, grid, block, 0, st, s);
-      else launch_pdl(k_sort_count<8>, grid, block, 0, st, s);
-      launch_pdl(k_sort_scan, dim3((unsigned)ceil_div(bins, 8)), dim3(256), 0, st, s.count, s.total, (int)p.blocks, bins);
-      if (p.rounds == 2) launch_pdl(k_sort_scatter<2>, grid, block, sm, st, s);
-      else if (p.rounds == 4) launch_pdl(k_sort_scatter<4>, grid, block, sm, st, s);
-      else launch_pdl(k_sort_scatter<8>, grid, block, sm, st, s);
+      auto of_bits = [&](auto r) {
+        if (p.bits == 8) sort_pass<r.value, 8>(s, st);
+        else if (p.bits == 9) sort_pass<r.value, 9>(s, st);
+        else sort_pass<r.value, kMaxBits>(s, st);
+      };
+      if (p.rounds == 2) of_bits(std::integral_constant<int, 2>());
+      else if (p.rounds == 4) of_bits(std::integral_constant<int, 4>());
+      else of_bits(std::integral_constant<int, 8>());
       at ^= 1;
     }
     at ^= 1;
   }
-  if (e != cudaSuccess) return e;
   const uint32_t *k = key[at], *v = val[at];
   for (int l = 0; l < p.levels; ++l) {
     const bool last = l + 1 == p.levels;
