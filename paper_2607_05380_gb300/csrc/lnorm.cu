@@ -42,7 +42,7 @@ void by_row(int d, bool vec, F f) {
   else if (d <= 512) f(Width<2, 1>(), One());
   else if (d <= 1024) f(Width<4, 1>(), One());
   else if (d <= 2048) f(Width<8, 1>(), One());
-  else if (d <= 12 * 256) f(Width<12, 1>(), One());
+  else if (d <= 3584) f(Width<14, 1>(), One());
   else if (d <= 4096) f(Width<16, 1>(), One());
   else if (d <= 5120) f(Width<20, 1>(), One());
   else if (d <= 6144) f(Width<24, 1>(), One());
@@ -225,7 +225,7 @@ struct BwdArgs {
 };
 
 template <typename T, int kW, int kV, int kE>
-__global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 12 && kE == 1) ? 1 : 2) k_ln_bwd(const BwdArgs<T> g) {
+__global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 14 && kE == 1) ? 1 : 2) k_ln_bwd(const BwdArgs<T> g) {
   using L = Lane<T, kW, kV, kE>;
   constexpr int kRows = threads(kW) / 32 / kW;   // rows at a time
   constexpr int kCols = 32 * kW * kV * 8;
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 12 && kE == 1) 
 #pragma unroll
     for (int e = 0; e < kE; ++e) dw[i][e] = db[i][e] = 0.f;
   // the next rows are asked for before these are worked on, where there are registers for them
-  constexpr bool kAhead = kE == 8 ? kV <= 2 && sizeof(T) == 2 : kV == 1 && kW < 32;
+  constexpr bool kAhead = kE == 8 ? kV <= 2 && sizeof(T) == 2 : kV == 1 && kW < 32 && kW != 14;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + grp;
   L s, t, o;
