@@ -27,6 +27,7 @@ namespace {
 constexpr int32_t kMaxD = 1 << 17;
 constexpr int64_t kMaxN = (int64_t(1) << 31) - 4096, kMaxElems = int64_t(1) << 40;
 constexpr uint32_t kSkip = 0x80000000u;   // an entry of the partial rows that holds nothing
+constexpr uint32_t kEnds = 0x80000000u;   // beside a row's number: the last entry of its run
 
 struct Ids {
   const void* p;
@@ -668,8 +669,7 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
   }
   const int lanes = 1 << g.shift, groups = (int)blockDim.x >> g.shift, at = threadIdx.x & (lanes - 1);
   const int grp = threadIdx.x >> g.shift, per_block = groups * g.chunk;
-  uint32_t* key_at = (uint32_t*)(rows + 2 * blockDim.x * (kI * kE));
-  uint32_t* val_at = key_at + per_block;
+  uint2* entry = (uint2*)(rows + 2 * blockDim.x * (kI * kE));   // a row of src, kEnds on the last one of a run; the key
   const int64_t b0 = (int64_t)blockIdx.x * per_block, c0 = ((int64_t)blockIdx.y * kI * lanes + at) * kE;
   const int n_here = (int)min((int64_t)per_block, g.m - b0);
   const int i_first = min(grp * g.chunk, n_here), count = min(g.chunk, n_here - i_first);
@@ -695,66 +695,61 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
   // an entry's row, the lanes' columns side by side
   auto slot = [&](int entry, int i) { return rows + (entry * kI + i) * (lanes * kE) + at * kE; };
   for (int i = threadIdx.x; i < n_here; i += blockDim.x) {
-    const uint32_t key = g.key[b0 + i];
-    key_at[i] = key;
-    val_at[i] = g.val ? g.val[b0 + i] : (uint32_t)(b0 + i);
+    const uint32_t key = g.key[b0 + i], next = b0 + i + 1 < g.m ? g.key[b0 + i + 1] & ~kSkip : kLast;
+    entry[i] = make_uint2((g.val ? g.val[b0 + i] : (uint32_t)(b0 + i)) | ((key & ~kSkip) != next ? kEnds : 0u), key);
     // the first token of a row says that the row has one
     if (g.first && blockIdx.y == 0 && key < (uint32_t)g.vocab && (b0 + i == 0 || g.key[b0 + i - 1] != key)) g.seen[key] = 1;
   }
   const uint32_t block_before = b0 ? g.key[b0 - 1] & ~kSkip : kLast;
   const uint32_t block_after = b0 + n_here < g.m ? g.key[b0 + n_here] & ~kSkip : kLast;
   __syncthreads();
-  const uint32_t before = i_first ? key_at[i_first - 1] & ~kSkip : block_before;
-  const uint32_t after = i_first + count < n_here ? key_at[i_first + count] & ~kSkip : block_after;
-  uint32_t cur = count ? key_at[i_first] & ~kSkip : kLast;
-  uint32_t left0 = cur | kSkip, left1 = kLast;   // what the group leaves: nothing yet
-  bool open = before == cur;                     // the run began before the group
-  auto leave = [&](int entry) {
+  const uint32_t before = i_first ? entry[i_first - 1].y & ~kSkip : block_before;
+  const uint32_t key0 = count ? entry[i_first].y & ~kSkip : kLast, key1 = count ? entry[i_first + count - 1].y & ~kSkip : kLast;
+  uint32_t left0 = key0 | kSkip, left1 = key1 | kSkip;   // what the group leaves: nothing yet
+  bool open = before == key0;                            // the run began before the group
+  auto leave = [&](int which, uint32_t key) {
 #pragma unroll
-    for (int i = 0; i < kI; ++i) Cols<float, kE>::put(slot(2 * grp + entry, i), acc[i]);
-    if (entry) left1 = cur;
-    else left0 = cur;
+    for (int i = 0; i < kI; ++i) Cols<float, kE>::put(slot(2 * grp + which, i), acc[i]);
+    if (which) left1 = key;
+    else left0 = key;
   };
   clear();
   // all groups of a warp take the same number of steps, so that they meet again after each
 #pragma unroll 1
   for (int i0 = 0; i0 < g.chunk; i0 += kU) {
     Cols<T, kE> v[kU][kI];
-    uint32_t key[kU];
+    uint2 in[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      key[u] = i0 + u < count ? key_at[i_first + i0 + u] : kLast;
-      const bool there = key[u] < (uint32_t)g.vocab;   // (neither skipped nor outside the table)
-      const T* row = g.src + (there ? (int64_t)val_at[i_first + i0 + u] * g.ld : 0) + c0;
+      in[u] = i0 + u < count ? entry[i_first + i0 + u] : make_uint2(0u, kLast);
+      const bool there = in[u].y < (uint32_t)g.vocab;   // (neither skipped nor outside the table)
+      const T* row = g.src + (there ? (int64_t)(in[u].x & ~kEnds) * g.ld : 0) + c0;
 #pragma unroll
       for (int i = 0; i < kI; ++i) v[u][i].load(row + i * lanes * kE, there && c0 + i * lanes * kE < g.d);
     }
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      if (key[u] != kLast && (key[u] & ~kSkip) != cur) {
-        if (any) {
-          if (open) leave(0);
-          else write(cur);
-        }
-        clear();
-        cur = key[u] & ~kSkip, open = false;
-      }
-      __syncwarp();
-      any = any || key[u] < (uint32_t)g.vocab;
+      any = any || in[u].y < (uint32_t)g.vocab;
 #pragma unroll
       for (int i = 0; i < kI; ++i)
 #pragma unroll
         for (int e = 0; e < kE; ++e) acc[i][e] += v[u][i].get(e);   // (zeros where there is none)
+      if (in[u].x & kEnds) {
+        const uint32_t key = in[u].y & ~kSkip;
+        if (any) {
+          if (open) leave(0, key);
+          else write(key);
+        }
+        clear();
+        open = false;
+      }
+      __syncwarp();
     }
   }
-  if (any) {
-    if (open) leave(0);
-    else if (after == cur) leave(1);
-    else write(cur);
-  }
+  if (any) leave(open ? 0 : 1, key1);   // a run that goes on
   if (at == 0) {   // (a group without entries: kLast)
     keys[2 * grp] = left0;
-    keys[2 * grp + 1] = left1 == kLast ? cur | kSkip : left1;
+    keys[2 * grp + 1] = left1;
   }
   __syncthreads();
   const int n = 2 * ((n_here + g.chunk - 1) / g.chunk);   // entries that the block's groups have left
