@@ -5,7 +5,7 @@
 //
 // Lookup: a gather, bound by HBM; a few lanes a token, several tokens in flight.
 //
-// Gradient: the tokens are sorted by id (radix sort, stable), so that each row of
+// Gradient of more than a few tokens: they are sorted by id (radix sort, stable), so that each row of
 // the gradient is the sum of a run of tokens and is written once, in a fixed
 // order of additions, without atomics on values.  A group of lanes adds up a
 // chunk of C sorted tokens: runs inside the chunk are finished there; a run
@@ -517,29 +517,6 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_sort_cluster(const SortA
     if (i0 + 32 * r < g.n) g.key_out[i0 + 32 * r] = key[r], g.val_out[i0 + 32 * r] = val[r];
 }
 
-// A few tokens: each one's place is the number of those before it (256 tokens 2 us,
-// but 1000 of them 21).
-constexpr int kFew = 256;
-__global__ void __launch_bounds__(kFew) k_sort_few(const SortArgs g) {
-  __shared__ __align__(16) uint32_t ks[kFew];
-  pdl_trigger();
-  pdl_wait();
-  const int i = threadIdx.x, n4 = ((int)g.n + 3) >> 2;
-  if (clears(g)) return;
-  const uint32_t key = i < g.n ? g.ids.at(i) : kLast;
-  ks[i] = key;
-  __syncthreads();
-  uint32_t to = 0;
-#pragma unroll 4
-  for (int j = 0; j < n4; ++j) {
-    const uint4 k = reinterpret_cast<const uint4*>(ks)[j];
-    to += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
-    to += (k.x == key && 4 * j < i) + (k.y == key && 4 * j + 1 < i) + (k.z == key && 4 * j + 2 < i) +
-          (k.w == key && 4 * j + 3 < i);
-  }
-  if (i < g.n) g.key_out[to] = key, g.val_out[to] = i;
-}
-
 // Up to 4096 tokens: every pass in one block.
 constexpr int kTileThreads = 1024;
 template <int kR>
@@ -803,6 +780,94 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
   }
 }
 
+// --------------------------------------------------------------- few tokens
+// A few tokens: one launch without a sort.  A block zeroes a run of the table's rows,
+// but those that have tokens; it sums those rows that are its number modulo the
+// blocks', for each of which its eight warps look through 32 tokens each, and their
+// sums are joined in order.  (Sorted, and summed and joined in launches of their own: 12 us
+// instead of 5 for 36 tokens.)
+constexpr int kFew = 256;
+template <typename T, typename O>
+struct FewArgs {
+  Ids ids;
+  const T* dy;
+  O* out;
+  int64_t ld;
+  int32_t n, d;
+  float scale;
+};
+template <typename T, typename O, int kE>
+__global__ void __launch_bounds__(kFew) k_grad_few(const FewArgs<T, O> g) {
+  constexpr int kWarps = kFew / 32, kU = 4;   // kU: rows in flight
+  __shared__ uint32_t key[kFew], hit[kFew];
+  __shared__ int n_hit;
+  __shared__ __align__(16) float part[kWarps][32 * kE];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const uint32_t blocks = gridDim.x, vocab = (uint32_t)g.ids.vocab;
+  pdl_trigger();
+  pdl_wait();
+  key[t] = t < g.n ? g.ids.at(t) : kLast;
+  if (t == 0) n_hit = 0;
+  __syncthreads();
+  if (key[t] < vocab && key[t] % blocks == blockIdx.x) {
+    bool first = true;
+    for (int j = 0; j < t; ++j) first = first && key[j] != key[t];
+    if (first) hit[atomicAdd(&n_hit, 1)] = key[t];   // (in any order: it decides on no sum)
+  }
+  // rows to be zeroed: a run of the table's, at once where no token has one of them
+  const int64_t per = ceil_div(vocab, blocks), z0 = min((int64_t)vocab, blockIdx.x * per), z1 = min((int64_t)vocab, z0 + per);
+  const bool near = key[t] >= z0 && key[t] < z1;
+  if (!__syncthreads_or(near)) {
+    constexpr int kWide = 16 / sizeof(O);
+    const int64_t e0 = z0 * g.d, e1 = z1 * g.d;
+    const int64_t v0 = min(e1, e0 + (int64_t)(-(uintptr_t)(g.out + e0) / sizeof(O) % kWide)), v1 = v0 + (e1 - v0) / kWide * kWide;
+    const float wide[kWide] = {};
+    for (int64_t e = v0 + t * kWide; e < v1; e += kFew * kWide) Cols<O, kWide>::put(g.out + e, wide);
+    for (int64_t e = e0 + t; e < v0; e += kFew) g.out[e] = Elem<O>::from_f(0.f);
+    for (int64_t e = v1 + t; e < e1; e += kFew) g.out[e] = Elem<O>::from_f(0.f);
+  } else {
+    const float zero[kE] = {};
+    for (int64_t r = z0 + warp; r < z1; r += kWarps) {
+      bool has = false;
+#pragma unroll
+      for (int i = 0; i < kFew / 32; ++i) has = has || key[32 * i + lane] == (uint32_t)r;
+      if (__any_sync(0xffffffffu, has)) continue;
+      for (int64_t c = lane * kE; c < g.d; c += 32 * kE) Cols<O, kE>::put(g.out + r * g.d + c, zero);
+    }
+  }
+  const int hits = n_hit;
+  for (int h = 0; h < hits; ++h) {
+    const uint32_t row = hit[h];
+    const uint32_t mine = __ballot_sync(0xffffffffu, key[t] == row);
+    for (int64_t c0 = 0; c0 < g.d; c0 += 32 * kE) {
+      const int64_t c = c0 + lane * kE;
+      float acc[kE] = {};
+      for (uint32_t left = mine; left;) {
+        Cols<T, kE> v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int i = 32 * warp + __ffs(left) - 1;
+          v[u].load(g.dy + (left ? (int64_t)i * g.ld : 0) + c, left != 0 && c < g.d);
+          left &= left - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int e = 0; e < kE; ++e) acc[e] += v[u].get(e);   // (zeros where there is none)
+      }
+      Cols<float, kE>::put(&part[warp][lane * kE], acc);
+      __syncthreads();
+      for (int i = t; i < 32 * kE; i += kFew) {
+        float sum = part[0][i];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) sum += part[w][i];
+        if (c0 + i < g.d) g.out[(int64_t)row * g.d + c0 + i] = Elem<O>::from_f(sum * g.scale);
+      }
+      __syncthreads();
+    }
+  }
+}
+
 // --------------------------------------------------------------------- host
 constexpr int kLevels = 16;   // a level has at most a quarter of the entries before
 
@@ -914,6 +979,16 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
                      cudaStream_t st) {
   int most = 8;
   while (most > 1 && !(fits(dy, lddy, d, sizeof(T), most) && fits(out, d, d, sizeof(O), most))) most /= 2;
+  if (n <= kFew) {
+    const FewArgs<T, O> a{ids, dy, out, lddy, (int32_t)n, d, scale};
+    while (most > 1 && 16 * most >= d) most /= 2;   // (no idle lanes)
+    const dim3 grid((unsigned)std::min(ids.vocab, 8 * kSms)), block(kFew);
+    if (most == 8) launch_pdl(k_grad_few<T, O, 8>, grid, block, 0, st, a);
+    else if (most == 4) launch_pdl(k_grad_few<T, O, 4>, grid, block, 0, st, a);
+    else if (most == 2) launch_pdl(k_grad_few<T, O, 2>, grid, block, 0, st, a);
+    else launch_pdl(k_grad_few<T, O, 1>, grid, block, 0, st, a);
+    return cudaGetLastError();
+  }
   const Plan p(n, ids.vocab, d, most);
   SortArgs s{};
   s.ids = ids, s.n = n, s.bits_all = p.bits_all, s.blocks = (int32_t)p.blocks;
@@ -924,9 +999,7 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
   cudaError_t e = cudaSuccess;
   int at = 0;
   const dim3 one(1 + (unsigned)std::min<int64_t>(ids.vocab >> 16, kSms));   // the block that sorts, and 64 KB to clear a block
-  if (n <= kFew) {
-    launch_pdl(k_sort_few, one, dim3(one.x > 1 ? kFew : (unsigned)round_up(n, 32)), 0, st, s);
-  } else if (n <= kTileThreads) {
+  if (n <= kTileThreads) {
     launch_pdl(k_sort_tile<1>, one, dim3(kTileThreads), tile_smem<1>(), st, s);
   } else if (n <= 4 * kTileThreads) {
     static_assert(tile_smem<4>() <= 64 * 1024, "a block's shared memory");
@@ -1053,7 +1126,7 @@ tp_status pack_embed_bytes(int64_t n, int32_t vocab, int32_t d, int64_t* backwar
   const tp_status s = check(n, 4, vocab, d);
   if (s != TP_OK) return s;
   if (!backward_bytes) return ops_fail(TP_EINVAL, "null argument");
-  *backward_bytes = n ? plan_bytes(n, vocab, d) : 0;
+  *backward_bytes = n > kFew ? plan_bytes(n, vocab, d) : 0;
   return TP_OK;
 }
 
@@ -1074,8 +1147,8 @@ tp_status pack_embed_backward(const void* dy, int64_t lddy, const void* ids, int
   }
   if (!dy || !ids) return ops_fail(TP_EINVAL, "null argument");
   if ((uintptr_t)ids & (id_bytes - 1)) return ops_fail(TP_EINVAL, "ids must be aligned to their size");
-  const int64_t need = plan_bytes(n, vocab, d);
-  if (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255))
+  const int64_t need = n > kFew ? plan_bytes(n, vocab, d) : 0;
+  if (need && (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255)))
     return ops_fail(TP_EINVAL, "a workspace of %lld bytes, 256-byte aligned, is needed", (long long)need);
   if ((s = ops_device()) != TP_OK) return s;
   const Ids i{ids, id_bytes == 8, vocab};

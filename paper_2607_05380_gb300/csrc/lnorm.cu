@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
 // worked on.
 constexpr int many_threads(int kW) { return kW == 1 ? 128 : 32 * kW; }
 constexpr int many_blocks(int kW, int kV) {   // an SM: as many threads as leave the registers for a row and the next one
-  const int n = 65536 / 56 / many_threads(kW);
+  const int n = 65536 / 48 / many_threads(kW);
   return n < 1 ? 1 : n < 16 ? n : 16;
 }
 template <typename T, int kW, int kV, int kE>

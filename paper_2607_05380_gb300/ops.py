@@ -446,7 +446,7 @@ def embed_backward(dy, ids, vocab, scale=1.0, dtype=torch.float32, stream=None):
     n_work = _embed_bytes(n, vocab, d)
     st = _stream(on)
     dt = _empty((vocab, d), dtype=dtype, device=dy.device)
-    work, _keep = _work(n_work, st, dy)
+    work, _keep = _work(n_work, st, dy) if n_work else (None, None)
     status = _lib().pack_embed_backward(gp, ldg, ip, size, n, vocab, d, scale, prec, out, dt.data_ptr(), work, n_work, st)
     if status:
         _fail(status)
@@ -566,7 +566,7 @@ def quantise_f8(x, block_rows=1, stream=None):
     status = _lib().pack_quantise_f8(xp, ldx, rows, k, block_rows, prec, q.data_ptr(), ldq, scale.data_ptr(), st)
     if status:
         _fail(status)
-    return q if ldq == k else q[:, :k], scale
+    return q if ldq == k else q.as_strided((rows, k), (ldq, 1)), scale
 
 
 @functools.lru_cache(maxsize=1024)

@@ -27,12 +27,13 @@ def _bytes(fn, *a):
 
 def test_workspace_sizes(tp):
     L = tp.load_library()
-    for n, vocab, d in ((1, 1, 1), (5000, 300, 33), (50000, 1 << 20, 64), (2000000, 7, 128), (1 << 22, 1 << 30, 256)):
+    for n, vocab, d in ((257, 1, 1), (5000, 300, 33), (50000, 1 << 20, 64), (2000000, 7, 128), (1 << 22, 1 << 30, 256)):
         st, b = _bytes(L.pack_embed_bytes, n, vocab, d)
         # two lists of ids and places, a byte per row of the table
         assert st == tp.TP_OK and b >= 16 * n + vocab
         assert b <= 24 * n + vocab + 2 * (n // 64 + 2) * (d * 4 + 4) + 65536
     assert _bytes(L.pack_embed_bytes, 0, 10, 10) == (tp.TP_OK, 0)
+    assert _bytes(L.pack_embed_bytes, 256, 10, 10) == (tp.TP_OK, 0)   # a few tokens are not sorted
     assert _bytes(L.pack_layer_norm_bytes, 5, 100) == (tp.TP_OK, 5 * 2 * 100 * 4)
     assert _bytes(L.pack_layer_norm_bytes, 0, 100) == (tp.TP_OK, 0)
     assert _bytes(L.pack_product_f8_bytes, 1000, 100, 300, 1) == (tp.TP_OK, 0)
@@ -57,7 +58,7 @@ def test_embed_refusals(tp, bad):
 @pytest.mark.parametrize("ws,n", [(None, MANY), (ODD, MANY), (SOME, 100)])
 def test_workspaces_refused(tp, ws, n):
     L = tp.load_library()
-    assert L.pack_embed_backward(SOME, 16, SOME, 4, 5, 9, 16, 1.0, 0, 1, SOME, ws, n, None) == tp.TP_EINVAL
+    assert L.pack_embed_backward(SOME, 16, SOME, 4, 500, 9, 16, 1.0, 0, 1, SOME, ws, n, None) == tp.TP_EINVAL
     assert L.pack_layer_norm_backward(SOME, 64, SOME, 64, SOME, SOME, None, 0, 5, 64, 0, SOME, SOME, SOME, ws, n, None) == tp.TP_EINVAL
     assert L.pack_product_f8(SOME, 101, SOME, SOME, 101, SOME, None, 1000, 101, 300, 0, SOME, ws, n, None) == tp.TP_EINVAL
 
