@@ -104,18 +104,22 @@ struct Split {
   int e, shift, items;
   int64_t width() const { return (int64_t)(e * items) << shift; }
 };
-// The sums' split of n tokens: a warp a row where the row is wide enough for it,
-// with as few columns a lane as that takes, because the longest chain of a lane's
-// work is what counts; but of more tokens than that keeps the GPU busy with, more
-// columns a lane, because then the instructions a token are (800 440 tokens of 64
+// The sums' split of n tokens: a warp a row where the row is wide enough for it, in
+// as few columns a lane as blocks for the whole GPU allow, because the longest chain
+// of a lane's work is what counts (1000 tokens of 192 columns: eight columns a lane
+// 24 us, one 16); but of more tokens than keep it busy, more columns a lane,
+// because then the instructions a token are (800 440 tokens of 64
 // columns, both passes: two columns a lane 187 us, four 164, eight 179).  e_most:
 // what the addresses allow.
 Split split_cols(int64_t n, int d, int e_most) {
   Split s{1, 5, 1};
-  while (s.e < e_most && s.e * 32 < d) s.e *= 2;
+  while (s.width() < d && ceil_div(n, 256) * ceil_div(d, s.width()) > 2 * kSms)
+    if (s.e < e_most) s.e *= 2;
+    else if (s.e == 1 && s.items < 4) ++s.items;
+    else break;
   while (s.shift > 3 && (s.e << (s.shift - 1)) >= d) --s.shift;   // (lanes idle in rows of less than eight columns: more, shorter lists)
   while (s.e < e_most && s.shift > 3 && (n >> 4) << (s.shift - 1) >= (int64_t)128 * 32 * kSms) s.e *= 2, --s.shift;
-  if (s.e == 1) s.items = (int)std::min<int64_t>(4, ceil_div(d, 32));
+  if (s.e > 1) s.items = 1;
   return s;
 }
 // f(kE, kI) of a split
@@ -572,12 +576,12 @@ struct RunArgs {
   uint8_t* seen;                // the table's rows that have a token: the first level says, beside the second the others
                                 // are zeroed
   int64_t m, ld;
-  int32_t chunk, d, vocab, shift, run_blocks, first, wide;   // wide: out's rows start at multiples of 16 bytes
+  int32_t chunk, d, vocab, shift, run_blocks, first, wide;   // wide: zero_rows by 16 bytes
   float scale;
 };
 
-// Rows without a token become zero.  Where they do not lie on multiples of 16 bytes
-// (but the table does), a thread takes 16 bytes whatever rows they belong to.
+// Rows without a token become zero: a thread takes 16 bytes of the table, whatever
+// rows they belong to.
 template <typename O>
 __device__ __forceinline__ void zero_flat(const uint8_t* seen, O* out, int64_t vocab, int d, int64_t block, int64_t blocks) {
   constexpr int kE = 16 / sizeof(O);
@@ -605,8 +609,10 @@ __device__ __forceinline__ void zero_flat(const uint8_t* seen, O* out, int64_t v
     }
   }
 }
-// A warp takes 32 rows, 2^shift lanes a row, by 16-byte stores where the rows lie on
-// multiples of 16 bytes.
+// The same with fewer instructions where there is a warp's turn for every 32 rows:
+// 2^shift lanes a row, by 16-byte stores where the rows lie on multiples of 16 bytes;
+// and for a table that does not start at one.  (3000 rows of 192, where 94 warps had
+// one: 22 us of a backward pass, 16 the other way.)
 template <typename O, int kE>
 __device__ __forceinline__ void zero_rows(const uint8_t* seen, O* out, int64_t vocab, int d, int64_t block, int64_t blocks) {
   const int lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
@@ -799,15 +805,15 @@ struct FewArgs {
 template <typename T, typename O, int kE>
 __global__ void __launch_bounds__(kFew) k_grad_few(const FewArgs<T, O> g) {
   constexpr int kWarps = kFew / 32, kU = 4;   // kU: rows in flight
-  __shared__ uint32_t key[kFew], hit[kFew];
-  __shared__ int n_hit;
+  __shared__ uint32_t key[kFew], hit[kFew], near[kFew];
+  __shared__ int n_hit, n_near;
   __shared__ __align__(16) float part[kWarps][32 * kE];
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const uint32_t blocks = gridDim.x, vocab = (uint32_t)g.ids.vocab;
   pdl_trigger();
   pdl_wait();
   key[t] = t < g.n ? g.ids.at(t) : kLast;
-  if (t == 0) n_hit = 0;
+  if (t == 0) n_hit = n_near = 0;
   __syncthreads();
   if (key[t] < vocab && key[t] % blocks == blockIdx.x) {
     bool first = true;
@@ -816,26 +822,33 @@ __global__ void __launch_bounds__(kFew) k_grad_few(const FewArgs<T, O> g) {
   }
   // rows to be zeroed: a run of the table's, at once where no token has one of them
   const int64_t per = ceil_div(vocab, blocks), z0 = min((int64_t)vocab, blockIdx.x * per), z1 = min((int64_t)vocab, z0 + per);
-  const bool near = key[t] >= z0 && key[t] < z1;
-  if (!__syncthreads_or(near)) {
-    constexpr int kWide = 16 / sizeof(O);
-    const int64_t e0 = z0 * g.d, e1 = z1 * g.d;
-    const int64_t v0 = min(e1, e0 + (int64_t)(-(uintptr_t)(g.out + e0) / sizeof(O) % kWide)), v1 = v0 + (e1 - v0) / kWide * kWide;
-    const float wide[kWide] = {};
-    for (int64_t e = v0 + t * kWide; e < v1; e += kFew * kWide) Cols<O, kWide>::put(g.out + e, wide);
-    for (int64_t e = e0 + t; e < v0; e += kFew) g.out[e] = Elem<O>::from_f(0.f);
-    for (int64_t e = v1 + t; e < e1; e += kFew) g.out[e] = Elem<O>::from_f(0.f);
-  } else {
-    const float zero[kE] = {};
-    for (int64_t r = z0 + warp; r < z1; r += kWarps) {
-      bool has = false;
-#pragma unroll
-      for (int i = 0; i < kFew / 32; ++i) has = has || key[32 * i + lane] == (uint32_t)r;
-      if (__any_sync(0xffffffffu, has)) continue;
-      for (int64_t c = lane * kE; c < g.d; c += 32 * kE) Cols<O, kE>::put(g.out + r * g.d + c, zero);
+  if (key[t] >= z0 && key[t] < z1) near[atomicAdd(&n_near, 1)] = key[t];
+  __syncthreads();
+  const int hits = n_hit, nears = n_near;
+  constexpr int kWide = 16 / sizeof(O);
+  const int64_t e0 = z0 * g.d, e1 = z1 * g.d;
+  const int64_t v0 = min(e1, e0 + (int64_t)(-(uintptr_t)(g.out + e0) / sizeof(O) % kWide)), v1 = v0 + (e1 - v0) / kWide * kWide;
+  // has one of the rows from a to b a token?
+  auto taken = [&](int64_t a, int64_t b) {
+    bool is = false;
+    for (int i = 0; i < nears; ++i) is = is || (near[i] >= a && near[i] <= b);
+    return is;
+  };
+  auto one = [&](int64_t e) {
+    const int64_t r = nears ? e / g.d : 0;
+    if (!nears || !taken(r, r)) g.out[e] = Elem<O>::from_f(0.f);
+  };
+  const float wide[kWide] = {};
+  for (int64_t e = v0 + t * kWide; e < v1; e += kFew * kWide) {
+    const int64_t r = nears ? e / g.d : 0, last = nears ? (e + kWide - 1) / g.d : 0;
+    if (!nears || !taken(r, last)) {
+      Cols<O, kWide>::put(g.out + e, wide);
+    } else {
+      for (int i = 0; i < kWide; ++i) one(e + i);
     }
   }
-  const int hits = n_hit;
+  for (int64_t e = e0 + t; e < v0; e += kFew) one(e);
+  for (int64_t e = v1 + t; e < e1; e += kFew) one(e);
   for (int h = 0; h < hits; ++h) {
     const uint32_t row = hit[h];
     const uint32_t mine = __ballot_sync(0xffffffffu, key[t] == row);
@@ -1042,7 +1055,7 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
     auto fill = [&](auto& a) {
       a.key = k, a.val = v, a.out = out, a.m = p.m[l], a.chunk = p.chunk[l], a.run_blocks = (int32_t)p.run_blocks[l];
       a.key_out = last ? nullptr : (uint32_t*)(ws + p.part_key[l]), a.part = last ? nullptr : (float*)(ws + p.part[l]);
-      a.d = d, a.vocab = ids.vocab, a.scale = scale, a.seen = s.seen, a.wide = fits(out, d, d, sizeof(O), 16 / sizeof(O));
+      a.d = d, a.vocab = ids.vocab, a.scale = scale, a.seen = s.seen, a.wide = fits(out, d, d, sizeof(O), 16 / sizeof(O)) && ids.vocab >= 32 * 32 * 2 * kSms;
     };
     if (l == 0) {
       RunArgs<T, O> a{};
@@ -1053,7 +1066,7 @@ cudaError_t backward(const T* dy, int64_t lddy, const Ids& ids, int64_t n, int32
       RunArgs<float, O> a{};
       fill(a);
       a.src = (const float*)(ws + p.part[l - 1]), a.ld = d;
-      const int64_t zero_blocks = l > 1 ? 0 : std::min<int64_t>(ceil_div((int64_t)ids.vocab * d, 1024 * 32), 2 * kSms);
+      const int64_t zero_blocks = l > 1 ? 0 : std::min<int64_t>(ceil_div((int64_t)ids.vocab * d, 1024 * 8), 2 * kSms);
       e = run_level(a, p.split, kJoinThreads, zero_blocks, st);
     }
     if (e != cudaSuccess) return e;
