@@ -10,7 +10,10 @@
 // Bound by HBM, and in bf16 nearly as much by the generator: 32 bits an
 // element are 20 multiplier pairs for four of them.  Of those, what depends on
 // the row alone or on the column alone is computed once for the several that a
-// thread takes: the first round and half of the next two.
+// thread takes: the first round and half of the next two.  8192 x 2048, bf16: with
+// a residual 20 us (0.75 of the copy rate), without 17 (0.58); without the
+// generator 33 for both instead of 37.  Products of 64 bits instead of their two
+// halves apart: the same or slower.
 #include <algorithm>
 
 #include "lanes.cuh"

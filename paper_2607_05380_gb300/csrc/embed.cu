@@ -3,17 +3,23 @@
 //
 //   y[i] = scale table[ids[i]],   dtable[v] = scale sum_{i: ids[i] = v} dy[i]
 //
-// Lookup: a gather, bound by HBM; a few lanes a token, several tokens in flight.
+// Lookup: a gather, bound by HBM (800 440 tokens of 64 columns from a table of a
+// million rows, fp32 to bf16: 38 us, 4.8 TB/s of what it has to move); a few lanes
+// a token, ids one turn ahead.
 //
-// Gradient of more than a few tokens: they are sorted by id (radix sort, stable), so that each row of
-// the gradient is the sum of a run of tokens and is written once, in a fixed
-// order of additions, without atomics on values.  A group of lanes adds up a
-// chunk of C sorted tokens: runs inside the chunk are finished there; a run
-// that crosses its ends leaves a 32-bit partial row, at most two a chunk, and
-// these are a sorted list again, which the same kernel takes until one chunk is
-// left.  A value with many thousands of tokens is so spread over the GPU like
-// any others.  Rows without a token are zeroed beside the first level's sums: a
-// bit per row says which they are.
+// Gradient of more than a few tokens: they are sorted by id (radix sort, stable), so
+// that each row of the gradient is the sum of a run of tokens and is written once, in
+// a fixed order of additions, without atomics on values.  A group of lanes adds up a
+// chunk of sorted tokens: runs inside the chunk are finished there; what crosses its
+// ends is joined with the block's other groups' in shared memory, and what crosses
+// the block's ends, at most two 32-bit rows, is a sorted list again, which the same
+// kernel takes until one block is left.  A value with many thousands of tokens is so
+// spread over the GPU like any others.  The first level says, in a byte a row, which
+// rows have tokens; beside the second the others are zeroed.
+//
+// Of few tokens bound by the chain of launches (49 152 of 128 columns, 20 011 rows:
+// sort 18 us, sums 9.5, the join and the zeroes 8.5), of many by the sort's scattered
+// stores and HBM (800 440 of 64 and a million rows: sort 52 us, sums 38, zeroes 28).
 #include <algorithm>
 #include <type_traits>
 
@@ -341,7 +347,9 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kR], int shift, 
   __syncthreads();
 }
 
-// Many tokens: three launches a pass, a tile of kRounds tokens a thread a block.
+// Many tokens: three launches a pass, a tile of kRounds tokens a thread a block (800 440
+// tokens, two passes: counts 12 us, their scans 6, scattered stores 34; a bit per
+// row of the table set by atomics beside them 150 more).
 constexpr int kSortThreads = 512;
 
 template <int kRounds, int kBits>
@@ -434,8 +442,9 @@ __global__ void __launch_bounds__(kSortThreads, kRounds <= 4 ? 3 : 2) k_sort_sca
 // Up to 64 K tokens: every pass in one launch of a cluster of kCluster blocks,
 // which keep the tokens in registers and hand them over through each other's
 // shared memory.  A block sorts its own by the digit first: neighbours then go
-// to neighbouring places (one 4-byte store each to a place of its own: 38 us for
-// 49152 tokens and two passes).
+// to neighbouring places (49 152 tokens, two passes: 18 us; one 4-byte store each to
+// a place of its own 38).  A pass takes 8 us: the ranks 2.8, the blocks' counts and
+// scans 1.5, handing over 1 to 2, two barriers of the cluster 1.5.
 constexpr int kCluster = 16, kClusterThreads = 512;
 __device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t rank) {
   uint32_t a;

@@ -11,6 +11,14 @@
 // two large sums).  The norm is taken of s as it is stored: the statistics
 // that are kept for the backward pass are then exactly those of the s that it
 // reads, and it needs one round of sums per row instead of two.
+//
+// Bound by HBM and by the chain of a row's loads, sums and stores (8192 rows of 2048,
+// bf16: forward with a residual 25 us, 0.80 of the measured copy rate, backward
+// with dsum 26, 0.77, and 4 for the blocks' sums), by single elements more by the
+// latter (2003 rows of 5001, fp32: forward 25 us, 0.48, backward 28, 0.64).  A row's
+// two forward sums by one barrier, from the warps' means and centred squares: slower
+// by its divisions (28 us); resident blocks with the next row ahead, where rows come
+// by 16 bytes: 29.
 #include <algorithm>
 #include <type_traits>
 
