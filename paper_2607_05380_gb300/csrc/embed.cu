@@ -197,41 +197,39 @@ __global__ void __launch_bounds__(256) k_lookup(const LookArgs<T, O> g) {
   }
 }
 
-// Rows of an odd number of columns: four neighbouring elements of y a thread,
-// whatever rows they belong to, by one store.  (140077 tokens of 33 columns, fp32:
-// a warp a row 13 us.)
+// Rows of an odd number of columns: 16 bytes of y a thread, whatever rows they belong
+// to.  A block's tokens are a multiple of eight, so that it starts at a multiple of
+// 16 bytes.  (140 077 tokens of 33 columns, fp32: a warp a row 13 us.)
+constexpr int kFlatTokens = 2048;   // of a block, at most
 template <typename T, typename O>
-__global__ void __launch_bounds__(256) k_lookup_flat(const LookArgs<T, O> g) {
-  constexpr int kU = 2;   // times 256 groups of four a block
+__global__ void __launch_bounds__(256) k_lookup_flat(const LookArgs<T, O> g, int tokens) {
+  constexpr int kE = 16 / sizeof(O);
+  __shared__ uint32_t id[kFlatTokens + 1];
   pdl_trigger();
   pdl_wait();
-  const int64_t total = g.n * g.d, e0 = (int64_t)blockIdx.x * (1024 * kU), t0 = e0 / g.d;
-  const uint32_t off = (uint32_t)(e0 - t0 * g.d);
-  float v[kU][4];
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t e = off + 4 * (threadIdx.x + 256 * u);
+  const int64_t t0 = (int64_t)blockIdx.x * tokens;
+  const int here = (int)min((int64_t)tokens, g.n - t0);
+  for (int i = threadIdx.x; i <= here; i += 256) id[i] = i < here ? g.ids.at(t0 + i) : (uint32_t)g.ids.vocab;
+  __syncthreads();
+  const uint32_t total = (uint32_t)here * (uint32_t)g.d;
+  O* y = g.y + t0 * g.d;
+#pragma unroll 2
+  for (uint32_t e = threadIdx.x * kE; e < total; e += 256 * kE) {
     uint32_t row = e / (uint32_t)g.d, c = e - row * (uint32_t)g.d;
-    uint32_t id = t0 + row < g.n ? g.ids.at(t0 + row) : (uint32_t)g.ids.vocab;
+    float v[kE];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = id < (uint32_t)g.ids.vocab;
-      v[u][i] = there ? Elem<T>::to_f(g.table[(int64_t)id * g.ldt + c]) * g.scale : 0.f;
-      if (++c == (uint32_t)g.d) {
-        c = 0, ++row;
-        id = t0 + row < g.n ? g.ids.at(t0 + row) : (uint32_t)g.ids.vocab;
-      }
+    for (int i = 0; i < kE; ++i) {
+      const uint32_t k = row < (uint32_t)here ? id[row] : (uint32_t)g.ids.vocab;
+      const bool there = k < (uint32_t)g.ids.vocab;
+      v[i] = there ? Elem<T>::to_f(g.table[(int64_t)k * g.ldt + c]) * g.scale : 0.f;
+      if (++c == (uint32_t)g.d) c = 0, ++row;
     }
-  }
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const int64_t at = e0 + 4 * (threadIdx.x + 256 * u);
-    if (at + 4 <= total) {
-      Cols<O, 4>::put(g.y + at, v[u]);
+    if (e + kE <= total) {
+      Cols<O, kE>::put(y + e, v);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (at + i < total) g.y[at + i] = Elem<O>::from_f(v[u][i]);
+      for (int i = 0; i < kE; ++i)
+        if (e + i < total) y[e + i] = Elem<O>::from_f(v[i]);
     }
   }
 }
@@ -1093,10 +1091,13 @@ void lookup(const Ids& ids, int64_t n, const T* table, int64_t ldt, int32_t d, f
   while (s.shift < 5 && (s.e << s.shift) < d) ++s.shift;
   LookArgs<T, O> a{ids, table, y, n, ldt, d, s.shift, scale};
   if (most == 1 && ((uintptr_t)y & 15) == 0) {
-    launch_pdl(k_lookup_flat<T, O>, dim3((unsigned)ceil_div(n * d, 2048)), dim3(256), 0, st, a);
+    const int tokens = std::min(kFlatTokens, std::max(8, 8192 / d / 8 * 8));
+    launch_pdl(k_lookup_flat<T, O>, dim3((unsigned)ceil_div(n, tokens)), dim3(256), 0, st, a, tokens);
     return;
   }
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(256 >> s.shift) * 2), 8 * kSms), (unsigned)ceil_div(d, s.width()));
+  // no more blocks than run at once, which take the same number of turns
+  const int64_t turns = ceil_div(n, (int64_t)(256 >> s.shift) * 2), each = ceil_div(turns, 8 * kSms);
+  const dim3 grid((unsigned)ceil_div(turns, each), (unsigned)ceil_div(d, s.width()));
   with_split(s, [&](auto c, auto i) { launch_pdl(k_lookup<T, O, c.value, i.value>, grid, dim3(256), 0, st, a); });
 }
 
