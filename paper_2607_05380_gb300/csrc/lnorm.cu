@@ -18,7 +18,8 @@
 // latter (2003 rows of 5001, fp32: forward 25 us, 0.48, backward 28, 0.64).  A row's
 // two forward sums by one barrier, from the warps' means and centred squares: slower
 // by its divisions (28 us); resident blocks with the next row ahead, where rows come
-// by 16 bytes: 29.
+// by 16 bytes: 29.  Rows of odd widths by 16-byte groups with single elements at their
+// ends: 32 and 46 (the ends' branches and selections in every row).
 #include <algorithm>
 #include <type_traits>
 

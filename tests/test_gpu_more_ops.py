@@ -303,6 +303,32 @@ def test_layer_norm_strides(tp, dtype, pad, off):
         _within(v, val, tol, name)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,pad,off,dsum_off", [
+    (1025, 0, 0, 0), (2039, 0, 0, 0), (2041, 8, 0, 0), (2500, 16, 0, 0), (4087, 0, 0, 0), (4088, 0, 7, 7), (4089, 8, 0, 0),
+    (5001, 0, 0, 0), (5111, 0, 0, 1), (5113, 24, 0, 0), (6135, 0, 0, 8), (6137, 0, 0, 0), (8183, 0, 0, 0), (8185, 0, 0, 0)])
+@pytest.mark.parametrize("rows", [63, 64, 71, 1301])
+def test_layer_norm_odd_widths(tp, dtype, d, pad, off, dsum_off, rows):
+    """Rows that begin at every place of a 16-byte group: a store that left its row would spoil the next one."""
+    g = _gen(d + rows)
+    x, res, dy = (_rand(g, rows, d, dtype, pad=pad, off=off) for _ in range(3))
+    dsum = _rand(g, rows, d, dtype, pad=pad, off=dsum_off)
+    w, b = 1 + 0.2 * torch.randn(d, generator=g, device="cuda"), torch.randn(d, generator=g, device="cuda")
+    for with_res in (True, False):
+        rr, bb, ds = (res, b, dsum) if with_res else (None, None, None)
+        y, s, stats = tp.layer_norm(x, w, bb, rr, eps=EPS, save=True)
+        ref = _norm64(x, w, bb, rr, dtype)
+        assert torch.equal(s, ref[0])
+        _within(y, ref[6], ref[7], "y")
+        keep = torch.zeros(rows * (d + pad) + 16, dtype=dtype, device="cuda")[off:][:rows * (d + pad)].view(rows, d + pad)[:, :d]
+        keep.copy_(s)
+        got = tp.layer_norm_backward(dy, keep, w, stats, ds)
+        for name, v, (val, tol) in zip(("dx", "dw", "db"), got, _norm_grad64(dy, w, ds, *ref[2:6], dtype)):
+            _within(v, val, tol + 1e-30, name)
+        again = tp.layer_norm_backward(dy, keep, w, stats, ds)
+        assert all(torch.equal(p, q) for p, q in zip(got, again))
+
+
 def test_layer_norm_differences(tp):
     """The gradients against differences of the forward pass (fp32)."""
     g = _gen(2)
