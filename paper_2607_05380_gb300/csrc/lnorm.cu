@@ -392,7 +392,7 @@ void forward(const FwdArgs<T>& a, cudaStream_t st) {
       constexpr int kRows = many_threads(s.w) / 32 / s.w, smem = 2 * 32 * s.w * s.v * 8 * 4;
       const int64_t blocks = ceil_div(a.rows, kRows), most = many_blocks(s.w, s.v) * kSms;
       if (blocks > most && smem <= 64 * 1024) {
-        if (smem > 48 * 1024) {
+        if (smem + sizeof(float[2][2][1][32]) > 48 * 1024) {   // (with the kernel's static ones)
           static OncePerDevice once;
           once([] {
             return cudaFuncSetAttribute(k_ln_fwd_many<T, decltype(s)::w, decltype(s)::v, 1>,
