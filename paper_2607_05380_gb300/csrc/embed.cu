@@ -199,8 +199,12 @@ __global__ void __launch_bounds__(256) k_lookup(const LookArgs<T, O> g) {
 
 // Rows of an odd number of columns: 16 bytes of y a thread, whatever rows they belong
 // to.  A block's tokens are a multiple of eight, so that it starts at a multiple of
-// 16 bytes.  (140 077 tokens of 33 columns, fp32: a warp a row 13 us.)
+// 16 bytes.  (140 077 tokens of 33 columns, fp32: a warp a row 13 us, this 10.)  Of fewer
+// tokens, whose blocks do not fill the GPU, lanes over a row (bf16, us, this and
+// those: 2000 of 129 2.8 and 2.7, of 2047 11.3 and 8.4; 10 000 5.1 and 5.5, 25 and
+// 34; of 33 3.2 and 3.3).
 constexpr int kFlatTokens = 2048;   // of a block, at most
+constexpr int64_t kFlatFrom = 8192;
 template <typename T, typename O>
 __global__ void __launch_bounds__(256) k_lookup_flat(const LookArgs<T, O> g, int tokens) {
   constexpr int kE = 16 / sizeof(O);
@@ -1090,8 +1094,9 @@ void lookup(const Ids& ids, int64_t n, const T* table, int64_t ldt, int32_t d, f
   Split s{most, 0, most == 1 ? (int)std::min<int64_t>(4, ceil_div(d, 32)) : 1};
   while (s.shift < 5 && (s.e << s.shift) < d) ++s.shift;
   LookArgs<T, O> a{ids, table, y, n, ldt, d, s.shift, scale};
-  if (most == 1 && ((uintptr_t)y & 15) == 0) {
-    const int tokens = std::min(kFlatTokens, std::max(8, 8192 / d / 8 * 8));
+  if (most == 1 && n >= kFlatFrom && ((uintptr_t)y & 15) == 0) {
+    const int64_t share = std::max<int64_t>(8, ceil_div(n, 2 * kSms) / 8 * 8);   // no fewer blocks than two an SM
+    const int tokens = (int)std::min<int64_t>(std::min(kFlatTokens, std::max(8, 8192 / d / 8 * 8)), share);
     launch_pdl(k_lookup_flat<T, O>, dim3((unsigned)ceil_div(n, tokens)), dim3(256), 0, st, a, tokens);
     return;
   }

@@ -102,6 +102,18 @@ def test_embed(tp, types, shape):
     assert torch.equal(dt, tp.embed_backward(dy, ids, vocab, scale, dtype=table_t))
 
 
+@pytest.mark.parametrize("types", [(F32, BF), (BF, BF), (F32, F32), (BF, F32)])
+@pytest.mark.parametrize("n,d", [(8191, 33), (8192, 33), (8193, 1), (8200, 1025), (9001, 3), (40001, 129), (70003, 7)])
+def test_embed_odd_widths(tp, types, n, d):
+    """Rows of odd widths, many and not quite as many: a float32 product, rounded to the output's type."""
+    g = _gen(n + d)
+    ids = _ids(g, n, 500, torch.int32)
+    table = _rand(g, 500, d, types[0])
+    ok = (ids >= 0) & (ids < 500)
+    want = torch.where(ok[:, None], table.float()[torch.where(ok, ids, 0).long()] * 0.3, 0.0).to(types[1])
+    assert torch.equal(tp.embed(ids, table, 0.3, dtype=types[1]), want)
+
+
 @pytest.mark.parametrize("pad,off", [(8, 0), (3, 0), (0, 1), (5, 3)])
 def test_embed_strides(tp, pad, off):
     """Spaced rows, odd addresses and ids of more than one dimension give the same values."""
