@@ -653,9 +653,9 @@ __global__ void __launch_bounds__(1024) k_runs(const RunArgs<T, O> g) {
   pdl_trigger();
   pdl_wait();
   if ((int)blockIdx.x >= g.run_blocks) {
-    if (blockIdx.y) return;
     constexpr int kWide = 16 / sizeof(O);
-    const int64_t block = blockIdx.x - g.run_blocks, blocks = gridDim.x - g.run_blocks;
+    const int64_t block = (int64_t)(blockIdx.x - g.run_blocks) * gridDim.y + blockIdx.y;
+    const int64_t blocks = (int64_t)(gridDim.x - g.run_blocks) * gridDim.y;
     if (g.wide) zero_rows<O, kWide>(g.seen, g.out, g.vocab, g.d, block, blocks);
     else if (((uintptr_t)g.out & 15) == 0) zero_flat(g.seen, g.out, g.vocab, g.d, block, blocks);
     else zero_rows<O, 1>(g.seen, g.out, g.vocab, g.d, block, blocks);
@@ -947,7 +947,8 @@ int64_t plan_bytes(int64_t n, int32_t vocab, int32_t d) {
 template <typename T, typename O>
 cudaError_t run_level(RunArgs<T, O> a, const Split& s, int threads, int64_t zero_blocks, cudaStream_t st) {
   a.shift = s.shift;
-  const dim3 grid((unsigned)(a.run_blocks + zero_blocks), (unsigned)ceil_div(a.d, s.width()));
+  const int64_t across = ceil_div(a.d, s.width());
+  const dim3 grid((unsigned)(a.run_blocks + ceil_div(zero_blocks, across)), (unsigned)across);
   const size_t smem = (size_t)2 * threads * s.e * s.items * 4 + (size_t)(threads >> s.shift) * a.chunk * 8;
   cudaError_t e = cudaSuccess;
   with_split(s, [&](auto c, auto i) {
