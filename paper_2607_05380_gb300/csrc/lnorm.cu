@@ -18,8 +18,7 @@
 // latter (2003 rows of 5001, fp32: forward 25 us, 0.48, backward 28, 0.64).  A row's
 // two forward sums by one barrier, from the warps' means and centred squares: slower
 // by its divisions (28 us); resident blocks with the next row ahead, where rows come
-// by 16 bytes: 29.  Rows of odd widths by 16-byte groups with single elements at their
-// ends: 32 and 46 (the ends' branches and selections in every row).
+// by 16 bytes: 29.
 #include <algorithm>
 #include <type_traits>
 
@@ -90,9 +89,12 @@ struct FwdArgs {
   float eps;
 };
 
-// kW warps per row, 8 kV elements per lane.
+// kW warps per row, 8 kV elements per lane.  Rows of sixteen warps ask for the weights late,
+// which leaves the registers for a second block an SM (8192 x 8192: bf16 145 us, so
+// 116; fp32 195, 170).
 template <typename T, int kW, int kV, int kE>
-__global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
+__global__ void __launch_bounds__(threads(kW), kW == 16 && kV == 2 && kE == 8 ? 2 : 0) k_ln_fwd(const FwdArgs<T> g) {
+  constexpr bool kLate = kW == 16 && kE == 8 && (kV == 2 || sizeof(T) == 4);
   using L = Lane<T, kW, kV, kE>;
   __shared__ float red[2][1][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -106,8 +108,10 @@ __global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
   Lane<float, kW, kV, kE> w, b;
   x.load(g.x + row * g.ldx, wl, d);
   if (g.res) res.load(g.res + row * g.ldr, wl, d);
-  w.load(g.w, wl, d);
-  if (g.b) b.load(g.b, wl, d);
+  if (!kLate) {
+    w.load(g.w, wl, d);
+    if (g.b) b.load(g.b, wl, d);
+  }
   float v[L::kGroups][kE], a[1] = {0.f};
 #pragma unroll
   for (int i = 0; i < L::kGroups; ++i) {
@@ -132,6 +136,10 @@ __global__ void __launch_bounds__(threads(kW)) k_ln_fwd(const FwdArgs<T> g) {
       v[i][e] -= mean;
       if (L::col(i, wl) < d) a[0] += v[i][e] * v[i][e];
     }
+  if (kLate) {
+    w.load(g.w, wl, d);
+    if (g.b) b.load(g.b, wl, d);
+  }
   row_sums<kW>(a, red[1], warp, lane, grp);
   const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
   if (live && wl == 0 && g.stats) g.stats[row] = make_float2(mean, r);
@@ -351,6 +359,237 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 14 && kE == 1) 
   }
 }
 
+// ------------------------------------------------ rows of odd widths, packed
+// Rows that start `off` elements past a multiple of 16 bytes, all matrices' alike (as
+// packed rows of an odd width do): a row is taken as one that begins at that multiple.
+// Loads are whole groups of eight; what of a row's first and last one is the rows'
+// beside it is cleared, and the last row's last group, behind which the matrix ends,
+// is read by elements.  A block's rows, a multiple of eight apart, have the same off.
+// bf16 only, and only of many rows: 8192 rows of 4097, us, by single elements and so:
+// forward 102, 62, backward 114, 72; of 7001: 159, 107 and 219, 110; 2000 rows of
+// 4097: 24.6, 18.7 and 27.7, 26.2, of 2003: 11.1, 10.7 and 12.9, 17.3 (fp32, 8192 of 4097:
+// 118, 95 and 94, 105; of 7001: 155, 179 and 229, 193).  Eight columns a lane and twice the
+// warps: forward 86.
+using Half = __nv_bfloat16;
+template <int kW>
+struct OddLane {
+  using L = Lane<Half, kW, 2, 8>;
+  L in;
+  static __device__ __forceinline__ bool full(int i, int wl, int off, int end) {
+    return L::col(i, wl) >= off && L::col(i, wl) + 8 <= end;
+  }
+  // p: the multiple of 16 bytes; end = off + d, or 0 for no row; last: of the matrix
+  __device__ __forceinline__ void load(const Half* p, int wl, int end, bool last) {
+    if (!last) {
+      in.load(p, wl, end);
+      return;
+    }
+    in.load(p, wl, end & ~7);   // (the groups that end inside the row)
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i)
+      if (L::col(i, wl) < end && L::col(i, wl) + 8 > end) {
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (L::col(i, wl) + e < end) w[e >> 1] |= (uint32_t)__bfloat16_as_ushort(p[L::col(i, wl) + e]) << (16 * (e & 1));
+        in.u[i][0] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+  }
+  // nothing of the rows beside it
+  __device__ __forceinline__ void clip(int wl, int off, int end) {
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i)
+      if (!full(i, wl, off, end)) {
+        uint32_t w[4] = {in.u[i][0].x, in.u[i][0].y, in.u[i][0].z, in.u[i][0].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = L::col(i, wl) + 2 * e;
+          w[e] &= (c >= off && c < end ? 0xFFFFu : 0u) | (c + 1 >= off && c + 1 < end ? 0xFFFF0000u : 0u);
+        }
+        in.u[i][0] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+  }
+  static __device__ __forceinline__ void put(Half* p, int i, int wl, int off, int end, const float (&v)[8]) {
+    if (full(i, wl, off, end)) {
+      L::put(p, i, wl, end, v);
+    } else if (L::col(i, wl) < end) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::col(i, wl) + e;
+        if (c >= off && c < end) p[c] = Elem<Half>::from_f(v[e]);
+      }
+    }
+  }
+};
+
+constexpr int odd_blocks(int kW) { return 20 / kW < 1 ? 1 : 20 / kW; }   // an SM
+template <int kW>
+__global__ void __launch_bounds__(32 * kW, odd_blocks(kW)) k_ln_fwd_odd(const FwdArgs<Half> g) {
+  using O = OddLane<kW>;
+  using L = typename O::L;
+  constexpr int kCols = 32 * kW * 16;
+  extern __shared__ __align__(16) float ws[];   // weights, then biases, `off` places on
+  __shared__ float red[2][2][1][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wl = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  int64_t row = blockIdx.x;
+  const int off = (int)(((uintptr_t)(g.x + row * g.ldx) & 15) / sizeof(Half)), end = off + g.d;
+  O x, res;
+  auto ask = [&](int64_t at) {
+    const int till = at < g.rows ? end : 0;
+    x.load(g.x + at * g.ldx - off, wl, till, at == g.rows - 1);
+    if (g.res) res.load(g.res + at * g.ldr - off, wl, till, at == g.rows - 1);
+  };
+  ask(row);
+  for (int c = threadIdx.x; c < kCols; c += 32 * kW) {
+    const bool in = c >= off && c < end;
+    ws[c] = in ? g.w[c - off] : 0.f;
+    ws[kCols + c] = in && g.b ? g.b[c - off] : 0.f;
+  }
+  __syncthreads();
+  int turn = 0;
+  for (; row < g.rows; row += gridDim.x, turn ^= 1) {
+    float v[L::kGroups][8], a[1] = {0.f};
+    x.clip(wl, off, end);
+    if (g.res) res.clip(wl, off, end);
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      x.in.get(i, v[i]);
+      if (g.res) {
+        float r[8];
+        res.in.get(i, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = Elem<Half>::to_f(Elem<Half>::from_f(v[i][e] + r[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[0] += v[i][e];   // (outside the row: zeros)
+    }
+    ask(row + gridDim.x);
+    if (g.sum)
+#pragma unroll
+      for (int i = 0; i < L::kGroups; ++i) O::put(g.sum + row * g.d - off, i, wl, off, end, v[i]);
+    row_sums<kW>(a, red[turn][0], warp, lane, 0);
+    const float mean = a[0] / (float)g.d;
+    a[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      const bool all = O::full(i, wl, off, end);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::col(i, wl) + e;
+        v[i][e] = all || (c >= off && c < end) ? v[i][e] - mean : 0.f;
+        a[0] += v[i][e] * v[i][e];
+      }
+    }
+    row_sums<kW>(a, red[turn][1], warp, lane, 0);
+    const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
+    if (threadIdx.x == 0 && g.stats) g.stats[row] = make_float2(mean, r);
+    if (g.y)
+#pragma unroll
+      for (int i = 0; i < L::kGroups; ++i) {
+        const float* w = ws + L::col(i, wl);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 w4 = reinterpret_cast<const float4*>(w)[h], b4 = reinterpret_cast<const float4*>(w + kCols)[h];
+          v[i][4 * h] = v[i][4 * h] * r * w4.x + b4.x, v[i][4 * h + 1] = v[i][4 * h + 1] * r * w4.y + b4.y;
+          v[i][4 * h + 2] = v[i][4 * h + 2] * r * w4.z + b4.z, v[i][4 * h + 3] = v[i][4 * h + 3] * r * w4.w + b4.w;
+        }
+        O::put(g.y + row * g.d - off, i, wl, off, end, v[i]);
+      }
+  }
+}
+
+template <int kW>
+__global__ void __launch_bounds__(32 * kW, kW > 8 ? 1 : 2) k_ln_bwd_odd(const BwdArgs<Half> g) {
+  using O = OddLane<kW>;
+  using L = typename O::L;
+  constexpr int kCols = 32 * kW * 16;
+  extern __shared__ __align__(16) float ws[];   // weights, `off` places on
+  __shared__ float red[2][2][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wl = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  int64_t row = blockIdx.x;
+  const int off = (int)(((uintptr_t)(g.s + row * g.lds) & 15) / sizeof(Half)), end = off + g.d;
+  O s, t, o;
+  float2 st;
+  auto ask = [&](int64_t at) {
+    const int till = at < g.rows ? end : 0;
+    const bool last = at == g.rows - 1;
+    s.load(g.s + at * g.lds - off, wl, till, last);
+    t.load(g.dy + at * g.lddy - off, wl, till, last);
+    if (g.dsum) o.load(g.dsum + at * g.lddsum - off, wl, till, last);
+    st = till ? g.stats[at] : make_float2(0.f, 0.f);
+  };
+  ask(row);
+  for (int c = threadIdx.x; c < kCols; c += 32 * kW) ws[c] = c >= off && c < end ? g.w[c - off] : 0.f;
+  __syncthreads();
+  auto weights = [&](int i, float (&v)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(ws + L::col(i, wl))[0], b = reinterpret_cast<const float4*>(ws + L::col(i, wl))[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  };
+  float dw[L::kGroups][8], db[L::kGroups][8];
+#pragma unroll
+  for (int i = 0; i < L::kGroups; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
+  int turn = 0;
+  for (; row < g.rows; row += gridDim.x, turn ^= 1) {
+    O sn = s, tn = t;   // this row
+    const O on = o;
+    sn.clip(wl, off, end);
+    tn.clip(wl, off, end);
+    const float mean = st.x, r = st.y;
+    ask(row + gridDim.x);
+    float a[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {   // (outside the row dy and the weights are 0)
+      float sv[8], tv[8], wv[8];
+      sn.in.get(i, sv);
+      tn.in.get(i, tv);
+      weights(i, wv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float q = tv[e] * wv[e];
+        a[0] += q;
+        a[1] += q * ((sv[e] - mean) * r);
+      }
+    }
+    row_sums<kW>(a, red[turn], warp, lane, 0);
+    const float m0 = a[0] / (float)g.d, m1 = a[1] / (float)g.d;
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      float sv[8], tv[8], wv[8];
+      sn.in.get(i, sv);
+      tn.in.get(i, tv);
+      weights(i, wv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float h = (sv[e] - mean) * r;
+        dw[i][e] += tv[e] * h;
+        db[i][e] += tv[e];
+        tv[e] = r * (tv[e] * wv[e] - m0 - h * m1);
+      }
+      if (g.dsum) {
+        on.in.get(i, sv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tv[e] += sv[e];
+      }
+      O::put(g.dx + row * g.d - off, i, wl, off, end, tv);
+    }
+  }
+  if (g.part == nullptr) return;
+  float* part = g.part + (int64_t)blockIdx.x * 2 * g.d - off;
+#pragma unroll
+  for (int i = 0; i < L::kGroups; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = L::col(i, wl) + e;
+      if (c >= off && c < end) part[c] = dw[i][e], part[g.d + c] = db[i][e];
+    }
+}
+
 // dw and db = the blocks' sums: 32 columns a block, a run of blocks for each of
 // its 32 warps, whose loads are all in flight at once.
 __global__ void __launch_bounds__(1024) k_ln_dw(const float* part, int n, int d, float* dw, float* db) {
@@ -383,10 +622,39 @@ __global__ void __launch_bounds__(1024) k_ln_dw(const float* part, int n, int d,
 // take several rows at a time may find none: they leave sums of 0.)
 int bwd_blocks(int64_t rows, int d) { return (int)std::min<int64_t>(rows, d > 4096 ? kSms : kBwdBlocks); }
 
+// Rows of the kernels for packed odd widths: wide ones, and enough of them (measured
+// beside the kernels).
+bool odd_width(int64_t rows, int d, bool back) {
+  return d > 1024 && d <= 8192 - 8 && rows >= (back && d <= 4096 ? 4096 : 1024);
+}
+// Do this matrix's rows lie as those of a packed one do that starts at a multiple of 16 bytes?
+bool odd_like(const void* p, int64_t ld, int64_t d) { return ((uintptr_t)p & 15) == 0 && (!p || (ld - d) % 8 == 0); }
+template <typename F>
+void by_odd(int d, F f) {
+  if (d <= 2048 - 8) f(Width<4, 2>());
+  else if (d <= 4096 - 8) f(Width<8, 2>());
+  else if (d <= 5120 - 8) f(Width<10, 2>());
+  else if (d <= 6144 - 8) f(Width<12, 2>());
+  else f(Width<16, 2>());
+}
+
 template <typename T>
 void forward(const FwdArgs<T>& a, cudaStream_t st) {
   const bool vec = a.d % 8 == 0 && aligned16(a.x, a.ldx, sizeof(T)) && aligned16(a.res, a.ldr, sizeof(T)) &&
                    aligned16(a.w, 0, 4) && aligned16(a.b, 0, 4) && aligned16(a.sum, 0, 4) && aligned16(a.y, 0, 4);
+  if constexpr (sizeof(T) == 2) {
+    if (!vec && odd_width(a.rows, a.d, false) && odd_like(a.x, a.ldx, a.d) && odd_like(a.res, a.ldr, a.d) &&
+        odd_like(a.sum, a.d, a.d) && odd_like(a.y, a.d, a.d)) {
+      by_odd(a.d, [&](auto s) {
+        constexpr int smem = 2 * 32 * s.w * 16 * 4;
+        static OncePerDevice once;
+        once([] { return cudaFuncSetAttribute(k_ln_fwd_odd<decltype(s)::w>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024); });
+        const unsigned blocks = (unsigned)std::min<int64_t>(a.rows, odd_blocks(s.w) * kSms) / 8 * 8;
+        launch_pdl(k_ln_fwd_odd<s.w>, dim3(blocks), dim3(32 * s.w), smem, st, a);
+      });
+      return;
+    }
+  }
   by_row(a.d, vec, [&](auto s, auto e) {
     if constexpr (e.value == 1) {
       constexpr int kRows = many_threads(s.w) / 32 / s.w, smem = 2 * 32 * s.w * s.v * 8 * 4;
@@ -407,13 +675,25 @@ void forward(const FwdArgs<T>& a, cudaStream_t st) {
     launch_pdl(k_ln_fwd<T, s.w, s.v, e.value>, grid, block, 0, st, a);
   });
 }
+// Returns the blocks, of at most `blocks`, that leave sums.
 template <typename T>
-void backward(const BwdArgs<T>& a, int blocks, cudaStream_t st) {
+int backward(const BwdArgs<T>& a, int blocks, cudaStream_t st) {
   const bool vec = a.d % 8 == 0 && aligned16(a.dy, a.lddy, sizeof(T)) && aligned16(a.s, a.lds, sizeof(T)) &&
                    aligned16(a.dsum, a.lddsum, sizeof(T)) && aligned16(a.dx, 0, 4);
+  if constexpr (sizeof(T) == 2) {
+    if (!vec && odd_width(a.rows, a.d, true) && odd_like(a.s, a.lds, a.d) && odd_like(a.dy, a.lddy, a.d) &&
+        odd_like(a.dsum, a.lddsum, a.d) && odd_like(a.dx, a.d, a.d)) {
+      blocks = blocks / 8 * 8;
+      by_odd(a.d, [&](auto s) {
+        launch_pdl(k_ln_bwd_odd<s.w>, dim3((unsigned)blocks), dim3(32 * s.w), 32 * s.w * 16 * 4, st, a);
+      });
+      return blocks;
+    }
+  }
   by_row(a.d, vec, [&](auto s, auto e) {
     launch_pdl(k_ln_bwd<T, s.w, s.v, e.value>, dim3((unsigned)blocks), dim3(threads(s.w)), 0, st, a);
   });
+  return blocks;
 }
 
 tp_status check(int64_t rows, int32_t d, int32_t precision) {
@@ -480,7 +760,7 @@ tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* sum
   }
   if (!dy || !sum || !w || !stats || !dx) return ops_fail(TP_EINVAL, "null argument");
   if ((uintptr_t)stats & 7) return ops_fail(TP_EINVAL, "stats must be 8-byte aligned");
-  const int blocks = bwd_blocks(rows, d);
+  int blocks = bwd_blocks(rows, d);
   const bool sums = dw || db;
   const int64_t need = sums ? (int64_t)blocks * 2 * d * 4 : 0;
   if (need && (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255)))
@@ -488,10 +768,10 @@ tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* sum
   if ((s = ops_device()) != TP_OK) return s;
   float* part = sums ? (float*)workspace : nullptr;
   if (precision == TP_FP32)
-    backward(BwdArgs<float>{(const float*)dy, (const float*)sum, (const float*)dsum, w, (const float2*)stats, (float*)dx,
+    blocks = backward(BwdArgs<float>{(const float*)dy, (const float*)sum, (const float*)dsum, w, (const float2*)stats, (float*)dx,
                             part, lddy, lds, lddsum, rows, d}, blocks, st);
   else
-    backward(BwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)dy, (const __nv_bfloat16*)sum, (const __nv_bfloat16*)dsum, w,
+    blocks = backward(BwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)dy, (const __nv_bfloat16*)sum, (const __nv_bfloat16*)dsum, w,
                                     (const float2*)stats, (__nv_bfloat16*)dx, part, lddy, lds, lddsum, rows, d}, blocks, st);
   if (sums)
     launch_pdl(k_ln_dw, dim3((unsigned)ceil_div(2 * d, 32)), dim3(1024), 0, st, (const float*)part, blocks, d, dw, db);
