@@ -253,6 +253,21 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 14 && kE == 1) 
   const int grp = warp / kW, wl = threadIdx.x - grp * 32 * kW;
   pdl_trigger();
   pdl_wait();
+  // the next rows are asked for before these are worked on, where there are registers for them
+  constexpr bool kAhead = kE == 8 ? kV <= 2 && sizeof(T) == 2 : kV == 1 && kW < 32 && kW != 14;
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + grp;
+  L s, t, o;
+  float2 st;
+  auto ask = [&](int64_t at) {
+    const int d = at < g.rows ? g.d : 0;   // a row past the last one has no elements
+    s.load(g.s + at * g.lds, wl, d);
+    t.load(g.dy + at * g.lddy, wl, d);
+    if (g.dsum) o.load(g.dsum + at * g.lddsum, wl, d);
+    st = d ? g.stats[at] : make_float2(0.f, 0.f);
+  };
+  // (a few loads in flight: 100 rows of 4096, bf16, 9.5 us without, 7.9; all of them, 7.0, cost 8192 rows 61 instead of 50)
+#pragma unroll 4
   for (int c = threadIdx.x; c < kCols; c += threads(kW)) ws[c] = c < g.d ? g.w[c] : 0.f;
   __syncthreads();
   auto weights = [&](int i, float (&v)[kE]) {
@@ -269,19 +284,6 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 14 && kE == 1) 
   for (int i = 0; i < L::kGroups; ++i)
 #pragma unroll
     for (int e = 0; e < kE; ++e) dw[i][e] = db[i][e] = 0.f;
-  // the next rows are asked for before these are worked on, where there are registers for them
-  constexpr bool kAhead = kE == 8 ? kV <= 2 && sizeof(T) == 2 : kV == 1 && kW < 32 && kW != 14;
-  const int64_t stride = (int64_t)gridDim.x * kRows;
-  int64_t row = (int64_t)blockIdx.x * kRows + grp;
-  L s, t, o;
-  float2 st;
-  auto ask = [&](int64_t at) {
-    const int d = at < g.rows ? g.d : 0;   // a row past the last one has no elements
-    s.load(g.s + at * g.lds, wl, d);
-    t.load(g.dy + at * g.lddy, wl, d);
-    if (g.dsum) o.load(g.dsum + at * g.lddsum, wl, d);
-    st = d ? g.stats[at] : make_float2(0.f, 0.f);
-  };
   if (kAhead) ask(row);
   int turn = 0;
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < g.rows; base += stride, row += stride, turn ^= 1) {
@@ -592,6 +594,7 @@ __global__ void __launch_bounds__(32 * kW, kW > 8 ? 1 : 2) k_ln_bwd_odd(const Bw
 
 // dw and db = the blocks' sums: 32 columns a block, a run of blocks for each of
 // its 32 warps, whose loads are all in flight at once.
+// (Of fewer blocks than warps, a warp a block.)
 __global__ void __launch_bounds__(1024) k_ln_dw(const float* part, int n, int d, float* dw, float* db) {
   __shared__ float s[32][33];
   pdl_trigger();
@@ -608,8 +611,8 @@ __global__ void __launch_bounds__(1024) k_ln_dw(const float* part, int n, int d,
   s[k][lane] = a;
   __syncthreads();
   if (k == 0 && c < 2 * d) {
-#pragma unroll
-    for (int q = 1; q < 32; ++q) a += s[q][lane];
+#pragma unroll 31
+    for (int q = 1; q < min(n, 32); ++q) a += s[q][lane];
     if (c >= d) {
       if (db) db[c - d] = a;
     } else if (dw) {
@@ -774,7 +777,7 @@ tp_status pack_layer_norm_backward(const void* dy, int64_t lddy, const void* sum
     blocks = backward(BwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)dy, (const __nv_bfloat16*)sum, (const __nv_bfloat16*)dsum, w,
                                     (const float2*)stats, (__nv_bfloat16*)dx, part, lddy, lds, lddsum, rows, d}, blocks, st);
   if (sums)
-    launch_pdl(k_ln_dw, dim3((unsigned)ceil_div(2 * d, 32)), dim3(1024), 0, st, (const float*)part, blocks, d, dw, db);
+    launch_pdl(k_ln_dw, dim3((unsigned)ceil_div(2 * d, 32)), dim3(32 * std::min(blocks, 32)), 0, st, (const float*)part, blocks, d, dw, db);
   return done(cudaGetLastError(), "pack_layer_norm_backward");
 }
 
