@@ -19,9 +19,9 @@
 // halves of 128 columns with barriers and MMA issuers of their own, sixteen epilogue
 // warps, 16 or 64 columns a load, the next chunk's load before the multiply-adds,
 // CTAs of 128 x 256; scales through shared memory and packed multiply-adds were
-// slower (178 and 162 us in all against 156).
+// slower (178 and 162 us in all against 154).
 //
-// Quantisation: bound by issue slots (8192 x 4096, bf16, scales a row: 28 us, 0.53 of
+// Quantisation: bound by issue slots (8192 x 4096, bf16, scales a row: 26 us, 0.57 of
 // the copy rate), blocks of 128 rows by 16-byte loads.
 //
 // Waits are bounded as in prod.cu, and set the same error word.
@@ -268,7 +268,7 @@ void quantise(const QuantArgs<T>& a, int block_rows, cudaStream_t st) {
     return;
   }
   const int64_t total = a.rows * a.blocks, across = ceil_div(a.blocks, 4);
-  // (8192 x 4096, bf16: blocks for two turns of the GPU 28 us, as many as run at once 32)
+  // (8192 x 4096, bf16: blocks for two turns of the GPU take 0.87 of the time of as many as run at once)
   const dim3 grid((unsigned)across, (unsigned)std::min<int64_t>(ceil_div(a.rows, 8), std::max<int64_t>(1, 12 * kSms / across)));
   if (vec) launch_pdl(k_quant_rows<T>, grid, dim3(256), 0, st, a);
   else launch_pdl(k_quant_rows1<T>, dim3((unsigned)std::min<int64_t>(ceil_div(total, 8), 16 * kSms)), dim3(256), 0, st, a);
@@ -590,7 +590,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
               else mbar_arrive_relaxed(&tl->tempty[buf]);
             }
           }
-          
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[c + e] = fmaf(__uint_as_float(v[e]), f, acc[c + e]);
         }
