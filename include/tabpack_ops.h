@@ -188,9 +188,11 @@ tp_status pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t
  * x, residual: T [rows, d] (residual may be NULL), w, b: float32 [d] (b may
  * be NULL), d in 1..16384, eps >= 0.  Outputs, any of them NULL: sum: T
  * [rows, d], s; y: T [rows, d], rounded once; stats: float32 [rows, 2], 8-byte
- * aligned, m and r of every row.  A row's sum and its sum of squares are fp32
- * values: where the squares overflow r is 0, and where they and eps are 0 it
- * is infinite and y NaN.                                                    */
+ * aligned, m and r of every row.  sum may be x or residual, if rows of it are d
+ * apart.  A row's sums are fp32 values, of the differences from its first
+ * element and of their squares: constant rows give b exactly, others errors of
+ * the size of their spread, whatever their mean; where the squares overflow r is
+ * 0, and where they and eps are 0 it is infinite and y NaN.                 */
 tp_status pack_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* w, const float* b,
                           int64_t rows, int32_t d, float eps, int32_t precision, void* sum, void* y, float* stats,
                           void* cuda_stream);
@@ -198,6 +200,7 @@ tp_status pack_layer_norm(const void* x, int64_t ldx, const void* residual, int6
 /* Its gradients: with h = (s - m) r and t = dy w, dx = r (t - mean(t) - h
  * mean(t h)) + dsum, which is the gradient of x and of residual alike; dw and
  * db = the sums over the rows of dy h and of dy.
+ * m is the mean as it was kept, a float32 value: h is off by up to 2^-24 |m| r.
  *   dy, s: T [rows, d], s as it was stored; stats: of the forward call; dsum:
  *   T [rows, d], the gradient that reaches the stored sum from elsewhere (may
  *   be NULL); dx: T [rows, d]; dw, db: float32 [d] (either may be NULL; with

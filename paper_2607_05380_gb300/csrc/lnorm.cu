@@ -12,6 +12,12 @@
 // that are kept for the backward pass are then exactly those of the s that it
 // reads, and it needs one round of sums per row instead of two.
 //
+// A sum of fp32 values is off by some 2^-24 of their size, which where a row is all but
+// constant is more than its deviation (389 times 12345.6: h was 0.30 and not 0).  So what
+// is summed is the difference from the row's first element q, exact where it is small:
+//   u = s - q,  m = q + mean(u),  s - m = u - mean(u)
+// whose error is of the size of the row's spread, whatever its mean.
+//
 // Bound by HBM and by the chain of a row's loads, sums and stores (8192 rows of 2048,
 // bf16: forward with a residual 25 us, 0.80 of the measured copy rate, backward
 // with dsum 26, 0.77, and 4 for the blocks' sums), by single elements more by the
@@ -78,6 +84,22 @@ __device__ __forceinline__ void row_sums(float (&v)[kN], float (*red)[32], int w
   }
 }
 
+// The element that a row's others are compared with: its first one, or 0 where that is so large that differences could
+// overflow, or no number.
+template <typename T>
+struct Pivot {
+  T x, res;
+  __device__ __forceinline__ void load(const T* px, const T* pres, bool there) {
+    x = there ? *px : Elem<T>::from_f(0.f);
+    if (pres) res = there ? *pres : Elem<T>::from_f(0.f);
+  }
+  __device__ __forceinline__ float get(bool with_res) const {
+    float q = Elem<T>::to_f(x);
+    if (with_res) q = Elem<T>::to_f(Elem<T>::from_f(q + Elem<T>::to_f(res)));
+    return fabsf(q) < 0x1p120f ? q : 0.f;
+  }
+};
+
 template <typename T>
 struct FwdArgs {
   const T *x, *res;
@@ -87,6 +109,7 @@ struct FwdArgs {
   int64_t ldx, ldr, rows;
   int32_t d;
   float eps;
+  bool over;   // the sum is written over x or residual
 };
 
 // kW warps per row, 8 kV elements per lane.  Rows of sixteen warps ask for the weights late,
@@ -105,14 +128,18 @@ __global__ void __launch_bounds__(threads(kW), kW == 16 && kV == 2 && kE == 8 ? 
   pdl_trigger();
   pdl_wait();
   L x, res;
+  Pivot<T> first;
   Lane<float, kW, kV, kE> w, b;
   x.load(g.x + row * g.ldx, wl, d);
   if (g.res) res.load(g.res + row * g.ldr, wl, d);
+  first.load(g.x + row * g.ldx, g.res ? g.res + row * g.ldr : nullptr, live);
   if (!kLate) {
     w.load(g.w, wl, d);
     if (g.b) b.load(g.b, wl, d);
   }
   float v[L::kGroups][kE], a[1] = {0.f};
+  const float pivot = first.get(g.res != nullptr);
+  if (g.over) __syncthreads();   // every warp has the row's first element
 #pragma unroll
   for (int i = 0; i < L::kGroups; ++i) {
     x.get(i, v[i]);
@@ -122,9 +149,12 @@ __global__ void __launch_bounds__(threads(kW), kW == 16 && kV == 2 && kE == 8 ? 
 #pragma unroll
       for (int e = 0; e < kE; ++e) v[i][e] = Elem<T>::to_f(Elem<T>::from_f(v[i][e] + r[e]));
     }
-#pragma unroll
-    for (int e = 0; e < kE; ++e) a[0] += v[i][e];   // (past the row: zeros)
     if (g.sum) L::put(g.sum + row * g.d, i, wl, d, v[i]);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      v[i][e] -= pivot;
+      if (L::col(i, wl) < d) a[0] += v[i][e];
+    }
   }
   row_sums<kW>(a, red[0], warp, lane, grp);
   const float mean = a[0] / (float)g.d;
@@ -142,7 +172,7 @@ __global__ void __launch_bounds__(threads(kW), kW == 16 && kV == 2 && kE == 8 ? 
   }
   row_sums<kW>(a, red[1], warp, lane, grp);
   const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
-  if (live && wl == 0 && g.stats) g.stats[row] = make_float2(mean, r);
+  if (live && wl == 0 && g.stats) g.stats[row] = make_float2(pivot + mean, r);
   if (!g.y) return;
 #pragma unroll
   for (int i = 0; i < L::kGroups; ++i) {
@@ -177,10 +207,12 @@ __global__ void __launch_bounds__(many_threads(kW), many_blocks(kW, kV)) k_ln_fw
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + grp;
   L x, res;
+  Pivot<T> first;
   auto ask = [&](int64_t at) {
     const int d = at < g.rows ? g.d : 0;   // a row past the last one has no elements
     x.load(g.x + at * g.ldx, wl, d);
     if (g.res) res.load(g.res + at * g.ldr, wl, d);
+    first.load(g.x + at * g.ldx, g.res ? g.res + at * g.ldr : nullptr, d > 0);
   };
   ask(row);
   for (int c = threadIdx.x; c < kCols; c += many_threads(kW)) {
@@ -192,6 +224,7 @@ __global__ void __launch_bounds__(many_threads(kW), many_blocks(kW, kV)) k_ln_fw
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < g.rows; base += stride, row += stride, turn ^= 1) {
     const int d = row < g.rows ? g.d : 0;
     float v[L::kGroups][kE], a[1] = {0.f};
+    const float pivot = first.get(g.res != nullptr);
 #pragma unroll
     for (int i = 0; i < L::kGroups; ++i) {
       x.get(i, v[i]);
@@ -201,13 +234,16 @@ __global__ void __launch_bounds__(many_threads(kW), many_blocks(kW, kV)) k_ln_fw
 #pragma unroll
         for (int e = 0; e < kE; ++e) v[i][e] = Elem<T>::to_f(Elem<T>::from_f(v[i][e] + r[e]));
       }
-#pragma unroll
-      for (int e = 0; e < kE; ++e) a[0] += v[i][e];   // (past the row: zeros)
     }
     if (base + stride < g.rows) ask(row + stride);
     if (g.sum)
 #pragma unroll
       for (int i = 0; i < L::kGroups; ++i) L::put(g.sum + row * g.d, i, wl, d, v[i]);
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      v[i][0] -= pivot;
+      a[0] += L::col(i, wl) < g.d ? v[i][0] : 0.f;
+    }
     // (two sets of sums in turn: the next row's may be written while these are read)
     row_sums<kW>(a, red[turn][0], warp, lane, grp);
     const float mean = a[0] / (float)g.d;
@@ -219,7 +255,7 @@ __global__ void __launch_bounds__(many_threads(kW), many_blocks(kW, kV)) k_ln_fw
     }
     row_sums<kW>(a, red[turn][1], warp, lane, grp);
     const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
-    if (d && wl == 0 && g.stats) g.stats[row] = make_float2(mean, r);
+    if (d && wl == 0 && g.stats) g.stats[row] = make_float2(pivot + mean, r);
     if (g.y)
 #pragma unroll
       for (int i = 0; i < L::kGroups; ++i) {
@@ -465,10 +501,12 @@ __global__ void __launch_bounds__(32 * kW, odd_blocks(kW)) k_ln_fwd_odd(const Fw
   int64_t row = blockIdx.x;
   const int off = (int)(((uintptr_t)(g.x + row * g.ldx) & 15) / sizeof(Half)), end = off + g.d;
   O x, res;
+  Pivot<Half> first;
   auto ask = [&](int64_t at) {
     const int till = at < g.rows ? end : 0;
     x.load(g.x + at * g.ldx - off, wl, till, at == g.rows - 1);
     if (g.res) res.load(g.res + at * g.ldr - off, wl, till, at == g.rows - 1);
+    first.load(g.x + at * g.ldx, g.res ? g.res + at * g.ldr : nullptr, till > 0);
   };
   ask(row);
   for (int c = threadIdx.x; c < kCols; c += 32 * kW) {
@@ -480,6 +518,7 @@ __global__ void __launch_bounds__(32 * kW, odd_blocks(kW)) k_ln_fwd_odd(const Fw
   int turn = 0;
   for (; row < g.rows; row += gridDim.x, turn ^= 1) {
     float v[L::kGroups][8], a[1] = {0.f};
+    const float pivot = first.get(g.res != nullptr);
     x.clip(wl, off, end);
     if (g.res) res.clip(wl, off, end);
 #pragma unroll
@@ -491,13 +530,21 @@ __global__ void __launch_bounds__(32 * kW, odd_blocks(kW)) k_ln_fwd_odd(const Fw
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[i][e] = Elem<Half>::to_f(Elem<Half>::from_f(v[i][e] + r[e]));
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) a[0] += v[i][e];   // (outside the row: zeros)
     }
     ask(row + gridDim.x);
     if (g.sum)
 #pragma unroll
       for (int i = 0; i < L::kGroups; ++i) O::put(g.sum + row * g.d - off, i, wl, off, end, v[i]);
+#pragma unroll
+    for (int i = 0; i < L::kGroups; ++i) {
+      const bool all = O::full(i, wl, off, end);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::col(i, wl) + e;
+        v[i][e] -= pivot;
+        a[0] += all || (c >= off && c < end) ? v[i][e] : 0.f;
+      }
+    }
     row_sums<kW>(a, red[turn][0], warp, lane, 0);
     const float mean = a[0] / (float)g.d;
     a[0] = 0.f;
@@ -513,7 +560,7 @@ __global__ void __launch_bounds__(32 * kW, odd_blocks(kW)) k_ln_fwd_odd(const Fw
     }
     row_sums<kW>(a, red[turn][1], warp, lane, 0);
     const float r = 1.f / sqrtf(a[0] / (float)g.d + g.eps);
-    if (threadIdx.x == 0 && g.stats) g.stats[row] = make_float2(mean, r);
+    if (threadIdx.x == 0 && g.stats) g.stats[row] = make_float2(pivot + mean, r);
     if (g.y)
 #pragma unroll
       for (int i = 0; i < L::kGroups; ++i) {
@@ -755,12 +802,13 @@ tp_status pack_layer_norm(const void* x, int64_t ldx, const void* residual, int6
   if ((uintptr_t)stats & 7) return ops_fail(TP_EINVAL, "stats must be 8-byte aligned");
   if ((s = ops_device()) != TP_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  const bool over = sum && (sum == x || sum == residual);
   if (precision == TP_FP32)
     forward(FwdArgs<float>{(const float*)x, (const float*)residual, w, b, (float*)sum, (float*)y, (float2*)stats, ldx, ldr,
-                           rows, d, eps}, st);
+                           rows, d, eps, over}, st);
   else
     forward(FwdArgs<__nv_bfloat16>{(const __nv_bfloat16*)x, (const __nv_bfloat16*)residual, w, b, (__nv_bfloat16*)sum,
-                                   (__nv_bfloat16*)y, (float2*)stats, ldx, ldr, rows, d, eps}, st);
+                                   (__nv_bfloat16*)y, (float2*)stats, ldx, ldr, rows, d, eps, over}, st);
   return done(cudaGetLastError(), "pack_layer_norm");
 }
 
