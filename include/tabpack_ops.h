@@ -229,7 +229,10 @@ tp_status pack_quantise_f8(const void* x, int64_t ldx, int64_t rows, int32_t k, 
  *             q[r, k] w[c, k] + bias[c]
  * q: e4m3 [rows, k], scale: float32 [rows, ceil(k / 128)]; w: e4m3 [n, k],
  * w_scale: float32 [ceil(n / 128), ceil(k / 128)]; bias: float32 [n] or NULL; y:
- * T [rows, n].  1 <= k, n <= 131072.  fp32 sums; rounded once.
+ * T [rows, n].  1 <= k, n <= 131072.  fp32 sums; rounded once.  The two scales
+ * may be any numbers: where the product of a row's and a column block's is no
+ * normal fp32 number they are applied one after the other, by a path that takes
+ * that row some hundred times as long.
  * aligned: whether q and w start at multiples of 16 bytes, as their rows do
  * (ldq and ldw): others are copied into the workspace first.                */
 tp_status pack_product_f8_bytes(int64_t rows, int32_t k, int32_t n, int32_t aligned, int64_t* workspace);

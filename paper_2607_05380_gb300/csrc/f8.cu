@@ -26,6 +26,9 @@
 //
 // Waits are bounded as in prod.cu, and set the same error word.
 #include <algorithm>
+#include <type_traits>
+
+#include <cuda_fp16.h>
 
 #include "lanes.cuh"
 #include "prod.cuh"
@@ -349,11 +352,74 @@ struct Tail {
 
 struct F8Args {
   CUtensorMap a, b;
+  const uint8_t *q, *w;            // what the maps read
+  int64_t ldq, ldw;
   const float *sx, *sw, *bias;
   void* y;
   int* err;
-  int32_t M, N, kb, tm, tn, f32;   // kb: K blocks; tiles
+  int32_t M, N, k, kb, tm, tn, f32;   // kb: K blocks; tiles
 };
+
+// A K block's sum is multiplied by the product f = a b of its two scales, but where that leaves the normal numbers and
+// the result need not (2^-70 2^-75 times up to 2^25; 2^64 2^64 times 0) by the larger one and then by the smaller,
+// so that nothing in between leaves them either.
+__device__ __forceinline__ bool two_steps(float a, float b, float f) {
+  const float m = fabsf(f);
+  return (m < 0x1p-126f && a != 0.f && b != 0.f) || m == __int_as_float(0x7F800000);
+}
+__device__ __forceinline__ float add_scaled(float sum, float a, float b, float acc) {
+  const float f = a * b;
+  if (!two_steps(a, b, f)) return fmaf(sum, f, acc);
+  const bool first = fabsf(a) > fabsf(b);
+  return fmaf(sum * (first ? a : b), first ? b : a, acc);
+}
+__device__ __forceinline__ uint32_t f16_of(uint32_t two) {   // two e4m3 numbers (the lower 16 bits)
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+__device__ __forceinline__ float2 f32_of(uint32_t two) { return __half22float2(*reinterpret_cast<const __half2*>(&two)); }
+// A K block's products of one row of q with kN rows of w, without the tensor cores (each product is exact).
+template <int kN, bool kVec>
+__device__ __forceinline__ void block_sums(const uint8_t* q, const uint8_t* const (&w)[kN], int kb, int k_all, const uint8_t* q_lo,
+                                           const uint8_t* q_hi, const uint8_t* w_lo, const uint8_t* w_hi, float (&sum)[kN]) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) sum[j] = 0.f;
+#pragma unroll 1
+  for (int k = kb * kBlock; k < min((kb + 1) * kBlock, k_all); k += 16) {
+    const uint4 a4 = bytes16<kVec>(q + k, k_all - k, q_lo, q_hi);
+    const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w};
+    uint4 b4[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) b4[j] = bytes16<kVec>(w[j] + k, k_all - k, w_lo, w_hi);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 x = f32_of(f16_of(a[i >> 1] >> (16 * (i & 1))));
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const uint32_t b[4] = {b4[j].x, b4[j].y, b4[j].z, b4[j].w};
+        const float2 y = f32_of(f16_of(b[i >> 1] >> (16 * (i & 1))));
+        sum[j] = fmaf(x.y, y.y, fmaf(x.x, y.x, sum[j]));
+      }
+    }
+  }
+}
+// Four neighbouring results over K blocks, for the rows that two_steps was true of.  (Four at a time: a warp's 128
+// columns of the longest K, 131072, well inside what the other warps wait for it.)
+__device__ __forceinline__ void four_sums(const F8Args& g, int row, int col, int kb0, int kb1, float (&acc)[4]) {
+  const uint8_t *q = g.q + (int64_t)row * g.ldq, *w[4];
+  const float *sx = g.sx + (int64_t)row * g.kb, *sw = g.sw + (int64_t)(min(col, g.N - 1) / kBlock) * g.kb;
+  const uint8_t *q_end = g.q + (g.M - 1) * g.ldq + g.k, *w_end = g.w + (g.N - 1) * g.ldw + g.k;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = g.w + (int64_t)min(col + j, g.N - 1) * g.ldw, acc[j] = 0.f;
+#pragma unroll 1
+  for (int kb = kb0; kb < kb1; ++kb) {
+    float sum[4];
+    block_sums<4, true>(q, w, kb, g.k, g.q, q_end, g.w, w_end, sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = add_scaled(sum[j], sx[kb], sw[kb], acc[j]);
+  }
+}
 
 // One K block: four MMAs (K = 32 each, 32 bytes apart) into an accumulator of
 // its own; then `bar` and `bar2` (in every CTA of the tile) are told.
@@ -568,8 +634,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
 #pragma unroll
       for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
       float ax = sx[kb_first], aw = sw[kb_first];
+      bool apart = false;   // a K block of this row wants two steps
       for (int kb = kb_first; kb < kb_end; ++kb) {
         const float f = ax * aw;
+        apart = apart || two_steps(ax, aw, f);
         if (kb + 1 < kb_end) ax = sx[kb + 1], aw = sw[kb + 1];
         if (!wait_here(&tl->tfull[buf], buf_phase, abort_flag, err, 2 * kWaitNs, 66)) {
           ok = false;
@@ -596,6 +664,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_prod_f8(const __grid_constant__
         if (++buf == kBufs) {
           buf = 0;
           buf_phase ^= 1u;
+        }
+      }
+      // (a branch for it in the loop above, per K block: 8192 x 4096 -> 4096 134 us instead of 121)
+      if (ok && __any_sync(0xffffffffu, apart)) {
+        float* buf = (float*)out_buf;
+#pragma unroll
+        for (int c = 0; c < kCols; c += 32) {
+          __syncwarp();
+#pragma unroll 1
+          for (int e = 0; apart && e < 32; e += 4) {
+            float v[4];
+            four_sums(g, row, c0 + c + e, kb_first, kb_end, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) buf[lane * 32 + ((e + j) ^ lane)] = v[j];
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[c + e] = apart ? buf[lane * 32 + (e ^ lane)] : acc[c + e];
         }
       }
       if constexpr (kSplit > 1) {
@@ -752,14 +837,11 @@ struct FewArgs {
   int64_t ldx, ldw;
   int32_t rows, k, n, kb, f32;
 };
-__device__ __forceinline__ uint32_t f16_of(uint32_t two) {   // two e4m3 numbers (the lower 16 bits)
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
-  return r;
-}
 constexpr int kStride = 20;   // floats between tokens of a partial sum: conflict-free stores
+// (One CTA an SM asked for: left to itself the compiler takes two of sixteen warps, and spills.  16 rows of 8192 ->
+// 2048: 11.9 us instead of 6.2.)
 template <int kNT, int kWarps, bool kVec>
-__global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
+__global__ void __launch_bounds__(32 * kWarps, kNT == 2 && kWarps == 16 ? 1 : 0) k_few_f8(const FewArgs g) {
   __shared__ float red[kWarps][8 * kNT][kStride];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
   const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * kNT;
@@ -778,6 +860,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
   const float* sw = g.sw + (int64_t)(n0 / kBlock) * g.kb;
+  bool apart = false;   // a K block of one of the rows wants two steps
   for (int b = warp; b < g.kb; b += kWarps) {
     // a lane's 32 bytes of a row's 128: two pieces of 16, 64 apart; both operands agree on the order of k
     uint4 wv[2][2], xv[kNT][2];
@@ -799,7 +882,9 @@ __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int m = m0 + 8 * j + 2 * t + c;
-        s[j][c] = m < g.rows ? g.sx[(int64_t)m * g.kb + b] * ws : 0.f;
+        const float one = m < g.rows ? g.sx[(int64_t)m * g.kb + b] : 0.f;
+        s[j][c] = one * ws;
+        apart = apart || two_steps(one, ws, s[j][c]);
       }
     float blk[kNT][4];
 #pragma unroll
@@ -839,6 +924,25 @@ __global__ void __launch_bounds__(32 * kWarps) k_few_f8(const FewArgs g) {
     red[warp][8 * j + 2 * t + 1][gid] = acc[j][1];
     red[warp][8 * j + 2 * t][gid + 8] = acc[j][2];
     red[warp][8 * j + 2 * t + 1][gid + 8] = acc[j][3];
+  }
+  if (__any_sync(0xffffffffu, apart)) {
+    __syncwarp();
+#pragma unroll 1
+    for (int i = lane; i < 16 * 8 * kNT; i += 32) {
+      const int m = m0 + (i >> 4), n = n0 + (i & 15);
+      if (m >= g.rows || n >= g.n) continue;
+      const uint8_t *x = g.x + (int64_t)m * g.ldx, *w[1] = {g.w + (int64_t)n * g.ldw};
+      float sum[1], v = 0.f;
+      bool any = false;
+#pragma unroll 1
+      for (int b = warp; b < g.kb; b += kWarps) {
+        const float ax = g.sx[(int64_t)m * g.kb + b], aw = sw[b];
+        block_sums<1, kVec>(x, w, b, g.k, g.x, x_end, g.w, w_end, sum);
+        v = add_scaled(sum[0], ax, aw, v);
+        any = any || two_steps(ax, aw, ax * aw);
+      }
+      if (any) red[warp][i >> 4][i & 15] = v;
+    }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 16 * 8 * kNT; i += 32 * kWarps) {
@@ -955,8 +1059,9 @@ tp_status pack_product_f8(const void* q, int64_t ldq, const float* scale, const 
     if (!q_ok) q = qs, ldq = ldp;
     if (!w_ok) w = ws, ldw = ldp;
   }
+  g.q = (const uint8_t*)q, g.w = (const uint8_t*)w, g.ldq = ldq, g.ldw = ldw;
   g.sx = scale, g.sw = w_scale, g.bias = bias, g.y = y;
-  g.M = (int32_t)rows, g.N = n, g.kb = (int32_t)ceil_div(k, kBlock), g.f32 = precision == TP_FP32;
+  g.M = (int32_t)rows, g.N = n, g.k = k, g.kb = (int32_t)ceil_div(k, kBlock), g.f32 = precision == TP_FP32;
   e = run_product(g, q, ldq, w, ldw, k, st);
   return done(e, "pack_product_f8");
 }
