@@ -21,7 +21,7 @@
 // Bound by HBM and by the chain of a row's loads, sums and stores (8192 rows of 2048,
 // bf16: forward with a residual 25 us, 0.80 of the measured copy rate, backward
 // with dsum 26, 0.77, and 4 for the blocks' sums), by single elements more by the
-// latter (2003 rows of 5001, fp32: forward 25 us, 0.48, backward 28, 0.64).  A row's
+// latter (2003 rows of 5001, fp32: forward 21 us, 0.56, backward 25, 0.72).  A row's
 // two forward sums by one barrier, from the warps' means and centred squares: slower
 // by its divisions (28 us); resident blocks with the next row ahead, where rows come
 // by 16 bytes: 29.
@@ -114,7 +114,7 @@ struct FwdArgs {
 
 // kW warps per row, 8 kV elements per lane.  Rows of sixteen warps ask for the weights late,
 // which leaves the registers for a second block an SM (8192 x 8192: bf16 145 us, so
-// 116; fp32 195, 170).
+// 107; fp32 195, 166).
 template <typename T, int kW, int kV, int kE>
 __global__ void __launch_bounds__(threads(kW), kW == 16 && kV == 2 && kE == 8 ? 2 : 0) k_ln_fwd(const FwdArgs<T> g) {
   constexpr bool kLate = kW == 16 && kE == 8 && (kV == 2 || sizeof(T) == 4);
@@ -431,10 +431,10 @@ __global__ void __launch_bounds__(threads(kW), kW > 8 && !(kW == 14 && kE == 1) 
 // beside it is cleared, and the last row's last group, behind which the matrix ends,
 // is read by elements.  A block's rows, a multiple of eight apart, have the same off.
 // bf16 only, and only of many rows: 8192 rows of 4097, us, by single elements and so:
-// forward 102, 62, backward 114, 72; of 7001: 159, 107 and 219, 110; 2000 rows of
-// 4097: 24.6, 18.7 and 27.7, 26.2, of 2003: 11.1, 10.7 and 12.9, 17.3 (fp32, 8192 of 4097:
-// 118, 95 and 94, 105; of 7001: 155, 179 and 229, 193).  Eight columns a lane and twice the
-// warps: forward 86.
+// forward 94, 68, backward 111, 71; of 7001: 157, 114 and 213, 110; 2000 rows of
+// 4097: 25, 20 and 27, 25, of 2003: 11.1, 11.0 and 12.9, 17.3 (fp32, 8192 of 4097:
+// 98, 95 and 94, 105; of 7001: 155, 179 and 229, 193).  Eight columns a lane and twice the
+// warps: forward 86.  The first element's part in the forward times: 4 to 6 us of the 8192 rows.
 using Half = __nv_bfloat16;
 template <int kW>
 struct OddLane {
